@@ -345,6 +345,167 @@ kvc_status kvc_layout_set_kernel_timing(kvc_layout *layout, int on);
 kvc_status kvc_layout_kernel_time(kvc_layout *layout, uint32_t *launches, double *total_ms,
                                   double *min_ms, double *max_ms);
 
+/* ------------------------------------------------------------------ a step's tokens (Sec. 2.1)
+ *
+ * The engine's side of the paged pool, between an unpack of loaded blocks and the next pack: the
+ * tokens of a step get slots, their keys and values are written, and attention reads the blocks.
+ * The paper takes these for granted ("the KV cache of a serving engine"); they are here so that a
+ * caller can run a step on the same layout handle and the same device-resident block tables that
+ * pack and unpack take.  Conventions of all calls below:
+ *   - every pointer inside a descriptor is DEVICE memory of the current device, and stays valid until
+ *     the kernels have run; nothing is copied to the host and nothing is waited for;
+ *   - lengths, ids and slots live on the device, so the host cannot check them: the kernels do.  A
+ *     length is clamped to what its buffers hold, an entry that names no block of the pool is
+ *     skipped and counted (kvc_poll_device_status: n_skipped, once per place that met it);
+ *   - calls enqueue kernels on `stream` only and allocate nothing after the handle's first launch, so
+ *     they can be captured into a CUDA graph (not as the handle's first call);
+ *   - results are the same bits every time: no sum depends on the order in which blocks run.
+ * A descriptor's `reserved` must be 0. */
+
+typedef enum { KVC_DTYPE_BF16 = 0, KVC_DTYPE_FP16 = 1 } kvc_dtype;
+
+#define KVC_MAP_MAX_REQUESTS 16384u
+
+/* Block tables and slots of a step, from request lengths (the device-side counterpart of
+ * kvc_map_request).  Request r holds context_lens[r] tokens and gets new_lens[r] more (negative
+ * counts as 0).  With B tokens per block it holds hb = ceil(context / B) blocks, whose ids are the
+ * first entries of row r of block_tables, and needs ha = ceil((context + new) / B); the missing ones
+ * are taken from free_blocks in request order (request 0's first), and their ids are written to
+ * entries hb .. ha-1 of the row.  A request without new tokens takes none.  Other entries are left
+ * as they are.  Token rows are numbered in request order; for row i, of request r and position p:
+ *   positions[i] = p, slots[i] = block_tables[r][p / B] * B + p % B, token_request[i] = r
+ * and slots[i] = -1 where there is no such block: behind max_blocks entries, behind the end of the
+ * free list (the table entry is then -1 too), or an entry outside the pool.  Rows behind the last
+ * token, up to token_capacity, get slot -1, position 0 and request -1, which kvc_append skips, so a
+ * captured step can be replayed with fewer tokens.
+ *   cu_tokens[r] = first row of request r, cu_tokens[n_requests] = rows of the step (may exceed
+ *     token_capacity: rows past it are not written)
+ *   total_lens[r] = context + new        (optional)
+ *   counts[3] = rows of the step, blocks taken from the free list, rows without a block because the
+ *     table row or the free list was too short   (optional)
+ * The row of a table may be longer than max_blocks (table_stride entries apart).  At most
+ * KVC_MAP_MAX_REQUESTS requests (TOO_LARGE).  One kernel.  The layout gives block size and pool size
+ * only; its pool is not touched.  Outputs must not overlap inputs or one another, except that
+ * block_tables is both.
+ * Errors: INVALID_ARG, TOO_LARGE, ALIGNMENT (a pointer not a multiple of its element), CUDA. */
+typedef struct {
+    const int32_t *context_lens; /* [n_requests] */
+    const int32_t *new_lens;     /* [n_requests] */
+    const int32_t *free_blocks;  /* [n_free] */
+    int32_t *block_tables;       /* [n_requests][table_stride] in/out */
+    uint64_t table_stride;       /* entries */
+    uint32_t max_blocks;
+    uint32_t n_requests;
+    uint32_t n_free;
+    uint32_t token_capacity;     /* rows of positions, slots, token_request */
+    int32_t *cu_tokens;          /* [n_requests + 1] out */
+    int32_t *positions;          /* [token_capacity] out */
+    int64_t *slots;              /* [token_capacity] out */
+    int32_t *token_request;      /* [token_capacity] out, or NULL */
+    int32_t *total_lens;         /* [n_requests] out, or NULL */
+    int32_t *counts;             /* [3] out, or NULL */
+    uint64_t reserved;
+} kvc_map_tokens_desc;
+kvc_status kvc_map_tokens(kvc_layout *layout, const kvc_map_tokens_desc *desc, void *stream);
+
+/* Queries, keys and values of a step's tokens: norm, rotation, cache write, in one pass.  For every
+ * token row t with slots[t] >= 0, and every head x of head_dim elements,
+ *   y = x * rsqrt(mean(x^2) + eps) * weight        (queries and keys, if q_weight / k_weight is given)
+ *   (y_i, y_j) <- (y_i cos - y_j sin, y_j cos + y_i sin)   over the first rot_dim elements
+ * with pair n = 0 .. rot_dim/2-1 being (n, n + rot_dim/2), or (2n, 2n+1) if interleaved != 0, and
+ * cos = cos_sin[positions[t]][n], sin = cos_sin[positions[t]][rot_dim/2 + n] (32-bit; the caller's
+ * table fixes the frequencies).  Queries go to q_out; keys and values (values unchanged) to the
+ * slot's place in planes K (0) and V (1) of `layer`.  Computed in 32 bits, rounded once.
+ * Rows with slots[t] < 0 are skipped: neither q_out nor the pool is touched.  So are rows whose slot
+ * lies behind the pool, or whose position lies outside the cos_sin table (with rot_dim > 0); those
+ * are counted.  Two rows with the same slot: either one's keys and values.
+ * Layout: kv_planes = 2, elem_bytes = 2, head_dim a multiple of 8 up to 256; rot_dim a multiple of 16
+ * up to head_dim, or 0 (positions and cos_sin are then unused).  Strides are in elements; elements
+ * of a head are adjacent.  Pointers of q, k, v, q_out and the weights, and all strides in bytes, are
+ * multiples of 16 bytes (ALIGNMENT).  q_out may be q itself with the same strides.  n_q_heads = 0:
+ * keys and values only.  One kernel.
+ * Errors: INVALID_ARG, ALIGNMENT, CUDA. */
+typedef struct {
+    uint32_t layer;
+    uint32_t dtype;              /* kvc_dtype: of q, k, v, weights, q_out and the pool */
+    const void *q, *k, *v;       /* [n_tokens][heads][head_dim] */
+    void *q_out;                 /* [n_tokens][n_q_heads][head_dim] */
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+    int64_t v_token_stride, v_head_stride, out_token_stride, out_head_stride;
+    const int64_t *slots;        /* [n_tokens] */
+    const int32_t *positions;    /* [n_tokens] */
+    const float *cos_sin;        /* [max_positions][cos_sin_stride] */
+    uint64_t cos_sin_stride;     /* floats, at least rot_dim */
+    const void *q_weight;        /* [head_dim], or NULL: no norm of the queries */
+    const void *k_weight;        /* [head_dim], or NULL: no norm of the keys */
+    float eps;
+    uint32_t n_tokens, n_q_heads, rot_dim, max_positions;
+    uint32_t interleaved;        /* 0 or 1 */
+    uint64_t reserved;
+} kvc_append_desc;
+kvc_status kvc_append(kvc_layout *layout, const kvc_append_desc *desc, void *stream);
+
+/* Causal attention of a step's queries over the paged pool.  Request r owns query rows
+ * cu_tokens[r] .. cu_tokens[r+1]-1, the LAST tokens of its seq_lens[r]: row i of them stands at
+ * position p = seq_lens[r] - (rows of r) + i and sees key j if
+ *   j <= p  and  (window == 0  or  p - j < window  or  j < sinks)
+ * (window: the last `window` tokens including its own; sinks: first tokens that stay visible behind
+ * it).  Key and value j lie in block block_tables[r][j / B] of planes K and V of `layer`.  Query head
+ * h reads KV head h / (n_q_heads / num_kv_heads).
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,   lse = ln sum_j exp(scale * q . k_j)   (optional)
+ * A row that sees nothing (position before 0, or only keys that are not there) gives zeros and
+ * lse = -inf.  Rows outside [cu_tokens[0], cu_tokens[n_requests]) are left as they are; so is nothing
+ * else.  Keys past max_blocks * B, and keys in entries that name no block of the pool, are not
+ * there; the latter are counted.  Slots that no query of the call sees may hold anything; those that
+ * some query sees must hold finite values (a value of infinity or NaN may reach rows of the same
+ * request that do not see it).
+ * Products are taken in the pool's type with 32-bit sums; the softmax is in 32 bits, its weights are
+ * rounded to the pool's type for the second product.
+ * max_q_len is a hint, at least the largest number of query rows of one request (0: unknown): it
+ * chooses between kernels, never changes what is computed.  Any mix of prompts and single tokens may
+ * be in one call.
+ * Layout: kv_planes = 2, elem_bytes = 2, head_dim 64 or 128, n_q_heads a multiple of num_kv_heads.
+ * Strides in elements; pointers of q and out and strides in bytes are multiples of 16 bytes.  `out`
+ * must not overlap q.  scale > 0.
+ * workspace: at least kvc_attention_workspace_bytes(...) bytes, 256-byte aligned, contents irrelevant
+ * before and after.  Calls that may run at the same time (other streams, captured graphs that are
+ * replayed concurrently) need workspaces of their own; calls on one stream can share one.
+ * kvc_attention: n_groups must be 0, group_starts and prefix_lens NULL.  Two kernels.
+ *
+ * kvc_attention_shared: the same result, for requests that share prefixes (the device-side
+ * counterpart of kvc_map_requests_shared).  Group g is requests group_starts[g] ..
+ * group_starts[g+1]-1 (ascending; requests in no group share nothing); their first prefix_lens[g]
+ * tokens are the same, and their keys and values are read ONCE for the whole group, through the
+ * table of the group's first request.  prefix_lens need not be a multiple of the block size.  window
+ * and sinks must be 0, 1 <= n_groups <= n_requests.  Three kernels.
+ * Errors: INVALID_ARG, ALIGNMENT, TOO_LARGE (n_tokens * query heads per KV head >= 2^31), CUDA. */
+typedef struct {
+    uint32_t layer;
+    uint32_t dtype;              /* kvc_dtype: of q, out and the pool */
+    const void *q;               /* [n_tokens][n_q_heads][head_dim] */
+    void *out;                   /* [n_tokens][n_q_heads][head_dim] */
+    float *lse;                  /* [n_tokens][n_q_heads], or NULL */
+    int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+    const int32_t *cu_tokens;    /* [n_requests + 1] */
+    const int32_t *seq_lens;     /* [n_requests] tokens in the cache, those of this call among them */
+    const int32_t *block_tables; /* [n_requests][table_stride] */
+    uint64_t table_stride;       /* entries */
+    uint32_t max_blocks;
+    uint32_t n_tokens, n_requests, n_q_heads, max_q_len;
+    float scale;
+    uint32_t window, sinks;
+    const int32_t *group_starts; /* [n_groups + 1] */
+    const int32_t *prefix_lens;  /* [n_groups] */
+    uint32_t n_groups;
+    uint32_t reserved;
+    void *workspace;
+    uint64_t workspace_bytes;
+} kvc_attention_desc;
+kvc_status kvc_attention_workspace_bytes(kvc_layout *layout, uint32_t n_tokens, uint32_t n_requests,
+                                         uint32_t n_q_heads, uint32_t n_groups, uint64_t *bytes);
+kvc_status kvc_attention(kvc_layout *layout, const kvc_attention_desc *desc, void *stream);
+kvc_status kvc_attention_shared(kvc_layout *layout, const kvc_attention_desc *desc, void *stream);
+
 /* ------------------------------------------------------------------ staging ring (Sec. 6.4) */
 
 typedef struct kvc_ring kvc_ring;

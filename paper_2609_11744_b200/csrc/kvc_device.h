@@ -1,0 +1,88 @@
+// Device helpers shared by the kernels that compute on the pool's elements.
+#ifndef KVC_DEVICE_H
+#define KVC_DEVICE_H
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+// Programmatic dependent launch: the grid may be scheduled while the stream's previous kernel
+// drains; nothing in global memory is touched before this returns, and every block calls it, so a
+// later kernel that waits for this one has waited for the earlier ones too.
+__device__ __forceinline__ void kvc_pdl_wait()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <typename A>
+inline cudaError_t kvc_launch_pdl(void (*kernel)(const A), const A &a, dim3 grid, uint32_t threads, uint32_t smem,
+                                  cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+// Two 16-bit elements <-> two floats.
+template <typename T>
+__device__ __forceinline__ float2 kvc_to_float2(uint32_t v);
+template <>
+__device__ __forceinline__ float2 kvc_to_float2<__nv_bfloat16>(uint32_t v)
+{
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+}
+template <>
+__device__ __forceinline__ float2 kvc_to_float2<__half>(uint32_t v)
+{
+    __half2 h;
+    memcpy(&h, &v, 4);
+    return __half22float2(h);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t kvc_from_float2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t kvc_from_float2<__nv_bfloat16>(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    uint32_t v;
+    memcpy(&v, &h, 4);
+    return v;
+}
+template <>
+__device__ __forceinline__ uint32_t kvc_from_float2<__half>(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    uint32_t v;
+    memcpy(&v, &h, 4);
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void kvc_unpack8(const uint4 &v, float (&x)[8])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = kvc_to_float2<T>(w[i]);
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint4 kvc_pack8(const float (&x)[8])
+{
+    return make_uint4(kvc_from_float2<T>(x[0], x[1]), kvc_from_float2<T>(x[2], x[3]),
+                      kvc_from_float2<T>(x[4], x[5]), kvc_from_float2<T>(x[6], x[7]));
+}
+
+#endif

@@ -139,6 +139,18 @@ struct kvc_layout {
     std::vector<cudaEvent_t> spare_events;
 };
 
+// Creates the handle's device state on first use; afterwards checks that its device is current.
+kvc_status kvc_ensure_device(kvc_layout *lay);
+
+// Where plane p of layer l starts (host arithmetic on the descriptor).
+inline const unsigned char *kvc_plane_ptr(const kvc_layout *lay, uint32_t l, uint32_t p)
+{
+    if (!lay->plane_ptrs.empty())
+        return static_cast<const unsigned char *>(lay->plane_ptrs[(size_t)l * lay->d.kv_planes + p]);
+    return static_cast<const unsigned char *>(lay->d.base) + (uint64_t)l * lay->d.layer_stride +
+           (uint64_t)p * lay->d.plane_stride;
+}
+
 // Launches the copy kernel; with kernel timing on, between two events on the same stream.
 kvc_status kvc_launch_timed(kvc_layout *lay, int dir, int variant, const KvcLaunch &a, uint32_t grid,
                             uint32_t smem, cudaStream_t st);

@@ -13,7 +13,9 @@ namespace {
 
 inline bool mult16(uint64_t v) { return (v & 15u) == 0; }
 
-kvc_status ensure_device(kvc_layout *lay)
+}  // namespace
+
+kvc_status kvc_ensure_device(kvc_layout *lay)
 {
     if (lay->dev_ready) {
         // a handle belongs to the device that was current at its first launch
@@ -51,8 +53,6 @@ kvc_status ensure_device(kvc_layout *lay)
     lay->dev_ready = true;
     return KVC_OK;
 }
-
-}  // namespace
 
 // Fills the geometry and the launch shape that do not depend on the ids.
 kvc_status kvc_make_plan(kvc_layout *lay, uint64_t n_ent, const void *slot_probe, KvcLaunch *a,
@@ -342,7 +342,7 @@ kvc_status copy_one(kvc_layout *lay, int dir, const int32_t *ids, uint32_t n_blo
                                        : kvc_unpack_batch(lay, &op, 1, 0, stream);
         }
     }
-    kvc_status s = ensure_device(lay);
+    kvc_status s = kvc_ensure_device(lay);
     if (s != KVC_OK)
         return s;
     KvcLaunch a;
@@ -435,7 +435,7 @@ kvc_status copy_batch(kvc_layout *lay, int dir, const kvc_chunk_op *ops, uint32_
                 return s;
         }
     }
-    kvc_status s = ensure_device(lay);
+    kvc_status s = kvc_ensure_device(lay);
     if (s != KVC_OK)
         return s;
     KvcLaunch a;

@@ -1,0 +1,490 @@
+// The step's tokens: block tables and slots built from request lengths (kvc_map_tokens), and the
+// per-head norm, rotation and cache write of their queries, keys and values (kvc_append).
+#include <string.h>
+
+#include <algorithm>
+
+#include "kvc_internal.h"
+#include "kvc_device.h"
+
+namespace {
+
+// ------------------------------------------------------------------------------------ map_tokens
+//
+// hb = ceil(context / B) blocks are held already, ha = ceil((context + new) / B) are needed; the
+// ha - hb new ones come from the free list in request order, so the exclusive prefix sums of `new`
+// (token rows) and of ha - hb (free-list positions) give every output independently of the others.
+// Every block redoes the two sums over all requests -- 8 bytes each, read from L2 -- instead of
+// waiting for another block's result: one launch, no flags, the same integers every time.  What
+// bounds the call is that chain (two dependent loads, one block scan, one binary search in shared
+// memory, one table read), not the 16 bytes it writes per token.
+struct MapArgs {
+    const int32_t *context_lens, *new_lens, *free_blocks;
+    int32_t *tables;
+    int64_t table_stride;
+    uint32_t max_blocks, n_requests, n_free, capacity, block_size, num_blocks;
+    int32_t *cu, *total_lens, *positions, *request, *counts;
+    int64_t *slots;
+    uint32_t *status;
+};
+
+#define MAP_THREADS 512u
+
+__device__ __forceinline__ int32_t sat32(int64_t v) { return v > 0x7FFFFFFFll ? 0x7FFFFFFF : (int32_t)v; }
+
+struct MapReq {
+    int32_t ctx, add;  // tokens held, tokens of this step (ctx + add <= INT32_MAX)
+    uint32_t hb, ha;   // blocks held, blocks needed (both at most max_blocks)
+};
+
+__device__ __forceinline__ MapReq map_req(const MapArgs &a, uint32_t r)
+{
+    MapReq q;
+    q.ctx = max(a.context_lens[r], 0);
+    q.add = max(min(a.new_lens[r], 0x7FFFFFFF - q.ctx), 0);
+    const uint32_t b = a.block_size;
+    const uint32_t end = (uint32_t)q.ctx + (uint32_t)q.add;
+    q.ha = min(end / b + (end % b != 0), a.max_blocks);
+    q.hb = min((uint32_t)q.ctx / b + ((uint32_t)q.ctx % b != 0), q.ha);
+    if (q.add == 0)
+        q.ha = q.hb;  // nothing is added: nothing is taken
+    return q;
+}
+
+// Largest r in [0, n) with v[r] <= x (v ascending, v[0] = 0).
+__device__ __forceinline__ uint32_t last_at_most(const int32_t *v, uint32_t n, int32_t x)
+{
+    uint32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (v[mid] <= x)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+__global__ void __launch_bounds__(MAP_THREADS) kvc_map_tokens_kernel(const MapArgs a)
+{
+    extern __shared__ int32_t sm[];
+    const uint32_t R = a.n_requests;
+    int32_t *cu = sm;               // [R + 1] first token row of each request
+    int32_t *fb = sm + R + 1;       // [R + 1] first free-list position of each request
+    int32_t *ctx = sm + 2 * (R + 1);  // [R] tokens held
+    __shared__ int64_t warp_sum[2][MAP_THREADS / 32];
+    kvc_pdl_wait();
+
+    const uint32_t per = (R + MAP_THREADS - 1) / MAP_THREADS;
+    const uint32_t r0 = min(threadIdx.x * per, R), r1 = min(r0 + per, R);
+    int64_t st = 0, sb = 0;
+    for (uint32_t r = r0; r < r1; ++r) {
+        const MapReq q = map_req(a, r);
+        st += q.add;
+        sb += q.ha - q.hb;
+    }
+    const uint32_t lane = threadIdx.x & 31u, w = threadIdx.x >> 5;
+    int64_t it = st, ib = sb;
+#pragma unroll
+    for (uint32_t o = 1; o < 32; o *= 2) {
+        const int64_t x = __shfl_up_sync(~0u, it, o), y = __shfl_up_sync(~0u, ib, o);
+        if (lane >= o) {
+            it += x;
+            ib += y;
+        }
+    }
+    if (lane == 31) {
+        warp_sum[0][w] = it;
+        warp_sum[1][w] = ib;
+    }
+    __syncthreads();
+    int64_t bt = 0, bb = 0, tt = 0, tb = 0;  // sums of earlier warps, sums of all
+    for (uint32_t k = 0; k < MAP_THREADS / 32; ++k) {
+        if (k < w) {
+            bt += warp_sum[0][k];
+            bb += warp_sum[1][k];
+        }
+        tt += warp_sum[0][k];
+        tb += warp_sum[1][k];
+    }
+    bt += it - st;
+    bb += ib - sb;
+    int64_t no_block = 0;
+    const bool first = blockIdx.x == 0;
+    for (uint32_t r = r0; r < r1; ++r) {
+        const MapReq q = map_req(a, r);
+        cu[r] = sat32(bt);
+        fb[r] = sat32(bb);
+        ctx[r] = q.ctx;
+        if (first) {
+            a.cu[r] = sat32(bt);
+            if (a.total_lens)
+                a.total_lens[r] = q.ctx + q.add;
+            // tokens past the blocks that the table and the free list provide
+            const int64_t have = (int64_t)q.hb + min(max((int64_t)a.n_free - bb, (int64_t)0), (int64_t)(q.ha - q.hb));
+            const int64_t limit = max(have * a.block_size, (int64_t)q.ctx);
+            no_block += max((int64_t)q.ctx + q.add - limit, (int64_t)0);
+        }
+        bt += q.add;
+        bb += q.ha - q.hb;
+    }
+    if (threadIdx.x == 0) {
+        cu[R] = sat32(tt);
+        fb[R] = sat32(tb);
+    }
+    __syncthreads();
+    if (first) {
+        if (threadIdx.x == 0)
+            a.cu[R] = sat32(tt);
+        if (a.counts) {
+#pragma unroll
+            for (uint32_t o = 16; o; o /= 2)
+                no_block += __shfl_xor_sync(~0u, no_block, o);
+            if (lane == 0)
+                warp_sum[0][w] = no_block;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                int64_t sum = 0;
+                for (uint32_t k = 0; k < MAP_THREADS / 32; ++k)
+                    sum += warp_sum[0][k];
+                a.counts[0] = sat32(tt);
+                a.counts[1] = (int32_t)min(tb, (int64_t)a.n_free);
+                a.counts[2] = sat32(sum);
+            }
+        }
+    }
+
+    const uint32_t B = a.block_size;
+    const uint32_t step = gridDim.x * MAP_THREADS, at = blockIdx.x * MAP_THREADS + threadIdx.x;
+    // new table entries
+    const uint32_t n_new = (uint32_t)fb[R];
+    for (uint64_t i = at; i < n_new; i += step) {
+        const uint32_t r = last_at_most(fb, R, (int32_t)i);
+        const uint32_t hb = min((uint32_t)ctx[r] / B + ((uint32_t)ctx[r] % B != 0), a.max_blocks);
+        a.tables[(int64_t)r * a.table_stride + hb + (i - (uint32_t)fb[r])] = i < a.n_free ? a.free_blocks[i] : -1;
+    }
+    // token rows; the rows behind the last token are marked as holding none
+    const uint32_t n_tok = min((uint32_t)cu[R], a.capacity);
+    for (uint64_t i = at; i < a.capacity; i += step) {
+        int64_t slot = -1;
+        int32_t pos = 0, req = -1;
+        if (i < n_tok) {
+            const uint32_t r = last_at_most(cu, R, (int32_t)i);
+            req = (int32_t)r;
+            pos = ctx[r] + (int32_t)(i - (uint32_t)cu[r]);
+            const uint32_t bi = (uint32_t)pos / B, off = (uint32_t)pos % B;
+            if (bi < a.max_blocks) {
+                const uint32_t hb = (uint32_t)ctx[r] / B + ((uint32_t)ctx[r] % B != 0);
+                int32_t id = -1;
+                bool have = true;
+                if (bi < hb) {  // the block that the context's last token lies in
+                    id = a.tables[(int64_t)r * a.table_stride + bi];
+                } else {
+                    const uint32_t f = (uint32_t)fb[r] + (bi - hb);
+                    have = f < a.n_free;
+                    if (have)
+                        id = a.free_blocks[f];
+                }
+                if ((uint32_t)id < a.num_blocks)
+                    slot = (int64_t)id * B + off;
+                else if (have)
+                    atomicAdd(a.status, 1u);  // an entry that names no block of the pool
+            }
+        }
+        a.slots[i] = slot;
+        a.positions[i] = pos;
+        if (a.request)
+            a.request[i] = req;
+    }
+}
+
+// ------------------------------------------------------------------------------------ append
+//
+// y = x * rsqrt(mean(x^2) + eps) * w over each head, then the rotation of its first `rot` values by
+// the row of the cos/sin table at the token's position; values are copied.  All in 32 bits, rounded
+// once to the pool's type.  Bound by memory: every element is read once and written once.  A team
+// of head_dim / 8 lanes (rounded up to a power of two) holds one head, 16 bytes a lane, so the
+// mean is a few shuffles and the partner of a "halves" pair is one shuffle away.  A warp serves
+// several heads of ONE token, so its table row, slot and addresses are fetched once; four heads are
+// loaded before the first is used, which keeps 64 bytes a lane in flight.
+struct AppendArgs {
+    const unsigned char *q, *k, *v;
+    unsigned char *q_out, *k_plane, *v_plane;
+    int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;  // strides in bytes
+    uint64_t block_stride;
+    const int64_t *slots;
+    const int32_t *positions;
+    const float *cos_sin;
+    int64_t cs_stride;  // floats
+    const void *q_weight, *k_weight;
+    float eps;
+    uint32_t n_tokens, hq, hkv, d, rot, max_pos, block_size, num_blocks;
+    uint32_t lanes;   // lanes per head: a power of two >= d / 8
+    uint32_t chunk;   // heads per warp unit
+    uint32_t chunks;  // units per token
+    uint32_t *status;
+};
+
+#define APPEND_THREADS 256u
+#define APPEND_UNROLL 4
+
+template <typename T, bool NEIGHBOURS>
+__global__ void __launch_bounds__(APPEND_THREADS) kvc_append_kernel(const AppendArgs a)
+{
+    kvc_pdl_wait();
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t team = lane / a.lanes, teams = 32u / a.lanes, l = lane % a.lanes;
+    const bool on = l * 8u < a.d;
+    const uint32_t heads = a.hq + 2 * a.hkv;
+    const uint64_t units = (uint64_t)a.n_tokens * a.chunks;
+    const uint32_t warps = gridDim.x * (APPEND_THREADS / 32u);
+    const float inv_d = 1.0f / (float)a.d;
+    const bool rotated = a.rot != 0 && l * 8u < a.rot;
+    const uint32_t half = a.rot / 16u;  // lanes in one half of the rotated part
+    for (uint64_t u = blockIdx.x * (APPEND_THREADS / 32u) + (threadIdx.x >> 5); u < units; u += warps) {
+        const uint32_t tok = (uint32_t)(u / a.chunks);
+        const uint32_t h0 = (uint32_t)(u - (uint64_t)tok * a.chunks) * a.chunk;
+        const uint32_t h1 = min(h0 + a.chunk, heads);
+        const int64_t slot = a.slots[tok];
+        if (slot < 0)
+            continue;  // a row without a token
+        const int32_t pos = a.rot ? a.positions[tok] : 0;
+        const uint64_t id = (uint64_t)slot / a.block_size;
+        if (id >= a.num_blocks || (a.rot && (uint32_t)pos >= a.max_pos)) {
+            if (lane == 0 && h0 == 0)
+                atomicAdd(a.status, 1u);
+            continue;
+        }
+        const uint64_t cache = id * a.block_stride +
+                               ((uint64_t)slot - id * a.block_size) * a.hkv * a.d * sizeof(T);
+        // the eight values of this lane use angles [a0, a0 + 8) (halves) or [a0, a0 + 4) (neighbours)
+        float cs[8], sn[8];
+        if (rotated) {
+            const float *row = a.cos_sin + (int64_t)pos * a.cs_stride;
+            const uint32_t a0 = NEIGHBOURS ? l * 4u : (l < half ? l : l - half) * 8u;
+#pragma unroll
+            for (int i = 0; i < (NEIGHBOURS ? 4 : 8); ++i) {
+                cs[i] = row[a0 + i];
+                sn[i] = row[a.rot / 2 + a0 + i];
+            }
+        }
+        for (uint32_t hb = h0 + team; hb < h1 + team; hb += teams * APPEND_UNROLL) {
+            uint4 raw[APPEND_UNROLL];
+#pragma unroll
+            for (int i = 0; i < APPEND_UNROLL; ++i) {
+                const uint32_t h = hb + i * teams;
+                raw[i] = make_uint4(0, 0, 0, 0);
+                if (h < h1 && on) {
+                    const unsigned char *src = h < a.hq ? a.q + tok * a.q_tok + h * a.q_head
+                                               : h < a.hq + a.hkv ? a.k + tok * a.k_tok + (h - a.hq) * a.k_head
+                                                                  : a.v + tok * a.v_tok + (h - a.hq - a.hkv) * a.v_head;
+                    raw[i] = *reinterpret_cast<const uint4 *>(src + l * 16u);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < APPEND_UNROLL; ++i) {
+                const uint32_t h = hb + i * teams;
+                const bool is_v = h >= a.hq + a.hkv;
+                uint4 res = raw[i];
+                // the shuffles below are taken by whole warps: teams past the last head go through
+                // them with zeros, and one condition of the loop is the same for all teams of a warp
+                float x[8];
+                kvc_unpack8<T>(raw[i], x);
+                const void *weight = h < a.hq ? a.q_weight : a.k_weight;
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    sum += x[e] * x[e];
+                for (uint32_t o = a.lanes / 2; o; o /= 2)
+                    sum += __shfl_xor_sync(~0u, sum, o);
+                if (weight && on && !is_v && h < h1) {
+                    const float inv = rsqrtf(sum * inv_d + a.eps);
+                    float wv[8];
+                    kvc_unpack8<T>(reinterpret_cast<const uint4 *>(weight)[l], wv);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[e] = x[e] * inv * wv[e];
+                }
+                if (NEIGHBOURS) {
+                    if (rotated) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = x[2 * e], q = x[2 * e + 1];
+                            x[2 * e] = p * cs[e] - q * sn[e];
+                            x[2 * e + 1] = q * cs[e] + p * sn[e];
+                        }
+                    }
+                } else if (a.rot) {
+                    const uint32_t from = team * a.lanes + (rotated ? (l < half ? l + half : l - half) : l);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float p = __shfl_sync(~0u, x[e], from);
+                        if (rotated)
+                            x[e] = l < half ? x[e] * cs[e] - p * sn[e] : x[e] * cs[e] + p * sn[e];
+                    }
+                }
+                if (!is_v)
+                    res = kvc_pack8<T>(x);
+                if (h < h1 && on) {
+                    unsigned char *dst = h < a.hq ? a.q_out + tok * a.o_tok + h * a.o_head
+                                         : (is_v ? a.v_plane : a.k_plane) + cache +
+                                               (uint64_t)(h - a.hq - (is_v ? a.hkv : 0u)) * a.d * sizeof(T);
+                    *reinterpret_cast<uint4 *>(dst + l * 16u) = res;
+                }
+            }
+        }
+    }
+}
+
+inline bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+}  // namespace
+
+extern "C" {
+
+kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *stream)
+{
+    if (!lay || !d || d->reserved != 0)
+        return KVC_ERR_INVALID_ARG;
+    if (d->n_requests > KVC_MAP_MAX_REQUESTS)
+        return KVC_ERR_TOO_LARGE;
+    if (!d->cu_tokens || (d->n_requests && (!d->context_lens || !d->new_lens)) || (d->n_free && !d->free_blocks) ||
+        (d->token_capacity && (!d->positions || !d->slots)) || (d->n_requests && d->max_blocks && !d->block_tables) ||
+        d->token_capacity > 0x7FFFFFFFu || d->n_free > 0x7FFFFFFFu ||
+        (d->n_requests > 1 && d->table_stride < d->max_blocks))
+        return KVC_ERR_INVALID_ARG;
+    if (!aligned(d->cu_tokens, 4) || !aligned(d->context_lens, 4) || !aligned(d->new_lens, 4) ||
+        !aligned(d->free_blocks, 4) || !aligned(d->block_tables, 4) || !aligned(d->positions, 4) ||
+        !aligned(d->slots, 8) || !aligned(d->token_request, 4) || !aligned(d->total_lens, 4) || !aligned(d->counts, 4))
+        return KVC_ERR_ALIGNMENT;
+    kvc_status s = kvc_ensure_device(lay);
+    if (s != KVC_OK)
+        return s;
+    MapArgs a;
+    a.context_lens = d->context_lens;
+    a.new_lens = d->new_lens;
+    a.free_blocks = d->free_blocks;
+    a.tables = d->block_tables;
+    a.table_stride = (int64_t)d->table_stride;
+    a.max_blocks = d->max_blocks;
+    a.n_requests = d->n_requests;
+    a.n_free = d->n_free;
+    a.capacity = d->token_capacity;
+    a.block_size = lay->d.block_size;
+    a.num_blocks = lay->d.num_blocks;
+    a.cu = d->cu_tokens;
+    a.total_lens = d->total_lens;
+    a.positions = d->positions;
+    a.request = d->token_request;
+    a.counts = d->counts;
+    a.slots = d->slots;
+    a.status = lay->d_status;
+    const uint32_t smem = (3 * d->n_requests + 2) * sizeof(int32_t);
+    if (smem > 48 * 1024 &&
+        cudaFuncSetAttribute(kvc_map_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)((3 * KVC_MAP_MAX_REQUESTS + 2) * sizeof(int32_t))) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return KVC_ERR_CUDA;
+    }
+    // two rows a thread: a few more blocks shorten the binary searches' share, a few fewer the scans'
+    const uint32_t want = (uint32_t)(((uint64_t)d->token_capacity + 2 * MAP_THREADS - 1) / (2 * MAP_THREADS));
+    const uint32_t grid = std::max<uint32_t>(1u, std::min<uint32_t>(want, (uint32_t)lay->sm_count));
+    if (kvc_launch_pdl(kvc_map_tokens_kernel, a, dim3(grid), MAP_THREADS, smem, (cudaStream_t)stream) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return KVC_ERR_CUDA;
+    }
+    ++lay->launches;
+    return KVC_OK;
+}
+
+kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
+{
+    if (!lay || !d || d->reserved != 0)
+        return KVC_ERR_INVALID_ARG;
+    const uint32_t hkv = lay->d.num_kv_heads, dim = lay->d.head_dim;
+    if (d->layer >= lay->d.num_layers || lay->d.kv_planes != 2 || lay->d.elem_bytes != 2 ||
+        (d->dtype != KVC_DTYPE_BF16 && d->dtype != KVC_DTYPE_FP16))
+        return KVC_ERR_INVALID_ARG;
+    if (dim % 8 || dim > 256 || d->rot_dim > dim || d->rot_dim % 16 || d->interleaved > 1u ||
+        !(d->eps >= 0.f) || d->n_tokens > 0x7FFFFFFFu || d->n_q_heads > 0x10000u)
+        return KVC_ERR_INVALID_ARG;
+    if (d->n_tokens == 0)
+        return KVC_OK;
+    if (!d->k || !d->v || !d->slots || (d->n_q_heads && (!d->q || !d->q_out)) ||
+        (d->rot_dim && (!d->positions || !d->cos_sin || d->cos_sin_stride < d->rot_dim)))
+        return KVC_ERR_INVALID_ARG;
+    if (!aligned(d->k, 16) || !aligned(d->v, 16) || !aligned(d->q, 16) || !aligned(d->q_out, 16) ||
+        !aligned(d->q_weight, 16) || !aligned(d->k_weight, 16) || !aligned(d->slots, 8) ||
+        !aligned(d->positions, 4) || !aligned(d->cos_sin, 4))
+        return KVC_ERR_ALIGNMENT;
+    if ((d->q_token_stride | d->q_head_stride | d->k_token_stride | d->k_head_stride | d->v_token_stride |
+         d->v_head_stride | d->out_token_stride | d->out_head_stride) % 8)
+        return KVC_ERR_ALIGNMENT;
+    kvc_status s = kvc_ensure_device(lay);
+    if (s != KVC_OK)
+        return s;
+    AppendArgs a;
+    a.q = static_cast<const unsigned char *>(d->q);
+    a.k = static_cast<const unsigned char *>(d->k);
+    a.v = static_cast<const unsigned char *>(d->v);
+    a.q_out = static_cast<unsigned char *>(d->q_out);
+    a.k_plane = const_cast<unsigned char *>(kvc_plane_ptr(lay, d->layer, 0));
+    a.v_plane = const_cast<unsigned char *>(kvc_plane_ptr(lay, d->layer, 1));
+    a.q_tok = 2 * d->q_token_stride;
+    a.q_head = 2 * d->q_head_stride;
+    a.k_tok = 2 * d->k_token_stride;
+    a.k_head = 2 * d->k_head_stride;
+    a.v_tok = 2 * d->v_token_stride;
+    a.v_head = 2 * d->v_head_stride;
+    a.o_tok = 2 * d->out_token_stride;
+    a.o_head = 2 * d->out_head_stride;
+    a.block_stride = lay->block_stride;
+    a.slots = d->slots;
+    a.positions = d->positions;
+    a.cos_sin = d->cos_sin;
+    a.cs_stride = (int64_t)d->cos_sin_stride;
+    a.q_weight = d->q_weight;
+    a.k_weight = d->k_weight;
+    a.eps = d->eps;
+    a.n_tokens = d->n_tokens;
+    a.hq = d->n_q_heads;
+    a.hkv = hkv;
+    a.d = dim;
+    a.rot = d->rot_dim;
+    a.max_pos = d->max_positions;
+    a.block_size = lay->d.block_size;
+    a.num_blocks = lay->d.num_blocks;
+    a.status = lay->d_status;
+    a.lanes = 1;
+    while (a.lanes * 8 < dim)
+        a.lanes *= 2;
+    // Heads per warp: the fewest that fill the machine's warps once -- a warp that serves more heads
+    // of its token fetches the table row once for them, one that serves fewer spreads a small call
+    // over more SMs.
+    const uint32_t heads = a.hq + 2 * hkv, teams = 32 / a.lanes;
+    const uint64_t warps = (uint64_t)lay->sm_count * 8 * (APPEND_THREADS / 32);
+    uint64_t chunk = (uint64_t)d->n_tokens * heads / warps;
+    chunk = (chunk + teams - 1) / teams * teams;
+    chunk = std::max<uint64_t>(chunk, teams);
+    a.chunk = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(chunk, 2ull * APPEND_UNROLL * teams), heads);
+    a.chunks = (heads + a.chunk - 1) / a.chunk;
+    const uint64_t units = (uint64_t)d->n_tokens * a.chunks;
+    const uint32_t per_block = APPEND_THREADS / 32;
+    const uint32_t grid = (uint32_t)std::min<uint64_t>((units + per_block - 1) / per_block, 0x7FFFFFFFull);
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e;
+    if (d->dtype == KVC_DTYPE_BF16)
+        e = d->interleaved ? kvc_launch_pdl(kvc_append_kernel<__nv_bfloat16, true>, a, dim3(grid), APPEND_THREADS, 0, st)
+                           : kvc_launch_pdl(kvc_append_kernel<__nv_bfloat16, false>, a, dim3(grid), APPEND_THREADS, 0, st);
+    else
+        e = d->interleaved ? kvc_launch_pdl(kvc_append_kernel<__half, true>, a, dim3(grid), APPEND_THREADS, 0, st)
+                           : kvc_launch_pdl(kvc_append_kernel<__half, false>, a, dim3(grid), APPEND_THREADS, 0, st);
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return KVC_ERR_CUDA;
+    }
+    ++lay->launches;
+    return KVC_OK;
+}
+
+}  // extern "C"

@@ -29,6 +29,8 @@ KVC_RING_DEVICE, KVC_RING_HOST_MAPPED, KVC_RING_DEVICE_STAGED = 0, 1, 2
 KVC_CHUNK_LAYER_MAJOR, KVC_CHUNK_BLOCK_MAJOR = 0, 1
 KVC_MAP_FULL_CHUNKS_ONLY = 1
 KVC_GROUP_FORCE_KERNEL = 0x100
+KVC_DTYPE_BF16, KVC_DTYPE_FP16 = 0, 1
+KVC_MAP_MAX_REQUESTS = 16384
 
 
 class KvcError(RuntimeError):
@@ -107,6 +109,40 @@ CHUNK_OP_DTYPE = np.dtype([("slot", np.uint64), ("ids", np.uint64), ("n_blocks",
                            ("reserved", np.uint32)])
 assert CHUNK_OP_DTYPE.itemsize == 24
 
+class kvc_map_tokens_desc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("context_lens", "new_lens", "free_blocks", "block_tables")] + \
+               [("table_stride", ctypes.c_uint64)] + \
+               [(k, ctypes.c_uint32) for k in ("max_blocks", "n_requests", "n_free", "token_capacity")] + \
+               [(k, ctypes.c_void_p) for k in ("cu_tokens", "positions", "slots", "token_request", "total_lens",
+                                               "counts")] + [("reserved", ctypes.c_uint64)]
+
+
+class kvc_append_desc(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_uint32), ("dtype", ctypes.c_uint32)] + \
+               [(k, ctypes.c_void_p) for k in ("q", "k", "v", "q_out")] + \
+               [(k, ctypes.c_int64) for k in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                              "v_token_stride", "v_head_stride", "out_token_stride",
+                                              "out_head_stride")] + \
+               [(k, ctypes.c_void_p) for k in ("slots", "positions", "cos_sin")] + \
+               [("cos_sin_stride", ctypes.c_uint64), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float)] + \
+               [(k, ctypes.c_uint32) for k in ("n_tokens", "n_q_heads", "rot_dim", "max_positions", "interleaved")] + \
+               [("reserved", ctypes.c_uint64)]
+
+
+class kvc_attention_desc(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_uint32), ("dtype", ctypes.c_uint32)] + \
+               [(k, ctypes.c_void_p) for k in ("q", "out", "lse")] + \
+               [(k, ctypes.c_int64) for k in ("q_token_stride", "q_head_stride", "out_token_stride",
+                                              "out_head_stride")] + \
+               [(k, ctypes.c_void_p) for k in ("cu_tokens", "seq_lens", "block_tables")] + \
+               [("table_stride", ctypes.c_uint64)] + \
+               [(k, ctypes.c_uint32) for k in ("max_blocks", "n_tokens", "n_requests", "n_q_heads", "max_q_len")] + \
+               [("scale", ctypes.c_float), ("window", ctypes.c_uint32), ("sinks", ctypes.c_uint32),
+                ("group_starts", ctypes.c_void_p), ("prefix_lens", ctypes.c_void_p), ("n_groups", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64)]
+
+
 _EVENT_FN = {
     "create": ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.POINTER(ctypes.c_void_p)),
     "destroy": ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p),
@@ -169,6 +205,11 @@ def lib() -> ctypes.CDLL:
         "kvc_layout_set_kernel_timing": (ci, [vp, ci]),
         "kvc_layout_kernel_time": (ci, [vp, P(u32), P(ctypes.c_double), P(ctypes.c_double),
                                         P(ctypes.c_double)]),
+        "kvc_map_tokens": (ci, [vp, P(kvc_map_tokens_desc), vp]),
+        "kvc_append": (ci, [vp, P(kvc_append_desc), vp]),
+        "kvc_attention_workspace_bytes": (ci, [vp, u32, u32, u32, u32, P(u64)]),
+        "kvc_attention": (ci, [vp, P(kvc_attention_desc), vp]),
+        "kvc_attention_shared": (ci, [vp, P(kvc_attention_desc), vp]),
         "kvc_staging_ring_create": (ci, [u64, u32, ci, vp, u64, P(vp)]),
         "kvc_staging_ring_destroy": (ci, [vp]),
         "kvc_staging_ring_acquire": (ci, [vp, i64, P(u32), P(vp), P(vp)]),
@@ -296,9 +337,10 @@ def kvc_status_str(status: int) -> str:
 class LayoutHandle:
     """Owns a ``kvc_layout*``."""
 
-    def __init__(self, handle: int, keep):
+    def __init__(self, handle: int, keep, heads: Tuple[int, int] = (0, 0)):
         self.handle = handle
         self._keep = keep
+        self.heads = heads   # (KV heads, head_dim)
 
     def __del__(self):
         try:
@@ -329,7 +371,7 @@ def kvc_layout_create(num_layers: int, kv_planes: int, num_blocks: int, block_si
     d.chunk_order = chunk_order
     out = ctypes.c_void_p()
     _check(lib().kvc_layout_create(ctypes.byref(d), ctypes.byref(out)), "kvc_layout_create")
-    return LayoutHandle(out.value, keep)
+    return LayoutHandle(out.value, keep, (num_kv_heads, head_dim))
 
 
 def kvc_layout_create_dense(pool, num_layers, kv_planes, num_blocks, block_size, num_kv_heads,
@@ -343,7 +385,7 @@ def kvc_layout_create_dense(pool, num_layers, kv_planes, num_blocks, block_size,
            "kvc_layout_desc_init_dense")
     out = ctypes.c_void_p()
     _check(lib().kvc_layout_create(ctypes.byref(d), ctypes.byref(out)), "kvc_layout_create")
-    return LayoutHandle(out.value, [pool])
+    return LayoutHandle(out.value, [pool], (num_kv_heads, head_dim))
 
 
 def kvc_layout_destroy(layout: LayoutHandle) -> None:
@@ -541,6 +583,174 @@ def kvc_poll_device_status(layout, stream=None) -> Tuple[int, int]:
     _check(lib().kvc_poll_device_status(layout.handle, _stream(stream), ctypes.byref(a),
                                         ctypes.byref(b)), "kvc_poll_device_status")
     return a.value, b.value
+
+
+# ------------------------------------------------------------------ a step's tokens
+# These calls take torch tensors and check what the C side cannot see: types, shapes, contiguity and
+# the device.  Every tensor must be on the current CUDA device.
+_dtypes = None
+
+
+def _torch_dtypes():
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {"i32": torch.int32, "i64": torch.int64, "f32": torch.float32, "cuda": torch.cuda,
+                   "kv": {torch.bfloat16: KVC_DTYPE_BF16, torch.float16: KVC_DTYPE_FP16}}
+    return _dtypes
+
+
+def _arg(t, name: str, dtype, shape, device: int, optional: bool = False) -> int:
+    """Address of a contiguous tensor of the given type and shape (None: any size) on `device`."""
+    if t is None:
+        if optional:
+            return 0
+        raise TypeError("%s is missing" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if t.get_device() != device:
+        raise ValueError("%s is not on the current CUDA device" % name)
+    if len(t.shape) != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
+        raise ValueError("%s has shape %s, wanted %s" % (name, tuple(t.shape), shape))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+def _heads(t, name: str, dtype, tokens, heads, dim, device: int):
+    """(address, token stride, head stride) of a [tokens, heads, dim] tensor with adjacent elements."""
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if t.get_device() != device:
+        raise ValueError("%s is not on the current CUDA device" % name)
+    if t.dim() != 3 or t.shape[0] != tokens or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
+        raise ValueError("%s has shape %s, wanted %s" % (name, tuple(t.shape), (tokens, heads, dim)))
+    st, sh, se = t.stride()
+    if se != 1 and dim > 1 and t.numel():
+        raise ValueError("the elements of a head of %s must be adjacent" % name)
+    # a dimension of one has no stride of its own: any will do
+    return t.data_ptr(), st if t.shape[0] > 1 else 0, sh if t.shape[1] > 1 else 0
+
+
+def _table(t, requests: int, device: int):
+    """(address, stride, entries per row) of a [requests, max_blocks] table whose rows may be apart."""
+    if t.dtype is not _torch_dtypes()["i32"]:
+        raise TypeError("block_tables must be torch.int32, not %s" % t.dtype)
+    if t.get_device() != device:
+        raise ValueError("block_tables is not on the current CUDA device")
+    if t.dim() != 2 or t.shape[0] != requests:
+        raise ValueError("block_tables has shape %s, wanted (%d, max_blocks)" % (tuple(t.shape), requests))
+    if t.shape[1] > 1 and t.stride(1) != 1 or requests > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError("the entries of a row of block_tables must be adjacent, and its rows apart")
+    return t.data_ptr(), t.stride(0) if requests > 1 else t.shape[1], t.shape[1]
+
+
+def kvc_map_tokens(layout, context_lens, new_lens, free_blocks, block_tables, cu_tokens, positions, slots,
+                   token_request=None, total_lens=None, counts=None, stream=None) -> None:
+    """Block tables, positions and slots of a step's tokens from request lengths, all on the GPU.
+
+    context_lens, new_lens [R] and free_blocks [F] are int32; block_tables [R, max_blocks] int32 is
+    completed in place; cu_tokens [R + 1] int32, positions [T] int32, slots [T] int64 and, if given,
+    token_request [T], total_lens [R] and counts [3] int32 are written."""
+    t = _torch_dtypes()
+    i32, dev = t["i32"], t["cuda"].current_device()
+    n, cap = context_lens.shape[0], positions.shape[0]
+    tab, stride, wide = _table(block_tables, n, dev)
+    d = kvc_map_tokens_desc(
+        _arg(context_lens, "context_lens", i32, (n,), dev), _arg(new_lens, "new_lens", i32, (n,), dev),
+        _arg(free_blocks, "free_blocks", i32, (None,), dev), tab, stride, wide, n, free_blocks.shape[0], cap,
+        _arg(cu_tokens, "cu_tokens", i32, (n + 1,), dev), _arg(positions, "positions", i32, (cap,), dev),
+        _arg(slots, "slots", t["i64"], (cap,), dev), _arg(token_request, "token_request", i32, (cap,), dev, True),
+        _arg(total_lens, "total_lens", i32, (n,), dev, True), _arg(counts, "counts", i32, (3,), dev, True), 0)
+    _check(lib().kvc_map_tokens(layout.handle, ctypes.byref(d), _stream(stream)), "kvc_map_tokens")
+
+
+def kvc_append(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, q_weight=None, k_weight=None,
+               eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """Norm and rotate queries and keys, write queries to q_out and keys and values to the pool's slots.
+
+    q, q_out [T, Hq, D] (or both None), k, v [T, Hkv, D]: bf16 or fp16, any token and head strides;
+    slots [T] int64; positions [T] int32 and cos_sin [max_positions, rot_dim] float32 (or both None:
+    no rotation); q_weight, k_weight [D] of the type of k, or None: no norm."""
+    t = _torch_dtypes()
+    dev, dt = t["cuda"].current_device(), k.dtype
+    if dt not in t["kv"]:
+        raise TypeError("k must be torch.bfloat16 or torch.float16, not %s" % dt)
+    n, hkv, dim = k.shape
+    if (hkv, dim) != layout.heads:
+        raise ValueError("k has %d heads of %d, the layout %d of %d" % ((hkv, dim) + layout.heads))
+    if (q is None) != (q_out is None) or (positions is None) != (cos_sin is None):
+        raise TypeError("q and q_out, and positions and cos_sin, go together")
+    qp = op = (0, 0, 0)
+    hq = 0
+    if q is not None:
+        hq = q.shape[1]
+        qp, op = _heads(q, "q", dt, n, hq, dim, dev), _heads(q_out, "q_out", dt, n, hq, dim, dev)
+    kp, vp = _heads(k, "k", dt, n, hkv, dim, dev), _heads(v, "v", dt, n, hkv, dim, dev)
+    rot = rows = cs = pos = 0
+    if cos_sin is not None:
+        pos = _arg(positions, "positions", t["i32"], (n,), dev)
+        cs = _arg(cos_sin, "cos_sin", t["f32"], (None, None), dev)
+        rows, rot = cos_sin.shape
+    d = kvc_append_desc(layer, t["kv"][dt], qp[0], kp[0], vp[0], op[0], qp[1], qp[2], kp[1], kp[2], vp[1], vp[2],
+                        op[1], op[2], _arg(slots, "slots", t["i64"], (n,), dev), pos, cs, rot,
+                        _arg(q_weight, "q_weight", dt, (dim,), dev, True),
+                        _arg(k_weight, "k_weight", dt, (dim,), dev, True), eps, n, hq, rot, rows, int(interleaved), 0)
+    _check(lib().kvc_append(layout.handle, ctypes.byref(d), _stream(stream)), "kvc_append")
+
+
+def kvc_attention_workspace_bytes(layout, n_tokens: int, n_requests: int, n_q_heads: int, n_groups: int = 0) -> int:
+    """Bytes of workspace for calls of at most these sizes (n_groups = 0: kvc_attention)."""
+    out = ctypes.c_uint64()
+    _check(lib().kvc_attention_workspace_bytes(layout.handle, n_tokens, n_requests, n_q_heads, n_groups,
+                                               ctypes.byref(out)), "kvc_attention_workspace_bytes")
+    return out.value
+
+
+def _attention(name, layout, layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, window, sinks, lse,
+               max_q_len, group_starts, prefix_lens, stream):
+    t = _torch_dtypes()
+    i32, dev, dt = t["i32"], t["cuda"].current_device(), q.dtype
+    if dt not in t["kv"]:
+        raise TypeError("q must be torch.bfloat16 or torch.float16, not %s" % dt)
+    n, hq, dim = q.shape
+    if dim != layout.heads[1]:
+        raise ValueError("q has heads of %d, the layout of %d" % (dim, layout.heads[1]))
+    r = seq_lens.shape[0]
+    tab, stride, wide = _table(block_tables, r, dev)
+    qp, op = _heads(q, "q", dt, n, hq, dim, dev), _heads(out, "out", dt, n, hq, dim, dev)
+    groups = 0 if prefix_lens is None else prefix_lens.shape[0]
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
+    d = kvc_attention_desc(
+        layer, t["kv"][dt], qp[0], op[0], _arg(lse, "lse", t["f32"], (n, hq), dev, True), qp[1], qp[2], op[1], op[2],
+        _arg(cu_tokens, "cu_tokens", i32, (r + 1,), dev), _arg(seq_lens, "seq_lens", i32, (r,), dev), tab, stride, wide,
+        n, r, hq, max_q_len, dim ** -0.5 if scale is None else scale, window, sinks,
+        _arg(group_starts, "group_starts", i32, (groups + 1,), dev, not groups),
+        _arg(prefix_lens, "prefix_lens", i32, (groups,), dev, not groups), groups, 0, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size())
+    _check(getattr(lib(), name)(layout.handle, ctypes.byref(d), _stream(stream)), name)
+
+
+def kvc_attention(layout, layer: int, q, out, block_tables, seq_lens, cu_tokens, workspace, scale=None, window: int = 0,
+                  sinks: int = 0, lse=None, max_q_len: int = 0, stream=None) -> None:
+    """Causal attention over the paged pool, with an optional sliding window and first tokens that
+    stay visible.
+
+    q, out [T, Hq, D] bf16 or fp16; block_tables [R, max_blocks], seq_lens [R], cu_tokens [R + 1]
+    int32; lse [T, Hq] float32 or None; workspace: a tensor of at least
+    kvc_attention_workspace_bytes.  scale defaults to D ** -0.5; max_q_len is a hint, the most query
+    rows of one request (0: unknown)."""
+    _attention("kvc_attention", layout, layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, window,
+               sinks, lse, max_q_len, None, None, stream)
+
+
+def kvc_attention_shared(layout, layer: int, q, out, block_tables, seq_lens, cu_tokens, group_starts, prefix_lens,
+                         workspace, scale=None, lse=None, max_q_len: int = 0, stream=None) -> None:
+    """kvc_attention for groups of requests with a common prefix, whose keys and values are read once
+    per group: group_starts [G + 1] and prefix_lens [G] int32."""
+    _attention("kvc_attention_shared", layout, layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, 0, 0,
+               lse, max_q_len, group_starts, prefix_lens, stream)
 
 
 # ------------------------------------------------------------------ staging ring
