@@ -220,11 +220,19 @@ struct Carver {
     }
 };
 
-// The parts that a kernel of `blocks` blocks and `rows` rows a pair can leave.  With `pairs` == 0: at
-// most two a block.  Otherwise every pair leaves its parts: run + pair is a slot of its own, since
-// along the order of units each new part has a larger run or a larger pair.
-void carve(Carver &c, KvcParts &p, uint32_t blocks, uint32_t rows, uint32_t head_dim, uint64_t pairs, uint64_t sequences)
+// The parts that the kernel for many rows (tiles) or few can leave.  With whole sequences: at most two
+// a block.  By pair, every pair leaves its parts: run + pair is a slot of its own, since along the
+// order of units each new part has a larger run or a larger pair.
+struct Shape {
+    uint32_t head_dim, hkv, g;
+    uint64_t tokens, requests, groups;
+};
+
+void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, bool tiles, uint64_t sequences, bool by_pair)
 {
+    const uint32_t blocks = tiles ? kvc_attn_tiles_blocks(lay) : kvc_attn_rows_blocks(lay);
+    const uint32_t rows = tiles ? KVC_ATTN_TILE_ROWS : KVC_ATTN_SMALL_ROWS, head_dim = s.head_dim;
+    const uint64_t pairs = by_pair ? kvc_max_pairs(sequences, s.tokens, s.g, s.hkv, rows) : 0;
     const uint64_t slots = pairs ? (uint64_t)blocks + pairs : 2ull * blocks;
     memset(&p, 0, sizeof(p));
     p.blocks = blocks;
@@ -241,20 +249,17 @@ void carve(Carver &c, KvcParts &p, uint32_t blocks, uint32_t rows, uint32_t head
     }
 }
 
-struct Shape {
-    uint32_t head_dim, hkv, g;
-    uint64_t tokens, requests, groups;
-};
-
 // Bytes of the parts of one phase, for either kernel that may serve it.
 uint64_t phase_bytes(const kvc_layout *lay, const Shape &s, uint64_t sequences, bool pairs)
 {
-    KvcParts p;
-    Carver c = {nullptr, 0};
-    const uint32_t rows = KVC_ATTN_SMALL_ROWS;
-    carve(c, p, kvc_attn_rows_blocks(lay), rows, s.head_dim, pairs ? kvc_max_pairs(sequences, s.tokens, s.g, s.hkv, rows) : 0,
-          sequences);
-    return c.used;
+    uint64_t most = 0;
+    for (const bool tiles : {false, true}) {
+        KvcParts p;
+        Carver c = {nullptr, 0};
+        carve(c, p, lay, s, tiles, sequences, pairs);
+        most = std::max(most, c.used);
+    }
+    return most;
 }
 
 uint64_t workspace_bytes(const kvc_layout *lay, const Shape &s)
@@ -363,33 +368,42 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     cudaStream_t st = (cudaStream_t)stream;
     const bool bf16 = d->dtype == KVC_DTYPE_BF16, wide = l.head_dim == 128;
     Carver c = {static_cast<unsigned char *>(d->workspace), 0};
-    const uint32_t rows = KVC_ATTN_SMALL_ROWS, blocks = kvc_attn_rows_blocks(lay);
+    // Sixteen rows or fewer fit the kernel for few rows, which reads the keys once for them; with more
+    // it would read them once for every sixteen, and the matrix unit takes over.
+    const uint64_t q_len = std::min<uint64_t>(d->max_q_len ? d->max_q_len : d->n_tokens, d->n_tokens);
+    const bool many = q_len * a.g > KVC_ATTN_SMALL_ROWS;
+    const auto launch = [&](bool tiles) {
+        ++lay->launches;
+        return tiles ? kvc_launch_attn_tiles(a, d->dtype, l.head_dim, a.parts.blocks, st)
+                     : kvc_launch_attn_rows(a, d->dtype, l.head_dim, a.parts.blocks, st);
+    };
     cudaError_t e;
     if (!shared) {
         a.phase = KVC_PHASE_WHOLE;
-        carve(c, a.parts, blocks, rows, l.head_dim, 0, d->n_requests);
-        e = kvc_launch_attn_rows(a, d->dtype, l.head_dim, blocks, st);
+        carve(c, a.parts, lay, shape, many, d->n_requests, false);
+        e = launch(many);
         if (e == cudaSuccess)
             e = bf16 ? (wide ? join_split<__nv_bfloat16, 128>(a, st) : join_split<__nv_bfloat16, 64>(a, st))
                      : (wide ? join_split<__half, 128>(a, st) : join_split<__half, 64>(a, st));
-        lay->launches += 2;
     } else {
         JoinShared j;
+        // a group has at least as many rows as a request, and usually several requests
+        const bool many_prefix = std::max<uint64_t>(q_len, (d->n_tokens + d->n_groups - 1) / d->n_groups) * a.g > KVC_ATTN_SMALL_ROWS;
         a.phase = KVC_PHASE_PREFIX;
-        carve(c, a.parts, blocks, rows, l.head_dim, kvc_max_pairs(d->n_groups, d->n_tokens, a.g, a.hkv, rows), d->n_groups);
+        carve(c, a.parts, lay, shape, many_prefix, d->n_groups, true);
         j.prefix = a.parts;
-        e = kvc_launch_attn_rows(a, d->dtype, l.head_dim, blocks, st);
+        e = launch(many_prefix);
         a.phase = KVC_PHASE_SUFFIX;
-        carve(c, a.parts, blocks, rows, l.head_dim, kvc_max_pairs(d->n_requests, d->n_tokens, a.g, a.hkv, rows), d->n_requests);
+        carve(c, a.parts, lay, shape, many, d->n_requests, true);
         j.suffix = a.parts;
         if (e == cudaSuccess)
-            e = kvc_launch_attn_rows(a, d->dtype, l.head_dim, blocks, st);
+            e = launch(many);
         j.a = a;
         if (e == cudaSuccess)
             e = bf16 ? (wide ? join_shared<__nv_bfloat16, 128>(j, st) : join_shared<__nv_bfloat16, 64>(j, st))
                      : (wide ? join_shared<__half, 128>(j, st) : join_shared<__half, 64>(j, st));
-        lay->launches += 3;
     }
+    ++lay->launches;
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return KVC_ERR_CUDA;

@@ -14,10 +14,13 @@
 
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "kvc_device.h"
 #include "kvc_internal.h"
 
-#define KVC_ATTN_SMALL_ROWS 16u  // rows of a pair in the kernel for few rows
+#define KVC_ATTN_SMALL_ROWS 16u   // rows of a pair in the kernel for few rows
+#define KVC_ATTN_TILE_ROWS 256u   // and in the kernel for many
 
 enum {
     KVC_PHASE_WHOLE = 0,   // sequences are requests, all of their keys
@@ -77,6 +80,8 @@ inline uint64_t kvc_max_pairs(uint64_t sequences, uint64_t tokens, uint64_t g, u
 // Implemented in kvc_attention_rows.cu (few rows) and kvc_attention_tiles.cu (many).
 uint32_t kvc_attn_rows_blocks(const kvc_layout *lay);
 cudaError_t kvc_launch_attn_rows(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
+uint32_t kvc_attn_tiles_blocks(const kvc_layout *lay);
+cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
 
 #ifdef __CUDACC__
 
@@ -233,10 +238,12 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
     const uint32_t per = (n_seq + THREADS - 1) / THREADS;
     const uint32_t s0 = min(threadIdx.x * per, n_seq), s1 = min(s0 + per, n_seq);
     unsigned long long units = 0, pairs = 0;
+#pragma unroll 1
     for (uint32_t s = s0; s < s1; ++s) {
         const KvcSeq q = kvc_seq(a, s);
         unsigned long long sum = 0;
         uint32_t n = 0;
+#pragma unroll 1
         for (uint32_t rt = 0; rt * ROWS < (uint32_t)q.rows; ++rt, ++n)
             sum += kvc_range<ROWS, TK>(a, q, rt).n;
         units += sum * a.hkv;
@@ -279,12 +286,14 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
     const bool table = a.phase != KVC_PHASE_WHOLE && blockIdx.x == 0;
     if (mine || table) {
         unsigned long long u = bu, p = bp;
+#pragma unroll 1
         for (uint32_t s = s0; s < s1; ++s) {
             if (table)
                 a.parts.base[s] = (uint32_t)min(p, 0xFFFFFFFFull);
             const KvcSeq q = kvc_seq(a, s);
             unsigned long long per_head = 0;
             uint32_t n = 0;
+#pragma unroll 1
             for (uint32_t rt = 0; rt * ROWS < (uint32_t)q.rows; ++rt, ++n)
                 per_head += kvc_range<ROWS, TK>(a, q, rt).n;
             if (mine && begin >= u && begin < u + per_head * a.hkv) {
@@ -292,6 +301,7 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
                 unsigned long long b = u + h * per_head;
                 KvcRange r;
                 uint32_t rt = 0;
+#pragma unroll 1
                 for (;; ++rt) {
                     r = kvc_range<ROWS, TK>(a, q, rt);
                     if (begin < b + r.n)
@@ -338,12 +348,12 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
 
 // The position of a row, for the mask.  In the PREFIX phase the rows of a group belong to several
 // requests, and the row's own is looked up.
-__device__ __forceinline__ int32_t kvc_row_pos(const KvcAttn &a, const KvcCursor &c, uint32_t row)
+__device__ __forceinline__ int32_t kvc_row_pos(const KvcAttn &a, const KvcSeq &q, uint32_t row)
 {
     const int32_t tok = (int32_t)(row / a.g);
     if (a.phase != KVC_PHASE_PREFIX)
-        return c.q.pos + tok;
-    const int32_t t = c.q.qa + tok;
+        return q.pos + tok;
+    const int32_t t = q.qa + tok;
     const uint32_t r = kvc_last_at_most(a.cu_q, a.n_requests, t);
     const int32_t qa = a.cu_q[r], n = kvc_clamp(a.cu_q[r + 1], qa, (int32_t)a.n_tokens) - qa;
     return max(a.seq_lens[r], 0) - n + (t - qa);

@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
             const unsigned char *src = a.q;
             pos[half] = -1;
             if (real[half]) {
-                pos[half] = kvc_row_pos(a, c, row);
+                pos[half] = kvc_row_pos(a, c.q, row);
                 src += (int64_t)(c.q.qa + (int32_t)(row / a.g)) * a.q_tok + (int64_t)(c.h * a.g + row % a.g) * a.q_head;
             }
 #pragma unroll

@@ -1,0 +1,834 @@
+// Attention over the paged pool for many query rows (prompts, and the shared prefix of a group): tiles
+// of 256 rows against tiles of 128 keys on the fifth-generation tensor cores.
+//
+// Per row: s_j = scale * q . k_j, o = sum_j 2^(s_j' - m) v_j / sum_j 2^(s_j' - m), s' in base 2; one pass
+// with the running maximum and sum of a softmax in 32 bits.
+//
+// One block a SM, specialised by warp:
+//   warps 0-3, 4-7  softmax of rows 0-127 and 128-255, a row a thread: read S from tensor memory, take
+//                   the maximum, write the weights P (pool's type) over S, keep m and l in registers;
+//                   at the end of a pair read O and write the result.  They also load the queries.
+//   warp 8          one thread issues the matrix instructions: S = Q K^T from shared memory, O += P V
+//                   with P from tensor memory and V as it lies (keys x head, so head-major for this product)
+//   warps 9, 10     load K and V tiles through the block table into rings of shared-memory stages, in the
+//                   128-byte swizzle that the matrix unit reads: a tensor copy for the keys of each block, or
+//                   16-byte asynchronous copies where a tile is not made of whole blocks
+//   warp 11         one thread walks the run's pairs and hands them to the others
+// Two row tiles share each K and V tile, and while one is in its softmax the other's products run.
+// Bound by the exponentials and the matrix unit alike: 128 x 128 scores take 1024 cycles on each.
+// O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use: weights are then
+// at most 2^8, which neither type nor the 32-bit sums mind, and almost all tiles skip the rescaling.
+// Every wait is bounded; one that gives up makes all roles leave and is counted.
+#include <cuda.h>
+#include <stddef.h>
+#include <string.h>
+
+#include "kvc_attention.h"
+
+namespace {
+
+constexpr int ROWS = KVC_ATTN_TILE_ROWS;
+constexpr int TK = 128;
+constexpr int THREADS = 384;
+constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper than the K ring
+
+template <int D>
+struct Shape {
+    static constexpr int TILE = TK * D * 2;           // a K or V tile; also half of the queries
+    static constexpr int HALF = TK * 128;             // 64 elements (128 bytes) of 128 rows
+    static constexpr int KS = D == 128 ? 3 : 4, VS = D == 128 ? 2 : 4;
+    static constexpr int Q = 0, K = 2 * TILE, V = K + KS * TILE, END = V + VS * TILE;
+    static constexpr int SMEM = END + 1024;           // room to align the stages to the swizzle's 1024 bytes
+};
+
+// tensor memory columns
+constexpr uint32_t COL_S = 0, COL_O = 256, COLS = 512;
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void bar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+
+// Bounded wait.  `dead` is set by the first wait of the block that gives up, and ends the others.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *dead, uint32_t *status)
+{
+    if (bar_try(bar, parity))
+        return true;
+#pragma unroll 1
+    for (uint32_t i = 0; i < KVC_WAIT_LIMIT; ++i) {
+        if (bar_try(bar, parity))
+            return true;
+        if (*dead)
+            return false;
+    }
+    if (!atomicExch(const_cast<uint32_t *>(dead), 1u))
+        atomicAdd(status + 1, 1u);
+    return false;
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// Shared-memory operand: 128-byte swizzle, 8-row groups 1024 bytes apart along the rows (or keys), and,
+// where the other dimension is the contiguous one, its 64-element blocks `lead` bytes apart.
+// The low word is built once for each buffer; a place inside one is 16 bytes a step away, and no sum
+// carries, since shared memory ends below the field's 2^18 bytes.
+constexpr uint32_t OPERAND_HIGH = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t operand(uint32_t addr, uint32_t lead) { return (addr >> 4) | ((lead >> 4) << 16); }
+
+// Instruction descriptor: 32-bit sums, both operands of type T, M = 128, N = n; b_by_column: B's n is contiguous.
+template <typename T>
+__host__ __device__ constexpr uint32_t kind(uint32_t n, bool b_by_column)
+{
+    const uint32_t f = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+    return (1u << 4) | (f << 7) | (f << 10) | ((b_by_column ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(what), "r"((uint32_t)add), "r"(OPERAND_HIGH) : "memory");
+}
+
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "mov.b64 db, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(what), "r"((uint32_t)add), "r"(OPERAND_HIGH) : "memory");
+}
+
+// The barrier is arrived at once when all matrix instructions issued so far have completed.
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld32(float *x, uint32_t addr)
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(x);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr) : "memory");
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const float *x)
+{
+    const uint32_t *r = reinterpret_cast<const uint32_t *>(x);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+                 "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+                 : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+
+// Two 32-bit floats in one 64-bit register pair, for the two-wide arithmetic.
+__device__ __forceinline__ uint64_t pair2(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpair2(uint64_t v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// A word whose lowest n bits are set (n < 0: none, n > 31: all).
+__device__ __forceinline__ uint32_t low_bits(int32_t n) { return n <= 0 ? 0u : n > 31 ? ~0u : (1u << n) - 1u; }
+
+struct Bars {
+    uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];  // p_full: of each half of the keys
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+    uint64_t seg_full[4], seg_empty[4], drained;
+};
+
+// The units of one pair in the block's run, as the scheduling warp hands them to the others: what lies
+// between pairs is then in the code once and not in every role.
+struct Segment {
+    KvcSeq q;
+    KvcRange r;
+    uint32_t h, rt, t, n;  // KV head, row tile; first tile and number of tiles (0: the run is over)
+    uint32_t pair;
+    unsigned long long pair_begin;
+};
+constexpr uint32_t SEGMENTS = 4;
+constexpr uint32_t SEGMENT_READERS = 11;  // 8 softmax warps, 2 loading warps, the issuing thread
+
+// The next segment, copied to registers.  Every lane of the role's warp calls this (or the one thread).
+struct SegmentReader {
+    uint32_t slot = 0, parity = 0;
+    template <bool WARP>
+    __device__ __forceinline__ bool next(const Segment *ring, Bars *bars, Segment &out, volatile uint32_t *dead, uint32_t *status)
+    {
+        bool ok = bar_wait(smem_addr(&bars->seg_full[slot]), parity, dead, status);
+        if (WARP)
+            ok = __all_sync(~0u, ok);
+        if (!ok)
+            return false;
+        out = ring[slot];
+        if (WARP)
+            __syncwarp();
+        if (!WARP || (threadIdx.x & 31u) == 0)
+            bar_arrive(smem_addr(&bars->seg_empty[slot]));
+        if (++slot == SEGMENTS) {
+            slot = 0;
+            parity ^= 1;
+        }
+        return out.n != 0;
+    }
+};
+
+#define BAR(name) ((uint32_t)offsetof(Bars, name))
+
+// A role's count of uses of a ring: stage and parity.
+template <int N>
+struct Ring {
+    uint32_t stage = 0, parity = 0;
+    __device__ void next()
+    {
+        if (++stage == N) {
+            stage = 0;
+            parity ^= 1;
+        }
+    }
+};
+
+// The launch's parameters: with `boxes` != 0 a tile's keys come in that many boxes of box_keys keys, each
+// inside one block of the pool, through a tensor map of the plane.
+struct alignas(64) TilesArgs {
+    CUtensorMap k_map, v_map;  // [block][token][head][element], boxes of [1][box_keys][1][64]
+    KvcAttn a;
+    uint32_t boxes, box_keys;
+};
+
+__device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap *map, uint32_t x, uint32_t head, uint32_t tok, uint32_t block,
+                                         uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(head), "r"(tok), "r"(block), "r"(bar) : "memory");
+}
+
+// One of the two loading warps: all tiles of the block's run, K or V.  A tile comes as boxes, a lane a
+// box, where blocks and tiles divide one another.  What is not a key's may be garbage in K, whose scores
+// are replaced; in V it meets a weight of zero, which infinity or NaN would survive, so a tile of V that is
+// not all keys is copied key by key, with zeros between.
+template <int D, bool KEYS>
+__device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *segments, uint32_t tiles, Bars *bars,
+                                          uint32_t (*there)[4], volatile uint32_t *dead, uint32_t lane)
+{
+    using S = Shape<D>;
+    constexpr int STAGES = KEYS ? S::KS : S::VS;
+    constexpr int PER = 512 / (D * 2);  // keys per round of 32 lanes
+    const KvcAttn &a = args.a;
+    uint64_t *full = KEYS ? bars->k_full : bars->v_full, *empty = KEYS ? bars->k_empty : bars->v_empty;
+    SegmentReader reader;
+    Segment c;
+    Ring<STAGES> ring;
+    uint32_t slot = 0, issued = 0;
+    bool ok = true;
+#pragma unroll 1
+    while (ok && reader.next<true>(segments, bars, c, dead, a.status))
+#pragma unroll 1
+    for (uint32_t u = 0; u < c.n; ++u) {
+        const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + u) * TK);
+        const auto key = [&](int32_t j) { return j < c.r.hi && (j >= c.r.lo || j < c.r.sink_end); };
+        bool boxed = args.boxes != 0;
+        uint32_t id = 0, tok = 0;
+        bool have = false;  // this lane's box holds keys
+        if (boxed) {
+            // lane i < boxes: block j / B; the lanes after them the same boxes' second 64 elements
+            const uint32_t box = lane % args.boxes;
+            const int32_t jb = j0 + (int32_t)(box * args.box_keys), je = jb + (int32_t)args.box_keys;
+            if (jb < c.r.hi && (je > c.r.lo || jb < c.r.sink_end)) {
+                const uint32_t block = (uint32_t)jb / a.block_size;
+                tok = (uint32_t)jb - block * a.block_size;
+                id = (uint32_t)a.tables[(int64_t)c.q.table * a.table_stride + block];
+                have = id < a.num_blocks;
+                if (KEYS && !have && lane < args.boxes)
+                    atomicAdd(a.status, 1u);
+            }
+            const uint32_t good = __ballot_sync(~0u, have);
+            if (KEYS) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t at = i * 32 + lane;
+                    const uint32_t w = __ballot_sync(~0u, key(j0 + (int32_t)at) && (good >> (at / args.box_keys) & 1u));
+                    if (lane == 0)
+                        there[slot][i] = w;
+                }
+            } else {
+                // keys that other rows of the call see are as good as this pair's own
+                const int32_t end = a.phase == KVC_PHASE_PREFIX ? c.r.hi : min(c.q.pos + c.q.rows / (int32_t)a.g, kvc_key_cap(a));
+                boxed = (j0 >= c.r.lo && j0 + TK <= end) || j0 + TK <= c.r.sink_end;
+                if (boxed) {  // boxes past this pair's last key
+                    const int32_t last = j0 + (int32_t)((lane % args.boxes) * args.box_keys);
+                    if (last >= c.r.hi) {
+                        const uint32_t block = (uint32_t)last / a.block_size;
+                        tok = (uint32_t)last - block * a.block_size;
+                        id = (uint32_t)a.tables[(int64_t)c.q.table * a.table_stride + block];
+                        have = id < a.num_blocks;
+                    }
+                    boxed = __all_sync(~0u, have);
+                }
+            }
+        }
+        int64_t off[4];
+        if (!boxed) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t j = j0 + i * 32 + (int32_t)lane;
+                off[i] = -1;
+                if (key(j)) {
+                    off[i] = kvc_key_offset(a, c.q.table, j, c.h, D * 2);
+                    if (KEYS && off[i] < 0)
+                        atomicAdd(a.status, 1u);
+                }
+                if (KEYS) {
+                    const uint32_t w = __ballot_sync(~0u, off[i] >= 0);
+                    if (lane == 0)
+                        there[slot][i] = w;
+                }
+            }
+        }
+        slot = (slot + 1) % THERE;
+        if (!(ok = __all_sync(~0u, bar_wait(smem_addr(&empty[ring.stage]), ring.parity ^ 1u, dead, a.status))))
+            break;
+        const uint32_t tile = tiles + ring.stage * S::TILE, bar = smem_addr(&full[ring.stage]);
+        if (boxed) {
+            const uint32_t n = __popc(__ballot_sync(~0u, have && lane < args.boxes));
+            // (the words of `there` are ordered before the barrier's phase by lane 0's arrival)
+            if (lane == 0)
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * args.box_keys * (uint32_t)D * 2u)
+                             : "memory");
+            __syncwarp();
+            if (have && lane < args.boxes * (D / 64)) {
+                const uint32_t half = lane / args.boxes, box = lane - half * args.boxes;
+                box_load(tile + half * S::HALF + box * args.box_keys * 128u, KEYS ? &args.k_map : &args.v_map, half * 64u, c.h, tok, id, bar);
+            }
+        } else {
+            const unsigned char *plane = KEYS ? a.k : a.v;
+            const uint32_t chunk = lane % (D / 8), sub = lane / (D / 8);
+            const uint32_t base = tile + (chunk >> 3) * S::HALF;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll 4
+                for (int i = 0; i < 32 / PER; ++i) {
+                    const uint32_t row = i * PER + sub;
+                    const int64_t o = __shfl_sync(~0u, off[q], row);
+                    copy16(base + (q * 32 + row) * 128u + (((chunk & 7u) ^ (row & 7u)) << 4), plane + (o >= 0 ? o : 0) + chunk * 16u,
+                           o >= 0 ? 16u : 0u);
+                }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_async();
+            __syncwarp();
+            if (lane == 0)
+                bar_arrive(bar);
+        }
+        ring.next();
+        ++issued;
+    }
+    // no copy of ours runs on when the block ends, on no way out
+#pragma unroll 1
+    for (uint32_t n = issued < STAGES ? 0u : issued - STAGES; n < issued; ++n)
+#pragma unroll 1
+        for (uint32_t i = 0; i < KVC_WAIT_LIMIT && !bar_try(smem_addr(&full[n % STAGES]), n / STAGES & 1u); ++i)
+            ;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid_constant__ TilesArgs args)
+{
+    using S = Shape<D>;
+    const KvcAttn &a = args.a;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Bars bars;
+    __shared__ uint32_t there[THERE][4];
+    __shared__ uint32_t s_dead, s_tmem;
+    __shared__ Segment segments[SEGMENTS];
+    kvc_pdl_wait();
+
+    const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
+    const KvcRun run = kvc_find_run<ROWS, TK, THREADS>(a, n_seq);
+    if (run.begin >= run.end)
+        return;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t tiles = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    unsigned char *tiles_ptr = smem_raw + (tiles - smem_addr(smem_raw));
+    volatile uint32_t *dead = &s_dead;
+    if (threadIdx.x == 0) {
+        s_dead = 0;
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_addr(&bars.q_full[i]), 128);
+            bar_init(smem_addr(&bars.s_full[i]), 1);
+            bar_init(smem_addr(&bars.p_full[i][0]), 128);
+            bar_init(smem_addr(&bars.p_full[i][1]), 128);
+            bar_init(smem_addr(&bars.o_done[i]), 1);
+        }
+        for (int i = 0; i < 4; ++i) {
+            bar_init(smem_addr(&bars.k_full[i]), 1);
+            bar_init(smem_addr(&bars.k_empty[i]), 1);
+            bar_init(smem_addr(&bars.v_full[i]), 1);
+            bar_init(smem_addr(&bars.v_empty[i]), 1);
+            bar_init(smem_addr(&bars.seg_full[i]), 1);
+            bar_init(smem_addr(&bars.seg_empty[i]), SEGMENT_READERS);
+        }
+        bar_init(smem_addr(&bars.drained), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8)
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(COLS) : "memory");
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = s_tmem;
+
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        // ---------------------------------------------------------------- softmax
+        const uint32_t sub = warp >> 2, tid = threadIdx.x & 127u;
+        const uint32_t lanes = (warp & 3u) << 21;  // this warp's 32 rows of tensor memory
+        const uint32_t s_col = tmem + COL_S + sub * 128u + lanes, o_col = tmem + COL_O + sub * 128u + lanes;
+        SegmentReader reader;
+        Segment c;
+        uint32_t s_parity = 0, o_parity = 0, slot = 0;
+        const uint32_t bar = smem_addr(&bars);
+        const uint32_t s_full = bar + BAR(s_full) + sub * 8u, p_full = bar + BAR(p_full) + sub * 16u, o_done = bar + BAR(o_done) + sub * 8u;
+        bool ok = true;
+        while (ok && reader.next<true>(segments, &bars, c, dead, a.status)) {
+            const uint32_t row0 = c.rt * ROWS + sub * 128u, rows_all = (uint32_t)c.q.rows;
+            const uint32_t n_units = c.n;
+            const bool from_start = c.t == 0, to_end = c.t + n_units == c.r.n;
+            if (row0 < rows_all) {
+                // queries: 16 bytes a thread and turn, rows of 128 bytes in the swizzle
+                constexpr uint32_t STEP = 128u / (D / 8), TURNS = 128u / STEP;
+                const uint32_t chunk = tid % (D / 8), r0 = tid / (D / 8);
+                uint32_t tok = (row0 + r0) / a.g, head = row0 + r0 - tok * a.g;
+                const uint32_t tok_step = STEP / a.g, head_step = STEP - tok_step * a.g;
+                const unsigned char *src = a.q + (int64_t)c.q.qa * a.q_tok + (int64_t)(c.h * a.g) * a.q_head + chunk * 16u;
+                unsigned char *dst = tiles_ptr + S::Q + sub * S::TILE + (chunk >> 3) * S::HALF;
+#pragma unroll
+                for (uint32_t t = 0; t < TURNS; t += 8) {
+                    uint4 x[8];
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e) {
+                        x[e] = row0 + r0 + (t + e) * STEP < rows_all
+                                   ? *reinterpret_cast<const uint4 *>(src + (int64_t)tok * a.q_tok + (int64_t)head * a.q_head)
+                                   : make_uint4(0, 0, 0, 0);
+                        tok += tok_step;
+                        head += head_step;
+                        if (head >= a.g) {
+                            head -= a.g;
+                            ++tok;
+                        }
+                    }
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e) {
+                        const uint32_t r = r0 + (t + e) * STEP;
+                        *reinterpret_cast<uint4 *>(dst + r * 128u + (((chunk & 7u) ^ (r & 7u)) << 4)) = x[e];
+                    }
+                }
+                fence_async();
+                bar_arrive(smem_addr(&bars.q_full[sub]));
+
+                const bool real = row0 + tid < rows_all;
+                const int32_t pos = real ? kvc_row_pos(a, c.q, row0 + tid) : -1;
+                float m = -INFINITY, l = 0.f;  // m: the maximum in use, base 2
+#pragma unroll 1
+                for (uint32_t i = 0; i < n_units; ++i) {
+                    const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + i) * TK);
+                    if (!(ok = __all_sync(~0u, bar_wait(s_full, s_parity, dead, a.status))))
+                        break;
+                    s_parity ^= 1;
+                    fence_after();
+                    float s[TK];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        tmem_ld32(s + q * 32, s_col + q * 32);
+                    uint32_t mask[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        mask[q] = *const_cast<volatile uint32_t *>(&there[(slot + i) % THERE][q]);
+                    tmem_wait_ld();
+                    const bool all = (mask[0] & mask[1] & mask[2] & mask[3]) == ~0u && j0 + TK - 1 <= pos &&
+                                     (a.window == 0 || pos - j0 < a.window || j0 + TK - 1 < a.sinks);
+                    if (__any_sync(~0u, !all)) {
+                        // kvc_sees() for 32 keys at a time: at most pos, and after pos - window or before sinks
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int32_t j = j0 + q * 32;
+                            uint32_t see = mask[q] & low_bits(pos + 1 - j);
+                            if (a.window)
+                                see &= ~low_bits(pos - a.window + 1 - j) | low_bits(a.sinks - j);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                s[q * 32 + k] = see >> k & 1u ? s[q * 32 + k] : -INFINITY;
+                        }
+                    }
+                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int k = 0; k < TK; k += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            t[e] = fmaxf(t[e], fmaxf(s[k + e], s[k + 4 + e]));
+                    const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * a.scale_log2;
+                    if (i == 0) {
+                        m = top;
+                    } else {
+                        const bool move = top > m + 8.f || (m == -INFINITY && top != m);
+                        if (__any_sync(~0u, move)) {
+                            const float f = !move ? 1.f : m == -INFINITY ? 0.f : exp2_fast(m - top);
+                            if (move)
+                                m = top;
+                            l *= f;
+                            // the products so far have to be in O before it is scaled
+                            if (!(ok = __all_sync(~0u, bar_wait(o_done, o_parity ^ 1u, dead, a.status))))
+                                break;
+                            fence_after();
+#pragma unroll 1
+                            for (int q = 0; q < D; q += 32) {
+                                float o[32];
+                                tmem_ld32(o, o_col + q);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k)
+                                    o[k] *= f;
+                                tmem_st32(o_col + q, o);
+                            }
+                        }
+                    }
+                    const float base = m == -INFINITY ? 0.f : m;
+                    const uint64_t scale2 = pair2(a.scale_log2, a.scale_log2), base2 = pair2(-base, -base);
+                    uint64_t sum2 = 0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float2 x = unpair2(fma2(pair2(s[q * 32 + 2 * k], s[q * 32 + 2 * k + 1]), scale2, base2));
+                            const float y0 = exp2_fast(x.x), y1 = exp2_fast(x.y);
+                            sum2 = add2(sum2, pair2(y0, y1));
+                            p[k] = kvc_from_float2<T>(y0, y1);
+                        }
+                        tmem_st16(s_col + q * 16, p);
+                        if (q & 1) {  // half of the weights: its products can start
+                            tmem_wait_st();
+                            fence_before();
+                            bar_arrive(p_full + (q >> 1) * 8u);
+                        }
+                    }
+                    const float2 sum = unpair2(sum2);
+                    l += sum.x + sum.y;
+                    o_parity ^= 1;  // flips with every product that this arrival lets start
+                }
+                if (!ok)
+                    break;
+                if (!(ok = __all_sync(~0u, bar_wait(o_done, o_parity ^ 1u, dead, a.status))))
+                    break;
+                fence_after();
+                const uint32_t i = row0 + tid;
+                if (a.phase == KVC_PHASE_WHOLE && from_start && to_end) {
+                    const uint32_t tok = i / a.g;
+                    const uint32_t head = c.h * a.g + (i - tok * a.g);
+                    const int64_t row = c.q.qa + (int32_t)tok;
+                    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
+                    unsigned char *dst = a.out + row * a.o_tok + (int64_t)head * a.o_head;
+#pragma unroll 1
+                    for (int q = 0; q < D; q += 32) {
+                        float o[32];
+                        tmem_ld32(o, o_col + q);
+                        tmem_wait_ld();
+                        if (real)
+#pragma unroll
+                            for (int k = 0; k < 32; k += 8) {
+                                float x[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    x[e] = l == 0.f ? 0.f : o[k + e] * inv;
+                                *reinterpret_cast<uint4 *>(dst + (q + k) * 2) = kvc_pack8<T>(x);
+                            }
+                    }
+                    if (real && a.lse)
+                        a.lse[row * a.hq + head] = (m + log2f(l)) * 0.693147180559945309f;
+                } else {
+                    const bool room = a.phase == KVC_PHASE_WHOLE || c.pair < a.parts.max_pairs;
+                    const uint64_t at = (a.phase == KVC_PHASE_WHOLE ? 2ull * blockIdx.x + (from_start ? 1 : 0)
+                                                                    : (uint64_t)blockIdx.x + c.pair) * ROWS + sub * 128u + tid;
+#pragma unroll 1
+                    for (int q = 0; q < D; q += 32) {
+                        float o[32];
+                        tmem_ld32(o, o_col + q);
+                        tmem_wait_ld();
+                        if (real && room)
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4)
+                                *reinterpret_cast<float4 *>(a.parts.o + at * D + q + k) =
+                                    make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                    }
+                    if (real && room)
+                        a.parts.ml[at] = make_float2(m, l);
+                    if (a.phase != KVC_PHASE_WHOLE && from_start && sub == 0 && tid == 0 && room)
+                        a.parts.range[c.pair] = make_ulonglong2(c.pair_begin, c.pair_begin + c.r.n);
+                }
+            }
+            slot = (slot + n_units) % THERE;
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == 9) {
+            load_role<D, true>(args, segments, tiles + S::K, &bars, there, dead, lane);
+        } else if (warp == 10) {
+            load_role<D, false>(args, segments, tiles + S::V, &bars, there, dead, lane);
+        } else if (warp == 8 && lane == 0) {
+            // ------------------------------------------------------------ matrix instructions
+            // The unit takes few instructions ahead, so what this thread does between them is time that
+            // the unit may stand still: addresses and parities live in registers.
+            constexpr uint32_t KIND_S = kind<T>(TK, false), KIND_O = kind<T>(D, true);
+            const uint32_t q_at = operand(tiles + S::Q, 16), k_at = operand(tiles + S::K, 16), v_at = operand(tiles + S::V, S::HALF);
+            const uint32_t bar = smem_addr(&bars);
+            SegmentReader reader;
+            Segment c;
+            Ring<S::KS> k;
+            Ring<S::VS> v;
+            uint32_t q_parity = 0, p_parity = 0;  // a bit for each row tile
+            bool ok = true;
+            const auto wait = [&](uint32_t at, uint32_t parity) { return ok = bar_wait(bar + at, parity & 1u, dead, a.status); };
+            const auto scores = [&](uint32_t sub) {
+                const uint32_t qa = q_at + sub * (S::TILE >> 4), ka = k_at + k.stage * (S::TILE >> 4), d = tmem + COL_S + sub * 128u;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint32_t at = ((i >> 2) * S::HALF + (i & 3) * 32) >> 4;
+                    mma_ss(d, qa + at, ka + at, KIND_S, i > 0);
+                }
+                mma_commit(bar + BAR(s_full) + sub * 8u);
+            };
+            while (reader.next<false>(segments, &bars, c, dead, a.status)) {
+                const bool two = (uint32_t)c.q.rows - c.rt * ROWS > 128u;
+                const uint32_t n_units = c.n;
+                if (!wait(BAR(k_full) + k.stage * 8u, k.parity))
+                    break;
+#pragma unroll
+                for (uint32_t sub = 0; sub < 2; ++sub)
+                    if ((sub == 0 || two) && ok && wait(BAR(q_full) + sub * 8u, q_parity >> sub)) {
+                        q_parity ^= 1u << sub;
+                        scores(sub);
+                    }
+                if (!ok)
+                    break;
+                mma_commit(bar + BAR(k_empty) + k.stage * 8u);
+                k.next();
+#pragma unroll 1
+                for (uint32_t i = 0; i < n_units; ++i) {
+                    const bool more = i + 1 < n_units;
+                    if (!wait(BAR(v_full) + v.stage * 8u, v.parity) || (more && !wait(BAR(k_full) + k.stage * 8u, k.parity)))
+                        break;
+                    const uint32_t va = v_at + v.stage * (S::TILE >> 4);
+#pragma unroll
+                    for (uint32_t sub = 0; sub < 2; ++sub) {
+                        if (sub == 1 && !two)
+                            continue;
+                        const uint32_t d = tmem + COL_O + sub * 128u, pa = tmem + COL_S + sub * 128u;
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            if (!ok || !wait(BAR(p_full) + (sub * 2 + half) * 8u, p_parity >> sub))
+                                break;
+                            fence_after();
+#pragma unroll
+                            for (int j = half * (TK / 32); j < (half + 1) * (TK / 32); ++j)
+                                mma_ts(d, pa + j * 8, va + j * (2048 >> 4), KIND_O, j > 0 || i > 0);
+                        }
+                        if (!ok)
+                            break;
+                        p_parity ^= 1u << sub;
+                        mma_commit(bar + BAR(o_done) + sub * 8u);
+                        if (more)
+                            scores(sub);
+                    }
+                    if (!ok)
+                        break;
+                    mma_commit(bar + BAR(v_empty) + v.stage * 8u);
+                    v.next();
+                    if (more) {
+                        mma_commit(bar + BAR(k_empty) + k.stage * 8u);
+                        k.next();
+                    }
+                }
+                if (!ok)
+                    break;
+            }
+            // nothing of ours runs on when the block gives tensor memory back, on no way out
+            mma_commit(smem_addr(&bars.drained));
+#pragma unroll 1
+            for (uint32_t i = 0; i < KVC_WAIT_LIMIT && !bar_try(smem_addr(&bars.drained), 0); ++i)
+                ;
+        }
+        if (warp == 11 && lane == 0) {
+            // ------------------------------------------------------------ the run, pair by pair
+            KvcCursor c = run.at;
+            uint32_t slot = 0, parity = 1, pair = run.pair;
+            unsigned long long pair_begin = run.pair_begin;
+            for (unsigned long long u = run.begin;;) {
+                if (!bar_wait(smem_addr(&bars.seg_empty[slot]), parity, dead, a.status))
+                    break;
+                Segment &s = segments[slot];
+                s.n = u < run.end ? (uint32_t)min((unsigned long long)(c.r.n - c.t), run.end - u) : 0u;
+                s.q = c.q;
+                s.r = c.r;
+                s.h = c.h;
+                s.rt = c.rt;
+                s.t = c.t;
+                s.pair = pair;
+                s.pair_begin = pair_begin;
+                const uint32_t n = s.n;
+                bar_arrive(smem_addr(&bars.seg_full[slot]));
+                if (n == 0)
+                    break;
+                if (++slot == SEGMENTS) {
+                    slot = 0;
+                    parity ^= 1;
+                }
+                u += n;
+                if (c.t + n == c.r.n) {
+                    pair_begin += c.r.n;
+                    ++pair;
+                }
+                c.t += n - 1;
+                kvc_next<ROWS, TK>(a, n_seq, c);
+            }
+        }
+        __syncwarp();
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        fence_after();
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS));
+    }
+}
+
+// A tensor map of one plane of the pool: [block][token][head][element].
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+bool encode(EncodeTiled fn, CUtensorMap *map, const KvcAttn &a, const unsigned char *plane, uint32_t dtype, uint32_t head_dim,
+            uint32_t box_keys)
+{
+    const cuuint64_t dims[4] = {head_dim, a.hkv, a.block_size, a.num_blocks};
+    const cuuint64_t strides[3] = {head_dim * 2ull, a.tok_stride, a.block_stride};
+    const cuuint32_t box[4] = {64, 1, box_keys, 1}, steps[4] = {1, 1, 1, 1};
+    return fn(map, dtype == KVC_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+              const_cast<unsigned char *>(plane), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int D>
+cudaError_t launch(const TilesArgs &args, uint32_t blocks, cudaStream_t st)
+{
+    const cudaError_t e = cudaFuncSetAttribute(kvc_attn_tiles_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               Shape<D>::SMEM);
+    if (e != cudaSuccess)
+        return e;
+    return kvc_launch_pdl(kvc_attn_tiles_kernel<T, D>, args, dim3(blocks), THREADS, Shape<D>::SMEM, st);
+}
+
+}  // namespace
+
+uint32_t kvc_attn_tiles_blocks(const kvc_layout *lay) { return (uint32_t)lay->sm_count; }
+
+cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st)
+{
+    TilesArgs args;
+    memset(&args, 0, sizeof(args));
+    args.a = a;
+    // Boxes where a tile is made of whole blocks, or a block of whole tiles, eight keys (one period of
+    // the swizzle) at least; a map's strides end at 2^40 bytes.  Else the tiles are copied key by key.
+    const uint32_t B = a.block_size;
+    if (((B >= 8 && B < (uint32_t)TK && TK % B == 0) || B % TK == 0) && a.block_stride < (1ull << 40)) {
+        args.box_keys = B < (uint32_t)TK ? B : (uint32_t)TK;
+        args.boxes = TK / args.box_keys;
+        const EncodeTiled fn = encode_tiled();
+        if (!fn || !encode(fn, &args.k_map, a, a.k, dtype, head_dim, args.box_keys) ||
+            !encode(fn, &args.v_map, a, a.v, dtype, head_dim, args.box_keys))
+            return cudaErrorUnknown;
+    }
+    if (dtype == KVC_DTYPE_BF16)
+        return head_dim == 128 ? launch<__nv_bfloat16, 128>(args, blocks, st) : launch<__nv_bfloat16, 64>(args, blocks, st);
+    return head_dim == 128 ? launch<__half, 128>(args, blocks, st) : launch<__half, 64>(args, blocks, st);
+}
