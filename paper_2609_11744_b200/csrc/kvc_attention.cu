@@ -81,8 +81,8 @@ __device__ __forceinline__ void write_row(const KvcAttn &a, int64_t tok, uint32_
         a.lse[tok * a.hq + head] = (m + log2f(l)) * 0.693147180559945309f;
 }
 
-// Whole sequences: block x looks at the boundary between runs x - 1 and x.  The first boundary inside
-// a pair joins that pair: the part of the run before it, then those of the runs after it that begin
+// Whole sequences: block x looks at the boundary between runs x and x + 1.  The first boundary inside
+// a pair's units joins that pair: the part of the run before it, then those of the runs after it that begin
 // inside the pair.
 constexpr int JOIN_WARPS = 8;
 
@@ -93,10 +93,11 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
     kvc_pdl_wait();
     const uint32_t c = blockIdx.x + 1;
     const KvcSplit sp = a.parts.split[c];
-    const unsigned long long N = a.parts.blocks, U = sp.units;
+    const unsigned long long N = a.parts.blocks, U = sp.length;
     if (sp.end == sp.begin || (c - 1) * U / N > sp.begin)
         return;
     const uint32_t last = (uint32_t)((sp.end * N - 1) / U);  // the run that holds the pair's last unit
+    const bool no_empty = U >= N;  // (64-bit divisions are what this kernel would otherwise spend its time on)
     const uint32_t n = last - c + 2;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     for (uint32_t row = blockIdx.y * (JOIN_WARPS / WPR) + warp / WPR; row < sp.rows; row += gridDim.y * (JOIN_WARPS / WPR)) {
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
             Part<D> p;
             const uint32_t run = c - 1 + i;
             p.p = &a.parts;
-            p.valid = i == 0 || run * U / N < (run + 1) * U / N;
+            p.valid = no_empty || i == 0 || run * U / N < (run + 1) * U / N;
             p.at = (2ull * run + (i == 0 ? 1 : 0)) * a.parts.rows + row;
             return p;
         };
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
 struct PhaseRow {
     uint32_t first, n;
     uint64_t pair, row;
-    unsigned long long units;
+    unsigned long long length;
 };
 
 __device__ __forceinline__ PhaseRow phase_row(const KvcParts &p, uint32_t seq, uint32_t head, uint32_t rows, uint32_t i)
@@ -144,16 +145,16 @@ __device__ __forceinline__ PhaseRow phase_row(const KvcParts &p, uint32_t seq, u
     const uint32_t tiles = (rows + p.rows - 1) / p.rows;
     r.pair = (uint64_t)p.base[seq] + (uint64_t)head * tiles + i / p.rows;
     r.row = i % p.rows;
-    r.units = *p.units;
+    r.length = *p.length;
     r.first = r.n = 0;
     // what lengths that contradict one another lead to is left out
-    if (i >= rows || r.pair >= p.max_pairs || r.units == 0)
+    if (i >= rows || r.pair >= p.max_pairs || r.length == 0)
         return r;
     const ulonglong2 u = p.range[r.pair];
-    if (u.x >= u.y || u.y > r.units)
+    if (u.x >= u.y || u.y > r.length)
         return r;
-    r.first = (uint32_t)(((u.x + 1) * p.blocks - 1) / r.units);
-    r.n = (uint32_t)((u.y * p.blocks - 1) / r.units) - r.first + 1;
+    r.first = (uint32_t)(((u.x + 1) * p.blocks - 1) / r.length);
+    r.n = (uint32_t)((u.y * p.blocks - 1) / r.length) - r.first + 1;
     return r;
 }
 
@@ -182,7 +183,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_shared_kernel(const 
     PhaseRow p;
     p.first = p.n = 0;
     p.pair = p.row = 0;
-    p.units = 1;
+    p.length = 1;
     const int32_t g = kvc_group_of(a, r);
     if (g >= 0) {
         const int32_t R = (int32_t)a.n_requests;
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_shared_kernel(const 
         const PhaseRow &at = in_prefix ? p : s;
         const unsigned long long run = at.first + (in_prefix ? i : i - p.n), N = from.blocks;
         q.p = &from;
-        q.valid = run * at.units / N < (run + 1) * at.units / N;
+        q.valid = at.length >= N || run * at.length / N < (run + 1) * at.length / N;
         q.at = (run + at.pair) * from.rows + at.row;
         return q;
     };
@@ -243,7 +244,7 @@ void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, bool t
     if (pairs) {
         c.take(p.base, sequences);
         c.take(p.range, pairs);
-        c.take(p.units, 1);
+        c.take(p.length, 1);
     } else {
         c.take(p.split, blocks);
     }
@@ -289,7 +290,7 @@ cudaError_t join_split(const KvcAttn &a, cudaStream_t st)
 {
     if (a.parts.rows == KVC_ATTN_SMALL_ROWS)  // few rows, possibly of many parts: a block to a row
         return kvc_launch_pdl(kvc_join_split_kernel<T, D, JOIN_WARPS>, a, dim3(a.parts.blocks - 1, 4), JOIN_WARPS * 32, 0, st);
-    return kvc_launch_pdl(kvc_join_split_kernel<T, D, 1>, a, dim3(a.parts.blocks - 1, 8), JOIN_WARPS * 32, 0, st);
+    return kvc_launch_pdl(kvc_join_split_kernel<T, D, 1>, a, dim3(a.parts.blocks - 1, 32), JOIN_WARPS * 32, 0, st);
 }
 
 template <typename T, int D>

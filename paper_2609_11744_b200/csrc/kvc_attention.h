@@ -4,11 +4,13 @@
 // token i / G, query head h * G + i % G.  A "pair" is (sequence, KV head, tile of ROWS rows); its
 // keys are walked in tiles of TK tokens.
 //
-// Units.  One (pair, key tile) is a unit.  All units of a call, in the order sequence, head, row
-// tile, key tile, are cut into gridDim.x equal runs, one per block, whatever the lengths of the
-// sequences: a block may begin and end inside a pair.  What it has then is partial -- weighted sum,
-// running maximum and sum of the rows -- and goes to the workspace; a second kernel joins the parts
-// of a pair in the order of its keys, so results do not depend on the order in which blocks run.
+// Units.  One (pair, key tile) is a unit.  The pairs of a call, in the order sequence, head, row tile, lie
+// behind one another on a line: a stretch of HEAD for what a pair costs whatever its keys (its queries,
+// filling the pipeline, its result), then its units.  The line is cut into gridDim.x equal runs, one per
+// block, whatever the lengths of the sequences: a block may begin and end inside a pair.  What it has
+// then is partial -- weighted sum, running maximum and sum of the rows -- and goes to the workspace; a
+// second kernel joins the parts of a pair in the order of its keys, so results do not depend on the
+// order in which blocks run.  A cut inside a pair's HEAD leaves the whole pair to the block behind it.
 #ifndef KVC_ATTENTION_H
 #define KVC_ATTENTION_H
 
@@ -28,10 +30,10 @@ enum {
     KVC_PHASE_SUFFIX = 2   // sequences are requests, the keys behind the shared prefix
 };
 
-// What a block records about the pair that its run of units begins inside of.
+// What a block records about the pair that its run begins inside of.
 struct KvcSplit {
-    unsigned long long begin, end;  // the pair's units
-    unsigned long long units;       // units of the call
+    unsigned long long begin, end;  // where the pair's units lie on the line
+    unsigned long long length;      // of the line
     int32_t qa;                     // first token row of the sequence
     uint32_t row0, rows, head;      // first row, rows of the pair, KV head
 };
@@ -42,8 +44,8 @@ struct KvcParts {
     float2 *ml;      // [slot][ROWS] running maximum (base 2) and sum
     KvcSplit *split; // [block]                                       (WHOLE)
     uint32_t *base;  // [sequence] index of its first pair            (PREFIX, SUFFIX)
-    ulonglong2 *range;  // [pair] its units                           (PREFIX, SUFFIX)
-    unsigned long long *units;  // units of the phase                 (PREFIX, SUFFIX)
+    ulonglong2 *range;  // [pair] where its units lie on the line     (PREFIX, SUFFIX)
+    unsigned long long *length;  // of the line                       (PREFIX, SUFFIX)
     uint32_t blocks; // gridDim.x of the kernel that writes them
     uint32_t rows;   // ROWS of that kernel
     uint32_t max_pairs;  // pairs that there is room for (PREFIX, SUFFIX): enough for token rows that
@@ -221,22 +223,35 @@ __device__ __forceinline__ void kvc_next(const KvcAttn &a, uint32_t n_seq, KvcCu
     c.r = kvc_range<ROWS, TK>(a, c.q, c.rt);
 }
 
-// One block's run of units: its ends, and its first unit's place.  Every thread of the block calls
-// this (THREADS of them) and gets the same answer.
+// One block's run: its first unit's place and the end of its stretch of the line.  Every thread of the
+// block calls this (THREADS of them) and gets the same answer.
 struct KvcRun {
-    unsigned long long begin, end, units;
-    unsigned long long pair_begin;  // unit at which the first unit's pair begins
-    uint32_t pair;                  // index of that pair
+    unsigned long long end;
+    unsigned long long units_at;  // where the units of the first unit's pair begin on the line
+    uint32_t pair;                // index of that pair
+    bool any;                     // whether there is a first unit
     KvcCursor at;
+    // units of the pair at `at` that belong to the run, from tile t
+    __device__ __forceinline__ uint32_t count(const KvcCursor &c, unsigned long long units_at) const
+    {
+        const unsigned long long from = units_at + c.t;
+        return end <= from ? 0u : (uint32_t)min((unsigned long long)(c.r.n - c.t), end - from);
+    }
 };
 
-template <int ROWS, int TK, int THREADS>
+template <int ROWS, int TK, int HEAD, int THREADS>
 __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
 {
     __shared__ unsigned long long sums[THREADS / 32][2];
     __shared__ KvcRun found;
-    const uint32_t per = (n_seq + THREADS - 1) / THREADS;
-    const uint32_t s0 = min(threadIdx.x * per, n_seq), s1 = min(s0 + per, n_seq);
+    // A sequence to a thread; or, where there are few sequences of many row tiles, one to a warp whose
+    // lanes take its row tiles in turn (one 8192-token prompt: 24 us for one thread, 2 us for a warp).
+    const uint32_t lane = threadIdx.x & 31u, w = threadIdx.x >> 5;
+    const bool wide = n_seq <= 4u * (THREADS / 32) && (uint64_t)a.n_tokens * a.g >= 4ull * ROWS * n_seq;
+    const uint32_t owners = wide ? THREADS / 32 : THREADS, owner = wide ? w : threadIdx.x;
+    const uint32_t rt0 = wide ? lane : 0u, rt_step = wide ? 32u : 1u;
+    const uint32_t per = (n_seq + owners - 1) / owners;
+    const uint32_t s0 = min(owner * per, n_seq), s1 = min(s0 + per, n_seq);
     unsigned long long units = 0, pairs = 0;
 #pragma unroll 1
     for (uint32_t s = s0; s < s1; ++s) {
@@ -244,13 +259,12 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
         unsigned long long sum = 0;
         uint32_t n = 0;
 #pragma unroll 1
-        for (uint32_t rt = 0; rt * ROWS < (uint32_t)q.rows; ++rt, ++n)
-            sum += kvc_range<ROWS, TK>(a, q, rt).n;
+        for (uint32_t rt = rt0; rt * ROWS < (uint32_t)q.rows; rt += rt_step, ++n)
+            sum += HEAD + kvc_range<ROWS, TK>(a, q, rt).n;
         units += sum * a.hkv;
         pairs += (unsigned long long)n * a.hkv;
     }
     unsigned long long iu = units, ip = pairs;
-    const uint32_t lane = threadIdx.x & 31u, w = threadIdx.x >> 5;
 #pragma unroll
     for (uint32_t o = 1; o < 32; o *= 2) {
         const unsigned long long x = __shfl_up_sync(~0u, iu, o), y = __shfl_up_sync(~0u, ip, o);
@@ -272,67 +286,94 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
         }
         total += sums[k][0];
     }
-    bu += iu - units;
-    bp += ip - pairs;
+    if (wide) {
+        units = sums[w][0];
+    } else {
+        bu += iu - units;
+        bp += ip - pairs;
+    }
     const unsigned long long begin = blockIdx.x * total / gridDim.x, end = (blockIdx.x + 1ull) * total / gridDim.x;
     if (threadIdx.x == 0) {
-        found.begin = begin;
         found.end = end;
-        found.units = total;
+        found.any = begin < end;
     }
-    // the thread whose sequences hold the first unit walks to it (of an empty run too: with fewer units
-    // than blocks, the first boundary inside a pair may be that of an empty run)
+    // the owner of the sequence that the run begins in walks to the place (of an empty run too: on a line
+    // shorter than the number of blocks, the first boundary inside a pair may be that of an empty run)
     const bool mine = begin >= bu && begin < bu + units;
     const bool table = a.phase != KVC_PHASE_WHOLE && blockIdx.x == 0;
     if (mine || table) {
         unsigned long long u = bu, p = bp;
 #pragma unroll 1
         for (uint32_t s = s0; s < s1; ++s) {
-            if (table)
+            if (table && rt0 == 0)
                 a.parts.base[s] = (uint32_t)min(p, 0xFFFFFFFFull);
             const KvcSeq q = kvc_seq(a, s);
+            const uint32_t n = ((uint32_t)q.rows + ROWS - 1) / ROWS;
             unsigned long long per_head = 0;
-            uint32_t n = 0;
 #pragma unroll 1
-            for (uint32_t rt = 0; rt * ROWS < (uint32_t)q.rows; ++rt, ++n)
-                per_head += kvc_range<ROWS, TK>(a, q, rt).n;
+            for (uint32_t rt = rt0; rt < n; rt += rt_step)
+                per_head += HEAD + kvc_range<ROWS, TK>(a, q, rt).n;
+            if (wide)
+#pragma unroll
+                for (uint32_t o = 16; o; o /= 2)
+                    per_head += __shfl_xor_sync(~0u, per_head, o);
             if (mine && begin >= u && begin < u + per_head * a.hkv) {
                 const uint32_t h = (uint32_t)((begin - u) / per_head);
                 unsigned long long b = u + h * per_head;
                 KvcRange r;
-                uint32_t rt = 0;
+                uint32_t rt = rt0;
+                bool here;
 #pragma unroll 1
-                for (;; ++rt) {
-                    r = kvc_range<ROWS, TK>(a, q, rt);
-                    if (begin < b + r.n)
+                for (;; rt += rt_step) {
+                    // row tiles rt - lane .. of which the lanes hold one each, or just rt
+                    uint32_t own = 0;
+                    if (rt < n) {
+                        r = kvc_range<ROWS, TK>(a, q, rt);
+                        own = HEAD + r.n;
+                    }
+                    unsigned long long sum = own;
+                    if (wide)
+#pragma unroll
+                        for (uint32_t o = 1; o < 32; o *= 2) {
+                            const unsigned long long x = __shfl_up_sync(~0u, sum, o);
+                            if (lane >= o)
+                                sum += x;
+                        }
+                    here = begin >= b + sum - own && begin < b + sum;
+                    if (wide ? __any_sync(~0u, here) : here) {
+                        b += sum - own + HEAD;
                         break;
-                    b += r.n;
+                    }
+                    b += wide ? __shfl_sync(~0u, sum, 31) : sum;
                 }
-                found.pair_begin = b;
-                found.pair = (uint32_t)(p + (unsigned long long)h * n + rt);
-                found.at.s = s;
-                found.at.h = h;
-                found.at.rt = rt;
-                found.at.t = (uint32_t)(begin - b);
-                found.at.q = q;
-                found.at.r = r;
+                if (here) {
+                    found.units_at = b;
+                    found.pair = (uint32_t)(p + (unsigned long long)h * n + rt);
+                    found.at.s = s;
+                    found.at.h = h;
+                    found.at.rt = rt;
+                    found.at.t = begin > b ? (uint32_t)(begin - b) : 0u;
+                    found.at.q = q;
+                    found.at.r = r;
+                }
             }
             u += per_head * a.hkv;
             p += (unsigned long long)n * a.hkv;
         }
     }
     __syncthreads();
-    const KvcRun run = found;
+    KvcRun run = found;
+    run.any = run.any && run.count(run.at, run.units_at) != 0;
     if (threadIdx.x == 0) {
         if (a.phase == KVC_PHASE_WHOLE) {
             KvcSplit sp;
             sp.begin = sp.end = 0;
-            sp.units = total;
+            sp.length = total;
             sp.qa = 0;
             sp.row0 = sp.rows = sp.head = 0;
             if (begin < total && run.at.t > 0) {
-                sp.begin = run.pair_begin;
-                sp.end = run.pair_begin + run.at.r.n;
+                sp.begin = run.units_at;
+                sp.end = run.units_at + run.at.r.n;
                 sp.qa = run.at.q.qa;
                 sp.row0 = run.at.rt * ROWS;
                 sp.rows = min((uint32_t)ROWS, (uint32_t)run.at.q.rows - sp.row0);
@@ -340,7 +381,7 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
             }
             a.parts.split[blockIdx.x] = sp;
         } else if (blockIdx.x == 0) {
-            *a.parts.units = total;
+            *a.parts.length = total;
         }
     }
     return run;

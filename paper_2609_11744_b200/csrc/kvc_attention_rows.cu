@@ -19,6 +19,7 @@ constexpr int THREADS = WARPS * 32;
 constexpr int TK = 64;             // keys per unit
 constexpr int WK = TK / WARPS;     // keys per warp and unit
 constexpr int ROWS = KVC_ATTN_SMALL_ROWS;
+constexpr int HEAD = 1;            // what a pair costs besides its units, in units
 
 template <int D>
 struct Shape {
@@ -108,8 +109,8 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
     kvc_pdl_wait();
 
     const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
-    const KvcRun run = kvc_find_run<ROWS, TK, THREADS>(a, n_seq);
-    if (run.begin >= run.end)
+    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, THREADS>(a, n_seq);
+    if (!run.any)
         return;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t ring = smem_addr(smem) + warp * S::STAGES * S::STAGE;
@@ -117,23 +118,29 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
     const uint32_t gr = lane >> 2, gc = lane & 3u;  // row and column pair of an accumulator
 
     KvcCursor ld = run.at, c = run.at;
-    unsigned long long u_ld = run.begin, u = run.begin;
+    unsigned long long ld_at = run.units_at, units_at = run.units_at;  // where their pairs' units lie on the line
     uint32_t pair = run.pair;
-    unsigned long long pair_begin = run.pair_begin;
-#pragma unroll 1
-    for (int i = 0; i < S::STAGES - 1; ++i) {
-        if (u_ld < run.end) {
-            const uint32_t there = load_unit<D>(a, ld, warp, lane, ring + (uint32_t)i * S::STAGE);
+    // the load cursor's unit, if it is in the run, and one step on
+    bool more = true;
+    const auto load = [&](uint32_t stage) {
+        if (more) {
+            const uint32_t there = load_unit<D>(a, ld, warp, lane, ring + stage * S::STAGE);
             if (lane == 0)
-                s_there[warp][i] = there;
+                s_there[warp][stage] = there;
+            const uint32_t n = ld.r.n;
             kvc_next<ROWS, TK>(a, n_seq, ld);
-            ++u_ld;
+            if (ld.t == 0)
+                ld_at += n + HEAD;
+            more = ld.s < n_seq && ld_at + ld.t < run.end;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-    }
+    };
+#pragma unroll 1
+    for (uint32_t i = 0; i < S::STAGES - 1; ++i)
+        load(i);
     uint32_t stage = 0;
 
-    while (u < run.end) {
+    for (uint32_t n_units; c.s < n_seq && (n_units = run.count(c, units_at)) != 0;) {
         // ---- a new pair (or the rest of one): its queries as matrix operands, 16 rows x D
         const uint32_t row0 = c.rt * ROWS, rows = min((uint32_t)ROWS, (uint32_t)c.q.rows - row0);
         uint32_t qf[KS][4];
@@ -160,21 +167,12 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
             o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
         const bool from_start = c.t == 0;
-        const uint32_t n_units = (uint32_t)min((unsigned long long)(c.r.n - c.t), run.end - u);
         const bool to_end = c.t + n_units == c.r.n;
 
         for (uint32_t i = 0; i < n_units; ++i) {
             // the stage that the previous unit used is free once every lane is past its reads
             __syncwarp();
-            uint32_t free_stage = stage == 0 ? S::STAGES - 1 : stage - 1;
-            if (u_ld < run.end) {
-                const uint32_t there = load_unit<D>(a, ld, warp, lane, ring + free_stage * S::STAGE);
-                if (lane == 0)
-                    s_there[warp][free_stage] = there;
-                kvc_next<ROWS, TK>(a, n_seq, ld);
-                ++u_ld;
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            load(stage == 0 ? S::STAGES - 1 : stage - 1);
             asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
             __syncwarp();
 
@@ -336,12 +334,11 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
                             a.parts.ml[at] = make_float2(tm[half], tl[half]);
                     }
                 if (a.phase != KVC_PHASE_WHOLE && from_start && lane == 0)
-                    a.parts.range[pair] = make_ulonglong2(pair_begin, pair_begin + c.r.n);
+                    a.parts.range[pair] = make_ulonglong2(units_at, units_at + c.r.n);
             }
         }
-        u += n_units;
         if (to_end) {
-            pair_begin += c.r.n;
+            units_at += c.r.n + HEAD;
             ++pair;
         }
         c.t += n_units - 1;

@@ -5,15 +5,16 @@
 // with the running maximum and sum of a softmax in 32 bits.
 //
 // One block a SM, specialised by warp:
-//   warps 0-3, 4-7  softmax of rows 0-127 and 128-255, a row a thread: read S from tensor memory, take
-//                   the maximum, write the weights P (pool's type) over S, keep m and l in registers;
-//                   at the end of a pair read O and write the result.  They also load the queries.
-//   warp 8          one thread issues the matrix instructions: S = Q K^T from shared memory, O += P V
+//   warps 0-7, 8-15 softmax of rows 0-127 and 128-255, two threads a row, one for each half of a tile's
+//                   keys: read S from tensor memory, agree on the maximum, write the weights P (pool's type)
+//                   over S, keep m and l in registers; at the end of a pair each writes half of O's columns.
+//                   They also load the queries.
+//   warp 16         one thread issues the matrix instructions: S = Q K^T from shared memory, O += P V
 //                   with P from tensor memory and V as it lies (keys x head, so head-major for this product)
-//   warps 9, 10     load K and V tiles through the block table into rings of shared-memory stages, in the
+//   warps 17, 18    load K and V tiles through the block table into rings of shared-memory stages, in the
 //                   128-byte swizzle that the matrix unit reads: a tensor copy for the keys of each block, or
 //                   16-byte asynchronous copies where a tile is not made of whole blocks
-//   warp 11         one thread walks the run's pairs and hands them to the others
+//   warp 19         one thread walks the run's pairs and hands them to the others
 // Two row tiles share each K and V tile, and while one is in its softmax the other's products run.
 // Bound by the exponentials and the matrix unit alike: 128 x 128 scores take 1024 cycles on each.
 // O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use: weights are then
@@ -28,15 +29,17 @@
 namespace {
 
 constexpr int ROWS = KVC_ATTN_TILE_ROWS;
-constexpr int TK = 128;
-constexpr int THREADS = 384;
+constexpr int TK = 128;             // keys of a K or V stage
+constexpr int HK = TK / 2;          // keys of one softmax thread
+constexpr int THREADS = 640;
+constexpr int HEAD = 3;             // what a pair costs besides its units, in units (measured: 13,000 cycles against 3,800)
 constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper than the K ring
 
 template <int D>
 struct Shape {
     static constexpr int TILE = TK * D * 2;           // a K or V tile; also half of the queries
     static constexpr int HALF = TK * 128;             // 64 elements (128 bytes) of 128 rows
-    static constexpr int KS = D == 128 ? 3 : 4, VS = D == 128 ? 2 : 4;
+    static constexpr int KS = D == 128 ? 2 : 4, VS = KS;
     static constexpr int Q = 0, K = 2 * TILE, V = K + KS * TILE, END = V + VS * TILE;
     static constexpr int SMEM = END + 1024;           // room to align the stages to the swizzle's 1024 bytes
 };
@@ -149,14 +152,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const float *x)
                  : "memory");
 }
 
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r)
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-                 : "memory");
-}
-
 // Two 32-bit floats in one 64-bit register pair, for the two-wide arithmetic.
 __device__ __forceinline__ uint64_t pair2(float lo, float hi)
 {
@@ -200,7 +195,7 @@ __device__ __forceinline__ float exp2_fast(float x)
 __device__ __forceinline__ uint32_t low_bits(int32_t n) { return n <= 0 ? 0u : n > 31 ? ~0u : (1u << n) - 1u; }
 
 struct Bars {
-    uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];  // p_full: of each half of the keys
+    uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];  // [row tile], p_full: and half of the keys
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
     uint64_t seg_full[4], seg_empty[4], drained;
 };
@@ -212,10 +207,10 @@ struct Segment {
     KvcRange r;
     uint32_t h, rt, t, n;  // KV head, row tile; first tile and number of tiles (0: the run is over)
     uint32_t pair;
-    unsigned long long pair_begin;
+    unsigned long long units_at;  // where the pair's units begin on the line
 };
 constexpr uint32_t SEGMENTS = 4;
-constexpr uint32_t SEGMENT_READERS = 11;  // 8 softmax warps, 2 loading warps, the issuing thread
+constexpr uint32_t SEGMENT_READERS = 19;  // 16 softmax warps, 2 loading warps, the issuing thread
 
 // The next segment, copied to registers.  Every lane of the role's warp calls this (or the one thread).
 struct SegmentReader {
@@ -408,11 +403,12 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     __shared__ uint32_t there[THERE][4];
     __shared__ uint32_t s_dead, s_tmem;
     __shared__ Segment segments[SEGMENTS];
+    __shared__ float row_top[2][2][128], row_sum[2][2][128];  // [row tile][half][row]
     kvc_pdl_wait();
 
     const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
-    const KvcRun run = kvc_find_run<ROWS, TK, THREADS>(a, n_seq);
-    if (run.begin >= run.end)
+    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, THREADS>(a, n_seq);
+    if (!run.any)
         return;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t tiles = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -421,7 +417,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     if (threadIdx.x == 0) {
         s_dead = 0;
         for (int i = 0; i < 2; ++i) {
-            bar_init(smem_addr(&bars.q_full[i]), 128);
+            bar_init(smem_addr(&bars.q_full[i]), 256);
             bar_init(smem_addr(&bars.s_full[i]), 1);
             bar_init(smem_addr(&bars.p_full[i][0]), 128);
             bar_init(smem_addr(&bars.p_full[i][1]), 128);
@@ -438,154 +434,74 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         bar_init(smem_addr(&bars.drained), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8)
+    if (warp == 16)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(COLS) : "memory");
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = s_tmem;
 
-    if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    if (warp < 16) {
+        // registers: 512 x 104 + 128 x 64 = 640 x 96 of the launch
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         // ---------------------------------------------------------------- softmax
-        const uint32_t sub = warp >> 2, tid = threadIdx.x & 127u;
+        const uint32_t sub = warp >> 3, half = warp >> 2 & 1u, tid = threadIdx.x & 127u;  // tid: the row
         const uint32_t lanes = (warp & 3u) << 21;  // this warp's 32 rows of tensor memory
-        const uint32_t s_col = tmem + COL_S + sub * 128u + lanes, o_col = tmem + COL_O + sub * 128u + lanes;
-        SegmentReader reader;
-        Segment c;
-        uint32_t s_parity = 0, o_parity = 0, slot = 0;
+        const uint32_t s_col = tmem + COL_S + sub * 128u + lanes, o_col = tmem + COL_O + sub * 128u + half * (D / 2) + lanes;
         const uint32_t bar = smem_addr(&bars);
-        const uint32_t s_full = bar + BAR(s_full) + sub * 8u, p_full = bar + BAR(p_full) + sub * 16u, o_done = bar + BAR(o_done) + sub * 8u;
-        bool ok = true;
-        while (ok && reader.next<true>(segments, &bars, c, dead, a.status)) {
+        const uint32_t s_full = bar + BAR(s_full) + sub * 8u, p_full = bar + BAR(p_full) + (sub * 2 + half) * 8u, o_done = bar + BAR(o_done) + sub * 8u;
+        // the two warps of the same rows meet here
+        const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1u + sub * 4u + (warp & 3u)) : "memory"); };
+        SegmentReader reader;
+        Segment c, d;
+        uint32_t s_parity = 0, o_parity = 0, slot = 0;
+        // Queries of a segment: 16 bytes a thread and turn, rows of 128 bytes in the swizzle.  All scores
+        // of the segment before have been seen, so their operand may go.
+        const auto load_queries = [&](const Segment &c) {
             const uint32_t row0 = c.rt * ROWS + sub * 128u, rows_all = (uint32_t)c.q.rows;
-            const uint32_t n_units = c.n;
-            const bool from_start = c.t == 0, to_end = c.t + n_units == c.r.n;
-            if (row0 < rows_all) {
-                // queries: 16 bytes a thread and turn, rows of 128 bytes in the swizzle
-                constexpr uint32_t STEP = 128u / (D / 8), TURNS = 128u / STEP;
-                const uint32_t chunk = tid % (D / 8), r0 = tid / (D / 8);
-                uint32_t tok = (row0 + r0) / a.g, head = row0 + r0 - tok * a.g;
-                const uint32_t tok_step = STEP / a.g, head_step = STEP - tok_step * a.g;
-                const unsigned char *src = a.q + (int64_t)c.q.qa * a.q_tok + (int64_t)(c.h * a.g) * a.q_head + chunk * 16u;
-                unsigned char *dst = tiles_ptr + S::Q + sub * S::TILE + (chunk >> 3) * S::HALF;
+            if (row0 >= rows_all)
+                return;
+            constexpr uint32_t STEP = 256u / (D / 8), TURNS = 128u / STEP;
+            const uint32_t at = threadIdx.x & 255u, chunk = at % (D / 8), r0 = at / (D / 8);
+            uint32_t tok = (row0 + r0) / a.g, head = row0 + r0 - tok * a.g;
+            const uint32_t tok_step = STEP / a.g, head_step = STEP - tok_step * a.g;
+            const unsigned char *src = a.q + (int64_t)c.q.qa * a.q_tok + (int64_t)(c.h * a.g) * a.q_head + chunk * 16u;
+            unsigned char *dst = tiles_ptr + S::Q + sub * S::TILE + (chunk >> 3) * S::HALF;
+            uint4 x[TURNS];
 #pragma unroll
-                for (uint32_t t = 0; t < TURNS; t += 8) {
-                    uint4 x[8];
-#pragma unroll
-                    for (uint32_t e = 0; e < 8; ++e) {
-                        x[e] = row0 + r0 + (t + e) * STEP < rows_all
-                                   ? *reinterpret_cast<const uint4 *>(src + (int64_t)tok * a.q_tok + (int64_t)head * a.q_head)
-                                   : make_uint4(0, 0, 0, 0);
-                        tok += tok_step;
-                        head += head_step;
-                        if (head >= a.g) {
-                            head -= a.g;
-                            ++tok;
-                        }
-                    }
-#pragma unroll
-                    for (uint32_t e = 0; e < 8; ++e) {
-                        const uint32_t r = r0 + (t + e) * STEP;
-                        *reinterpret_cast<uint4 *>(dst + r * 128u + (((chunk & 7u) ^ (r & 7u)) << 4)) = x[e];
-                    }
+            for (uint32_t e = 0; e < TURNS; ++e) {
+                x[e] = row0 + r0 + e * STEP < rows_all
+                           ? *reinterpret_cast<const uint4 *>(src + (int64_t)tok * a.q_tok + (int64_t)head * a.q_head)
+                           : make_uint4(0, 0, 0, 0);
+                tok += tok_step;
+                head += head_step;
+                if (head >= a.g) {
+                    head -= a.g;
+                    ++tok;
                 }
-                fence_async();
-                bar_arrive(smem_addr(&bars.q_full[sub]));
-
-                const bool real = row0 + tid < rows_all;
-                const int32_t pos = real ? kvc_row_pos(a, c.q, row0 + tid) : -1;
-                float m = -INFINITY, l = 0.f;  // m: the maximum in use, base 2
-#pragma unroll 1
-                for (uint32_t i = 0; i < n_units; ++i) {
-                    const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + i) * TK);
-                    if (!(ok = __all_sync(~0u, bar_wait(s_full, s_parity, dead, a.status))))
-                        break;
-                    s_parity ^= 1;
-                    fence_after();
-                    float s[TK];
+            }
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        tmem_ld32(s + q * 32, s_col + q * 32);
-                    uint32_t mask[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        mask[q] = *const_cast<volatile uint32_t *>(&there[(slot + i) % THERE][q]);
-                    tmem_wait_ld();
-                    const bool all = (mask[0] & mask[1] & mask[2] & mask[3]) == ~0u && j0 + TK - 1 <= pos &&
-                                     (a.window == 0 || pos - j0 < a.window || j0 + TK - 1 < a.sinks);
-                    if (__any_sync(~0u, !all)) {
-                        // kvc_sees() for 32 keys at a time: at most pos, and after pos - window or before sinks
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int32_t j = j0 + q * 32;
-                            uint32_t see = mask[q] & low_bits(pos + 1 - j);
-                            if (a.window)
-                                see &= ~low_bits(pos - a.window + 1 - j) | low_bits(a.sinks - j);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                s[q * 32 + k] = see >> k & 1u ? s[q * 32 + k] : -INFINITY;
-                        }
-                    }
-                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int k = 0; k < TK; k += 8)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            t[e] = fmaxf(t[e], fmaxf(s[k + e], s[k + 4 + e]));
-                    const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * a.scale_log2;
-                    if (i == 0) {
-                        m = top;
-                    } else {
-                        const bool move = top > m + 8.f || (m == -INFINITY && top != m);
-                        if (__any_sync(~0u, move)) {
-                            const float f = !move ? 1.f : m == -INFINITY ? 0.f : exp2_fast(m - top);
-                            if (move)
-                                m = top;
-                            l *= f;
-                            // the products so far have to be in O before it is scaled
-                            if (!(ok = __all_sync(~0u, bar_wait(o_done, o_parity ^ 1u, dead, a.status))))
-                                break;
-                            fence_after();
-#pragma unroll 1
-                            for (int q = 0; q < D; q += 32) {
-                                float o[32];
-                                tmem_ld32(o, o_col + q);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int k = 0; k < 32; ++k)
-                                    o[k] *= f;
-                                tmem_st32(o_col + q, o);
-                            }
-                        }
-                    }
-                    const float base = m == -INFINITY ? 0.f : m;
-                    const uint64_t scale2 = pair2(a.scale_log2, a.scale_log2), base2 = pair2(-base, -base);
-                    uint64_t sum2 = 0;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const float2 x = unpair2(fma2(pair2(s[q * 32 + 2 * k], s[q * 32 + 2 * k + 1]), scale2, base2));
-                            const float y0 = exp2_fast(x.x), y1 = exp2_fast(x.y);
-                            sum2 = add2(sum2, pair2(y0, y1));
-                            p[k] = kvc_from_float2<T>(y0, y1);
-                        }
-                        tmem_st16(s_col + q * 16, p);
-                        if (q & 1) {  // half of the weights: its products can start
-                            tmem_wait_st();
-                            fence_before();
-                            bar_arrive(p_full + (q >> 1) * 8u);
-                        }
-                    }
-                    const float2 sum = unpair2(sum2);
-                    l += sum.x + sum.y;
-                    o_parity ^= 1;  // flips with every product that this arrival lets start
-                }
-                if (!ok)
-                    break;
-                if (!(ok = __all_sync(~0u, bar_wait(o_done, o_parity ^ 1u, dead, a.status))))
+            for (uint32_t e = 0; e < TURNS; ++e) {
+                const uint32_t r = r0 + e * STEP;
+                *reinterpret_cast<uint4 *>(dst + r * 128u + (((chunk & 7u) ^ (r & 7u)) << 4)) = x[e];
+            }
+            fence_async();
+            bar_arrive(bar + BAR(q_full) + sub * 8u);
+        };
+        bool ok, open = false;  // open: a segment whose products have been started and whose result is to be written
+        uint32_t row0 = 0;
+        float m = 0.f, l = 0.f;  // m: the maximum in use, base 2; l: of this thread's keys
+        for (;;) {
+            // the next segment's queries first, so that its scores run while the one before is written
+            ok = reader.next<true>(segments, &bars, d, dead, a.status);
+            if (ok)
+                load_queries(d);
+            if (open) {
+                const bool from_start = c.t == 0, to_end = c.t + c.n == c.r.n, real = row0 + tid < (uint32_t)c.q.rows;
+                row_sum[sub][half][tid] = l;
+                meet();
+                l = row_sum[sub][0][tid] + row_sum[sub][1][tid];
+                if (!__all_sync(~0u, bar_wait(o_done, o_parity ^ 1u, dead, a.status)))
                     break;
                 fence_after();
                 const uint32_t i = row0 + tid;
@@ -594,9 +510,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     const uint32_t head = c.h * a.g + (i - tok * a.g);
                     const int64_t row = c.q.qa + (int32_t)tok;
                     const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
-                    unsigned char *dst = a.out + row * a.o_tok + (int64_t)head * a.o_head;
+                    unsigned char *dst = a.out + row * a.o_tok + (int64_t)head * a.o_head + half * D;
 #pragma unroll 1
-                    for (int q = 0; q < D; q += 32) {
+                    for (int q = 0; q < D / 2; q += 32) {
                         float o[32];
                         tmem_ld32(o, o_col + q);
                         tmem_wait_ld();
@@ -610,38 +526,131 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                                 *reinterpret_cast<uint4 *>(dst + (q + k) * 2) = kvc_pack8<T>(x);
                             }
                     }
-                    if (real && a.lse)
+                    if (real && a.lse && half == 0)
                         a.lse[row * a.hq + head] = (m + log2f(l)) * 0.693147180559945309f;
                 } else {
                     const bool room = a.phase == KVC_PHASE_WHOLE || c.pair < a.parts.max_pairs;
                     const uint64_t at = (a.phase == KVC_PHASE_WHOLE ? 2ull * blockIdx.x + (from_start ? 1 : 0)
                                                                     : (uint64_t)blockIdx.x + c.pair) * ROWS + sub * 128u + tid;
 #pragma unroll 1
-                    for (int q = 0; q < D; q += 32) {
+                    for (int q = 0; q < D / 2; q += 32) {
                         float o[32];
                         tmem_ld32(o, o_col + q);
                         tmem_wait_ld();
                         if (real && room)
 #pragma unroll
                             for (int k = 0; k < 32; k += 4)
-                                *reinterpret_cast<float4 *>(a.parts.o + at * D + q + k) =
+                                *reinterpret_cast<float4 *>(a.parts.o + at * D + half * (D / 2) + q + k) =
                                     make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     }
-                    if (real && room)
+                    if (real && room && half == 0)
                         a.parts.ml[at] = make_float2(m, l);
-                    if (a.phase != KVC_PHASE_WHOLE && from_start && sub == 0 && tid == 0 && room)
-                        a.parts.range[c.pair] = make_ulonglong2(c.pair_begin, c.pair_begin + c.r.n);
+                    if (a.phase != KVC_PHASE_WHOLE && from_start && sub == 0 && half == 0 && tid == 0 && room)
+                        a.parts.range[c.pair] = make_ulonglong2(c.units_at, c.units_at + c.r.n);
                 }
             }
-            slot = (slot + n_units) % THERE;
+            if (!ok)
+                break;
+            c = d;
+            row0 = c.rt * ROWS + sub * 128u;
+            open = row0 < (uint32_t)c.q.rows;
+            if (open) {
+                const int32_t pos = row0 + tid < (uint32_t)c.q.rows ? kvc_row_pos(a, c.q, row0 + tid) : -1;
+                m = -INFINITY;
+                l = 0.f;
+#pragma unroll 1
+                for (uint32_t i = 0; i < c.n; ++i) {
+                    const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + i) * TK + half * HK);
+                    if (!(ok = __all_sync(~0u, bar_wait(s_full, s_parity, dead, a.status))))
+                        break;
+                    s_parity ^= 1;
+                    fence_after();
+                    float s[HK];
+                    tmem_ld32(s, s_col + half * HK);
+                    tmem_ld32(s + 32, s_col + half * HK + 32);
+                    const volatile uint32_t *mask = &there[(slot + i) % THERE][half * 2];
+                    const uint32_t mask0 = mask[0], mask1 = mask[1];
+                    tmem_wait_ld();
+                    const bool all = (mask0 & mask1) == ~0u && j0 + HK - 1 <= pos &&
+                                     (a.window == 0 || pos - j0 < a.window || j0 + HK - 1 < a.sinks);
+                    if (__any_sync(~0u, !all)) {
+                        // kvc_sees() for 32 keys at a time: at most pos, and after pos - window or before sinks
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const int32_t j = j0 + q * 32;
+                            uint32_t see = (q ? mask1 : mask0) & low_bits(pos + 1 - j);
+                            if (a.window)
+                                see &= ~low_bits(pos - a.window + 1 - j) | low_bits(a.sinks - j);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                s[q * 32 + k] = see >> k & 1u ? s[q * 32 + k] : -INFINITY;
+                        }
+                    }
+                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int k = 0; k < HK; k += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            t[e] = fmaxf(t[e], fmaxf(s[k + e], s[k + 4 + e]));
+                    float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                    // the row's other half.  After this both halves of S have been read, so P may go over them; and
+                    // the next scores come only after both halves' weights, so no value is overwritten unread
+                    row_top[sub][half][tid] = top;
+                    meet();
+                    top = fmaxf(top, row_top[sub][half ^ 1u][tid]) * a.scale_log2;
+                    if (i == 0) {
+                        m = top;
+                    } else {
+                        const bool move = top > m + 8.f || (m == -INFINITY && top != m);
+                        if (__any_sync(~0u, move)) {
+                            const float f = !move ? 1.f : m == -INFINITY ? 0.f : exp2_fast(m - top);
+                            if (move)
+                                m = top;
+                            l *= f;
+                            // (these scores were issued after the products so far, which are in O then)
+#pragma unroll 1
+                            for (int q = 0; q < D / 2; q += 32) {
+                                float o[32];
+                                tmem_ld32(o, o_col + q);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k)
+                                    o[k] *= f;
+                                tmem_st32(o_col + q, o);
+                            }
+                        }
+                    }
+                    const float base = m == -INFINITY ? 0.f : m;
+                    const uint64_t scale2 = pair2(a.scale_log2, a.scale_log2), base2 = pair2(-base, -base);
+                    uint64_t sum2 = 0;
+                    uint32_t p[HK / 2];
+#pragma unroll
+                    for (int k = 0; k < HK / 2; ++k) {
+                        const float2 x = unpair2(fma2(pair2(s[2 * k], s[2 * k + 1]), scale2, base2));
+                        const float y0 = exp2_fast(x.x), y1 = exp2_fast(x.y);
+                        sum2 = add2(sum2, pair2(y0, y1));
+                        p[k] = kvc_from_float2<T>(y0, y1);
+                    }
+                    tmem_st32(s_col + half * (HK / 2), reinterpret_cast<const float *>(p));
+                    const float2 sum = unpair2(sum2);
+                    l += sum.x + sum.y;
+                    tmem_wait_st();
+                    fence_before();
+                    bar_arrive(p_full);
+                }
+                if (!ok)
+                    break;
+                o_parity ^= 1u;
+            }
+            slot = (slot + c.n) % THERE;
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (warp == 9) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 17) {
             load_role<D, true>(args, segments, tiles + S::K, &bars, there, dead, lane);
-        } else if (warp == 10) {
+        } else if (warp == 18) {
             load_role<D, false>(args, segments, tiles + S::V, &bars, there, dead, lane);
-        } else if (warp == 8 && lane == 0) {
+        } else if (warp == 16 && lane == 0) {
             // ------------------------------------------------------------ matrix instructions
             // The unit takes few instructions ahead, so what this thread does between them is time that
             // the unit may stand still: addresses and parities live in registers.
@@ -666,22 +675,18 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             };
             while (reader.next<false>(segments, &bars, c, dead, a.status)) {
                 const bool two = (uint32_t)c.q.rows - c.rt * ROWS > 128u;
-                const uint32_t n_units = c.n;
-                if (!wait(BAR(k_full) + k.stage * 8u, k.parity))
+                if (!wait(BAR(k_full) + k.stage * 8u, k.parity) || !wait(BAR(q_full), q_parity) ||
+                    (two && !wait(BAR(q_full) + 8u, q_parity >> 1)))
                     break;
-#pragma unroll
-                for (uint32_t sub = 0; sub < 2; ++sub)
-                    if ((sub == 0 || two) && ok && wait(BAR(q_full) + sub * 8u, q_parity >> sub)) {
-                        q_parity ^= 1u << sub;
-                        scores(sub);
-                    }
-                if (!ok)
-                    break;
+                q_parity ^= two ? 3u : 1u;
+                scores(0);
+                if (two)
+                    scores(1);
                 mma_commit(bar + BAR(k_empty) + k.stage * 8u);
                 k.next();
 #pragma unroll 1
-                for (uint32_t i = 0; i < n_units; ++i) {
-                    const bool more = i + 1 < n_units;
+                for (uint32_t i = 0; i < c.n; ++i) {
+                    const bool more = i + 1 < c.n;
                     if (!wait(BAR(v_full) + v.stage * 8u, v.parity) || (more && !wait(BAR(k_full) + k.stage * 8u, k.parity)))
                         break;
                     const uint32_t va = v_at + v.stage * (S::TILE >> 4);
@@ -691,20 +696,21 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                             continue;
                         const uint32_t d = tmem + COL_O + sub * 128u, pa = tmem + COL_S + sub * 128u;
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
+                        for (uint32_t half = 0; half < 2; ++half) {
                             if (!ok || !wait(BAR(p_full) + (sub * 2 + half) * 8u, p_parity >> sub))
-                                break;
+                                continue;
                             fence_after();
 #pragma unroll
-                            for (int j = half * (TK / 32); j < (half + 1) * (TK / 32); ++j)
+                            for (uint32_t j = half * (HK / 16); j < (half + 1) * (HK / 16); ++j)
                                 mma_ts(d, pa + j * 8, va + j * (2048 >> 4), KIND_O, j > 0 || i > 0);
                         }
                         if (!ok)
                             break;
                         p_parity ^= 1u << sub;
-                        mma_commit(bar + BAR(o_done) + sub * 8u);
-                        if (more)
+                        if (more)  // these scores' barrier stands for the products before them too
                             scores(sub);
+                        else
+                            mma_commit(bar + BAR(o_done) + sub * 8u);
                     }
                     if (!ok)
                         break;
@@ -724,45 +730,41 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             for (uint32_t i = 0; i < KVC_WAIT_LIMIT && !bar_try(smem_addr(&bars.drained), 0); ++i)
                 ;
         }
-        if (warp == 11 && lane == 0) {
+        if (warp == 19 && lane == 0) {
             // ------------------------------------------------------------ the run, pair by pair
             KvcCursor c = run.at;
-            uint32_t slot = 0, parity = 1, pair = run.pair;
-            unsigned long long pair_begin = run.pair_begin;
-            for (unsigned long long u = run.begin;;) {
+            uint32_t slot = 0, parity = 1, pair = run.pair, n;
+            unsigned long long units_at = run.units_at;
+            do {
                 if (!bar_wait(smem_addr(&bars.seg_empty[slot]), parity, dead, a.status))
                     break;
+                n = c.s < n_seq ? run.count(c, units_at) : 0u;
                 Segment &s = segments[slot];
-                s.n = u < run.end ? (uint32_t)min((unsigned long long)(c.r.n - c.t), run.end - u) : 0u;
+                s.n = n;
                 s.q = c.q;
                 s.r = c.r;
                 s.h = c.h;
                 s.rt = c.rt;
                 s.t = c.t;
                 s.pair = pair;
-                s.pair_begin = pair_begin;
-                const uint32_t n = s.n;
+                s.units_at = units_at;
                 bar_arrive(smem_addr(&bars.seg_full[slot]));
-                if (n == 0)
-                    break;
                 if (++slot == SEGMENTS) {
                     slot = 0;
                     parity ^= 1;
                 }
-                u += n;
-                if (c.t + n == c.r.n) {
-                    pair_begin += c.r.n;
-                    ++pair;
-                }
-                c.t += n - 1;
+                // (a run that ends inside the pair ends here: the next count is 0)
+                units_at += c.r.n + HEAD;
+                ++pair;
+                c.t = c.r.n - 1;
                 kvc_next<ROWS, TK>(a, n_seq, c);
-            }
+            } while (n != 0);
         }
         __syncwarp();
     }
     fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 16) {
         fence_after();
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS));
