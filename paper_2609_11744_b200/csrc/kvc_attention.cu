@@ -25,38 +25,42 @@ __device__ __forceinline__ void join_row(uint32_t n, const Get &get, Vec<D> &sum
 {
     constexpr int N = Vec<D>::N;
     const uint32_t lane = threadIdx.x & 31u, w = (threadIdx.x >> 5) % WPR;
-    m = -INFINITY;
-    for (uint32_t i = lane; i < n; i += 32)
+    const float2 none = make_float2(-INFINITY, 0.f);
+    const float2 mine = lane < n ? get(lane).ml() : none;  // the first 32 parts' (m, l), a lane each
+    m = mine.x;
+    for (uint32_t i = lane + 32; i < n; i += 32)
         m = fmaxf(m, get(i).ml().x);
 #pragma unroll
     for (uint32_t o = 16; o; o /= 2)
         m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
     const float ref = m == -INFINITY ? 0.f : m;
     l = 0.f;
-    for (uint32_t i = lane; i < n; i += 32) {
-        const float2 x = get(i).ml();
-        l += x.y * exp2f(x.x - ref);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        sum.v[e] = 0.f;
+    for (uint32_t first = 0; first < n; first += 32) {
+        const float2 x = first == 0 ? mine : first + lane < n ? get(first + lane).ml() : none;
+        const float f = exp2f(x.x - ref);
+        l += x.y * f;
+        const uint32_t end = min(n - first, 32u);
+#pragma unroll 4
+        for (uint32_t i = w; i < end; i += WPR) {
+            const auto part = get(first + i);
+            const float fi = __shfl_sync(~0u, f, i);
+            const float *src = part.o() + lane * N;
+            float v[N];
+            if (N == 4)
+                *reinterpret_cast<float4 *>(v) = part.valid ? *reinterpret_cast<const float4 *>(src) : make_float4(0, 0, 0, 0);
+            else
+                *reinterpret_cast<float2 *>(v) = part.valid ? *reinterpret_cast<const float2 *>(src) : make_float2(0, 0);
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                sum.v[e] += fi * v[e];
+        }
     }
 #pragma unroll
     for (uint32_t o = 16; o; o /= 2)
         l += __shfl_xor_sync(~0u, l, o);
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-        sum.v[e] = 0.f;
-#pragma unroll 4
-    for (uint32_t i = w; i < n; i += WPR) {
-        const auto part = get(i);
-        const float f = exp2f(part.ml().x - ref);
-        const float *src = part.o() + lane * N;
-        float x[N];
-        if (N == 4)
-            *reinterpret_cast<float4 *>(x) = part.valid ? *reinterpret_cast<const float4 *>(src) : make_float4(0, 0, 0, 0);
-        else
-            *reinterpret_cast<float2 *>(x) = part.valid ? *reinterpret_cast<const float2 *>(src) : make_float2(0, 0);
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            sum.v[e] += f * x[e];
-    }
 }
 
 template <int D>
@@ -100,35 +104,45 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
     const bool no_empty = U >= N;  // (64-bit divisions are what this kernel would otherwise spend its time on)
     const uint32_t n = last - c + 2;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-    for (uint32_t row = blockIdx.y * (JOIN_WARPS / WPR) + warp / WPR; row < sp.rows; row += gridDim.y * (JOIN_WARPS / WPR)) {
-        const auto get = [&](uint32_t i) {
-            Part<D> p;
-            const uint32_t run = c - 1 + i;
-            p.p = &a.parts;
-            p.valid = no_empty || i == 0 || run * U / N < (run + 1) * U / N;
-            p.at = (2ull * run + (i == 0 ? 1 : 0)) * a.parts.rows + row;
-            return p;
-        };
-        Vec<D> sum;
-        float m, l;
-        join_row<D, WPR>(n, get, sum, m, l);
+    // a warp's rows are summed BATCH at a time before any is written, so that their loads overlap
+    constexpr int BATCH = WPR == 1 ? 4 : 1;
+    constexpr uint32_t STEP = JOIN_WARPS / WPR;
+    for (uint32_t row0 = blockIdx.y * STEP * BATCH + warp / WPR; row0 < sp.rows; row0 += gridDim.y * STEP * BATCH) {
+        Vec<D> sum[BATCH];
+        float m[BATCH], l[BATCH];
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            const uint32_t row = min(row0 + b * STEP, sp.rows - 1);
+            const auto get = [&](uint32_t i) {
+                Part<D> p;
+                const uint32_t run = c - 1 + i;
+                p.p = &a.parts;
+                p.valid = no_empty || i == 0 || run * U / N < (run + 1) * U / N;
+                p.at = (2ull * run + (i == 0 ? 1 : 0)) * a.parts.rows + row;
+                return p;
+            };
+            join_row<D, WPR>(n, get, sum[b], m[b], l[b]);
+        }
         if (WPR > 1) {  // one row a block at a time: all warps take the same turns
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < Vec<D>::N; ++e)
-                s_sum[warp][lane * Vec<D>::N + e] = sum.v[e];
+                s_sum[warp][lane * Vec<D>::N + e] = sum[0].v[e];
             __syncthreads();
             if (warp == 0)
 #pragma unroll
                 for (int w = 1; w < WPR; ++w)
 #pragma unroll
                     for (int e = 0; e < Vec<D>::N; ++e)
-                        sum.v[e] += s_sum[w][lane * Vec<D>::N + e];
+                        sum[0].v[e] += s_sum[w][lane * Vec<D>::N + e];
         }
-        if (warp % WPR == 0) {
-            const uint32_t i = sp.row0 + row;
-            write_row<T, D>(a, sp.qa + (int32_t)(i / a.g), sp.head * a.g + i % a.g, sum, m, l);
-        }
+        if (warp % WPR == 0)
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const uint32_t i = sp.row0 + row0 + b * STEP;
+                if (row0 + b * STEP < sp.rows)
+                    write_row<T, D>(a, sp.qa + (int32_t)(i / a.g), sp.head * a.g + i % a.g, sum[b], m[b], l[b]);
+            }
     }
 }
 
@@ -290,7 +304,7 @@ cudaError_t join_split(const KvcAttn &a, cudaStream_t st)
 {
     if (a.parts.rows == KVC_ATTN_SMALL_ROWS)  // few rows, possibly of many parts: a block to a row
         return kvc_launch_pdl(kvc_join_split_kernel<T, D, JOIN_WARPS>, a, dim3(a.parts.blocks - 1, 4), JOIN_WARPS * 32, 0, st);
-    return kvc_launch_pdl(kvc_join_split_kernel<T, D, 1>, a, dim3(a.parts.blocks - 1, 32), JOIN_WARPS * 32, 0, st);
+    return kvc_launch_pdl(kvc_join_split_kernel<T, D, 1>, a, dim3(a.parts.blocks - 1, 8), JOIN_WARPS * 32, 0, st);
 }
 
 template <typename T, int D>

@@ -152,6 +152,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const float *x)
                  : "memory");
 }
 
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+
 // Two 32-bit floats in one 64-bit register pair, for the two-wide arithmetic.
 __device__ __forceinline__ uint64_t pair2(float lo, float hi)
 {
@@ -623,15 +631,18 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     const float base = m == -INFINITY ? 0.f : m;
                     const uint64_t scale2 = pair2(a.scale_log2, a.scale_log2), base2 = pair2(-base, -base);
                     uint64_t sum2 = 0;
-                    uint32_t p[HK / 2];
 #pragma unroll
-                    for (int k = 0; k < HK / 2; ++k) {
-                        const float2 x = unpair2(fma2(pair2(s[2 * k], s[2 * k + 1]), scale2, base2));
-                        const float y0 = exp2_fast(x.x), y1 = exp2_fast(x.y);
-                        sum2 = add2(sum2, pair2(y0, y1));
-                        p[k] = kvc_from_float2<T>(y0, y1);
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float2 x = unpair2(fma2(pair2(s[q * 32 + 2 * k], s[q * 32 + 2 * k + 1]), scale2, base2));
+                            const float y0 = exp2_fast(x.x), y1 = exp2_fast(x.y);
+                            sum2 = add2(sum2, pair2(y0, y1));
+                            p[k] = kvc_from_float2<T>(y0, y1);
+                        }
+                        tmem_st16(s_col + half * (HK / 2) + q * 16, p);
                     }
-                    tmem_st32(s_col + half * (HK / 2), reinterpret_cast<const float *>(p));
                     const float2 sum = unpair2(sum2);
                     l += sum.x + sum.y;
                     tmem_wait_st();
