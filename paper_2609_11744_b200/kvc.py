@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -205,11 +206,11 @@ def lib() -> ctypes.CDLL:
         "kvc_layout_set_kernel_timing": (ci, [vp, ci]),
         "kvc_layout_kernel_time": (ci, [vp, P(u32), P(ctypes.c_double), P(ctypes.c_double),
                                         P(ctypes.c_double)]),
-        "kvc_map_tokens": (ci, [vp, P(kvc_map_tokens_desc), vp]),
-        "kvc_append": (ci, [vp, P(kvc_append_desc), vp]),
+        "kvc_map_tokens": (ci, [vp, vp, vp]),
+        "kvc_append": (ci, [vp, vp, vp]),
         "kvc_attention_workspace_bytes": (ci, [vp, u32, u32, u32, u32, P(u64)]),
-        "kvc_attention": (ci, [vp, P(kvc_attention_desc), vp]),
-        "kvc_attention_shared": (ci, [vp, P(kvc_attention_desc), vp]),
+        "kvc_attention": (ci, [vp, vp, vp]),
+        "kvc_attention_shared": (ci, [vp, vp, vp]),
         "kvc_staging_ring_create": (ci, [u64, u32, ci, vp, u64, P(vp)]),
         "kvc_staging_ring_destroy": (ci, [vp]),
         "kvc_staging_ring_acquire": (ci, [vp, i64, P(u32), P(vp), P(vp)]),
@@ -586,34 +587,54 @@ def kvc_poll_device_status(layout, stream=None) -> Tuple[int, int]:
 
 
 # ------------------------------------------------------------------ a step's tokens
-# These calls take torch tensors and check what the C side cannot see: types, shapes, contiguity and
-# the device.  Every tensor must be on the current CUDA device.
-_dtypes = None
+# These calls take torch tensors and check what the C side cannot see: types, sizes, contiguity and
+# the device.  Every tensor must be on the current CUDA device.  They are made once a layer and step, so
+# the way through them is short: descriptors are packed in one go (struct format = C layout), and
+# a failed check is explained by a function of its own.
+class _Torch:
+    """What the calls need of torch, looked up once."""
 
-
-def _torch_dtypes():
-    global _dtypes
-    if _dtypes is None:
+    def __init__(self):
         import torch
-        _dtypes = {"i32": torch.int32, "i64": torch.int64, "f32": torch.float32, "cuda": torch.cuda,
-                   "kv": {torch.bfloat16: KVC_DTYPE_BF16, torch.float16: KVC_DTYPE_FP16}}
-    return _dtypes
+        self.i32, self.i64, self.f32 = torch.int32, torch.int64, torch.float32
+        self.kv = {torch.bfloat16: KVC_DTYPE_BF16, torch.float16: KVC_DTYPE_FP16}
+        torch.cuda.init()
+        c = torch._C
+        self.device = getattr(c, "_cuda_getDevice", torch.cuda.current_device)
+        self.stream = getattr(c, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _arg(t, name: str, dtype, shape, device: int, optional: bool = False) -> int:
-    """Address of a contiguous tensor of the given type and shape (None: any size) on `device`."""
+_torch = None
+_MAP_DESC = struct.Struct("@4PQ4I6PQ")
+_APPEND_DESC = struct.Struct("@2I4P8q3PQ2Pf5IQ")
+_ATTENTION_DESC = struct.Struct("@2I3P4q3PQ5If2I2P2IPQ")
+assert _MAP_DESC.size == ctypes.sizeof(kvc_map_tokens_desc)
+assert _APPEND_DESC.size == ctypes.sizeof(kvc_append_desc)
+assert _ATTENTION_DESC.size == ctypes.sizeof(kvc_attention_desc)
+
+
+def _step_call():
+    """(torch lookups, current device, library)."""
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch, _torch.device(), _lib or lib()
+
+
+def _complain(t, name, dtype, size, device):
     if t is None:
-        if optional:
-            return 0
         raise TypeError("%s is missing" % name)
     if t.dtype is not dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
     if t.get_device() != device:
         raise ValueError("%s is not on the current CUDA device" % name)
-    if len(t.shape) != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
-        raise ValueError("%s has shape %s, wanted %s" % (name, tuple(t.shape), shape))
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
+    raise ValueError("%s must be contiguous and have %d elements, not shape %s" % (name, size, tuple(t.shape)))
+
+
+def _arg(t, name: str, dtype, size: int, device: int) -> int:
+    """Address of a contiguous tensor of the given type and number of elements on `device`."""
+    if t is None or t.dtype is not dtype or t.get_device() != device or t.numel() != size or not t.is_contiguous():
+        _complain(t, name, dtype, size, device)
     return t.data_ptr()
 
 
@@ -623,26 +644,27 @@ def _heads(t, name: str, dtype, tokens, heads, dim, device: int):
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
     if t.get_device() != device:
         raise ValueError("%s is not on the current CUDA device" % name)
-    if t.dim() != 3 or t.shape[0] != tokens or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
+    if t.shape != (tokens, heads, dim):
         raise ValueError("%s has shape %s, wanted %s" % (name, tuple(t.shape), (tokens, heads, dim)))
     st, sh, se = t.stride()
     if se != 1 and dim > 1 and t.numel():
         raise ValueError("the elements of a head of %s must be adjacent" % name)
     # a dimension of one has no stride of its own: any will do
-    return t.data_ptr(), st if t.shape[0] > 1 else 0, sh if t.shape[1] > 1 else 0
+    return t.data_ptr(), st if tokens > 1 else 0, sh if heads > 1 else 0
 
 
-def _table(t, requests: int, device: int):
+def _table(t, requests: int, dtype, device: int):
     """(address, stride, entries per row) of a [requests, max_blocks] table whose rows may be apart."""
-    if t.dtype is not _torch_dtypes()["i32"]:
-        raise TypeError("block_tables must be torch.int32, not %s" % t.dtype)
+    if t.dtype is not dtype:
+        raise TypeError("block_tables must be %s, not %s" % (dtype, t.dtype))
     if t.get_device() != device:
         raise ValueError("block_tables is not on the current CUDA device")
     if t.dim() != 2 or t.shape[0] != requests:
         raise ValueError("block_tables has shape %s, wanted (%d, max_blocks)" % (tuple(t.shape), requests))
-    if t.shape[1] > 1 and t.stride(1) != 1 or requests > 1 and t.stride(0) < t.shape[1]:
+    wide, (row, entry) = t.shape[1], t.stride()
+    if wide > 1 and entry != 1 or requests > 1 and row < wide:
         raise ValueError("the entries of a row of block_tables must be adjacent, and its rows apart")
-    return t.data_ptr(), t.stride(0) if requests > 1 else t.shape[1], t.shape[1]
+    return t.data_ptr(), row if requests > 1 else wide, wide
 
 
 def kvc_map_tokens(layout, context_lens, new_lens, free_blocks, block_tables, cu_tokens, positions, slots,
@@ -652,17 +674,20 @@ def kvc_map_tokens(layout, context_lens, new_lens, free_blocks, block_tables, cu
     context_lens, new_lens [R] and free_blocks [F] are int32; block_tables [R, max_blocks] int32 is
     completed in place; cu_tokens [R + 1] int32, positions [T] int32, slots [T] int64 and, if given,
     token_request [T], total_lens [R] and counts [3] int32 are written."""
-    t = _torch_dtypes()
-    i32, dev = t["i32"], t["cuda"].current_device()
-    n, cap = context_lens.shape[0], positions.shape[0]
-    tab, stride, wide = _table(block_tables, n, dev)
-    d = kvc_map_tokens_desc(
-        _arg(context_lens, "context_lens", i32, (n,), dev), _arg(new_lens, "new_lens", i32, (n,), dev),
-        _arg(free_blocks, "free_blocks", i32, (None,), dev), tab, stride, wide, n, free_blocks.shape[0], cap,
-        _arg(cu_tokens, "cu_tokens", i32, (n + 1,), dev), _arg(positions, "positions", i32, (cap,), dev),
-        _arg(slots, "slots", t["i64"], (cap,), dev), _arg(token_request, "token_request", i32, (cap,), dev, True),
-        _arg(total_lens, "total_lens", i32, (n,), dev, True), _arg(counts, "counts", i32, (3,), dev, True), 0)
-    _check(lib().kvc_map_tokens(layout.handle, ctypes.byref(d), _stream(stream)), "kvc_map_tokens")
+    t, dev, L = _step_call()
+    i32, n, cap, free = t.i32, context_lens.numel(), positions.numel(), free_blocks.numel()
+    tab, stride, wide = _table(block_tables, n, i32, dev)
+    d = _MAP_DESC.pack(
+        _arg(context_lens, "context_lens", i32, n, dev), _arg(new_lens, "new_lens", i32, n, dev),
+        _arg(free_blocks, "free_blocks", i32, free, dev), tab, stride, wide, n, free, cap,
+        _arg(cu_tokens, "cu_tokens", i32, n + 1, dev), _arg(positions, "positions", i32, cap, dev),
+        _arg(slots, "slots", t.i64, cap, dev),
+        0 if token_request is None else _arg(token_request, "token_request", i32, cap, dev),
+        0 if total_lens is None else _arg(total_lens, "total_lens", i32, n, dev),
+        0 if counts is None else _arg(counts, "counts", i32, 3, dev), 0)
+    status = L.kvc_map_tokens(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
+    if status:
+        raise KvcError(status, "kvc_map_tokens")
 
 
 def kvc_append(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, q_weight=None, k_weight=None,
@@ -672,31 +697,35 @@ def kvc_append(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, q_
     q, q_out [T, Hq, D] (or both None), k, v [T, Hkv, D]: bf16 or fp16, any token and head strides;
     slots [T] int64; positions [T] int32 and cos_sin [max_positions, rot_dim] float32 (or both None:
     no rotation); q_weight, k_weight [D] of the type of k, or None: no norm."""
-    t = _torch_dtypes()
-    dev, dt = t["cuda"].current_device(), k.dtype
-    if dt not in t["kv"]:
+    t, dev, L = _step_call()
+    dt = k.dtype
+    kind = t.kv.get(dt)
+    if kind is None:
         raise TypeError("k must be torch.bfloat16 or torch.float16, not %s" % dt)
     n, hkv, dim = k.shape
     if (hkv, dim) != layout.heads:
         raise ValueError("k has %d heads of %d, the layout %d of %d" % ((hkv, dim) + layout.heads))
     if (q is None) != (q_out is None) or (positions is None) != (cos_sin is None):
         raise TypeError("q and q_out, and positions and cos_sin, go together")
-    qp = op = (0, 0, 0)
-    hq = 0
+    qp = qt = qh = op = ot = oh = hq = 0
     if q is not None:
         hq = q.shape[1]
-        qp, op = _heads(q, "q", dt, n, hq, dim, dev), _heads(q_out, "q_out", dt, n, hq, dim, dev)
-    kp, vp = _heads(k, "k", dt, n, hkv, dim, dev), _heads(v, "v", dt, n, hkv, dim, dev)
+        qp, qt, qh = _heads(q, "q", dt, n, hq, dim, dev)
+        op, ot, oh = _heads(q_out, "q_out", dt, n, hq, dim, dev)
+    kp, kt, kh = _heads(k, "k", dt, n, hkv, dim, dev)
+    vp, vt, vh = _heads(v, "v", dt, n, hkv, dim, dev)
     rot = rows = cs = pos = 0
     if cos_sin is not None:
-        pos = _arg(positions, "positions", t["i32"], (n,), dev)
-        cs = _arg(cos_sin, "cos_sin", t["f32"], (None, None), dev)
         rows, rot = cos_sin.shape
-    d = kvc_append_desc(layer, t["kv"][dt], qp[0], kp[0], vp[0], op[0], qp[1], qp[2], kp[1], kp[2], vp[1], vp[2],
-                        op[1], op[2], _arg(slots, "slots", t["i64"], (n,), dev), pos, cs, rot,
-                        _arg(q_weight, "q_weight", dt, (dim,), dev, True),
-                        _arg(k_weight, "k_weight", dt, (dim,), dev, True), eps, n, hq, rot, rows, int(interleaved), 0)
-    _check(lib().kvc_append(layout.handle, ctypes.byref(d), _stream(stream)), "kvc_append")
+        pos = _arg(positions, "positions", t.i32, n, dev)
+        cs = _arg(cos_sin, "cos_sin", t.f32, rows * rot, dev)
+    d = _APPEND_DESC.pack(layer, kind, qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, _arg(slots, "slots", t.i64, n, dev), pos, cs, rot,
+                          0 if q_weight is None else _arg(q_weight, "q_weight", dt, dim, dev),
+                          0 if k_weight is None else _arg(k_weight, "k_weight", dt, dim, dev), eps, n, hq, rot, rows,
+                          1 if interleaved else 0, 0)
+    status = L.kvc_append(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
+    if status:
+        raise KvcError(status, "kvc_append")
 
 
 def kvc_attention_workspace_bytes(layout, n_tokens: int, n_requests: int, n_q_heads: int, n_groups: int = 0) -> int:
@@ -709,27 +738,32 @@ def kvc_attention_workspace_bytes(layout, n_tokens: int, n_requests: int, n_q_he
 
 def _attention(name, layout, layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, window, sinks, lse,
                max_q_len, group_starts, prefix_lens, stream):
-    t = _torch_dtypes()
-    i32, dev, dt = t["i32"], t["cuda"].current_device(), q.dtype
-    if dt not in t["kv"]:
+    t, dev, L = _step_call()
+    i32, dt = t.i32, q.dtype
+    kind = t.kv.get(dt)
+    if kind is None:
         raise TypeError("q must be torch.bfloat16 or torch.float16, not %s" % dt)
     n, hq, dim = q.shape
     if dim != layout.heads[1]:
         raise ValueError("q has heads of %d, the layout of %d" % (dim, layout.heads[1]))
-    r = seq_lens.shape[0]
-    tab, stride, wide = _table(block_tables, r, dev)
-    qp, op = _heads(q, "q", dt, n, hq, dim, dev), _heads(out, "out", dt, n, hq, dim, dev)
-    groups = 0 if prefix_lens is None else prefix_lens.shape[0]
+    r = seq_lens.numel()
+    tab, stride, wide = _table(block_tables, r, i32, dev)
+    qp, qt, qh = _heads(q, "q", dt, n, hq, dim, dev)
+    op, ot, oh = _heads(out, "out", dt, n, hq, dim, dev)
+    gs = pl = groups = 0
+    if prefix_lens is not None:
+        groups = prefix_lens.numel()
+        gs, pl = _arg(group_starts, "group_starts", i32, groups + 1, dev), _arg(prefix_lens, "prefix_lens", i32, groups, dev)
     if workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
-    d = kvc_attention_desc(
-        layer, t["kv"][dt], qp[0], op[0], _arg(lse, "lse", t["f32"], (n, hq), dev, True), qp[1], qp[2], op[1], op[2],
-        _arg(cu_tokens, "cu_tokens", i32, (r + 1,), dev), _arg(seq_lens, "seq_lens", i32, (r,), dev), tab, stride, wide,
-        n, r, hq, max_q_len, dim ** -0.5 if scale is None else scale, window, sinks,
-        _arg(group_starts, "group_starts", i32, (groups + 1,), dev, not groups),
-        _arg(prefix_lens, "prefix_lens", i32, (groups,), dev, not groups), groups, 0, workspace.data_ptr(),
-        workspace.numel() * workspace.element_size())
-    _check(getattr(lib(), name)(layout.handle, ctypes.byref(d), _stream(stream)), name)
+    d = _ATTENTION_DESC.pack(
+        layer, kind, qp, op, 0 if lse is None else _arg(lse, "lse", t.f32, n * hq, dev), qt, qh, ot, oh,
+        _arg(cu_tokens, "cu_tokens", i32, r + 1, dev), _arg(seq_lens, "seq_lens", i32, r, dev), tab, stride, wide,
+        n, r, hq, max_q_len, dim ** -0.5 if scale is None else scale, window, sinks, gs, pl, groups, 0,
+        workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    status = getattr(L, name)(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
+    if status:
+        raise KvcError(status, name)
 
 
 def kvc_attention(layout, layer: int, q, out, block_tables, seq_lens, cu_tokens, workspace, scale=None, window: int = 0,
