@@ -50,9 +50,9 @@ __device__ __forceinline__ void join_row(uint32_t n, const Get &get, Vec<D> &sum
             const float *src = part.o() + lane * N;
             float v[N];
             if (N == 4)
-                *reinterpret_cast<float4 *>(v) = part.valid ? *reinterpret_cast<const float4 *>(src) : make_float4(0, 0, 0, 0);
+                *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(src);
             else
-                *reinterpret_cast<float2 *>(v) = part.valid ? *reinterpret_cast<const float2 *>(src) : make_float2(0, 0);
+                *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
 #pragma unroll
             for (int e = 0; e < N; ++e)
                 sum.v[e] += fi * v[e];
@@ -67,8 +67,7 @@ template <int D>
 struct Part {
     const KvcParts *p;
     uint64_t at;  // slot * ROWS + row
-    bool valid;   // a block without units has left nothing
-    __device__ float2 ml() const { return valid ? p->ml[at] : make_float2(-INFINITY, 0.f); }
+    __device__ float2 ml() const { return p->ml[at]; }
     __device__ const float *o() const { return p->o + at * D; }
 };
 
@@ -97,11 +96,9 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
     kvc_pdl_wait();
     const uint32_t c = blockIdx.x + 1;
     const KvcSplit sp = a.parts.split[c];
-    const unsigned long long N = a.parts.blocks, U = sp.length;
-    if (sp.end == sp.begin || (c - 1) * U / N > sp.begin)
+    if (sp.end == sp.begin || kvc_cut(c - 1, sp.length, sp.runs) > sp.begin)
         return;
-    const uint32_t last = (uint32_t)((sp.end * N - 1) / U);  // the run that holds the pair's last unit
-    const bool no_empty = U >= N;  // (64-bit divisions are what this kernel would otherwise spend its time on)
+    const uint32_t last = kvc_run_of(sp.end - 1, sp.length, sp.runs);  // the run that holds the pair's last unit
     const uint32_t n = last - c + 2;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     // a warp's rows are summed BATCH at a time before any is written, so that their loads overlap
@@ -117,7 +114,6 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
                 Part<D> p;
                 const uint32_t run = c - 1 + i;
                 p.p = &a.parts;
-                p.valid = no_empty || i == 0 || run * U / N < (run + 1) * U / N;
                 p.at = (2ull * run + (i == 0 ? 1 : 0)) * a.parts.rows + row;
                 return p;
             };
@@ -150,7 +146,6 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
 struct PhaseRow {
     uint32_t first, n;
     uint64_t pair, row;
-    unsigned long long length;
 };
 
 __device__ __forceinline__ PhaseRow phase_row(const KvcParts &p, uint32_t seq, uint32_t head, uint32_t rows, uint32_t i)
@@ -159,16 +154,17 @@ __device__ __forceinline__ PhaseRow phase_row(const KvcParts &p, uint32_t seq, u
     const uint32_t tiles = (rows + p.rows - 1) / p.rows;
     r.pair = (uint64_t)p.base[seq] + (uint64_t)head * tiles + i / p.rows;
     r.row = i % p.rows;
-    r.length = *p.length;
+    const unsigned long long length = p.length[0];
+    const uint32_t runs = (uint32_t)p.length[1];
     r.first = r.n = 0;
     // what lengths that contradict one another lead to is left out
-    if (i >= rows || r.pair >= p.max_pairs || r.length == 0)
+    if (i >= rows || r.pair >= p.max_pairs || length == 0)
         return r;
     const ulonglong2 u = p.range[r.pair];
-    if (u.x >= u.y || u.y > r.length)
+    if (u.x >= u.y || u.y > length)
         return r;
-    r.first = (uint32_t)(((u.x + 1) * p.blocks - 1) / r.length);
-    r.n = (uint32_t)((u.y * p.blocks - 1) / r.length) - r.first + 1;
+    r.first = kvc_run_of(u.x, length, runs);
+    r.n = kvc_run_of(u.y - 1, length, runs) - r.first + 1;
     return r;
 }
 
@@ -191,13 +187,12 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_shared_kernel(const 
     if ((int32_t)tok < a.cu_q[0])
         return;  // rows before the first sequence belong to none
     const uint32_t h = head / a.g, x = head % a.g;
-    const uint32_t r = kvc_last_at_most(a.cu_q, a.n_requests, (int32_t)tok);
+    const uint32_t r = kvc_last_at_most_warp(a.cu_q, a.n_requests, (int32_t)tok);
     const int32_t qa = a.cu_q[r], qe = kvc_clamp(a.cu_q[r + 1], qa, (int32_t)a.n_tokens);
     const PhaseRow s = phase_row(j.suffix, r, h, (uint32_t)(qe - qa) * a.g, (tok - (uint32_t)qa) * a.g + x);
     PhaseRow p;
     p.first = p.n = 0;
     p.pair = p.row = 0;
-    p.length = 1;
     const int32_t g = kvc_group_of(a, r);
     if (g >= 0) {
         const int32_t R = (int32_t)a.n_requests;
@@ -210,10 +205,8 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_shared_kernel(const 
         const bool in_prefix = i < p.n;
         const KvcParts &from = in_prefix ? j.prefix : j.suffix;
         const PhaseRow &at = in_prefix ? p : s;
-        const unsigned long long run = at.first + (in_prefix ? i : i - p.n), N = from.blocks;
         q.p = &from;
-        q.valid = at.length >= N || run * at.length / N < (run + 1) * at.length / N;
-        q.at = (run + at.pair) * from.rows + at.row;
+        q.at = (at.first + (in_prefix ? i : i - p.n) + at.pair) * from.rows + at.row;
         return q;
     };
     Vec<D> sum;
@@ -258,7 +251,7 @@ void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, bool t
     if (pairs) {
         c.take(p.base, sequences);
         c.take(p.range, pairs);
-        c.take(p.length, 1);
+        c.take(p.length, 2);
     } else {
         c.take(p.split, blocks);
     }
@@ -409,6 +402,7 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
         j.prefix = a.parts;
         e = launch(many_prefix);
         a.phase = KVC_PHASE_SUFFIX;
+        a.beside = 1;  // the two phases share nothing but what they read
         carve(c, a.parts, lay, shape, many, d->n_requests, true);
         j.suffix = a.parts;
         if (e == cudaSuccess)

@@ -11,6 +11,8 @@
 // then is partial -- weighted sum, running maximum and sum of the rows -- and goes to the workspace; a
 // second kernel joins the parts of a pair in the order of its keys, so results do not depend on the
 // order in which blocks run.  A cut inside a pair's HEAD leaves the whole pair to the block behind it.
+// A short line is cut into fewer runs, of LEAST at least: what a part costs to write and to join is then
+// not more than what the cut saves, and the blocks left over end at once.
 #ifndef KVC_ATTENTION_H
 #define KVC_ATTENTION_H
 
@@ -34,6 +36,7 @@ enum {
 struct KvcSplit {
     unsigned long long begin, end;  // where the pair's units lie on the line
     unsigned long long length;      // of the line
+    uint32_t runs, reserved;        // that it is cut into
     int32_t qa;                     // first token row of the sequence
     uint32_t row0, rows, head;      // first row, rows of the pair, KV head
 };
@@ -45,8 +48,8 @@ struct KvcParts {
     KvcSplit *split; // [block]                                       (WHOLE)
     uint32_t *base;  // [sequence] index of its first pair            (PREFIX, SUFFIX)
     ulonglong2 *range;  // [pair] where its units lie on the line     (PREFIX, SUFFIX)
-    unsigned long long *length;  // of the line                       (PREFIX, SUFFIX)
-    uint32_t blocks; // gridDim.x of the kernel that writes them
+    unsigned long long *length;  // of the line, and its runs         (PREFIX, SUFFIX)
+    uint32_t blocks; // gridDim.x of the kernel that writes them: runs at most
     uint32_t rows;   // ROWS of that kernel
     uint32_t max_pairs;  // pairs that there is room for (PREFIX, SUFFIX): enough for token rows that
                          // ascend, so only lengths that contradict one another can ask for more
@@ -69,6 +72,7 @@ struct KvcAttn {
     float scale_log2;
     int32_t window, sinks;
     uint32_t phase;
+    uint32_t beside;  // the kernel may run beside the stream's previous one (see kvc_pdl_begin)
     uint32_t *status;
     KvcParts parts;
 };
@@ -86,6 +90,19 @@ uint32_t kvc_attn_tiles_blocks(const kvc_layout *lay);
 cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
 
 #ifdef __CUDACC__
+
+// Where run c of `runs` begins on a line.  (64-bit divisions are worth avoiding: they are a good part of
+// what the kernels do before their first load.)
+__device__ __forceinline__ unsigned long long kvc_cut(uint32_t c, unsigned long long length, uint32_t runs)
+{
+    return length < (1ull << 20) ? c * (uint32_t)length / runs : c * length / runs;
+}
+// The run that holds place x (the last of those that begin there, which is the one that is not empty).
+__device__ __forceinline__ uint32_t kvc_run_of(unsigned long long x, unsigned long long length, uint32_t runs)
+{
+    return length < (1ull << 20) ? (((uint32_t)x + 1) * runs - 1) / (uint32_t)length
+                                 : (uint32_t)(((x + 1) * runs - 1) / length);
+}
 
 struct KvcSeq {
     int32_t qa, rows;   // first token row; rows (tokens * G)
@@ -105,6 +122,21 @@ __device__ __forceinline__ uint32_t kvc_last_at_most(const int32_t *v, uint32_t 
             lo = mid;
         else
             hi = mid;
+    }
+    return lo;
+}
+
+// The same for a whole warp at once: 32 places are looked at in one load.
+__device__ __forceinline__ uint32_t kvc_last_at_most_warp(const int32_t *v, uint32_t n, int32_t x)
+{
+    uint32_t lo = 0;
+    while (n > 1) {
+        const uint32_t step = (n + 31) / 32, at = (threadIdx.x & 31u) * step;
+        const uint32_t hit = __ballot_sync(~0u, at < n && v[lo + at] <= x);
+        // (a ballot of ascending values is a run of ones from lane 0; taken as 0 where even the first is larger)
+        const uint32_t k = hit ? 31u - __clz(hit) : 0u;
+        lo += k * step;
+        n = min(step, n - k * step);
     }
     return lo;
 }
@@ -239,7 +271,7 @@ struct KvcRun {
     }
 };
 
-template <int ROWS, int TK, int HEAD, int THREADS>
+template <int ROWS, int TK, int HEAD, int LEAST, int THREADS>
 __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
 {
     __shared__ unsigned long long sums[THREADS / 32][2];
@@ -292,7 +324,9 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
         bu += iu - units;
         bp += ip - pairs;
     }
-    const unsigned long long begin = blockIdx.x * total / gridDim.x, end = (blockIdx.x + 1ull) * total / gridDim.x;
+    const uint32_t runs = (uint32_t)max(1ull, min((unsigned long long)gridDim.x, total / LEAST));
+    const unsigned long long begin = blockIdx.x < runs ? kvc_cut(blockIdx.x, total, runs) : total;
+    const unsigned long long end = blockIdx.x < runs ? kvc_cut(blockIdx.x + 1, total, runs) : total;
     if (threadIdx.x == 0) {
         found.end = end;
         found.any = begin < end;
@@ -318,7 +352,8 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
                 for (uint32_t o = 16; o; o /= 2)
                     per_head += __shfl_xor_sync(~0u, per_head, o);
             if (mine && begin >= u && begin < u + per_head * a.hkv) {
-                const uint32_t h = (uint32_t)((begin - u) / per_head);
+                const uint32_t h = per_head < (1ull << 32) && begin - u < (1ull << 32) ? (uint32_t)(begin - u) / (uint32_t)per_head
+                                                                                        : (uint32_t)((begin - u) / per_head);
                 unsigned long long b = u + h * per_head;
                 KvcRange r;
                 uint32_t rt = rt0;
@@ -369,6 +404,8 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
             KvcSplit sp;
             sp.begin = sp.end = 0;
             sp.length = total;
+            sp.runs = runs;
+            sp.reserved = 0;
             sp.qa = 0;
             sp.row0 = sp.rows = sp.head = 0;
             if (begin < total && run.at.t > 0) {
@@ -381,7 +418,8 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
             }
             a.parts.split[blockIdx.x] = sp;
         } else if (blockIdx.x == 0) {
-            *a.parts.length = total;
+            a.parts.length[0] = total;
+            a.parts.length[1] = runs;
         }
     }
     return run;

@@ -20,6 +20,7 @@ constexpr int TK = 64;             // keys per unit
 constexpr int WK = TK / WARPS;     // keys per warp and unit
 constexpr int ROWS = KVC_ATTN_SMALL_ROWS;
 constexpr int HEAD = 1;            // what a pair costs besides its units, in units
+constexpr int LEAST = 2;           // units of a run at least
 
 template <int D>
 struct Shape {
@@ -106,12 +107,14 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint32_t s_there[WARPS][S::STAGES];
     __shared__ float s_m[WARPS][ROWS], s_l[WARPS][ROWS];
-    kvc_pdl_wait();
+    kvc_pdl_begin(a.beside);
 
     const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
-    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, THREADS>(a, n_seq);
-    if (!run.any)
+    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, LEAST, THREADS>(a, n_seq);
+    if (!run.any) {
+        kvc_pdl_end(a.beside);
         return;
+    }
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t ring = smem_addr(smem) + warp * S::STAGES * S::STAGE;
     float *merge = reinterpret_cast<float *>(smem + WARPS * S::STAGES * S::STAGE);
@@ -345,6 +348,7 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
         kvc_next<ROWS, TK>(a, n_seq, c);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    kvc_pdl_end(a.beside);
 }
 
 template <typename T, int D>

@@ -33,6 +33,7 @@ constexpr int TK = 128;             // keys of a K or V stage
 constexpr int HK = TK / 2;          // keys of one softmax thread
 constexpr int THREADS = 640;
 constexpr int HEAD = 3;             // what a pair costs besides its units, in units (measured: 13,000 cycles against 3,800)
+constexpr int LEAST = 5;            // units of a run at least
 constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper than the K ring
 
 template <int D>
@@ -136,6 +137,16 @@ __device__ __forceinline__ void tmem_ld32(float *x, uint32_t addr)
                    "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
                    "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
                    "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr) : "memory");
+}
+
+// 16 rows x 32 columns: four lanes to a row, x[4 * k + 2 * e + i] is row lane / 4 + 8 * e, column 8 * k + 2 * (lane % 4) + i.
+__device__ __forceinline__ void tmem_ld16x256(float *x, uint32_t addr)
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(x);
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(addr) : "memory");
 }
 
@@ -412,12 +423,14 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     __shared__ uint32_t s_dead, s_tmem;
     __shared__ Segment segments[SEGMENTS];
     __shared__ float row_top[2][2][128], row_sum[2][2][128];  // [row tile][half][row]
-    kvc_pdl_wait();
+    kvc_pdl_begin(a.beside);
 
     const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
-    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, THREADS>(a, n_seq);
-    if (!run.any)
+    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, LEAST, THREADS>(a, n_seq);
+    if (!run.any) {
+        kvc_pdl_end(a.beside);
         return;
+    }
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t tiles = (smem_addr(smem_raw) + 1023u) & ~1023u;
     unsigned char *tiles_ptr = smem_raw + (tiles - smem_addr(smem_raw));
@@ -512,49 +525,58 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 if (!__all_sync(~0u, bar_wait(o_done, o_parity ^ 1u, dead, a.status)))
                     break;
                 fence_after();
-                const uint32_t i = row0 + tid;
-                if (a.phase == KVC_PHASE_WHOLE && from_start && to_end) {
-                    const uint32_t tok = i / a.g;
-                    const uint32_t head = c.h * a.g + (i - tok * a.g);
-                    const int64_t row = c.q.qa + (int32_t)tok;
-                    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
-                    unsigned char *dst = a.out + row * a.o_tok + (int64_t)head * a.o_head + half * D;
+                // O in the other layout that tensor memory is read in: a lane holds two neighbouring columns of rows
+                // lane / 4 and lane / 4 + 8 of 16, so that four lanes write adjacent bytes of one row and a store
+                // touches 8 rows and not 32
+                const bool whole = a.phase == KVC_PHASE_WHOLE && from_start && to_end;
+                const bool room = a.phase == KVC_PHASE_WHOLE || c.pair < a.parts.max_pairs;
+                const uint64_t slot_row = (a.phase == KVC_PHASE_WHOLE ? 2ull * blockIdx.x + (from_start ? 1 : 0)
+                                                                      : (uint64_t)blockIdx.x + c.pair) * ROWS + sub * 128u;
+                const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
 #pragma unroll 1
-                    for (int q = 0; q < D / 2; q += 32) {
-                        float o[32];
-                        tmem_ld32(o, o_col + q);
+                for (uint32_t rows16 = 0; rows16 < 32; rows16 += 16) {
+                    unsigned char *dst[2];
+                    float f[2];
+                    bool write[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t in_warp = rows16 + (lane >> 2) + 8 * e, r = (warp & 3u) * 32u + in_warp;
+                        const uint32_t i = row0 + r, tok = i / a.g, head = c.h * a.g + (i - tok * a.g);
+                        f[e] = __shfl_sync(~0u, inv, in_warp);
+                        write[e] = i < (uint32_t)c.q.rows && room;
+                        dst[e] = whole ? a.out + (c.q.qa + (int64_t)tok) * a.o_tok + (int64_t)head * a.o_head + half * D + (lane & 3u) * 4u
+                                       : reinterpret_cast<unsigned char *>(a.parts.o + (slot_row + r) * D + half * (D / 2) + (lane & 3u) * 2u);
+                    }
+#pragma unroll 1
+                    for (uint32_t q = 0; q < D / 2; q += 32) {
+                        float o[16];
+                        tmem_ld16x256(o, o_col + (rows16 << 16) + q);
                         tmem_wait_ld();
-                        if (real)
 #pragma unroll
-                            for (int k = 0; k < 32; k += 8) {
-                                float x[8];
+                        for (int k = 0; k < 4; ++k)
 #pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    x[e] = l == 0.f ? 0.f : o[k + e] * inv;
-                                *reinterpret_cast<uint4 *>(dst + (q + k) * 2) = kvc_pack8<T>(x);
+                            for (int e = 0; e < 2; ++e) {
+                                const float x = o[k * 4 + e * 2], y = o[k * 4 + e * 2 + 1];
+                                if (!write[e])
+                                    continue;
+                                if (whole)
+                                    *reinterpret_cast<uint32_t *>(dst[e] + (q + k * 8) * 2) =
+                                        f[e] == 0.f ? 0u : kvc_from_float2<T>(x * f[e], y * f[e]);
+                                else
+                                    *reinterpret_cast<float2 *>(dst[e] + (q + k * 8) * 4) = make_float2(x, y);
                             }
                     }
-                    if (real && a.lse && half == 0)
-                        a.lse[row * a.hq + head] = (m + log2f(l)) * 0.693147180559945309f;
-                } else {
-                    const bool room = a.phase == KVC_PHASE_WHOLE || c.pair < a.parts.max_pairs;
-                    const uint64_t at = (a.phase == KVC_PHASE_WHOLE ? 2ull * blockIdx.x + (from_start ? 1 : 0)
-                                                                    : (uint64_t)blockIdx.x + c.pair) * ROWS + sub * 128u + tid;
-#pragma unroll 1
-                    for (int q = 0; q < D / 2; q += 32) {
-                        float o[32];
-                        tmem_ld32(o, o_col + q);
-                        tmem_wait_ld();
-                        if (real && room)
-#pragma unroll
-                            for (int k = 0; k < 32; k += 4)
-                                *reinterpret_cast<float4 *>(a.parts.o + at * D + half * (D / 2) + q + k) =
-                                    make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                }
+                if (real && half == 0) {
+                    if (!whole) {
+                        if (room)
+                            a.parts.ml[slot_row + tid] = make_float2(m, l);
+                        if (a.phase != KVC_PHASE_WHOLE && from_start && sub == 0 && tid == 0 && room)
+                            a.parts.range[c.pair] = make_ulonglong2(c.units_at, c.units_at + c.r.n);
+                    } else if (a.lse) {
+                        const uint32_t i = row0 + tid, tok = i / a.g;
+                        a.lse[(c.q.qa + (int64_t)tok) * a.hq + c.h * a.g + (i - tok * a.g)] = (m + log2f(l)) * 0.693147180559945309f;
                     }
-                    if (real && room && half == 0)
-                        a.parts.ml[at] = make_float2(m, l);
-                    if (a.phase != KVC_PHASE_WHOLE && from_start && sub == 0 && half == 0 && tid == 0 && room)
-                        a.parts.range[c.pair] = make_ulonglong2(c.units_at, c.units_at + c.r.n);
                 }
             }
             if (!ok)
@@ -780,6 +802,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS));
     }
+    kvc_pdl_end(a.beside);
 }
 
 // A tensor map of one plane of the pool: [block][token][head][element].

@@ -16,6 +16,21 @@ __device__ __forceinline__ void kvc_pdl_wait()
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// The same for a kernel that shares nothing with the one before it on the stream, and may run beside it
+// (`beside`): the kernel before has itself waited for all that came earlier, and kvc_pdl_end() makes
+// this one's end stand for the other's end too.  Every block calls both.
+__device__ __forceinline__ void kvc_pdl_begin(uint32_t beside)
+{
+    if (!beside)
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void kvc_pdl_end(uint32_t beside)
+{
+    if (beside)
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 template <typename A>
 inline cudaError_t kvc_launch_pdl(void (*kernel)(const A), const A &a, dim3 grid, uint32_t threads, uint32_t smem,
                                   cudaStream_t st)

@@ -3,6 +3,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kvc_internal.h"
 #include "kvc_device.h"
@@ -205,8 +206,9 @@ __global__ void __launch_bounds__(MAP_THREADS) kvc_map_tokens_kernel(const MapAr
 // once to the pool's type.  Bound by memory: every element is read once and written once.  A team
 // of head_dim / 8 lanes (rounded up to a power of two) holds one head, 16 bytes a lane, so the
 // mean is a few shuffles and the partner of a "halves" pair is one shuffle away.  A warp serves
-// several heads of ONE token, so its table row, slot and addresses are fetched once; four heads are
-// loaded before the first is used, which keeps 64 bytes a lane in flight.
+// several heads of ONE token, so its table row, slot and addresses are fetched once; eight heads a
+// team are loaded before the first is used, which keeps 128 bytes a lane in flight.  VEC: rows of the
+// cos/sin table are 16-byte aligned.
 struct AppendArgs {
     const unsigned char *q, *k, *v;
     unsigned char *q_out, *k_plane, *v_plane;
@@ -226,9 +228,9 @@ struct AppendArgs {
 };
 
 #define APPEND_THREADS 256u
-#define APPEND_UNROLL 4
+#define APPEND_UNROLL 8
 
-template <typename T, bool NEIGHBOURS>
+template <typename T, bool NEIGHBOURS, bool VEC>
 __global__ void __launch_bounds__(APPEND_THREADS) kvc_append_kernel(const AppendArgs a)
 {
     kvc_pdl_wait();
@@ -241,10 +243,23 @@ __global__ void __launch_bounds__(APPEND_THREADS) kvc_append_kernel(const Append
     const float inv_d = 1.0f / (float)a.d;
     const bool rotated = a.rot != 0 && l * 8u < a.rot;
     const uint32_t half = a.rot / 16u;  // lanes in one half of the rotated part
+    const uint32_t v0 = a.hq + a.hkv;  // first value head
     for (uint64_t u = blockIdx.x * (APPEND_THREADS / 32u) + (threadIdx.x >> 5); u < units; u += warps) {
         const uint32_t tok = (uint32_t)(u / a.chunks);
         const uint32_t h0 = (uint32_t)(u - (uint64_t)tok * a.chunks) * a.chunk;
         const uint32_t h1 = min(h0 + a.chunk, heads);
+        const unsigned char *const q = a.q + tok * a.q_tok, *const k = a.k + tok * a.k_tok, *const v = a.v + tok * a.v_tok;
+        uint4 raw[APPEND_UNROLL];
+        const auto load = [&](uint32_t hb) {
+#pragma unroll
+            for (int i = 0; i < APPEND_UNROLL; ++i) {
+                const uint32_t h = hb + i * teams;
+                const unsigned char *src = h < a.hq ? q + h * a.q_head : h < v0 ? k + (h - a.hq) * a.k_head : v + (h - v0) * a.v_head;
+                raw[i] = h < h1 && on ? *reinterpret_cast<const uint4 *>(src + l * 16u) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        // the first heads are on their way before the slot, the position and the angles are
+        load(h0 + team);
         const int64_t slot = a.slots[tok];
         if (slot < 0)
             continue;  // a row without a token
@@ -259,72 +274,73 @@ __global__ void __launch_bounds__(APPEND_THREADS) kvc_append_kernel(const Append
                                ((uint64_t)slot - id * a.block_size) * a.hkv * a.d * sizeof(T);
         // the eight values of this lane use angles [a0, a0 + 8) (halves) or [a0, a0 + 4) (neighbours)
         float cs[8], sn[8];
-        if (rotated) {
+        if (rotated && h0 < v0) {
             const float *row = a.cos_sin + (int64_t)pos * a.cs_stride;
             const uint32_t a0 = NEIGHBOURS ? l * 4u : (l < half ? l : l - half) * 8u;
+            if (VEC) {
 #pragma unroll
-            for (int i = 0; i < (NEIGHBOURS ? 4 : 8); ++i) {
-                cs[i] = row[a0 + i];
-                sn[i] = row[a.rot / 2 + a0 + i];
+                for (int i = 0; i < (NEIGHBOURS ? 1 : 2); ++i) {
+                    *reinterpret_cast<float4 *>(cs + 4 * i) = *reinterpret_cast<const float4 *>(row + a0 + 4 * i);
+                    *reinterpret_cast<float4 *>(sn + 4 * i) = *reinterpret_cast<const float4 *>(row + a.rot / 2 + a0 + 4 * i);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < (NEIGHBOURS ? 4 : 8); ++i) {
+                    cs[i] = row[a0 + i];
+                    sn[i] = row[a.rot / 2 + a0 + i];
+                }
             }
         }
-        for (uint32_t hb = h0 + team; hb < h1 + team; hb += teams * APPEND_UNROLL) {
-            uint4 raw[APPEND_UNROLL];
+        for (uint32_t hb = h0 + team;;) {
 #pragma unroll
             for (int i = 0; i < APPEND_UNROLL; ++i) {
                 const uint32_t h = hb + i * teams;
-                raw[i] = make_uint4(0, 0, 0, 0);
-                if (h < h1 && on) {
-                    const unsigned char *src = h < a.hq ? a.q + tok * a.q_tok + h * a.q_head
-                                               : h < a.hq + a.hkv ? a.k + tok * a.k_tok + (h - a.hq) * a.k_head
-                                                                  : a.v + tok * a.v_tok + (h - a.hq - a.hkv) * a.v_head;
-                    raw[i] = *reinterpret_cast<const uint4 *>(src + l * 16u);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < APPEND_UNROLL; ++i) {
-                const uint32_t h = hb + i * teams;
-                const bool is_v = h >= a.hq + a.hkv;
+                // (whole warps: a team past its unit's heads goes through the shuffles with zeros)
+                if (h - team >= h1)
+                    break;
+                const bool is_v = h >= v0;
                 uint4 res = raw[i];
-                // the shuffles below are taken by whole warps: teams past the last head go through
-                // them with zeros, and one condition of the loop is the same for all teams of a warp
-                float x[8];
-                kvc_unpack8<T>(raw[i], x);
-                const void *weight = h < a.hq ? a.q_weight : a.k_weight;
-                float sum = 0.f;
+                if (h - team < v0) {
+                    float x[8];
+                    kvc_unpack8<T>(raw[i], x);
+                    const void *weight = h < a.hq ? a.q_weight : a.k_weight;
+                    if (a.q_weight || a.k_weight) {
+                        float sum = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    sum += x[e] * x[e];
-                for (uint32_t o = a.lanes / 2; o; o /= 2)
-                    sum += __shfl_xor_sync(~0u, sum, o);
-                if (weight && on && !is_v && h < h1) {
-                    const float inv = rsqrtf(sum * inv_d + a.eps);
-                    float wv[8];
-                    kvc_unpack8<T>(reinterpret_cast<const uint4 *>(weight)[l], wv);
+                        for (int e = 0; e < 8; ++e)
+                            sum += x[e] * x[e];
+                        for (uint32_t o = a.lanes / 2; o; o /= 2)
+                            sum += __shfl_xor_sync(~0u, sum, o);
+                        if (weight && on) {
+                            const float inv = rsqrtf(sum * inv_d + a.eps);
+                            float wv[8];
+                            kvc_unpack8<T>(reinterpret_cast<const uint4 *>(weight)[l], wv);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[e] = x[e] * inv * wv[e];
-                }
-                if (NEIGHBOURS) {
-                    if (rotated) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float p = x[2 * e], q = x[2 * e + 1];
-                            x[2 * e] = p * cs[e] - q * sn[e];
-                            x[2 * e + 1] = q * cs[e] + p * sn[e];
+                            for (int e = 0; e < 8; ++e)
+                                x[e] = x[e] * inv * wv[e];
                         }
                     }
-                } else if (a.rot) {
-                    const uint32_t from = team * a.lanes + (rotated ? (l < half ? l + half : l - half) : l);
+                    if (NEIGHBOURS) {
+                        if (rotated) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float p = __shfl_sync(~0u, x[e], from);
-                        if (rotated)
-                            x[e] = l < half ? x[e] * cs[e] - p * sn[e] : x[e] * cs[e] + p * sn[e];
+                            for (int e = 0; e < 4; ++e) {
+                                const float y = x[2 * e], z = x[2 * e + 1];
+                                x[2 * e] = y * cs[e] - z * sn[e];
+                                x[2 * e + 1] = z * cs[e] + y * sn[e];
+                            }
+                        }
+                    } else if (a.rot) {
+                        const uint32_t from = team * a.lanes + (rotated ? (l < half ? l + half : l - half) : l);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float y = __shfl_sync(~0u, x[e], from);
+                            if (rotated)
+                                x[e] = l < half ? x[e] * cs[e] - y * sn[e] : x[e] * cs[e] + y * sn[e];
+                        }
                     }
+                    if (!is_v)
+                        res = kvc_pack8<T>(x);
                 }
-                if (!is_v)
-                    res = kvc_pack8<T>(x);
                 if (h < h1 && on) {
                     unsigned char *dst = h < a.hq ? a.q_out + tok * a.o_tok + h * a.o_head
                                          : (is_v ? a.v_plane : a.k_plane) + cache +
@@ -332,6 +348,10 @@ __global__ void __launch_bounds__(APPEND_THREADS) kvc_append_kernel(const Append
                     *reinterpret_cast<uint4 *>(dst + l * 16u) = res;
                 }
             }
+            hb += teams * APPEND_UNROLL;
+            if (hb - team >= h1)
+                break;
+            load(hb);
         }
     }
 }
@@ -386,9 +406,10 @@ kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *s
         (void)cudaGetLastError();
         return KVC_ERR_CUDA;
     }
-    // two rows a thread: a few more blocks shorten the binary searches' share, a few fewer the scans'
-    const uint32_t want = (uint32_t)(((uint64_t)d->token_capacity + 2 * MAP_THREADS - 1) / (2 * MAP_THREADS));
-    const uint32_t grid = std::max<uint32_t>(1u, std::min<uint32_t>(want, (uint32_t)lay->sm_count));
+    // a row a thread until four blocks a SM are there: a row is a chain of a search and a load, so more
+    // threads and not more rows a thread hide it
+    const uint32_t want = (uint32_t)(((uint64_t)d->token_capacity + MAP_THREADS - 1) / MAP_THREADS);
+    const uint32_t grid = std::max<uint32_t>(1u, std::min<uint32_t>(want, 4u * (uint32_t)lay->sm_count));
     if (kvc_launch_pdl(kvc_map_tokens_kernel, a, dim3(grid), MAP_THREADS, smem, (cudaStream_t)stream) != cudaSuccess) {
         (void)cudaGetLastError();
         return KVC_ERR_CUDA;
@@ -466,19 +487,23 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
     uint64_t chunk = (uint64_t)d->n_tokens * heads / warps;
     chunk = (chunk + teams - 1) / teams * teams;
     chunk = std::max<uint64_t>(chunk, teams);
-    a.chunk = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(chunk, 2ull * APPEND_UNROLL * teams), heads);
+    a.chunk = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(chunk, (uint64_t)APPEND_UNROLL * teams), heads);
     a.chunks = (heads + a.chunk - 1) / a.chunk;
     const uint64_t units = (uint64_t)d->n_tokens * a.chunks;
     const uint32_t per_block = APPEND_THREADS / 32;
     const uint32_t grid = (uint32_t)std::min<uint64_t>((units + per_block - 1) / per_block, 0x7FFFFFFFull);
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
-    if (d->dtype == KVC_DTYPE_BF16)
-        e = d->interleaved ? kvc_launch_pdl(kvc_append_kernel<__nv_bfloat16, true>, a, dim3(grid), APPEND_THREADS, 0, st)
-                           : kvc_launch_pdl(kvc_append_kernel<__nv_bfloat16, false>, a, dim3(grid), APPEND_THREADS, 0, st);
-    else
-        e = d->interleaved ? kvc_launch_pdl(kvc_append_kernel<__half, true>, a, dim3(grid), APPEND_THREADS, 0, st)
-                           : kvc_launch_pdl(kvc_append_kernel<__half, false>, a, dim3(grid), APPEND_THREADS, 0, st);
+    const bool vec = aligned(d->cos_sin, 16) && d->cos_sin_stride % 4 == 0;
+    const auto go = [&](auto type, auto neighbours, auto v) {
+        return kvc_launch_pdl(kvc_append_kernel<decltype(type), decltype(neighbours)::value, decltype(v)::value>, a, dim3(grid),
+                              APPEND_THREADS, 0, st);
+    };
+    const auto pick = [&](auto type) {
+        return d->interleaved ? (vec ? go(type, std::true_type(), std::true_type()) : go(type, std::true_type(), std::false_type()))
+                              : (vec ? go(type, std::false_type(), std::true_type()) : go(type, std::false_type(), std::false_type()));
+    };
+    e = d->dtype == KVC_DTYPE_BF16 ? pick(__nv_bfloat16()) : pick(__half());
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return KVC_ERR_CUDA;
