@@ -424,7 +424,7 @@ kvc_status kvc_map_tokens(kvc_layout *layout, const kvc_map_tokens_desc *desc, v
  * of a head are adjacent.  Pointers of q, k, v, q_out and the weights, and all strides in bytes, are
  * multiples of 16 bytes (ALIGNMENT).  q_out may be q itself with the same strides.  n_q_heads = 0:
  * keys and values only.  One kernel.
- * Errors: INVALID_ARG, ALIGNMENT, CUDA. */
+ * Errors: INVALID_ARG, ALIGNMENT, TOO_LARGE (over 2^31 thread blocks), CUDA. */
 typedef struct {
     uint32_t layer;
     uint32_t dtype;              /* kvc_dtype: of q, k, v, weights, q_out and the pool */

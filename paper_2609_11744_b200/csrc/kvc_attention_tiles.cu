@@ -171,32 +171,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r)
                  : "memory");
 }
 
-// Two 32-bit floats in one 64-bit register pair, for the two-wide arithmetic.
-__device__ __forceinline__ uint64_t pair2(float lo, float hi)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ float2 unpair2(uint64_t v)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -651,21 +625,21 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                         }
                     }
                     const float base = m == -INFINITY ? 0.f : m;
-                    const uint64_t scale2 = pair2(a.scale_log2, a.scale_log2), base2 = pair2(-base, -base);
+                    const uint64_t scale2 = kvc_pair(a.scale_log2, a.scale_log2), base2 = kvc_pair(-base, -base);
                     uint64_t sum2 = 0;
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         uint32_t p[16];
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            const float2 x = unpair2(fma2(pair2(s[q * 32 + 2 * k], s[q * 32 + 2 * k + 1]), scale2, base2));
+                            const float2 x = kvc_unpair(kvc_fma2(kvc_pair(s[q * 32 + 2 * k], s[q * 32 + 2 * k + 1]), scale2, base2));
                             const float y0 = exp2_fast(x.x), y1 = exp2_fast(x.y);
-                            sum2 = add2(sum2, pair2(y0, y1));
+                            sum2 = kvc_add2(sum2, kvc_pair(y0, y1));
                             p[k] = kvc_from_float2<T>(y0, y1);
                         }
                         tmem_st16(s_col + half * (HK / 2) + q * 16, p);
                     }
-                    const float2 sum = unpair2(sum2);
+                    const float2 sum = kvc_unpair(sum2);
                     l += sum.x + sum.y;
                     tmem_wait_st();
                     fence_before();

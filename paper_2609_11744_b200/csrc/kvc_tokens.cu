@@ -203,156 +203,190 @@ __global__ void __launch_bounds__(MAP_THREADS) kvc_map_tokens_kernel(const MapAr
 //
 // y = x * rsqrt(mean(x^2) + eps) * w over each head, then the rotation of its first `rot` values by
 // the row of the cos/sin table at the token's position; values are copied.  All in 32 bits, rounded
-// once to the pool's type.  Bound by memory: every element is read once and written once.  A team
-// of head_dim / 8 lanes (rounded up to a power of two) holds one head, 16 bytes a lane, so the
-// mean is a few shuffles and the partner of a "halves" pair is one shuffle away.  A warp serves
-// several heads of ONE token, so its table row, slot and addresses are fetched once; eight heads a
-// team are loaded before the first is used, which keeps 128 bytes a lane in flight.  VEC: rows of the
-// cos/sin table are 16-byte aligned.
+// once to the pool's type.  Every element is read once and written once, so memory is the bound, and
+// the arithmetic has to stay out of its way: with one lane to 16 bytes and the partner of each value
+// fetched by shuffle it took 110 instructions a lane and twice the time of the copy.  So a lane holds
+// both values of each of its pairs -- for "halves" 8 bytes of either half, four lanes' worth a sector --
+// and the weights are folded into the angles once a token: with c, s the angle's and e, o the pair,
+//     y_e = inv * ((w_e c) x_e - (w_o s) x_o),   y_o = inv * ((w_o c) x_o + (w_e s) x_e),
+// two pairs an instruction.  A team of head_dim / 8 lanes (rounded up to a power of two) holds one head;
+// a warp serves several heads of one token and one kind (queries, keys or values).
 struct AppendArgs {
-    const unsigned char *q, *k, *v;
+    const unsigned char *src[3];          // queries, keys, values
+    int64_t src_tok[3], src_head[3];      // strides in bytes
     unsigned char *q_out, *k_plane, *v_plane;
-    int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;  // strides in bytes
+    int64_t o_tok, o_head;
     uint64_t block_stride;
     const int64_t *slots;
     const int32_t *positions;
     const float *cos_sin;
     int64_t cs_stride;  // floats
-    const void *q_weight, *k_weight;
+    const void *weight[2];
     float eps;
-    uint32_t n_tokens, hq, hkv, d, rot, max_pos, block_size, num_blocks;
-    uint32_t lanes;   // lanes per head: a power of two >= d / 8
-    uint32_t chunk;   // heads per warp unit
-    uint32_t chunks;  // units per token
+    uint32_t n_tokens, heads[2], d, rot, max_pos, block_size, num_blocks;  // heads: queries; keys and values
+    uint32_t lanes;        // lanes per head: a power of two >= d / 8
+    uint32_t chunk;        // heads per warp unit
+    uint32_t q_chunks, kv_chunks;  // units per token
     uint32_t *status;
 };
 
 #define APPEND_THREADS 256u
-#define APPEND_UNROLL 8
+#ifndef APPEND_UNROLL
+#define APPEND_UNROLL 4
+#endif
+#ifndef APPEND_BLOCKS
+#define APPEND_BLOCKS 4
+#endif
+#ifndef APPEND_CHUNK
+#define APPEND_CHUNK 2  // turns of a warp at most
+#endif
 
+// A lane's eight values as two words of either piece, and as two pairs of floats an operand.
+struct AppendRaw {
+    uint2 a, b;
+};
+
+// NEIGHBOURS: pairs are (2n, 2n+1), else (n, n + rot/2).  VEC: rows of the cos/sin table are 16-byte aligned.
 template <typename T, bool NEIGHBOURS, bool VEC>
-__global__ void __launch_bounds__(APPEND_THREADS) kvc_append_kernel(const AppendArgs a)
+__global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kernel(const AppendArgs a)
 {
     kvc_pdl_wait();
     const uint32_t lane = threadIdx.x & 31u;
     const uint32_t team = lane / a.lanes, teams = 32u / a.lanes, l = lane % a.lanes;
-    const bool on = l * 8u < a.d;
-    const uint32_t heads = a.hq + 2 * a.hkv;
-    const uint64_t units = (uint64_t)a.n_tokens * a.chunks;
-    const uint32_t warps = gridDim.x * (APPEND_THREADS / 32u);
-    const float inv_d = 1.0f / (float)a.d;
-    const bool rotated = a.rot != 0 && l * 8u < a.rot;
-    const uint32_t half = a.rot / 16u;  // lanes in one half of the rotated part
-    const uint32_t v0 = a.hq + a.hkv;  // first value head
-    for (uint64_t u = blockIdx.x * (APPEND_THREADS / 32u) + (threadIdx.x >> 5); u < units; u += warps) {
-        const uint32_t tok = (uint32_t)(u / a.chunks);
-        const uint32_t h0 = (uint32_t)(u - (uint64_t)tok * a.chunks) * a.chunk;
-        const uint32_t h1 = min(h0 + a.chunk, heads);
-        const unsigned char *const q = a.q + tok * a.q_tok, *const k = a.k + tok * a.k_tok, *const v = a.v + tok * a.v_tok;
-        uint4 raw[APPEND_UNROLL];
-        const auto load = [&](uint32_t hb) {
-#pragma unroll
-            for (int i = 0; i < APPEND_UNROLL; ++i) {
-                const uint32_t h = hb + i * teams;
-                const unsigned char *src = h < a.hq ? q + h * a.q_head : h < v0 ? k + (h - a.hq) * a.k_head : v + (h - v0) * a.v_head;
-                raw[i] = h < h1 && on ? *reinterpret_cast<const uint4 *>(src + l * 16u) : make_uint4(0, 0, 0, 0);
-            }
-        };
-        // the first heads are on their way before the slot, the position and the angles are
-        load(h0 + team);
-        const int64_t slot = a.slots[tok];
-        if (slot < 0)
-            continue;  // a row without a token
-        const int32_t pos = a.rot ? a.positions[tok] : 0;
-        const uint64_t id = (uint64_t)slot / a.block_size;
-        if (id >= a.num_blocks || (a.rot && (uint32_t)pos >= a.max_pos)) {
-            if (lane == 0 && h0 == 0)
-                atomicAdd(a.status, 1u);
-            continue;
+    const bool on = l * 8u < a.d, turned = l * 8u < a.rot;
+    // first elements of the lane's two pieces of four
+    const uint32_t ea = !NEIGHBOURS && turned ? 4u * l : 8u * l, eb = !NEIGHBOURS && turned ? a.rot / 2 + 4u * l : 8u * l + 4u;
+    const uint32_t per_token = a.q_chunks + 2 * a.kv_chunks;
+    const uint64_t u = (uint64_t)blockIdx.x * (APPEND_THREADS / 32u) + (threadIdx.x >> 5);
+    const uint32_t tok = (uint32_t)(u / per_token);
+    if (tok >= a.n_tokens)
+        return;
+    uint32_t part = (uint32_t)(u - (uint64_t)tok * per_token), kind = 0;
+    if (part >= a.q_chunks) {
+        part -= a.q_chunks;
+        kind = 1;
+        if (part >= a.kv_chunks) {
+            part -= a.kv_chunks;
+            kind = 2;
         }
-        const uint64_t cache = id * a.block_stride +
-                               ((uint64_t)slot - id * a.block_size) * a.hkv * a.d * sizeof(T);
-        // the eight values of this lane use angles [a0, a0 + 8) (halves) or [a0, a0 + 4) (neighbours)
-        float cs[8], sn[8];
-        if (rotated && h0 < v0) {
-            const float *row = a.cos_sin + (int64_t)pos * a.cs_stride;
-            const uint32_t a0 = NEIGHBOURS ? l * 4u : (l < half ? l : l - half) * 8u;
-            if (VEC) {
+    }
+    const uint32_t h0 = part * a.chunk, h1 = min(h0 + a.chunk, a.heads[kind != 0]);
+    const unsigned char *src = a.src[kind] + tok * a.src_tok[kind];
+    const int64_t src_head = a.src_head[kind];
+    AppendRaw raw[APPEND_UNROLL];
+    const auto load = [&](uint32_t hb) {
 #pragma unroll
-                for (int i = 0; i < (NEIGHBOURS ? 1 : 2); ++i) {
-                    *reinterpret_cast<float4 *>(cs + 4 * i) = *reinterpret_cast<const float4 *>(row + a0 + 4 * i);
-                    *reinterpret_cast<float4 *>(sn + 4 * i) = *reinterpret_cast<const float4 *>(row + a.rot / 2 + a0 + 4 * i);
-                }
+        for (int i = 0; i < APPEND_UNROLL; ++i) {
+            const uint32_t h = hb + i * teams;
+            raw[i].a = raw[i].b = make_uint2(0, 0);
+            if (h < h1 && on) {
+                raw[i].a = *reinterpret_cast<const uint2 *>(src + h * src_head + ea * 2u);
+                raw[i].b = *reinterpret_cast<const uint2 *>(src + h * src_head + eb * 2u);
+            }
+        }
+    };
+    // the first heads are on their way before the slot, the position and the angles are
+    load(h0 + team);
+    const int64_t slot = a.slots[tok];
+    if (slot < 0)
+        return;  // a row without a token
+    const int32_t pos = a.rot ? a.positions[tok] : 0;
+    const uint64_t id = (uint64_t)slot < (1ull << 32) ? (uint32_t)slot / a.block_size : (uint64_t)slot / a.block_size;
+    if (id >= a.num_blocks || (a.rot && (uint32_t)pos >= a.max_pos)) {
+        if (lane == 0 && u == (uint64_t)tok * per_token)
+            atomicAdd(a.status, 1u);
+        return;
+    }
+    unsigned char *dst = kind == 0 ? a.q_out + tok * a.o_tok
+                                   : (kind == 1 ? a.k_plane : a.v_plane) + id * a.block_stride +
+                                         ((uint64_t)slot - id * a.block_size) * a.heads[1] * a.d * sizeof(T);
+    const int64_t dst_head = kind == 0 ? a.o_head : (int64_t)(a.d * sizeof(T));
+    // w_e c, -w_o s, w_o c, w_e s of the lane's four pairs
+    uint64_t ec[2], os[2], oc[2], es[2];
+    const void *weight = kind < 2 ? a.weight[kind] : nullptr;
+    if (kind < 2) {
+        float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f}, we[4] = {1.f, 1.f, 1.f, 1.f}, wo[4] = {1.f, 1.f, 1.f, 1.f};
+        if (turned) {
+            const float *row = a.cos_sin + (int64_t)pos * a.cs_stride + 4u * l;
+            if (VEC) {
+                const float4 x = *reinterpret_cast<const float4 *>(row), y = *reinterpret_cast<const float4 *>(row + a.rot / 2);
+                c[0] = x.x, c[1] = x.y, c[2] = x.z, c[3] = x.w;
+                s[0] = y.x, s[1] = y.y, s[2] = y.z, s[3] = y.w;
             } else {
 #pragma unroll
-                for (int i = 0; i < (NEIGHBOURS ? 4 : 8); ++i) {
-                    cs[i] = row[a0 + i];
-                    sn[i] = row[a.rot / 2 + a0 + i];
+                for (int i = 0; i < 4; ++i) {
+                    c[i] = row[i];
+                    s[i] = row[a.rot / 2 + i];
                 }
             }
         }
-        for (uint32_t hb = h0 + team;;) {
-#pragma unroll
-            for (int i = 0; i < APPEND_UNROLL; ++i) {
-                const uint32_t h = hb + i * teams;
-                // (whole warps: a team past its unit's heads goes through the shuffles with zeros)
-                if (h - team >= h1)
-                    break;
-                const bool is_v = h >= v0;
-                uint4 res = raw[i];
-                if (h - team < v0) {
-                    float x[8];
-                    kvc_unpack8<T>(raw[i], x);
-                    const void *weight = h < a.hq ? a.q_weight : a.k_weight;
-                    if (a.q_weight || a.k_weight) {
-                        float sum = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            sum += x[e] * x[e];
-                        for (uint32_t o = a.lanes / 2; o; o /= 2)
-                            sum += __shfl_xor_sync(~0u, sum, o);
-                        if (weight && on) {
-                            const float inv = rsqrtf(sum * inv_d + a.eps);
-                            float wv[8];
-                            kvc_unpack8<T>(reinterpret_cast<const uint4 *>(weight)[l], wv);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                x[e] = x[e] * inv * wv[e];
-                        }
-                    }
-                    if (NEIGHBOURS) {
-                        if (rotated) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float y = x[2 * e], z = x[2 * e + 1];
-                                x[2 * e] = y * cs[e] - z * sn[e];
-                                x[2 * e + 1] = z * cs[e] + y * sn[e];
-                            }
-                        }
-                    } else if (a.rot) {
-                        const uint32_t from = team * a.lanes + (rotated ? (l < half ? l + half : l - half) : l);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float y = __shfl_sync(~0u, x[e], from);
-                            if (rotated)
-                                x[e] = l < half ? x[e] * cs[e] - y * sn[e] : x[e] * cs[e] + y * sn[e];
-                        }
-                    }
-                    if (!is_v)
-                        res = kvc_pack8<T>(x);
-                }
-                if (h < h1 && on) {
-                    unsigned char *dst = h < a.hq ? a.q_out + tok * a.o_tok + h * a.o_head
-                                         : (is_v ? a.v_plane : a.k_plane) + cache +
-                                               (uint64_t)(h - a.hq - (is_v ? a.hkv : 0u)) * a.d * sizeof(T);
-                    *reinterpret_cast<uint4 *>(dst + l * 16u) = res;
-                }
+        if (weight && on) {
+            const unsigned char *w = static_cast<const unsigned char *>(weight);
+            const uint2 x = *reinterpret_cast<const uint2 *>(w + ea * 2u), y = *reinterpret_cast<const uint2 *>(w + eb * 2u);
+            const float2 p = kvc_to_float2<T>(x.x), q = kvc_to_float2<T>(x.y), r = kvc_to_float2<T>(y.x), t = kvc_to_float2<T>(y.y);
+            if (NEIGHBOURS) {
+                we[0] = p.x, wo[0] = p.y, we[1] = q.x, wo[1] = q.y, we[2] = r.x, wo[2] = r.y, we[3] = t.x, wo[3] = t.y;
+            } else {
+                we[0] = p.x, we[1] = p.y, we[2] = q.x, we[3] = q.y, wo[0] = r.x, wo[1] = r.y, wo[2] = t.x, wo[3] = t.y;
             }
-            hb += teams * APPEND_UNROLL;
-            if (hb - team >= h1)
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            ec[i] = kvc_pair(we[2 * i] * c[2 * i], we[2 * i + 1] * c[2 * i + 1]);
+            oc[i] = kvc_pair(wo[2 * i] * c[2 * i], wo[2 * i + 1] * c[2 * i + 1]);
+            es[i] = kvc_pair(we[2 * i] * s[2 * i], we[2 * i + 1] * s[2 * i + 1]);
+            os[i] = kvc_pair(-wo[2 * i] * s[2 * i], -wo[2 * i + 1] * s[2 * i + 1]);
+        }
+    }
+    const float inv_d = 1.0f / (float)a.d;
+    for (uint32_t hb = h0 + team;;) {
+#pragma unroll
+        for (int i = 0; i < APPEND_UNROLL; ++i) {
+            const uint32_t h = hb + i * teams;
+            if (h - team >= h1)  // (whole warps: a team past the unit's heads goes through the shuffles with zeros)
                 break;
-            load(hb);
+            AppendRaw res = raw[i];
+            if (kind < 2) {
+                const float2 p = kvc_to_float2<T>(res.a.x), q = kvc_to_float2<T>(res.a.y), r = kvc_to_float2<T>(res.b.x),
+                             t = kvc_to_float2<T>(res.b.y);
+                uint64_t e[2], o[2];
+                if (NEIGHBOURS) {
+                    e[0] = kvc_pair(p.x, q.x), o[0] = kvc_pair(p.y, q.y), e[1] = kvc_pair(r.x, t.x), o[1] = kvc_pair(r.y, t.y);
+                } else {
+                    e[0] = kvc_pair(p.x, p.y), e[1] = kvc_pair(q.x, q.y), o[0] = kvc_pair(r.x, r.y), o[1] = kvc_pair(t.x, t.y);
+                }
+                float inv = 1.f;
+                if (weight) {
+                    const float2 sq = kvc_unpair(kvc_fma2(o[1], o[1], kvc_fma2(o[0], o[0], kvc_fma2(e[1], e[1], kvc_mul2(e[0], e[0])))));
+                    float sum = sq.x + sq.y;
+                    for (uint32_t n = a.lanes / 2; n; n /= 2)
+                        sum += __shfl_xor_sync(~0u, sum, n);
+                    inv = rsqrtf(sum * inv_d + a.eps);
+                }
+                const uint64_t inv2 = kvc_pair(inv, inv);
+                float2 ye[2], yo[2];
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    ye[n] = kvc_unpair(kvc_mul2(inv2, kvc_fma2(os[n], o[n], kvc_mul2(ec[n], e[n]))));
+                    yo[n] = kvc_unpair(kvc_mul2(inv2, kvc_fma2(es[n], e[n], kvc_mul2(oc[n], o[n]))));
+                }
+                if (NEIGHBOURS) {
+                    res.a = make_uint2(kvc_from_float2<T>(ye[0].x, yo[0].x), kvc_from_float2<T>(ye[0].y, yo[0].y));
+                    res.b = make_uint2(kvc_from_float2<T>(ye[1].x, yo[1].x), kvc_from_float2<T>(ye[1].y, yo[1].y));
+                } else {
+                    res.a = make_uint2(kvc_from_float2<T>(ye[0].x, ye[0].y), kvc_from_float2<T>(ye[1].x, ye[1].y));
+                    res.b = make_uint2(kvc_from_float2<T>(yo[0].x, yo[0].y), kvc_from_float2<T>(yo[1].x, yo[1].y));
+                }
+            }
+            if (h < h1 && on) {
+                *reinterpret_cast<uint2 *>(dst + h * dst_head + ea * 2u) = res.a;
+                *reinterpret_cast<uint2 *>(dst + h * dst_head + eb * 2u) = res.b;
+            }
         }
+        hb += teams * APPEND_UNROLL;
+        if (hb - team >= h1)
+            break;
+        load(hb);
     }
 }
 
@@ -445,18 +479,18 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
     if (s != KVC_OK)
         return s;
     AppendArgs a;
-    a.q = static_cast<const unsigned char *>(d->q);
-    a.k = static_cast<const unsigned char *>(d->k);
-    a.v = static_cast<const unsigned char *>(d->v);
+    a.src[0] = static_cast<const unsigned char *>(d->q);
+    a.src[1] = static_cast<const unsigned char *>(d->k);
+    a.src[2] = static_cast<const unsigned char *>(d->v);
+    const int64_t tok[3] = {d->q_token_stride, d->k_token_stride, d->v_token_stride};
+    const int64_t head[3] = {d->q_head_stride, d->k_head_stride, d->v_head_stride};
+    for (int i = 0; i < 3; ++i) {
+        a.src_tok[i] = 2 * tok[i];
+        a.src_head[i] = 2 * head[i];
+    }
     a.q_out = static_cast<unsigned char *>(d->q_out);
     a.k_plane = const_cast<unsigned char *>(kvc_plane_ptr(lay, d->layer, 0));
     a.v_plane = const_cast<unsigned char *>(kvc_plane_ptr(lay, d->layer, 1));
-    a.q_tok = 2 * d->q_token_stride;
-    a.q_head = 2 * d->q_head_stride;
-    a.k_tok = 2 * d->k_token_stride;
-    a.k_head = 2 * d->k_head_stride;
-    a.v_tok = 2 * d->v_token_stride;
-    a.v_head = 2 * d->v_head_stride;
     a.o_tok = 2 * d->out_token_stride;
     a.o_head = 2 * d->out_head_stride;
     a.block_stride = lay->block_stride;
@@ -464,12 +498,12 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
     a.positions = d->positions;
     a.cos_sin = d->cos_sin;
     a.cs_stride = (int64_t)d->cos_sin_stride;
-    a.q_weight = d->q_weight;
-    a.k_weight = d->k_weight;
+    a.weight[0] = d->q_weight;
+    a.weight[1] = d->k_weight;
     a.eps = d->eps;
     a.n_tokens = d->n_tokens;
-    a.hq = d->n_q_heads;
-    a.hkv = hkv;
+    a.heads[0] = d->n_q_heads;
+    a.heads[1] = hkv;
     a.d = dim;
     a.rot = d->rot_dim;
     a.max_pos = d->max_positions;
@@ -482,16 +516,18 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
     // Heads per warp: the fewest that fill the machine's warps once -- a warp that serves more heads
     // of its token fetches the table row once for them, one that serves fewer spreads a small call
     // over more SMs.
-    const uint32_t heads = a.hq + 2 * hkv, teams = 32 / a.lanes;
-    const uint64_t warps = (uint64_t)lay->sm_count * 8 * (APPEND_THREADS / 32);
+    const uint32_t heads = d->n_q_heads + 2 * hkv, teams = 32 / a.lanes;
+    const uint64_t warps = (uint64_t)lay->sm_count * 4 * (APPEND_THREADS / 32);
     uint64_t chunk = (uint64_t)d->n_tokens * heads / warps;
-    chunk = (chunk + teams - 1) / teams * teams;
-    chunk = std::max<uint64_t>(chunk, teams);
-    a.chunk = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(chunk, (uint64_t)APPEND_UNROLL * teams), heads);
-    a.chunks = (heads + a.chunk - 1) / a.chunk;
-    const uint64_t units = (uint64_t)d->n_tokens * a.chunks;
+    chunk = std::max<uint64_t>((chunk + teams - 1) / teams * teams, teams);
+    a.chunk = (uint32_t)std::min<uint64_t>(chunk, (uint64_t)APPEND_CHUNK * APPEND_UNROLL * teams);
+    a.q_chunks = (d->n_q_heads + a.chunk - 1) / a.chunk;
+    a.kv_chunks = (hkv + a.chunk - 1) / a.chunk;
+    const uint64_t units = (uint64_t)d->n_tokens * (a.q_chunks + 2 * a.kv_chunks);
     const uint32_t per_block = APPEND_THREADS / 32;
-    const uint32_t grid = (uint32_t)std::min<uint64_t>((units + per_block - 1) / per_block, 0x7FFFFFFFull);
+    if ((units + per_block - 1) / per_block > 0x7FFFFFFFull)
+        return KVC_ERR_TOO_LARGE;
+    const uint32_t grid = (uint32_t)((units + per_block - 1) / per_block);
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
     const bool vec = aligned(d->cos_sin, 16) && d->cos_sin_stride % 4 == 0;
