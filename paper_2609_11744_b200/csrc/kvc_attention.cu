@@ -26,6 +26,40 @@ __device__ __forceinline__ void join_row(uint32_t n, const Get &get, Vec<D> &sum
     constexpr int N = Vec<D>::N;
     const uint32_t lane = threadIdx.x & 31u, w = (threadIdx.x >> 5) % WPR;
     const float2 none = make_float2(-INFINITY, 0.f);
+    if (WPR == 1 && n <= 4) {  // the usual case: everything at once, no lane needs another's
+        float2 x[4];
+        float v[4][N];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            x[i] = none;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                v[i][e] = 0.f;
+            if (i < n) {
+                const auto part = get(i);
+                x[i] = part.ml();
+                if (N == 4)
+                    *reinterpret_cast<float4 *>(v[i]) = *reinterpret_cast<const float4 *>(part.o() + lane * N);
+                else
+                    *reinterpret_cast<float2 *>(v[i]) = *reinterpret_cast<const float2 *>(part.o() + lane * N);
+            }
+        }
+        m = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
+        const float ref = m == -INFINITY ? 0.f : m;
+        l = 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            sum.v[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = exp2f(x[i].x - ref);
+            l += x[i].y * f;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                sum.v[e] += f * v[i][e];
+        }
+        return;
+    }
     const float2 mine = lane < n ? get(lane).ml() : none;  // the first 32 parts' (m, l), a lane each
     m = mine.x;
     for (uint32_t i = lane + 32; i < n; i += 32)
@@ -102,7 +136,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
     const uint32_t n = last - c + 2;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     // a warp's rows are summed BATCH at a time before any is written, so that their loads overlap
-    constexpr int BATCH = WPR == 1 ? 4 : 1;
+    constexpr int BATCH = WPR == 1 ? 2 : 1;
     constexpr uint32_t STEP = JOIN_WARPS / WPR;
     for (uint32_t row0 = blockIdx.y * STEP * BATCH + warp / WPR; row0 < sp.rows; row0 += gridDim.y * STEP * BATCH) {
         Vec<D> sum[BATCH];
@@ -297,7 +331,7 @@ cudaError_t join_split(const KvcAttn &a, cudaStream_t st)
 {
     if (a.parts.rows == KVC_ATTN_SMALL_ROWS)  // few rows, possibly of many parts: a block to a row
         return kvc_launch_pdl(kvc_join_split_kernel<T, D, JOIN_WARPS>, a, dim3(a.parts.blocks - 1, 4), JOIN_WARPS * 32, 0, st);
-    return kvc_launch_pdl(kvc_join_split_kernel<T, D, 1>, a, dim3(a.parts.blocks - 1, 8), JOIN_WARPS * 32, 0, st);
+    return kvc_launch_pdl(kvc_join_split_kernel<T, D, 1>, a, dim3(a.parts.blocks - 1, 16), JOIN_WARPS * 32, 0, st);
 }
 
 template <typename T, int D>
