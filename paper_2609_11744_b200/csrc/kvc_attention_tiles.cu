@@ -259,10 +259,10 @@ __device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap *map, u
                  ::"r"(dst), "l"(map), "r"(x), "r"(head), "r"(tok), "r"(block), "r"(bar) : "memory");
 }
 
-// One of the two loading warps: all tiles of the block's run, K or V.  A tile comes as boxes, a lane a
-// box, where blocks and tiles divide one another.  What is not a key's may be garbage in K, whose scores
-// are replaced; in V it meets a weight of zero, which infinity or NaN would survive, so a tile of V that is
-// not all keys is copied key by key, with zeros between.
+// One of the two loading warps: all tiles of the block's run, K or V.  A tile comes as boxes, where blocks
+// and tiles divide one another; a box's block id is looked up a tile ahead.  What is not a key's may be
+// garbage in K, whose scores are replaced; in V it meets a weight of zero, which infinity or NaN would
+// survive, so a tile of V that is not all keys is copied key by key, with zeros between.
 template <int D, bool KEYS>
 __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *segments, uint32_t tiles, Bars *bars,
                                           uint32_t (*there)[4], volatile uint32_t *dead, uint32_t lane)
@@ -270,36 +270,40 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
     using S = Shape<D>;
     constexpr int STAGES = KEYS ? S::KS : S::VS;
     constexpr int PER = 512 / (D * 2);  // keys per round of 32 lanes
+    constexpr uint32_t NONE = ~0u;
     const KvcAttn &a = args.a;
-    uint64_t *full = KEYS ? bars->k_full : bars->v_full, *empty = KEYS ? bars->k_empty : bars->v_empty;
+    const uint32_t full = smem_addr(KEYS ? bars->k_full : bars->v_full), empty = smem_addr(KEYS ? bars->k_empty : bars->v_empty);
+    const CUtensorMap *map = KEYS ? &args.k_map : &args.v_map;
+    const uint32_t boxes = args.boxes, box_at = (boxes ? lane % boxes : 0u) * args.box_keys;  // this lane's box
     SegmentReader reader;
     Segment c;
     Ring<STAGES> ring;
     uint32_t slot = 0, issued = 0;
     bool ok = true;
 #pragma unroll 1
-    while (ok && reader.next<true>(segments, bars, c, dead, a.status))
+    while (ok && reader.next<true>(segments, bars, c, dead, a.status)) {
+        // V may be read past the pair's last key, up to the sequence's: what other rows of the call see is as
+        // good as what this pair's do
+        const int32_t limit = KEYS || a.phase == KVC_PHASE_PREFIX ? c.r.hi : min(c.q.pos + c.q.rows / (int32_t)a.g, kvc_key_cap(a));
+        const int32_t *table = a.tables + (int64_t)c.q.table * a.table_stride;
+        const auto look = [&](uint32_t u) {  // the block id of this lane's box of tile u
+            const int32_t jb = (int32_t)(kvc_tile(c.r, c.t + u) * TK + box_at);
+            return jb < limit && (jb + (int32_t)args.box_keys > c.r.lo || jb < c.r.sink_end) ? (uint32_t)table[(uint32_t)jb / a.block_size] : NONE;
+        };
+        uint32_t next_id = boxes ? look(0) : NONE;
 #pragma unroll 1
-    for (uint32_t u = 0; u < c.n; ++u) {
-        const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + u) * TK);
-        const auto key = [&](int32_t j) { return j < c.r.hi && (j >= c.r.lo || j < c.r.sink_end); };
-        bool boxed = args.boxes != 0;
-        uint32_t id = 0, tok = 0;
-        bool have = false;  // this lane's box holds keys
-        if (boxed) {
-            // lane i < boxes: block j / B; the lanes after them the same boxes' second 64 elements
-            const uint32_t box = lane % args.boxes;
-            const int32_t jb = j0 + (int32_t)(box * args.box_keys), je = jb + (int32_t)args.box_keys;
-            if (jb < c.r.hi && (je > c.r.lo || jb < c.r.sink_end)) {
-                const uint32_t block = (uint32_t)jb / a.block_size;
-                tok = (uint32_t)jb - block * a.block_size;
-                id = (uint32_t)a.tables[(int64_t)c.q.table * a.table_stride + block];
-                have = id < a.num_blocks;
-                if (KEYS && !have && lane < args.boxes)
+        for (uint32_t u = 0; u < c.n; ++u) {
+            const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + u) * TK);
+            const uint32_t id = next_id;
+            if (boxes && u + 1 < c.n)
+                next_id = look(u + 1);
+            const auto key = [&](int32_t j) { return j < c.r.hi && (j >= c.r.lo || j < c.r.sink_end); };
+            const uint32_t good = __ballot_sync(~0u, id < a.num_blocks) & ((1u << boxes) - 1u);
+            bool boxed = boxes != 0;
+            if (boxed && KEYS) {
+                const int32_t jb = j0 + (int32_t)box_at;
+                if (lane < boxes && id >= a.num_blocks && jb < limit && (jb + (int32_t)args.box_keys > c.r.lo || jb < c.r.sink_end))
                     atomicAdd(a.status, 1u);
-            }
-            const uint32_t good = __ballot_sync(~0u, have);
-            if (KEYS) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t at = i * 32 + lane;
@@ -307,82 +311,70 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
                     if (lane == 0)
                         there[slot][i] = w;
                 }
-            } else {
-                // keys that other rows of the call see are as good as this pair's own
-                const int32_t end = a.phase == KVC_PHASE_PREFIX ? c.r.hi : min(c.q.pos + c.q.rows / (int32_t)a.g, kvc_key_cap(a));
-                boxed = (j0 >= c.r.lo && j0 + TK <= end) || j0 + TK <= c.r.sink_end;
-                if (boxed) {  // boxes past this pair's last key
-                    const int32_t last = j0 + (int32_t)((lane % args.boxes) * args.box_keys);
-                    if (last >= c.r.hi) {
-                        const uint32_t block = (uint32_t)last / a.block_size;
-                        tok = (uint32_t)last - block * a.block_size;
-                        id = (uint32_t)a.tables[(int64_t)c.q.table * a.table_stride + block];
-                        have = id < a.num_blocks;
+            } else if (boxed) {
+                boxed = ((j0 >= c.r.lo && j0 + TK <= limit) || j0 + TK <= c.r.sink_end) && good == (1u << boxes) - 1u;
+            }
+            int64_t off[4];
+            if (!boxed) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t j = j0 + i * 32 + (int32_t)lane;
+                    off[i] = -1;
+                    if (key(j)) {
+                        off[i] = kvc_key_offset(a, c.q.table, j, c.h, D * 2);
+                        if (KEYS && off[i] < 0)
+                            atomicAdd(a.status, 1u);
                     }
-                    boxed = __all_sync(~0u, have);
+                    if (KEYS) {
+                        const uint32_t w = __ballot_sync(~0u, off[i] >= 0);
+                        if (lane == 0)
+                            there[slot][i] = w;
+                    }
                 }
             }
-        }
-        int64_t off[4];
-        if (!boxed) {
+            slot = (slot + 1) % THERE;
+            if (!(ok = __all_sync(~0u, bar_wait(empty + ring.stage * 8u, ring.parity ^ 1u, dead, a.status))))
+                break;
+            const uint32_t tile = tiles + ring.stage * S::TILE, bar = full + ring.stage * 8u;
+            if (boxed) {
+                // (the words of `there` are ordered before the barrier's phase by lane 0's arrival)
+                if (lane == 0)
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                                 "r"((uint32_t)__popc(good) * args.box_keys * (uint32_t)D * 2u) : "memory");
+                __syncwarp();
+                // a lane a box: the lanes take turns at the copy unit, but their operands are ready (measured
+                // against one lane in a loop of 16 boxes: 2 us a tile less)
+                const uint32_t h = boxes * (D / 64) > lane ? lane / boxes : 0u, i = lane - h * boxes;
+                if (lane < boxes * (D / 64) && (good >> i & 1u))
+                    box_load(tile + h * S::HALF + box_at * 128u, map, h * 64u, c.h, boxes > 1 ? 0u : (uint32_t)j0 % a.block_size, id, bar);
+            } else {
+                const unsigned char *plane = KEYS ? a.k : a.v;
+                const uint32_t chunk = lane % (D / 8), sub = lane / (D / 8);
+                const uint32_t base = tile + (chunk >> 3) * S::HALF;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t j = j0 + i * 32 + (int32_t)lane;
-                off[i] = -1;
-                if (key(j)) {
-                    off[i] = kvc_key_offset(a, c.q.table, j, c.h, D * 2);
-                    if (KEYS && off[i] < 0)
-                        atomicAdd(a.status, 1u);
-                }
-                if (KEYS) {
-                    const uint32_t w = __ballot_sync(~0u, off[i] >= 0);
-                    if (lane == 0)
-                        there[slot][i] = w;
-                }
-            }
-        }
-        slot = (slot + 1) % THERE;
-        if (!(ok = __all_sync(~0u, bar_wait(smem_addr(&empty[ring.stage]), ring.parity ^ 1u, dead, a.status))))
-            break;
-        const uint32_t tile = tiles + ring.stage * S::TILE, bar = smem_addr(&full[ring.stage]);
-        if (boxed) {
-            const uint32_t n = __popc(__ballot_sync(~0u, have && lane < args.boxes));
-            // (the words of `there` are ordered before the barrier's phase by lane 0's arrival)
-            if (lane == 0)
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * args.box_keys * (uint32_t)D * 2u)
-                             : "memory");
-            __syncwarp();
-            if (have && lane < args.boxes * (D / 64)) {
-                const uint32_t half = lane / args.boxes, box = lane - half * args.boxes;
-                box_load(tile + half * S::HALF + box * args.box_keys * 128u, KEYS ? &args.k_map : &args.v_map, half * 64u, c.h, tok, id, bar);
-            }
-        } else {
-            const unsigned char *plane = KEYS ? a.k : a.v;
-            const uint32_t chunk = lane % (D / 8), sub = lane / (D / 8);
-            const uint32_t base = tile + (chunk >> 3) * S::HALF;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
+                for (int q = 0; q < 4; ++q)
 #pragma unroll 4
-                for (int i = 0; i < 32 / PER; ++i) {
-                    const uint32_t row = i * PER + sub;
-                    const int64_t o = __shfl_sync(~0u, off[q], row);
-                    copy16(base + (q * 32 + row) * 128u + (((chunk & 7u) ^ (row & 7u)) << 4), plane + (o >= 0 ? o : 0) + chunk * 16u,
-                           o >= 0 ? 16u : 0u);
-                }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_async();
-            __syncwarp();
-            if (lane == 0)
-                bar_arrive(bar);
+                    for (int i = 0; i < 32 / PER; ++i) {
+                        const uint32_t row = i * PER + sub;
+                        const int64_t o = __shfl_sync(~0u, off[q], row);
+                        copy16(base + (q * 32 + row) * 128u + (((chunk & 7u) ^ (row & 7u)) << 4), plane + (o >= 0 ? o : 0) + chunk * 16u,
+                               o >= 0 ? 16u : 0u);
+                    }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_async();
+                __syncwarp();
+                if (lane == 0)
+                    bar_arrive(bar);
+            }
+            ring.next();
+            ++issued;
         }
-        ring.next();
-        ++issued;
     }
     // no copy of ours runs on when the block ends, on no way out
 #pragma unroll 1
     for (uint32_t n = issued < STAGES ? 0u : issued - STAGES; n < issued; ++n)
 #pragma unroll 1
-        for (uint32_t i = 0; i < KVC_WAIT_LIMIT && !bar_try(smem_addr(&full[n % STAGES]), n / STAGES & 1u); ++i)
+        for (uint32_t i = 0; i < KVC_WAIT_LIMIT && !bar_try(full + (n % STAGES) * 8u, n / STAGES & 1u); ++i)
             ;
 }
 
@@ -393,7 +385,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     const KvcAttn &a = args.a;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Bars bars;
-    __shared__ uint32_t there[THERE][4];
+    __shared__ __align__(16) uint32_t there[THERE][4];
     __shared__ uint32_t s_dead, s_tmem;
     __shared__ Segment segments[SEGMENTS];
     __shared__ float row_top[2][2][128], row_sum[2][2][128];  // [row tile][half][row]
@@ -412,7 +404,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     if (threadIdx.x == 0) {
         s_dead = 0;
         for (int i = 0; i < 2; ++i) {
-            bar_init(smem_addr(&bars.q_full[i]), 256);
+            bar_init(smem_addr(&bars.q_full[i]), 8);
             bar_init(smem_addr(&bars.s_full[i]), 1);
             bar_init(smem_addr(&bars.p_full[i][0]), 128);
             bar_init(smem_addr(&bars.p_full[i][1]), 128);
@@ -481,7 +473,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 *reinterpret_cast<uint4 *>(dst + r * 128u + (((chunk & 7u) ^ (r & 7u)) << 4)) = x[e];
             }
             fence_async();
-            bar_arrive(bar + BAR(q_full) + sub * 8u);
+            __syncwarp();
+            if (lane == 0)
+                bar_arrive(bar + BAR(q_full) + sub * 8u);
         };
         bool ok, open = false;  // open: a segment whose products have been started and whose result is to be written
         uint32_t row0 = 0;
@@ -560,6 +554,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             open = row0 < (uint32_t)c.q.rows;
             if (open) {
                 const int32_t pos = row0 + tid < (uint32_t)c.q.rows ? kvc_row_pos(a, c.q, row0 + tid) : -1;
+                // the warp's rows that see the fewest keys at either end: a tile that both see whole needs no mask
+                const int32_t pos_lo = __reduce_min_sync(~0u, pos);
+                const int32_t old_hi = a.window ? __reduce_max_sync(~0u, pos) - a.window : -1;  // the last key behind all windows
                 m = -INFINITY;
                 l = 0.f;
 #pragma unroll 1
@@ -572,12 +569,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     float s[HK];
                     tmem_ld32(s, s_col + half * HK);
                     tmem_ld32(s + 32, s_col + half * HK + 32);
-                    const volatile uint32_t *mask = &there[(slot + i) % THERE][half * 2];
-                    const uint32_t mask0 = mask[0], mask1 = mask[1];
+                    uint32_t mask0, mask1;
+                    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(mask0), "=r"(mask1) : "r"(smem_addr(&there[(slot + i) % THERE][half * 2])));
                     tmem_wait_ld();
-                    const bool all = (mask0 & mask1) == ~0u && j0 + HK - 1 <= pos &&
-                                     (a.window == 0 || pos - j0 < a.window || j0 + HK - 1 < a.sinks);
-                    if (__any_sync(~0u, !all)) {
+                    if ((mask0 & mask1) != ~0u || j0 + HK - 1 > pos_lo || (j0 <= old_hi && j0 + HK - 1 >= a.sinks)) {
                         // kvc_sees() for 32 keys at a time: at most pos, and after pos - window or before sinks
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
