@@ -171,7 +171,10 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_split_kernel(const K
             for (int b = 0; b < BATCH; ++b) {
                 const uint32_t i = sp.row0 + row0 + b * STEP;
                 if (row0 + b * STEP < sp.rows)
-                    write_row<T, D>(a, sp.qa + (int32_t)(i / a.g), sp.head * a.g + i % a.g, sum[b], m[b], l[b]);
+                    {
+                    const uint32_t tok = kvc_div_g(a, i);
+                    write_row<T, D>(a, sp.qa + (int32_t)tok, sp.head * a.g + (i - tok * a.g), sum[b], m[b], l[b]);
+                }
             }
     }
 }
@@ -402,6 +405,9 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     a.hq = d->n_q_heads;
     a.hkv = l.num_kv_heads;
     a.g = shape.g;
+    const auto shift = [](uint32_t x) { return x & (x - 1) ? KVC_NO_SHIFT : (uint32_t)__builtin_ctz(x); };
+    a.g_shift = shift(a.g);
+    a.block_shift = shift(a.block_size);
     a.scale_log2 = d->scale * 1.44269504088896341f;
     a.window = (int32_t)d->window;
     a.sinks = (int32_t)d->sinks;

@@ -55,6 +55,8 @@ struct KvcParts {
                          // ascend, so only lengths that contradict one another can ask for more
 };
 
+#define KVC_NO_SHIFT 32u
+
 struct KvcAttn {
     const unsigned char *k, *v;  // planes of the layer
     uint64_t block_stride;
@@ -69,6 +71,7 @@ struct KvcAttn {
     float *lse;
     int64_t q_tok, q_head, o_tok, o_head;  // bytes
     uint32_t hq, hkv, g;
+    uint32_t g_shift, block_shift;  // log2 of g and of block_size, or KVC_NO_SHIFT
     float scale_log2;
     int32_t window, sinks;
     uint32_t phase;
@@ -90,6 +93,14 @@ uint32_t kvc_attn_tiles_blocks(const kvc_layout *lay);
 cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
 
 #ifdef __CUDACC__
+
+// Divisions by the two numbers that are nearly always powers of two (a division is some 25 instructions,
+// several of them between a block's start and its first load).
+__device__ __forceinline__ uint32_t kvc_div(uint32_t x, uint32_t d, uint32_t shift)
+{
+    return shift != KVC_NO_SHIFT ? x >> shift : x / d;
+}
+__device__ __forceinline__ uint32_t kvc_div_g(const KvcAttn &a, uint32_t x) { return kvc_div(x, a.g, a.g_shift); }
 
 // Where run c of `runs` begins on a line.  (64-bit divisions are worth avoiding: they are a good part of
 // what the kernels do before their first load.)
@@ -207,8 +218,8 @@ __device__ __forceinline__ KvcRange kvc_range(const KvcAttn &a, const KvcSeq &q,
         r.lo = 0;
         r.hi = q.len;
     } else {
-        const int32_t p0 = q.pos + (int32_t)(rt * ROWS / a.g);
-        const int32_t p1 = q.pos + (int32_t)((min((uint32_t)q.rows, (rt + 1) * ROWS) - 1) / a.g);
+        const int32_t p0 = q.pos + (int32_t)kvc_div_g(a, rt * ROWS);
+        const int32_t p1 = q.pos + (int32_t)kvc_div_g(a, min((uint32_t)q.rows, (rt + 1) * ROWS) - 1);
         r.hi = kvc_clamp(p1 + 1, 0, kvc_key_cap(a));
         r.lo = q.skip;
         if (a.window) {
@@ -285,9 +296,12 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
     const uint32_t per = (n_seq + owners - 1) / owners;
     const uint32_t s0 = min(owner * per, n_seq), s1 = min(s0 + per, n_seq);
     unsigned long long units = 0, pairs = 0;
+    KvcSeq q0;  // the owner's first sequence, usually its only one
 #pragma unroll 1
     for (uint32_t s = s0; s < s1; ++s) {
         const KvcSeq q = kvc_seq(a, s);
+        if (s == s0)
+            q0 = q;
         unsigned long long sum = 0;
         uint32_t n = 0;
 #pragma unroll 1
@@ -341,7 +355,7 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
         for (uint32_t s = s0; s < s1; ++s) {
             if (table && rt0 == 0)
                 a.parts.base[s] = (uint32_t)min(p, 0xFFFFFFFFull);
-            const KvcSeq q = kvc_seq(a, s);
+            const KvcSeq q = s == s0 ? q0 : kvc_seq(a, s);
             const uint32_t n = ((uint32_t)q.rows + ROWS - 1) / ROWS;
             unsigned long long per_head = 0;
 #pragma unroll 1
@@ -429,7 +443,7 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
 // requests, and the row's own is looked up.
 __device__ __forceinline__ int32_t kvc_row_pos(const KvcAttn &a, const KvcSeq &q, uint32_t row)
 {
-    const int32_t tok = (int32_t)(row / a.g);
+    const int32_t tok = (int32_t)kvc_div_g(a, row);
     if (a.phase != KVC_PHASE_PREFIX)
         return q.pos + tok;
     const int32_t t = q.qa + tok;
@@ -447,7 +461,7 @@ __device__ __forceinline__ bool kvc_sees(const KvcAttn &a, int32_t p, int32_t j)
 // Where key j of a sequence lies relative to its plane's base, or -1 (an id outside the pool).
 __device__ __forceinline__ int64_t kvc_key_offset(const KvcAttn &a, uint32_t table, int32_t j, uint32_t h, uint32_t head_bytes)
 {
-    const uint32_t b = (uint32_t)j / a.block_size, off = (uint32_t)j - b * a.block_size;
+    const uint32_t b = kvc_div(j, a.block_size, a.block_shift), off = (uint32_t)j - b * a.block_size;
     const uint32_t id = (uint32_t)a.tables[(int64_t)table * a.table_stride + b];
     if (id >= a.num_blocks)
         return -1;

@@ -68,19 +68,25 @@ __device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Issues the copies of this warp's keys of one unit; returns which of the 16 keys are there.
+// Where this lane's key of the cursor's unit lies, or -1; lanes 16 and up the same keys again.
 template <int D>
-__device__ __forceinline__ uint32_t load_unit(const KvcAttn &a, const KvcCursor &c, uint32_t warp, uint32_t lane, uint32_t stage)
+__device__ __forceinline__ int64_t look_up(const KvcAttn &a, const KvcCursor &c, uint32_t warp, uint32_t lane)
 {
-    using S = Shape<D>;
-    const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t) * TK + warp * WK);
-    const int32_t j = j0 + (int32_t)(lane & 15u);
+    const int32_t j = (int32_t)(kvc_tile(c.r, c.t) * TK + warp * WK + (lane & 15u));
     int64_t off = -1;
     if (j < c.r.hi && (j >= c.r.lo || j < c.r.sink_end)) {
-        off = kvc_key_offset(a, c.q.table, j, c.h, S::ROW);
+        off = kvc_key_offset(a, c.q.table, j, c.h, Shape<D>::ROW);
         if (off < 0 && lane < 16)
             atomicAdd(a.status, 1u);
     }
+    return off;
+}
+
+// Issues the copies of this warp's keys of one unit; returns which of the 16 are there.
+template <int D>
+__device__ __forceinline__ uint32_t load_unit(const KvcAttn &a, int64_t off, uint32_t lane, uint32_t stage)
+{
+    using S = Shape<D>;
     const uint32_t there = __ballot_sync(~0u, off >= 0) & 0xFFFFu;
     constexpr int PER = 32 / S::CHUNKS;  // keys per round
     const uint32_t chunk = lane % S::CHUNKS, sub = lane / S::CHUNKS;
@@ -123,18 +129,23 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
     KvcCursor ld = run.at, c = run.at;
     unsigned long long ld_at = run.units_at, units_at = run.units_at;  // where their pairs' units lie on the line
     uint32_t pair = run.pair;
-    // the load cursor's unit, if it is in the run, and one step on
+    // the load cursor's unit, if it is in the run, and one step on.  Places are looked up a unit ahead, so
+    // that the table's latency and the copies' follow one another only once
     bool more = true;
+    int64_t off = look_up<D>(a, ld, warp, lane);
     const auto load = [&](uint32_t stage) {
         if (more) {
-            const uint32_t there = load_unit<D>(a, ld, warp, lane, ring + stage * S::STAGE);
-            if (lane == 0)
-                s_there[warp][stage] = there;
+            const int64_t now = off;
             const uint32_t n = ld.r.n;
             kvc_next<ROWS, TK>(a, n_seq, ld);
             if (ld.t == 0)
                 ld_at += n + HEAD;
             more = ld.s < n_seq && ld_at + ld.t < run.end;
+            if (more)
+                off = look_up<D>(a, ld, warp, lane);
+            const uint32_t there = load_unit<D>(a, now, lane, ring + stage * S::STAGE);
+            if (lane == 0)
+                s_there[warp][stage] = there;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -151,12 +162,12 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
         const bool real[2] = {gr < rows, gr + 8 < rows};
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const uint32_t row = row0 + gr + 8 * half;
+            const uint32_t row = row0 + gr + 8 * half, tok = kvc_div_g(a, row);
             const unsigned char *src = a.q;
             pos[half] = -1;
             if (real[half]) {
                 pos[half] = kvc_row_pos(a, c.q, row);
-                src += (int64_t)(c.q.qa + (int32_t)(row / a.g)) * a.q_tok + (int64_t)(c.h * a.g + row % a.g) * a.q_head;
+                src += (int64_t)(c.q.qa + (int32_t)tok) * a.q_tok + (int64_t)(c.h * a.g + (row - tok * a.g)) * a.q_head;
             }
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
@@ -310,9 +321,9 @@ __global__ void __launch_bounds__(THREADS, 2) kvc_attn_rows_kernel(const KvcAttn
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
                     if (real[half]) {
-                        const uint32_t row = row0 + gr + 8 * half;
-                        const int64_t tok = c.q.qa + (int32_t)(row / a.g);
-                        const uint32_t head = c.h * a.g + row % a.g;
+                        const uint32_t row = row0 + gr + 8 * half, t = kvc_div_g(a, row);
+                        const int64_t tok = c.q.qa + (int32_t)t;
+                        const uint32_t head = c.h * a.g + (row - t * a.g);
                         const float inv = tl[half] == 0.f ? 0.f : 1.f / tl[half];  // a row that sees nothing: zeros
                         unsigned char *dst = a.out + tok * a.o_tok + (int64_t)head * a.o_head;
 #pragma unroll

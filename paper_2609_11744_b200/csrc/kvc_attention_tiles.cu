@@ -288,7 +288,7 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
         const int32_t *table = a.tables + (int64_t)c.q.table * a.table_stride;
         const auto look = [&](uint32_t u) {  // the block id of this lane's box of tile u
             const int32_t jb = (int32_t)(kvc_tile(c.r, c.t + u) * TK + box_at);
-            return jb < limit && (jb + (int32_t)args.box_keys > c.r.lo || jb < c.r.sink_end) ? (uint32_t)table[(uint32_t)jb / a.block_size] : NONE;
+            return jb < limit && (jb + (int32_t)args.box_keys > c.r.lo || jb < c.r.sink_end) ? (uint32_t)table[kvc_div((uint32_t)jb, a.block_size, a.block_shift)] : NONE;
         };
         uint32_t next_id = boxes ? look(0) : NONE;
 #pragma unroll 1
@@ -450,8 +450,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 return;
             constexpr uint32_t STEP = 256u / (D / 8), TURNS = 128u / STEP;
             const uint32_t at = threadIdx.x & 255u, chunk = at % (D / 8), r0 = at / (D / 8);
-            uint32_t tok = (row0 + r0) / a.g, head = row0 + r0 - tok * a.g;
-            const uint32_t tok_step = STEP / a.g, head_step = STEP - tok_step * a.g;
+            uint32_t tok = kvc_div_g(a, row0 + r0), head = row0 + r0 - tok * a.g;
+            const uint32_t tok_step = kvc_div_g(a, STEP), head_step = STEP - tok_step * a.g;
             const unsigned char *src = a.q + (int64_t)c.q.qa * a.q_tok + (int64_t)(c.h * a.g) * a.q_head + chunk * 16u;
             unsigned char *dst = tiles_ptr + S::Q + sub * S::TILE + (chunk >> 3) * S::HALF;
             uint4 x[TURNS];
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t in_warp = rows16 + (lane >> 2) + 8 * e, r = (warp & 3u) * 32u + in_warp;
-                        const uint32_t i = row0 + r, tok = i / a.g, head = c.h * a.g + (i - tok * a.g);
+                        const uint32_t i = row0 + r, tok = kvc_div_g(a, i), head = c.h * a.g + (i - tok * a.g);
                         f[e] = __shfl_sync(~0u, inv, in_warp);
                         write[e] = i < (uint32_t)c.q.rows && room;
                         dst[e] = whole ? a.out + (c.q.qa + (int64_t)tok) * a.o_tok + (int64_t)head * a.o_head + half * D + (lane & 3u) * 4u
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                         if (a.phase != KVC_PHASE_WHOLE && from_start && sub == 0 && tid == 0 && room)
                             a.parts.range[c.pair] = make_ulonglong2(c.units_at, c.units_at + c.r.n);
                     } else if (a.lse) {
-                        const uint32_t i = row0 + tid, tok = i / a.g;
+                        const uint32_t i = row0 + tid, tok = kvc_div_g(a, i);
                         a.lse[(c.q.qa + (int64_t)tok) * a.hq + c.h * a.g + (i - tok * a.g)] = (m + log2f(l)) * 0.693147180559945309f;
                     }
                 }
