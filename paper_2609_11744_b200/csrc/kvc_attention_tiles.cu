@@ -9,13 +9,16 @@
 //                   keys: read S from tensor memory, agree on the maximum, write the weights P (pool's type)
 //                   over S, keep m and l in registers; at the end of a pair each writes half of O's columns.
 //                   They also load the queries.
-//   warp 16         one thread issues the matrix instructions: S = Q K^T from shared memory, O += P V
+//   warp 16         issues the matrix instructions, one lane each but the whole warp along: S = Q K^T from shared memory, O += P V
 //                   with P from tensor memory and V as it lies (keys x head, so head-major for this product)
 //   warps 17, 18    load K and V tiles through the block table into rings of shared-memory stages, in the
 //                   128-byte swizzle that the matrix unit reads: a tensor copy for the keys of each block, or
 //                   16-byte asynchronous copies where a tile is not made of whole blocks
 //   warp 19         one thread walks the run's pairs and hands them to the others
-// Two row tiles share each K and V tile, and while one is in its softmax the other's products run.
+// Two row tiles share each K and V tile, and while one is in its softmax the other's products run.  A pair
+// of 128 rows or fewer has one row tile; its scores then alternate between the two score buffers, so that
+// those of the next tile are made while this one is in its softmax (measured on 32 one-token questions
+// about a 32,000-token document: 2.9 us a tile without, 1.6 us with).
 // Bound by the exponentials and the matrix unit alike: 128 x 128 scores take 1024 cycles on each.
 // O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use: weights are then
 // at most 2^8, which neither type nor the 32-bit sums mind, and almost all tiles skip the rescaling.
@@ -105,6 +108,17 @@ __host__ __device__ constexpr uint32_t kind(uint32_t n, bool b_by_column)
     return (1u << 4) | (f << 7) | (f << 10) | ((b_by_column ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
+// A value that all lanes hold, known to the compiler as such: matrix instructions take their operands from
+// the warp's uniform registers, and moving them there one by one costs more than the instruction.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(~0u, x, 0); }
+
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t what, bool add)
 {
     asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -188,7 +202,10 @@ __device__ __forceinline__ float exp2_fast(float x)
 __device__ __forceinline__ uint32_t low_bits(int32_t n) { return n <= 0 ? 0u : n > 31 ? ~0u : (1u << n) - 1u; }
 
 struct Bars {
-    uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];  // [row tile], p_full: and half of the keys
+    // [row tile, or score buffer where there is one row tile], p_full: and half of the keys.  o_done: a
+    // row tile's last product of a segment; with one row tile, the products of even and of odd tiles, so that a
+    // warp that looks one product late is never two phases behind
+    uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
     uint64_t seg_full[4], seg_empty[4], drained;
 };
@@ -203,23 +220,18 @@ struct Segment {
     unsigned long long units_at;  // where the pair's units begin on the line
 };
 constexpr uint32_t SEGMENTS = 4;
-constexpr uint32_t SEGMENT_READERS = 19;  // 16 softmax warps, 2 loading warps, the issuing thread
+constexpr uint32_t SEGMENT_READERS = 19;  // 16 softmax warps, 2 loading warps, the issuing warp
 
-// The next segment, copied to registers.  Every lane of the role's warp calls this (or the one thread).
+// The next segment, copied to registers.  Every lane of the role's warp calls this.
 struct SegmentReader {
     uint32_t slot = 0, parity = 0;
-    template <bool WARP>
     __device__ __forceinline__ bool next(const Segment *ring, Bars *bars, Segment &out, volatile uint32_t *dead, uint32_t *status)
     {
-        bool ok = bar_wait(smem_addr(&bars->seg_full[slot]), parity, dead, status);
-        if (WARP)
-            ok = __all_sync(~0u, ok);
-        if (!ok)
+        if (!__all_sync(~0u, bar_wait(smem_addr(&bars->seg_full[slot]), parity, dead, status)))
             return false;
         out = ring[slot];
-        if (WARP)
-            __syncwarp();
-        if (!WARP || (threadIdx.x & 31u) == 0)
+        __syncwarp();
+        if ((threadIdx.x & 31u) == 0)
             bar_arrive(smem_addr(&bars->seg_empty[slot]));
         if (++slot == SEGMENTS) {
             slot = 0;
@@ -281,7 +293,7 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
     uint32_t slot = 0, issued = 0;
     bool ok = true;
 #pragma unroll 1
-    while (ok && reader.next<true>(segments, bars, c, dead, a.status)) {
+    while (ok && reader.next(segments, bars, c, dead, a.status)) {
         // V may be read past the pair's last key, up to the sequence's: what other rows of the call see is as
         // good as what this pair's do
         const int32_t limit = KEYS || a.phase == KVC_PHASE_PREFIX ? c.r.hi : min(c.q.pos + c.q.rows / (int32_t)a.g, kvc_key_cap(a));
@@ -397,7 +409,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         kvc_pdl_end(a.beside);
         return;
     }
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31u;
     const uint32_t tiles = (smem_addr(smem_raw) + 1023u) & ~1023u;
     unsigned char *tiles_ptr = smem_raw + (tiles - smem_addr(smem_raw));
     volatile uint32_t *dead = &s_dead;
@@ -426,7 +438,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = uniform(s_tmem);
 
     if (warp < 16) {
         // registers: 512 x 104 + 128 x 64 = 640 x 96 of the launch
@@ -434,14 +446,13 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         // ---------------------------------------------------------------- softmax
         const uint32_t sub = warp >> 3, half = warp >> 2 & 1u, tid = threadIdx.x & 127u;  // tid: the row
         const uint32_t lanes = (warp & 3u) << 21;  // this warp's 32 rows of tensor memory
-        const uint32_t s_col = tmem + COL_S + sub * 128u + lanes, o_col = tmem + COL_O + sub * 128u + half * (D / 2) + lanes;
+        const uint32_t s_col = tmem + COL_S + lanes, o_col = tmem + COL_O + sub * 128u + half * (D / 2) + lanes;
         const uint32_t bar = smem_addr(&bars);
-        const uint32_t s_full = bar + BAR(s_full) + sub * 8u, p_full = bar + BAR(p_full) + (sub * 2 + half) * 8u, o_done = bar + BAR(o_done) + sub * 8u;
         // the two warps of the same rows meet here
         const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1u + sub * 4u + (warp & 3u)) : "memory"); };
         SegmentReader reader;
         Segment c, d;
-        uint32_t s_parity = 0, o_parity = 0, slot = 0;
+        uint32_t s_parity = 0, o_parity = 0, slot = 0;  // parities: a bit for each barrier of a pair
         // Queries of a segment: 16 bytes a thread and turn, rows of 128 bytes in the swizzle.  All scores
         // of the segment before have been seen, so their operand may go.
         const auto load_queries = [&](const Segment &c) {
@@ -478,11 +489,11 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 bar_arrive(bar + BAR(q_full) + sub * 8u);
         };
         bool ok, open = false;  // open: a segment whose products have been started and whose result is to be written
-        uint32_t row0 = 0;
+        uint32_t row0 = 0, last = 0;  // last: the barrier of the open segment's last product
         float m = 0.f, l = 0.f;  // m: the maximum in use, base 2; l: of this thread's keys
         for (;;) {
             // the next segment's queries first, so that its scores run while the one before is written
-            ok = reader.next<true>(segments, &bars, d, dead, a.status);
+            ok = reader.next(segments, &bars, d, dead, a.status);
             if (ok)
                 load_queries(d);
             if (open) {
@@ -490,7 +501,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 row_sum[sub][half][tid] = l;
                 meet();
                 l = row_sum[sub][0][tid] + row_sum[sub][1][tid];
-                if (!__all_sync(~0u, bar_wait(o_done, o_parity ^ 1u, dead, a.status)))
+                if (!__all_sync(~0u, bar_wait(bar + BAR(o_done) + last * 8u, o_parity >> last & 1u ^ 1u, dead, a.status)))
                     break;
                 fence_after();
                 // O in the other layout that tensor memory is read in: a lane holds two neighbouring columns of rows
@@ -552,6 +563,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             c = d;
             row0 = c.rt * ROWS + sub * 128u;
             open = row0 < (uint32_t)c.q.rows;
+            const bool two = (uint32_t)c.q.rows - c.rt * ROWS > 128u;
             if (open) {
                 const int32_t pos = row0 + tid < (uint32_t)c.q.rows ? kvc_row_pos(a, c.q, row0 + tid) : -1;
                 // the warp's rows that see the fewest keys at either end: a tile that both see whole needs no mask
@@ -562,13 +574,14 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
 #pragma unroll 1
                 for (uint32_t i = 0; i < c.n; ++i) {
                     const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + i) * TK + half * HK);
-                    if (!(ok = __all_sync(~0u, bar_wait(s_full, s_parity, dead, a.status))))
+                    const uint32_t buf = two ? sub : i & 1u, s_at = s_col + buf * 128u;
+                    if (!(ok = __all_sync(~0u, bar_wait(bar + BAR(s_full) + buf * 8u, s_parity >> buf & 1u, dead, a.status))))
                         break;
-                    s_parity ^= 1;
+                    s_parity ^= 1u << buf;
                     fence_after();
                     float s[HK];
-                    tmem_ld32(s, s_col + half * HK);
-                    tmem_ld32(s + 32, s_col + half * HK + 32);
+                    tmem_ld32(s, s_at + half * HK);
+                    tmem_ld32(s + 32, s_at + half * HK + 32);
                     uint32_t mask0, mask1;
                     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(mask0), "=r"(mask1) : "r"(smem_addr(&there[(slot + i) % THERE][half * 2])));
                     tmem_wait_ld();
@@ -606,7 +619,13 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                             if (move)
                                 m = top;
                             l *= f;
-                            // (these scores were issued after the products so far, which are in O then)
+                            // the products so far have to be in O.  With two row tiles these scores were issued after
+                            // them; with one, only the product before the last is known to be there
+                            if (!two) {
+                                if (!(ok = __all_sync(~0u, bar_wait(bar + BAR(o_done) + (buf ^ 1u) * 8u, o_parity >> (buf ^ 1u) & 1u ^ 1u, dead, a.status))))
+                                    break;
+                                fence_after();
+                            }
 #pragma unroll 1
                             for (int q = 0; q < D / 2; q += 32) {
                                 float o[32];
@@ -632,17 +651,34 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                             sum2 = kvc_add2(sum2, kvc_pair(y0, y1));
                             p[k] = kvc_from_float2<T>(y0, y1);
                         }
-                        tmem_st16(s_col + half * (HK / 2) + q * 16, p);
+                        tmem_st16(s_at + half * (HK / 2) + q * 16, p);
                     }
                     const float2 sum = kvc_unpair(sum2);
                     l += sum.x + sum.y;
                     tmem_wait_st();
                     fence_before();
-                    bar_arrive(p_full);
+                    bar_arrive(bar + BAR(p_full) + (buf * 2 + half) * 8u);
+                    if (!two)
+                        o_parity ^= 1u << buf;
                 }
                 if (!ok)
                     break;
-                o_parity ^= 1u;
+                last = two ? sub : (c.n - 1) & 1u;
+            } else {
+                // the single row tile uses the other row tile's barriers too.  Their phases are waited for one by
+                // one: a warp that skipped two could not tell a later one by its parity
+                for (uint32_t i = 1; i < c.n && ok; i += 2) {
+                    ok = __all_sync(~0u, bar_wait(bar + BAR(s_full) + 8u, s_parity >> 1, dead, a.status));
+                    s_parity ^= 2u;
+                    o_parity ^= 2u;
+                }
+                if (!ok)
+                    break;
+            }
+            if (two) {  // (warps of rows 128 up never look at the first barriers, and need not count them)
+                o_parity ^= 3u;
+                if (sub == 0)
+                    s_parity ^= (c.n & 1u) << 1;
             }
             slot = (slot + c.n) % THERE;
         }
@@ -652,7 +688,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             load_role<D, true>(args, segments, tiles + S::K, &bars, there, dead, lane);
         } else if (warp == 18) {
             load_role<D, false>(args, segments, tiles + S::V, &bars, there, dead, lane);
-        } else if (warp == 16 && lane == 0) {
+        } else if (warp == 16) {
             // ------------------------------------------------------------ matrix instructions
             // The unit takes few instructions ahead, so what this thread does between them is time that
             // the unit may stand still: addresses and parities live in registers.
@@ -665,61 +701,96 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             Ring<S::VS> v;
             uint32_t q_parity = 0, p_parity = 0;  // a bit for each row tile
             bool ok = true;
-            const auto wait = [&](uint32_t at, uint32_t parity) { return ok = bar_wait(bar + at, parity & 1u, dead, a.status); };
-            const auto scores = [&](uint32_t sub) {
-                const uint32_t qa = q_at + sub * (S::TILE >> 4), ka = k_at + k.stage * (S::TILE >> 4), d = tmem + COL_S + sub * 128u;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t at = ((i >> 2) * S::HALF + (i & 3) * 32) >> 4;
-                    mma_ss(d, qa + at, ka + at, KIND_S, i > 0);
-                }
-                mma_commit(bar + BAR(s_full) + sub * 8u);
+            const auto wait = [&](uint32_t at, uint32_t parity) {
+                return ok = __all_sync(~0u, bar_wait(bar + at, parity & 1u, dead, a.status));
             };
-            while (reader.next<false>(segments, &bars, c, dead, a.status)) {
-                const bool two = (uint32_t)c.q.rows - c.rt * ROWS > 128u;
+            const auto commit = [&](uint32_t at) {
+                if (elect_one())
+                    mma_commit(bar + at);
+            };
+            const auto scores = [&](uint32_t sub, uint32_t buf) {
+                const uint32_t qa = q_at + sub * (S::TILE >> 4), ka = k_at + k.stage * (S::TILE >> 4), d = tmem + COL_S + buf * 128u;
+                if (elect_one()) {
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t at = ((i >> 2) * S::HALF + (i & 3) * 32) >> 4;
+                        mma_ss(d, qa + at, ka + at, KIND_S, i > 0);
+                    }
+                    mma_commit(bar + BAR(s_full) + buf * 8u);
+                }
+            };
+            // O of row tile `sub` += P V, P from score buffer `buf`, in two halves as they come
+            const auto products = [&](uint32_t sub, uint32_t buf, bool first) {
+                const uint32_t d = tmem + COL_O + sub * 128u, pa = tmem + COL_S + buf * 128u, va = v_at + v.stage * (S::TILE >> 4);
+#pragma unroll
+                for (uint32_t half = 0; half < 2; ++half) {
+                    if (!ok || !wait(BAR(p_full) + (buf * 2 + half) * 8u, p_parity >> buf))
+                        continue;
+                    fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (uint32_t j = half * (HK / 16); j < (half + 1) * (HK / 16); ++j)
+                            mma_ts(d, pa + j * 8, va + j * (2048 >> 4), KIND_O, j > 0 || !first);
+                    }
+                }
+                p_parity ^= 1u << buf;
+            };
+            while (reader.next(segments, &bars, c, dead, a.status)) {
+                const bool two = uniform((uint32_t)c.q.rows - c.rt * ROWS > 128u);
+                const uint32_t n = uniform(c.n);
                 if (!wait(BAR(k_full) + k.stage * 8u, k.parity) || !wait(BAR(q_full), q_parity) ||
                     (two && !wait(BAR(q_full) + 8u, q_parity >> 1)))
                     break;
                 q_parity ^= two ? 3u : 1u;
-                scores(0);
-                if (two)
-                    scores(1);
-                mma_commit(bar + BAR(k_empty) + k.stage * 8u);
-                k.next();
-#pragma unroll 1
-                for (uint32_t i = 0; i < c.n; ++i) {
-                    const bool more = i + 1 < c.n;
-                    if (!wait(BAR(v_full) + v.stage * 8u, v.parity) || (more && !wait(BAR(k_full) + k.stage * 8u, k.parity)))
+                // scores are made `ahead` tiles ahead of the products that use the same buffer
+                const uint32_t ahead = two ? 1u : 2u;
+                for (uint32_t i = 0; i < min(ahead, n); ++i) {
+                    if (i > 0 && !wait(BAR(k_full) + k.stage * 8u, k.parity))
                         break;
-                    const uint32_t va = v_at + v.stage * (S::TILE >> 4);
+                    scores(0, i);
+                    if (two)
+                        scores(1, 1);
+                    commit(BAR(k_empty) + k.stage * 8u);
+                    k.next();
+                }
+                if (!ok)
+                    break;
+#pragma unroll 1
+                for (uint32_t i = 0; i < n; ++i) {
+                    const bool more = i + ahead < n;
+                    if (!wait(BAR(v_full) + v.stage * 8u, v.parity))
+                        break;
+                    if (two) {
 #pragma unroll
-                    for (uint32_t sub = 0; sub < 2; ++sub) {
-                        if (sub == 1 && !two)
-                            continue;
-                        const uint32_t d = tmem + COL_O + sub * 128u, pa = tmem + COL_S + sub * 128u;
-#pragma unroll
-                        for (uint32_t half = 0; half < 2; ++half) {
-                            if (!ok || !wait(BAR(p_full) + (sub * 2 + half) * 8u, p_parity >> sub))
-                                continue;
-                            fence_after();
-#pragma unroll
-                            for (uint32_t j = half * (HK / 16); j < (half + 1) * (HK / 16); ++j)
-                                mma_ts(d, pa + j * 8, va + j * (2048 >> 4), KIND_O, j > 0 || i > 0);
+                        for (uint32_t sub = 0; sub < 2; ++sub) {
+                            products(sub, sub, i == 0);
+                            if (!ok)
+                                break;
+                            if (!more)
+                                commit(BAR(o_done) + sub * 8u);
+                            if (sub == 1)
+                                commit(BAR(v_empty) + v.stage * 8u);
+                            if (more) {  // these scores' barrier stands for the products before them too
+                                if (sub == 0 && !wait(BAR(k_full) + k.stage * 8u, k.parity))
+                                    break;
+                                scores(sub, sub);
+                            }
                         }
+                    } else {
+                        const uint32_t buf = i & 1u;
+                        products(0, buf, i == 0);
                         if (!ok)
                             break;
-                        p_parity ^= 1u << sub;
-                        if (more)  // these scores' barrier stands for the products before them too
-                            scores(sub);
-                        else
-                            mma_commit(bar + BAR(o_done) + sub * 8u);
+                        commit(BAR(o_done) + buf * 8u);
+                        commit(BAR(v_empty) + v.stage * 8u);
+                        if (more && wait(BAR(k_full) + k.stage * 8u, k.parity))
+                            scores(0, buf);
                     }
                     if (!ok)
                         break;
-                    mma_commit(bar + BAR(v_empty) + v.stage * 8u);
                     v.next();
                     if (more) {
-                        mma_commit(bar + BAR(k_empty) + k.stage * 8u);
+                        commit(BAR(k_empty) + k.stage * 8u);
                         k.next();
                     }
                 }
@@ -727,7 +798,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     break;
             }
             // nothing of ours runs on when the block gives tensor memory back, on no way out
-            mma_commit(smem_addr(&bars.drained));
+            commit(BAR(drained));
 #pragma unroll 1
             for (uint32_t i = 0; i < KVC_WAIT_LIMIT && !bar_try(smem_addr(&bars.drained), 0); ++i)
                 ;

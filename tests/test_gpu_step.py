@@ -481,3 +481,30 @@ def test_a_step_from_lengths_to_a_packed_chunk_and_back():
     kvc.kvc_attention(lay, 1, q, again, moved, total, cu, ws, lse=lse2, max_q_len=20)
     assert torch.equal(again, out) and torch.equal(lse2, lse)
     assert kvc.kvc_poll_device_status(lay) == (0, 0)
+
+
+def test_attention_pairs_of_one_and_two_row_tiles_in_any_order():
+    """Requests whose queries fill one row tile or two, and keys of odd and even numbers of tiles, one after
+    the other in the same blocks."""
+    rng = np.random.default_rng(5)
+    for hq, hkv, d in ((8, 2, 128), (4, 4, 64)):
+        lens = rng.integers(1, 1400, 24).tolist()
+        rows = [min(x, int(rng.choice([1, 20, 33, 64, 70, 130, 200]))) for x in lens]
+        b = Batch(lens, rows, hq, hkv, d, BF16, 16, seed=hq)
+        for _ in range(3):
+            kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, b.workspace(), lse=b.lse, max_q_len=max(rows))
+        b.check()
+
+
+def test_attention_scores_that_rise_along_the_keys():
+    """Keys whose scores grow: the running maximum moves at every tile, and sums are rescaled each time."""
+    for rows, hq in ((1, 4), (60, 4), (200, 4)):
+        b = Batch([900], [rows], hq, 2, 64, BF16, 16, seed=4)
+        grow = torch.linspace(0.0, 40.0, 900)[:, None, None]
+        k = (b.keys[0].float() * 0.1 + grow).to(BF16)
+        b.q.copy_(b.q.abs())
+        b.keys[0] = k
+        for j in range(900):
+            b.planes[2][b.tables_np[0, j // 16], j % 16] = k[j].cuda()
+        kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, b.workspace(), lse=b.lse, max_q_len=rows)
+        b.check()
