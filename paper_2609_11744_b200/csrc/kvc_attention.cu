@@ -210,45 +210,62 @@ struct JoinShared {
     KvcParts prefix, suffix;
 };
 
-// Shared prefixes: a warp joins one row's parts of its group's prefix and of its own keys.
-template <typename T, int D>
+// Shared prefixes: WPR warps join one row's parts of its group's prefix and of its own keys.
+template <typename T, int D, int WPR>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) kvc_join_shared_kernel(const JoinShared j)
 {
     kvc_pdl_wait();
     const KvcAttn &a = j.a;
     const uint32_t top = (uint32_t)kvc_clamp(a.cu_q[a.n_requests], 0, (int32_t)a.n_tokens);
-    const uint64_t w = (uint64_t)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
-    if (w >= (uint64_t)top * a.hq)
-        return;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint64_t w = (uint64_t)blockIdx.x * (JOIN_WARPS / WPR) + warp / WPR;
     const uint32_t tok = (uint32_t)(w / a.hq), head = (uint32_t)(w - (uint64_t)tok * a.hq);
-    if ((int32_t)tok < a.cu_q[0])
-        return;  // rows before the first sequence belong to none
-    const uint32_t h = head / a.g, x = head % a.g;
-    const uint32_t r = kvc_last_at_most_warp(a.cu_q, a.n_requests, (int32_t)tok);
-    const int32_t qa = a.cu_q[r], qe = kvc_clamp(a.cu_q[r + 1], qa, (int32_t)a.n_tokens);
-    const PhaseRow s = phase_row(j.suffix, r, h, (uint32_t)(qe - qa) * a.g, (tok - (uint32_t)qa) * a.g + x);
-    PhaseRow p;
-    p.first = p.n = 0;
-    p.pair = p.row = 0;
-    const int32_t g = kvc_group_of(a, r);
-    if (g >= 0) {
-        const int32_t R = (int32_t)a.n_requests;
-        const int32_t r0 = kvc_clamp(a.group_starts[g], 0, R), r1 = kvc_clamp(a.group_starts[g + 1], r0, R);
-        const int32_t ga = kvc_clamp(a.cu_q[r0], 0, (int32_t)a.n_tokens), ge = kvc_clamp(a.cu_q[r1], ga, (int32_t)a.n_tokens);
-        p = phase_row(j.prefix, (uint32_t)g, h, (uint32_t)(ge - ga) * a.g, (tok - (uint32_t)ga) * a.g + x);
-    }
-    const auto get = [&](uint32_t i) {
-        Part<D> q;
-        const bool in_prefix = i < p.n;
-        const KvcParts &from = in_prefix ? j.prefix : j.suffix;
-        const PhaseRow &at = in_prefix ? p : s;
-        q.p = &from;
-        q.at = (at.first + (in_prefix ? i : i - p.n) + at.pair) * from.rows + at.row;
-        return q;
-    };
+    // rows outside the sequences belong to none
+    const bool real = w < (uint64_t)top * a.hq && (int32_t)tok >= a.cu_q[0];
+    if (WPR == 1 && !real)
+        return;
+    __shared__ float s_sum[JOIN_WARPS][D];
     Vec<D> sum;
-    float m, l;
-    join_row<D, 1>(p.n + s.n, get, sum, m, l);
+    float m = 0.f, l = 0.f;
+    if (real) {
+        const uint32_t h = head / a.g, x = head % a.g;
+        const uint32_t r = kvc_last_at_most_warp(a.cu_q, a.n_requests, (int32_t)tok);
+        const int32_t qa = a.cu_q[r], qe = kvc_clamp(a.cu_q[r + 1], qa, (int32_t)a.n_tokens);
+        const PhaseRow s = phase_row(j.suffix, r, h, (uint32_t)(qe - qa) * a.g, (tok - (uint32_t)qa) * a.g + x);
+        PhaseRow p;
+        p.first = p.n = 0;
+        p.pair = p.row = 0;
+        const int32_t g = kvc_group_of(a, r);
+        if (g >= 0) {
+            const int32_t R = (int32_t)a.n_requests;
+            const int32_t r0 = kvc_clamp(a.group_starts[g], 0, R), r1 = kvc_clamp(a.group_starts[g + 1], r0, R);
+            const int32_t ga = kvc_clamp(a.cu_q[r0], 0, (int32_t)a.n_tokens), ge = kvc_clamp(a.cu_q[r1], ga, (int32_t)a.n_tokens);
+            p = phase_row(j.prefix, (uint32_t)g, h, (uint32_t)(ge - ga) * a.g, (tok - (uint32_t)ga) * a.g + x);
+        }
+        const auto get = [&](uint32_t i) {
+            Part<D> q;
+            const bool in_prefix = i < p.n;
+            const KvcParts &from = in_prefix ? j.prefix : j.suffix;
+            const PhaseRow &at = in_prefix ? p : s;
+            q.p = &from;
+            q.at = (at.first + (in_prefix ? i : i - p.n) + at.pair) * from.rows + at.row;
+            return q;
+        };
+        join_row<D, WPR>(p.n + s.n, get, sum, m, l);
+    }
+    if (WPR > 1) {
+#pragma unroll
+        for (int e = 0; e < Vec<D>::N; ++e)
+            s_sum[warp][lane * Vec<D>::N + e] = sum.v[e];
+        __syncthreads();
+        if (!real || warp % WPR != 0)
+            return;
+#pragma unroll
+        for (int i = 1; i < WPR; ++i)
+#pragma unroll
+            for (int e = 0; e < Vec<D>::N; ++e)
+                sum.v[e] += s_sum[warp + i][lane * Vec<D>::N + e];
+    }
     write_row<T, D>(a, tok, head, sum, m, l);
 }
 
@@ -275,7 +292,7 @@ struct Shape {
 
 void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, bool tiles, uint64_t sequences, bool by_pair)
 {
-    const uint32_t blocks = tiles ? kvc_attn_tiles_blocks(lay) : kvc_attn_rows_blocks(lay);
+    const uint32_t blocks = tiles ? kvc_attn_tiles_blocks(lay) : kvc_attn_rows_blocks(lay, by_pair);
     const uint32_t rows = tiles ? KVC_ATTN_TILE_ROWS : KVC_ATTN_SMALL_ROWS, head_dim = s.head_dim;
     const uint64_t pairs = by_pair ? kvc_max_pairs(sequences, s.tokens, s.g, s.hkv, rows) : 0;
     const uint64_t slots = pairs ? (uint64_t)blocks + pairs : 2ull * blocks;
@@ -340,8 +357,13 @@ cudaError_t join_split(const KvcAttn &a, cudaStream_t st)
 template <typename T, int D>
 cudaError_t join_shared(const JoinShared &j, cudaStream_t st)
 {
+    // few rows: four warps each, for the SMs would stand idle while a row's parts are summed one after the other
+    // (1024 rows of some 20 parts: 15 us with one warp a row)
     const uint64_t rows = (uint64_t)j.a.n_tokens * j.a.hq;
-    return kvc_launch_pdl(kvc_join_shared_kernel<T, D>, j, dim3((uint32_t)((rows + JOIN_WARPS - 1) / JOIN_WARPS)),
+    if (rows <= 2048)
+        return kvc_launch_pdl(kvc_join_shared_kernel<T, D, 4>, j, dim3((uint32_t)((rows * 4 + JOIN_WARPS - 1) / JOIN_WARPS)),
+                              JOIN_WARPS * 32, 0, st);
+    return kvc_launch_pdl(kvc_join_shared_kernel<T, D, 1>, j, dim3((uint32_t)((rows + JOIN_WARPS - 1) / JOIN_WARPS)),
                           JOIN_WARPS * 32, 0, st);
 }
 

@@ -87,7 +87,7 @@ inline uint64_t kvc_max_pairs(uint64_t sequences, uint64_t tokens, uint64_t g, u
 }
 
 // Implemented in kvc_attention_rows.cu (few rows) and kvc_attention_tiles.cu (many).
-uint32_t kvc_attn_rows_blocks(const kvc_layout *lay);
+uint32_t kvc_attn_rows_blocks(const kvc_layout *lay, bool shared);
 cudaError_t kvc_launch_attn_rows(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
 uint32_t kvc_attn_tiles_blocks(const kvc_layout *lay);
 cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);

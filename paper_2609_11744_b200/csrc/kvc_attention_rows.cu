@@ -374,7 +374,9 @@ cudaError_t launch(const KvcAttn &a, uint32_t blocks, cudaStream_t st)
 
 }  // namespace
 
-uint32_t kvc_attn_rows_blocks(const kvc_layout *lay) { return 2u * (uint32_t)lay->sm_count; }
+// Two blocks a SM.  Beside a shared prefix, whose blocks hold some SMs for a part of the time, three, so that
+// equal runs still end together (64 requests on a 1024-token prefix: 88 us with two, 76 with three, 86 with four).
+uint32_t kvc_attn_rows_blocks(const kvc_layout *lay, bool shared) { return (shared ? 3u : 2u) * (uint32_t)lay->sm_count; }
 
 cudaError_t kvc_launch_attn_rows(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st)
 {

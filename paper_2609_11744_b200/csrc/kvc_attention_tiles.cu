@@ -36,7 +36,7 @@ constexpr int TK = 128;             // keys of a K or V stage
 constexpr int HK = TK / 2;          // keys of one softmax thread
 constexpr int THREADS = 640;
 constexpr int HEAD = 3;             // what a pair costs besides its units, in units (measured: 13,000 cycles against 3,800)
-constexpr int LEAST = 5;            // units of a run at least
+constexpr int LEAST = 3;            // units of a run at least
 constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper than the K ring
 
 template <int D>
@@ -448,8 +448,11 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         const uint32_t lanes = (warp & 3u) << 21;  // this warp's 32 rows of tensor memory
         const uint32_t s_col = tmem + COL_S + lanes, o_col = tmem + COL_O + sub * 128u + half * (D / 2) + lanes;
         const uint32_t bar = smem_addr(&bars);
-        // the two warps of the same rows meet here
-        const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1u + sub * 4u + (warp & 3u)) : "memory"); };
+        // The two warps of the same rows meet here.  One that leaves early, because a wait gave up, arrives
+        // once more for its partner, which can come here once at most before it finds the same: the next scores
+        // need the weights of both, and the end of a segment looks at `dead` first.
+        const uint32_t meeting = 1u + sub * 4u + (warp & 3u);
+        const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(meeting) : "memory"); };
         SegmentReader reader;
         Segment c, d;
         uint32_t s_parity = 0, o_parity = 0, slot = 0;  // parities: a bit for each barrier of a pair
@@ -496,13 +499,19 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             ok = reader.next(segments, &bars, d, dead, a.status);
             if (ok)
                 load_queries(d);
+            if (__any_sync(~0u, *dead)) {
+                ok = false;
+                break;
+            }
             if (open) {
                 const bool from_start = c.t == 0, to_end = c.t + c.n == c.r.n, real = row0 + tid < (uint32_t)c.q.rows;
                 row_sum[sub][half][tid] = l;
                 meet();
                 l = row_sum[sub][0][tid] + row_sum[sub][1][tid];
-                if (!__all_sync(~0u, bar_wait(bar + BAR(o_done) + last * 8u, o_parity >> last & 1u ^ 1u, dead, a.status)))
+                if (!__all_sync(~0u, bar_wait(bar + BAR(o_done) + last * 8u, o_parity >> last & 1u ^ 1u, dead, a.status))) {
+                    ok = false;
                     break;
+                }
                 fence_after();
                 // O in the other layout that tensor memory is read in: a lane holds two neighbouring columns of rows
                 // lane / 4 and lane / 4 + 8 of 16, so that four lanes write adjacent bytes of one row and a store
@@ -566,9 +575,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             const bool two = (uint32_t)c.q.rows - c.rt * ROWS > 128u;
             if (open) {
                 const int32_t pos = row0 + tid < (uint32_t)c.q.rows ? kvc_row_pos(a, c.q, row0 + tid) : -1;
-                // the warp's rows that see the fewest keys at either end: a tile that both see whole needs no mask
-                const int32_t pos_lo = __reduce_min_sync(~0u, pos);
-                const int32_t old_hi = a.window ? __reduce_max_sync(~0u, pos) - a.window : -1;  // the last key behind all windows
+                const int32_t old = a.window ? pos - a.window : -1;  // the last key behind the row's window
                 m = -INFINITY;
                 l = 0.f;
 #pragma unroll 1
@@ -585,7 +592,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     uint32_t mask0, mask1;
                     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(mask0), "=r"(mask1) : "r"(smem_addr(&there[(slot + i) % THERE][half * 2])));
                     tmem_wait_ld();
-                    if ((mask0 & mask1) != ~0u || j0 + HK - 1 > pos_lo || (j0 <= old_hi && j0 + HK - 1 >= a.sinks)) {
+                    if (__any_sync(~0u, (mask0 & mask1) != ~0u || j0 + HK - 1 > pos || (j0 <= old && j0 + HK - 1 >= a.sinks))) {
                         // kvc_sees() for 32 keys at a time: at most pos, and after pos - window or before sinks
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
@@ -682,6 +689,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             }
             slot = (slot + c.n) % THERE;
         }
+        if (__any_sync(~0u, *dead))
+            asm volatile("bar.arrive %0, 64;" ::"r"(meeting) : "memory");
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 17) {
