@@ -464,7 +464,11 @@ kvc_status kvc_append(kvc_layout *layout, const kvc_append_desc *desc, void *str
  * max_q_len is a hint, at least the largest number of query rows of one request (0: unknown): it
  * chooses between kernels, never changes what is computed.  Any mix of prompts and single tokens may
  * be in one call.
+ * A request has at most KVC_ATTENTION_MAX_KEYS tokens (a longer length counts as that), and so have
+ * window and sinks (INVALID_ARG).
  * Layout: kv_planes = 2, elem_bytes = 2, head_dim 64 or 128, n_q_heads a multiple of num_kv_heads.
+ * Any block size; with many query rows, sizes that divide 128 from 8 up, and multiples of 128, are the
+ * fast ones.
  * Strides in elements; pointers of q and out and strides in bytes are multiples of 16 bytes.  `out`
  * must not overlap q.  scale > 0.
  * workspace: at least kvc_attention_workspace_bytes(...) bytes, 256-byte aligned, contents irrelevant
@@ -476,9 +480,11 @@ kvc_status kvc_append(kvc_layout *layout, const kvc_append_desc *desc, void *str
  * counterpart of kvc_map_requests_shared).  Group g is requests group_starts[g] ..
  * group_starts[g+1]-1 (ascending; requests in no group share nothing); their first prefix_lens[g]
  * tokens are the same, and their keys and values are read ONCE for the whole group, through the
- * table of the group's first request.  prefix_lens need not be a multiple of the block size.  window
+ * table of the group's first request.  prefix_lens[g] is at most the length of every request of the
+ * group, and need not be a multiple of the block size.  window
  * and sinks must be 0, 1 <= n_groups <= n_requests.  Three kernels.
  * Errors: INVALID_ARG, ALIGNMENT, TOO_LARGE (n_tokens * query heads per KV head >= 2^31), CUDA. */
+#define KVC_ATTENTION_MAX_KEYS 0x40000000u
 typedef struct {
     uint32_t layer;
     uint32_t dtype;              /* kvc_dtype: of q, out and the pool */

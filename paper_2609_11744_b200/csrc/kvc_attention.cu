@@ -339,7 +339,7 @@ kvc_status check(const kvc_layout *lay, const kvc_attention_desc *d)
         (d->dtype != KVC_DTYPE_BF16 && d->dtype != KVC_DTYPE_FP16))
         return KVC_ERR_INVALID_ARG;
     if (d->n_q_heads == 0 || d->n_q_heads % l.num_kv_heads || !(d->scale > 0.f) || d->scale > 3.0e38f ||
-        d->window > 0x7FFFFFFFu || d->sinks > 0x7FFFFFFFu || d->n_requests > 0x7FFFFFFFu)
+        d->window > KVC_ATTENTION_MAX_KEYS || d->sinks > KVC_ATTENTION_MAX_KEYS || d->n_requests > 0x7FFFFFFFu)
         return KVC_ERR_INVALID_ARG;
     if ((uint64_t)d->n_tokens * (d->n_q_heads / l.num_kv_heads) > 0x7FFFFFFFull)
         return KVC_ERR_TOO_LARGE;

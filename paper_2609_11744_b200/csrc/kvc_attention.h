@@ -154,9 +154,11 @@ __device__ __forceinline__ uint32_t kvc_last_at_most_warp(const int32_t *v, uint
 
 __device__ __forceinline__ int32_t kvc_clamp(int32_t x, int32_t lo, int32_t hi) { return min(max(x, lo), hi); }
 
+// Keys of a request at most: a quarter of the integers' range, so that sums of a position, a window and a
+// tile's width stay inside it.
 __device__ __forceinline__ int32_t kvc_key_cap(const KvcAttn &a)
 {
-    return (int32_t)min((uint64_t)a.max_blocks * a.block_size, (uint64_t)0x7FFFFFFF);
+    return (int32_t)min((uint64_t)a.max_blocks * a.block_size, (uint64_t)KVC_ATTENTION_MAX_KEYS);
 }
 
 // The group that holds request r, or -1.
@@ -191,7 +193,7 @@ __device__ __forceinline__ KvcSeq kvc_seq(const KvcAttn &a, uint32_t s)
         q.qa = kvc_clamp(a.cu_q[s], 0, top);
         const int32_t n = kvc_clamp(a.cu_q[s + 1], q.qa, top) - q.qa;
         q.rows = n * (int32_t)a.g;
-        q.pos = max(a.seq_lens[s], 0) - n;
+        q.pos = kvc_clamp(a.seq_lens[s], 0, (int32_t)KVC_ATTENTION_MAX_KEYS) - n;
         q.skip = 0;
         q.len = 0;
         if (a.phase == KVC_PHASE_SUFFIX) {
@@ -449,7 +451,7 @@ __device__ __forceinline__ int32_t kvc_row_pos(const KvcAttn &a, const KvcSeq &q
     const int32_t t = q.qa + tok;
     const uint32_t r = kvc_last_at_most(a.cu_q, a.n_requests, t);
     const int32_t qa = a.cu_q[r], n = kvc_clamp(a.cu_q[r + 1], qa, (int32_t)a.n_tokens) - qa;
-    return max(a.seq_lens[r], 0) - n + (t - qa);
+    return kvc_clamp(a.seq_lens[r], 0, (int32_t)KVC_ATTENTION_MAX_KEYS) - n + (t - qa);
 }
 
 // Whether the row at position p sees key j (which lies in the pair's range).

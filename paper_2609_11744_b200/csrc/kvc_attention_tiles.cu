@@ -909,9 +909,11 @@ cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t hea
         args.box_keys = B < (uint32_t)TK ? B : (uint32_t)TK;
         args.boxes = TK / args.box_keys;
         const EncodeTiled fn = encode_tiled();
-        if (!fn || !encode(fn, &args.k_map, a, a.k, dtype, head_dim, args.box_keys) ||
+        if (!fn)
+            return cudaErrorNotSupported;
+        if (!encode(fn, &args.k_map, a, a.k, dtype, head_dim, args.box_keys) ||
             !encode(fn, &args.v_map, a, a.v, dtype, head_dim, args.box_keys))
-            return cudaErrorUnknown;
+            args.boxes = 0;  // a pool that no map describes
     }
     if (dtype == KVC_DTYPE_BF16)
         return head_dim == 128 ? launch<__nv_bfloat16, 128>(args, blocks, st) : launch<__nv_bfloat16, 64>(args, blocks, st);

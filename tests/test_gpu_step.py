@@ -508,3 +508,56 @@ def test_attention_scores_that_rise_along_the_keys():
             b.planes[2][b.tables_np[0, j // 16], j % 16] = k[j].cuda()
         kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, b.workspace(), lse=b.lse, max_q_len=rows)
         b.check()
+
+
+def test_append_with_an_unaligned_angle_table():
+    """A cos/sin table at an address that no vector load may use, against the same table aligned."""
+    t, hq, hkv, d = 40, 6, 2, 128
+    g = torch.Generator().manual_seed(6)
+    q, k, v = (torch.randn(t, h, d, generator=g).to(BF16).cuda() for h in (hq, hkv, hkv))
+    positions, slots = torch.randint(0, 90, (t,), generator=g, dtype=torch.int32).cuda(), torch.arange(t).cuda()
+    raw = torch.randn(90 * 64 + 1, generator=g).cuda()
+    got = []
+    for table in (raw[1:].view(90, 64), raw[1:].clone().view(90, 64)):
+        for interleaved in (False, True):
+            pool = torch.zeros(1, 2, 4, 16, hkv, d, dtype=BF16, device="cuda")
+            out = torch.zeros_like(q)
+            kvc.kvc_append(make_layout(pool, 16), 0, q, k, v, out, slots, positions, table, interleaved=interleaved)
+            got.append((out, pool))
+    for i in range(2):
+        assert torch.equal(got[i][0], got[i + 2][0]) and torch.equal(got[i][1], got[i + 2][1])
+
+
+def test_attention_window_and_sinks_at_their_limits():
+    b = Batch([300, 40], [70, 1], 4, 2, 64, BF16, 16, seed=9)
+    for rows in ([70, 1],):
+        kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, b.workspace(), window=1 << 30, sinks=1 << 30, lse=b.lse,
+                          max_q_len=max(rows))
+        b.check()
+        kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, b.workspace(), window=1 << 30, lse=b.lse, max_q_len=1)
+        b.check()
+
+
+def test_lengths_that_contradict_one_another_stay_inside_the_buffers():
+    """Token rows that descend or overlap, lengths past the table, groups out of order: whatever comes out, nothing
+    outside the buffers is touched, no wait gives up, and a sound call afterwards is right."""
+    g = torch.Generator().manual_seed(12)
+    for hint in (1, 64):
+        b = Batch([200, 90, 150], [3, 2, 40], 8, 2, 128, BF16, 16, seed=21, lead=1)
+        t = b.q.shape[0]
+        frame = torch.full((t + 8, 8, 128), 5.0, dtype=BF16, device="cuda")
+        ws = b.workspace(2)
+        guard = torch.full((ws.numel() + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        space = guard[: ws.numel()]
+        for cu in ([0, 46, 0, 46], [46, 0, 46, 0], [-5, 1000, 3, 2], [7, 7, 7, 7], [0, 2 ** 31 - 1, 1, 40]):
+            for lens in ([200, 90, 150], [2 ** 31 - 1, -3, 10 ** 6], [0, 0, 0]):
+                kvc.kvc_attention(b.lay, 1, b.q, frame[4: t + 4], b.tables, dev(lens), dev(cu), space, lse=b.lse, max_q_len=hint)
+                for groups, prefix in (([0, 2, 3], [64, 32]), ([3, 1, 0], [10 ** 9, -1]), ([-7, 99, 2], [17, 300])):
+                    kvc.kvc_attention_shared(b.lay, 1, b.q, frame[4: t + 4], b.tables, dev(lens), dev(cu), dev(groups), dev(prefix),
+                                             space, lse=b.lse, max_q_len=hint)
+        torch.cuda.synchronize()
+        assert (frame[:4] == 5.0).all() and (frame[t + 4:] == 5.0).all() and (guard[ws.numel():] == 0x5A).all()
+        assert kvc.kvc_poll_device_status(b.lay)[1] == 0
+        b.lse.fill_(7.0)
+        kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, space, lse=b.lse, max_q_len=40)
+        b.check()

@@ -84,7 +84,7 @@ BAD_ATTENTION = [
 
 
 @pytest.mark.parametrize("want,kw", BAD_ATTENTION + [
-    (INVALID, dict(n_groups=1)), (INVALID, dict(group_starts=A)), (INVALID, dict(prefix_lens=A)), (INVALID, dict(window=1 << 31))])
+    (INVALID, dict(n_groups=1)), (INVALID, dict(group_starts=A)), (INVALID, dict(prefix_lens=A)), (INVALID, dict(window=(1 << 30) + 1)), (INVALID, dict(sinks=1 << 31))])
 def test_attention_refuses(want, kw):
     assert status("kvc_attention", layout(), attention_desc(**kw)) == want
 
