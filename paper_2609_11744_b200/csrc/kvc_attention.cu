@@ -427,9 +427,8 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     a.hq = d->n_q_heads;
     a.hkv = l.num_kv_heads;
     a.g = shape.g;
-    const auto shift = [](uint32_t x) { return x & (x - 1) ? KVC_NO_SHIFT : (uint32_t)__builtin_ctz(x); };
-    a.g_shift = shift(a.g);
-    a.block_shift = shift(a.block_size);
+    a.g_shift = kvc_shift_of(a.g);
+    a.block_shift = kvc_shift_of(a.block_size);
     a.scale_log2 = d->scale * 1.44269504088896341f;
     a.window = (int32_t)d->window;
     a.sinks = (int32_t)d->sinks;

@@ -55,8 +55,6 @@ struct KvcParts {
                          // ascend, so only lengths that contradict one another can ask for more
 };
 
-#define KVC_NO_SHIFT 32u
-
 struct KvcAttn {
     const unsigned char *k, *v;  // planes of the layer
     uint64_t block_stride;
@@ -94,12 +92,6 @@ cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t hea
 
 #ifdef __CUDACC__
 
-// Divisions by the two numbers that are nearly always powers of two (a division is some 25 instructions,
-// several of them between a block's start and its first load).
-__device__ __forceinline__ uint32_t kvc_div(uint32_t x, uint32_t d, uint32_t shift)
-{
-    return shift != KVC_NO_SHIFT ? x >> shift : x / d;
-}
 __device__ __forceinline__ uint32_t kvc_div_g(const KvcAttn &a, uint32_t x) { return kvc_div(x, a.g, a.g_shift); }
 
 // Where run c of `runs` begins on a line.  (64-bit divisions are worth avoiding: they are a good part of
@@ -298,7 +290,8 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
     const uint32_t per = (n_seq + owners - 1) / owners;
     const uint32_t s0 = min(owner * per, n_seq), s1 = min(s0 + per, n_seq);
     unsigned long long units = 0, pairs = 0;
-    KvcSeq q0;  // the owner's first sequence, usually its only one
+    KvcSeq q0;  // the owner's first sequence, usually its only one, and the range of its first row tile, likewise
+    KvcRange r0;
 #pragma unroll 1
     for (uint32_t s = s0; s < s1; ++s) {
         const KvcSeq q = kvc_seq(a, s);
@@ -307,8 +300,12 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
         unsigned long long sum = 0;
         uint32_t n = 0;
 #pragma unroll 1
-        for (uint32_t rt = rt0; rt * ROWS < (uint32_t)q.rows; rt += rt_step, ++n)
-            sum += HEAD + kvc_range<ROWS, TK>(a, q, rt).n;
+        for (uint32_t rt = rt0; rt * ROWS < (uint32_t)q.rows; rt += rt_step, ++n) {
+            const KvcRange r = kvc_range<ROWS, TK>(a, q, rt);
+            sum += HEAD + r.n;
+            if (s == s0 && rt == 0)
+                r0 = r;
+        }
         units += sum * a.hkv;
         pairs += (unsigned long long)n * a.hkv;
     }
@@ -359,9 +356,10 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
                 a.parts.base[s] = (uint32_t)min(p, 0xFFFFFFFFull);
             const KvcSeq q = s == s0 ? q0 : kvc_seq(a, s);
             const uint32_t n = ((uint32_t)q.rows + ROWS - 1) / ROWS;
-            unsigned long long per_head = 0;
+            const bool one = !wide && n == 1 && s == s0;
+            unsigned long long per_head = one ? HEAD + r0.n : 0;
 #pragma unroll 1
-            for (uint32_t rt = rt0; rt < n; rt += rt_step)
+            for (uint32_t rt = one ? n : rt0; rt < n; rt += rt_step)
                 per_head += HEAD + kvc_range<ROWS, TK>(a, q, rt).n;
             if (wide)
 #pragma unroll
@@ -379,7 +377,7 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
                     // row tiles rt - lane .. of which the lanes hold one each, or just rt
                     uint32_t own = 0;
                     if (rt < n) {
-                        r = kvc_range<ROWS, TK>(a, q, rt);
+                        r = one ? r0 : kvc_range<ROWS, TK>(a, q, rt);
                         own = HEAD + r.n;
                     }
                     unsigned long long sum = own;

@@ -27,7 +27,7 @@ struct Shape {
     static constexpr int ROW = D * 2;                // bytes of a key
     static constexpr int CHUNKS = ROW / 16;          // 16-byte pieces of a key
     static constexpr int STAGE = 2 * WK * ROW;       // K and V of one warp's share of a unit
-    static constexpr int STAGES = D == 128 ? 3 : 6;  // 2 blocks of 4 x 24 KiB a SM, 16 KiB of each warp's in flight
+    static constexpr int STAGES = D == 128 ? 2 : 4;  // 64 KiB a block, two blocks a SM (three and six: the same rate, a longer start)
     static constexpr int MERGE = 2 * ROWS * D * 4;   // two warps' sums
     static constexpr int SMEM = WARPS * STAGES * STAGE + MERGE;
 };

@@ -48,6 +48,22 @@ inline cudaError_t kvc_launch_pdl(void (*kernel)(const A), const A &a, dim3 grid
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
+// Division by a number that is nearly always a power of two: `shift` is its logarithm, or KVC_NO_SHIFT.
+// (An integer division is some 25 instructions, and the kernels have several between their start and
+// their first load.)
+#define KVC_NO_SHIFT 32u
+inline uint32_t kvc_shift_of(uint32_t d)
+{
+    uint32_t s = 0;
+    while (s < 31 && (1u << s) < d)
+        ++s;
+    return (1u << s) == d ? s : KVC_NO_SHIFT;
+}
+__device__ __forceinline__ uint32_t kvc_div(uint32_t x, uint32_t d, uint32_t shift)
+{
+    return shift != KVC_NO_SHIFT ? x >> shift : x / d;
+}
+
 // Two 32-bit floats in one 64-bit register pair, for the two-wide arithmetic.
 __device__ __forceinline__ uint64_t kvc_pair(float lo, float hi)
 {

@@ -23,13 +23,11 @@ struct MapArgs {
     const int32_t *context_lens, *new_lens, *free_blocks;
     int32_t *tables;
     int64_t table_stride;
-    uint32_t max_blocks, n_requests, n_free, capacity, block_size, num_blocks;
+    uint32_t max_blocks, n_requests, n_free, capacity, block_size, block_shift, num_blocks;
     int32_t *cu, *total_lens, *positions, *request, *counts;
     int64_t *slots;
     uint32_t *status;
 };
-
-#define MAP_THREADS 512u
 
 __device__ __forceinline__ int32_t sat32(int64_t v) { return v > 0x7FFFFFFFll ? 0x7FFFFFFF : (int32_t)v; }
 
@@ -38,15 +36,20 @@ struct MapReq {
     uint32_t hb, ha;   // blocks held, blocks needed (both at most max_blocks)
 };
 
+// Blocks that n tokens (at most 2^31 - 1) take.
+__device__ __forceinline__ uint32_t map_blocks(const MapArgs &a, uint32_t n)
+{
+    const uint32_t q = kvc_div(n, a.block_size, a.block_shift);
+    return q + (q * a.block_size != n);
+}
+
 __device__ __forceinline__ MapReq map_req(const MapArgs &a, uint32_t r)
 {
     MapReq q;
     q.ctx = max(a.context_lens[r], 0);
     q.add = max(min(a.new_lens[r], 0x7FFFFFFF - q.ctx), 0);
-    const uint32_t b = a.block_size;
-    const uint32_t end = (uint32_t)q.ctx + (uint32_t)q.add;
-    q.ha = min(end / b + (end % b != 0), a.max_blocks);
-    q.hb = min((uint32_t)q.ctx / b + ((uint32_t)q.ctx % b != 0), q.ha);
+    q.ha = min(map_blocks(a, (uint32_t)q.ctx + (uint32_t)q.add), a.max_blocks);
+    q.hb = min(map_blocks(a, (uint32_t)q.ctx), q.ha);
     if (q.add == 0)
         q.ha = q.hb;  // nothing is added: nothing is taken
     return q;
@@ -66,6 +69,7 @@ __device__ __forceinline__ uint32_t last_at_most(const int32_t *v, uint32_t n, i
     return lo;
 }
 
+template <uint32_t MAP_THREADS>
 __global__ void __launch_bounds__(MAP_THREADS) kvc_map_tokens_kernel(const MapArgs a)
 {
     extern __shared__ int32_t sm[];
@@ -161,7 +165,7 @@ __global__ void __launch_bounds__(MAP_THREADS) kvc_map_tokens_kernel(const MapAr
     const uint32_t n_new = (uint32_t)fb[R];
     for (uint64_t i = at; i < n_new; i += step) {
         const uint32_t r = last_at_most(fb, R, (int32_t)i);
-        const uint32_t hb = min((uint32_t)ctx[r] / B + ((uint32_t)ctx[r] % B != 0), a.max_blocks);
+        const uint32_t hb = min(map_blocks(a, (uint32_t)ctx[r]), a.max_blocks);
         a.tables[(int64_t)r * a.table_stride + hb + (i - (uint32_t)fb[r])] = i < a.n_free ? a.free_blocks[i] : -1;
     }
     // token rows; the rows behind the last token are marked as holding none
@@ -173,9 +177,9 @@ __global__ void __launch_bounds__(MAP_THREADS) kvc_map_tokens_kernel(const MapAr
             const uint32_t r = last_at_most(cu, R, (int32_t)i);
             req = (int32_t)r;
             pos = ctx[r] + (int32_t)(i - (uint32_t)cu[r]);
-            const uint32_t bi = (uint32_t)pos / B, off = (uint32_t)pos % B;
+            const uint32_t bi = kvc_div((uint32_t)pos, B, a.block_shift), off = (uint32_t)pos - bi * B;
             if (bi < a.max_blocks) {
-                const uint32_t hb = (uint32_t)ctx[r] / B + ((uint32_t)ctx[r] % B != 0);
+                const uint32_t hb = map_blocks(a, (uint32_t)ctx[r]);
                 int32_t id = -1;
                 bool have = true;
                 if (bi < hb) {  // the block that the context's last token lies in
@@ -230,16 +234,14 @@ struct AppendArgs {
     uint32_t *status;
 };
 
-#define APPEND_THREADS 256u
-#ifndef APPEND_UNROLL
+#define APPEND_THREADS 64u
+// Small blocks, 16 a SM: a block's warps go through the same chain (slot, angles, heads) at the same time, and
+// small ones start and end more evenly (16384 tokens of 64 + 16 heads: 153 us with 256 threads, 141 with 128,
+// 134 with 64).  Four heads a team and turn, two turns: with one turn the angles are fetched too often, with more
+// or wider ones too few warps fit (155 to 260 us).
+#define APPEND_BLOCKS 16
 #define APPEND_UNROLL 4
-#endif
-#ifndef APPEND_BLOCKS
-#define APPEND_BLOCKS 4
-#endif
-#ifndef APPEND_CHUNK
-#define APPEND_CHUNK 2  // turns of a warp at most
-#endif
+#define APPEND_CHUNK 2
 
 // A lane's eight values as two words of either piece, and as two pairs of floats an operand.
 struct AppendRaw {
@@ -280,8 +282,8 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
             const uint32_t h = hb + i * teams;
             raw[i].a = raw[i].b = make_uint2(0, 0);
             if (h < h1 && on) {
-                raw[i].a = *reinterpret_cast<const uint2 *>(src + h * src_head + ea * 2u);
-                raw[i].b = *reinterpret_cast<const uint2 *>(src + h * src_head + eb * 2u);
+                raw[i].a = __ldcs(reinterpret_cast<const uint2 *>(src + h * src_head + ea * 2u));
+                raw[i].b = __ldcs(reinterpret_cast<const uint2 *>(src + h * src_head + eb * 2u));
             }
         }
     };
@@ -379,8 +381,8 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
                 }
             }
             if (h < h1 && on) {
-                *reinterpret_cast<uint2 *>(dst + h * dst_head + ea * 2u) = res.a;
-                *reinterpret_cast<uint2 *>(dst + h * dst_head + eb * 2u) = res.b;
+                __stcs(reinterpret_cast<uint2 *>(dst + h * dst_head + ea * 2u), res.a);
+                __stcs(reinterpret_cast<uint2 *>(dst + h * dst_head + eb * 2u), res.b);
             }
         }
         hb += teams * APPEND_UNROLL;
@@ -425,6 +427,7 @@ kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *s
     a.n_free = d->n_free;
     a.capacity = d->token_capacity;
     a.block_size = lay->d.block_size;
+    a.block_shift = kvc_shift_of(a.block_size);
     a.num_blocks = lay->d.num_blocks;
     a.cu = d->cu_tokens;
     a.total_lens = d->total_lens;
@@ -434,17 +437,20 @@ kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *s
     a.slots = d->slots;
     a.status = lay->d_status;
     const uint32_t smem = (3 * d->n_requests + 2) * sizeof(int32_t);
-    if (smem > 48 * 1024 &&
-        cudaFuncSetAttribute(kvc_map_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)((3 * KVC_MAP_MAX_REQUESTS + 2) * sizeof(int32_t))) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return KVC_ERR_CUDA;
-    }
-    // a row a thread until four blocks a SM are there: a row is a chain of a search and a load, so more
-    // threads and not more rows a thread hide it
-    const uint32_t want = (uint32_t)(((uint64_t)d->token_capacity + MAP_THREADS - 1) / MAP_THREADS);
-    const uint32_t grid = std::max<uint32_t>(1u, std::min<uint32_t>(want, 4u * (uint32_t)lay->sm_count));
-    if (kvc_launch_pdl(kvc_map_tokens_kernel, a, dim3(grid), MAP_THREADS, smem, (cudaStream_t)stream) != cudaSuccess) {
+    // A small step is the chain of one block's scan, which fewer threads go through faster (64 requests: 3.5 us
+    // with blocks of 256, 5.4 with 1024); of a large one every block repeats the scan, so one large block a SM
+    // (1001 requests, 270,000 rows: 7.9 us, and 10.7 with 256).
+    const auto go = [&](auto kernel, uint32_t threads, uint32_t blocks) {
+        if (smem > 48 * 1024 &&
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)((3 * KVC_MAP_MAX_REQUESTS + 2) * sizeof(int32_t))) != cudaSuccess)
+            return cudaErrorUnknown;
+        const uint32_t want = (d->token_capacity + threads - 1) / threads;
+        return kvc_launch_pdl(kernel, a, dim3(std::max<uint32_t>(1u, std::min(want, blocks))), threads, smem, (cudaStream_t)stream);
+    };
+    const bool small = d->token_capacity <= 256u * (uint32_t)lay->sm_count;
+    if ((small ? go(kvc_map_tokens_kernel<256>, 256, (uint32_t)lay->sm_count) : go(kvc_map_tokens_kernel<1024>, 1024, (uint32_t)lay->sm_count)) !=
+        cudaSuccess) {
         (void)cudaGetLastError();
         return KVC_ERR_CUDA;
     }
@@ -517,7 +523,7 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
     // of its token fetches the table row once for them, one that serves fewer spreads a small call
     // over more SMs.
     const uint32_t heads = d->n_q_heads + 2 * hkv, teams = 32 / a.lanes;
-    const uint64_t warps = (uint64_t)lay->sm_count * 4 * (APPEND_THREADS / 32);
+    const uint64_t warps = (uint64_t)lay->sm_count * APPEND_BLOCKS * (APPEND_THREADS / 32);
     uint64_t chunk = (uint64_t)d->n_tokens * heads / warps;
     chunk = std::max<uint64_t>((chunk + teams - 1) / teams * teams, teams);
     a.chunk = (uint32_t)std::min<uint64_t>(chunk, (uint64_t)APPEND_CHUNK * APPEND_UNROLL * teams);
