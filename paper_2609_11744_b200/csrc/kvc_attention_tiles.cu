@@ -191,6 +191,12 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+__device__ __forceinline__ void release_tmem(uint32_t tmem)
+{
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS));
+}
+
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
@@ -401,14 +407,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     __shared__ uint32_t s_dead, s_tmem;
     __shared__ Segment segments[SEGMENTS];
     __shared__ float row_top[2][2][128], row_sum[2][2][128];  // [row tile][half][row]
-    kvc_pdl_begin(a.beside);
-
-    const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
-    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, LEAST, THREADS>(a, n_seq);
-    if (!run.any) {
-        kvc_pdl_end(a.beside);
-        return;
-    }
+    // What touches no memory of the caller's comes before the wait for the stream's previous kernel.
     const uint32_t warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31u;
     const uint32_t tiles = (smem_addr(smem_raw) + 1023u) & ~1023u;
     unsigned char *tiles_ptr = smem_raw + (tiles - smem_addr(smem_raw));
@@ -432,12 +431,25 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         }
         bar_init(smem_addr(&bars.drained), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (args.boxes) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&args.k_map) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&args.v_map) : "memory");
+        }
     }
     if (warp == 16)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(COLS) : "memory");
     fence_before();
-    __syncthreads();
+    kvc_pdl_begin(a.beside);
+
+    const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
+    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, LEAST, THREADS>(a, n_seq);  // (has block-wide barriers)
     fence_after();
+    if (!run.any) {
+        if (warp == 16)
+            release_tmem(uniform(s_tmem));
+        kvc_pdl_end(a.beside);
+        return;
+    }
     const uint32_t tmem = uniform(s_tmem);
 
     if (warp < 16) {
@@ -848,8 +860,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     __syncthreads();
     if (warp == 16) {
         fence_after();
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS));
+        release_tmem(tmem);
     }
     kvc_pdl_end(a.beside);
 }
