@@ -358,8 +358,10 @@ kvc_status kvc_layout_kernel_time(kvc_layout *layout, uint32_t *launches, double
  *     length is clamped to what its buffers hold, an entry that names no block of the pool is
  *     skipped and counted (kvc_poll_device_status: n_skipped, once per place that met it);
  *   - calls enqueue kernels on `stream` only and allocate nothing after the handle's first launch, so
- *     they can be captured into a CUDA graph (not as the handle's first call);
- *   - results are the same bits every time: no sum depends on the order in which blocks run.
+ *     they can be captured into a CUDA graph, after one call of the same kind outside a capture;
+ *   - results are the same bits every time: no sum depends on the order in which blocks run;
+ *   - the first pack or unpack through the same handle after one of these calls waits for it even
+ *     with pdl = 3 (kvc_tuning); a copy through another handle with pdl = 3 does not.
  * A descriptor's `reserved` must be 0. */
 
 typedef enum { KVC_DTYPE_BF16 = 0, KVC_DTYPE_FP16 = 1 } kvc_dtype;

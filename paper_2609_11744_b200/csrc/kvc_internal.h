@@ -131,6 +131,8 @@ struct kvc_layout {
     cudaStream_t upload_stream;  // entry tables travel on their own stream
     cudaEvent_t upload_done;
     uint64_t launches;
+    bool after_step;  // a step's kernel (tokens, attention) was launched since the last copy: it lets later
+                      // kernels in early, so a copy that would not wait (pdl = 3) waits for this one
     std::vector<uint32_t> seen;  // scratch for duplicate detection: stamp per pool block
     uint32_t seen_stamp;
     // kernel timing (diagnostic): event pairs around launches not yet collected, and spare events

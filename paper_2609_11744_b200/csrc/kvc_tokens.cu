@@ -455,6 +455,7 @@ kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *s
         return KVC_ERR_CUDA;
     }
     ++lay->launches;
+    lay->after_step = true;
     return KVC_OK;
 }
 
@@ -551,6 +552,7 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
         return KVC_ERR_CUDA;
     }
     ++lay->launches;
+    lay->after_step = true;
     return KVC_OK;
 }
 

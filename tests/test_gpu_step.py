@@ -561,3 +561,23 @@ def test_lengths_that_contradict_one_another_stay_inside_the_buffers():
         b.lse.fill_(7.0)
         kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, space, lse=b.lse, max_q_len=40)
         b.check()
+
+
+def test_a_copy_that_does_not_wait_for_copies_waits_for_a_step():
+    """pdl = 3: chunks packed right behind kvc_append hold what it wrote."""
+    hkv, d, block, nb = 8, 128, 16, 512
+    pool = torch.zeros(1, 2, nb, block, hkv, d, dtype=BF16, device="cuda")
+    lay = make_layout(pool, block)
+    kvc.kvc_layout_set_tuning(lay, pdl=3)
+    t = nb * block
+    slots = torch.arange(t).cuda()
+    ids = torch.arange(nb, dtype=torch.int32).cuda()
+    chunks = torch.empty(nb // 64, kvc.kvc_layout_chunk_bytes(lay, 64), dtype=torch.uint8, device="cuda")
+    x = [torch.full((t, hkv, d), float(i + 1), dtype=BF16, device="cuda") for i in range(2)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        kvc.kvc_append(lay, 0, None, x[i % 2], x[i % 2], None, slots, None, None)
+        for c in range(nb // 64):
+            kvc.kvc_pack(lay, ids[c * 64: (c + 1) * 64], chunks[c])
+        torch.cuda.synchronize()
+        assert (chunks.view(BF16) == float(i % 2 + 1)).all()
