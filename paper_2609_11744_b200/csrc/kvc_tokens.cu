@@ -227,7 +227,7 @@ struct AppendArgs {
     int64_t cs_stride;  // floats
     const void *weight[2];
     float eps;
-    uint32_t n_tokens, heads[2], d, rot, max_pos, block_size, num_blocks;  // heads: queries; keys and values
+    uint32_t n_tokens, heads[2], d, rot, max_pos, block_size, block_shift, num_blocks;  // heads: queries; keys and values
     uint32_t lanes;        // lanes per head: a power of two >= d / 8
     uint32_t chunk;        // heads per warp unit
     uint32_t q_chunks, kv_chunks;  // units per token
@@ -237,7 +237,7 @@ struct AppendArgs {
 #define APPEND_THREADS 64u
 // Small blocks, 16 a SM: a block's warps go through the same chain (slot, angles, heads) at the same time, and
 // small ones start and end more evenly (16384 tokens of 64 + 16 heads: 153 us with 256 threads, 141 with 128,
-// 134 with 64).  Four heads a team and turn, two turns: with one turn the angles are fetched too often, with more
+// 132 with 64).  Four heads a team and turn, two turns: with one turn the angles are fetched too often, with more
 // or wider ones too few warps fit (155 to 260 us).
 #define APPEND_BLOCKS 16
 #define APPEND_UNROLL 4
@@ -259,11 +259,11 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
     // first elements of the lane's two pieces of four
     const uint32_t ea = !NEIGHBOURS && turned ? 4u * l : 8u * l, eb = !NEIGHBOURS && turned ? a.rot / 2 + 4u * l : 8u * l + 4u;
     const uint32_t per_token = a.q_chunks + 2 * a.kv_chunks;
-    const uint64_t u = (uint64_t)blockIdx.x * (APPEND_THREADS / 32u) + (threadIdx.x >> 5);
-    const uint32_t tok = (uint32_t)(u / per_token);
+    const uint32_t u = blockIdx.x * (APPEND_THREADS / 32u) + (threadIdx.x >> 5);  // (two warps in 2^31 blocks)
+    const uint32_t tok = u / per_token;
     if (tok >= a.n_tokens)
         return;
-    uint32_t part = (uint32_t)(u - (uint64_t)tok * per_token), kind = 0;
+    uint32_t part = u - tok * per_token, kind = 0;
     if (part >= a.q_chunks) {
         part -= a.q_chunks;
         kind = 1;
@@ -293,9 +293,9 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
     if (slot < 0)
         return;  // a row without a token
     const int32_t pos = a.rot ? a.positions[tok] : 0;
-    const uint64_t id = (uint64_t)slot < (1ull << 32) ? (uint32_t)slot / a.block_size : (uint64_t)slot / a.block_size;
+    const uint64_t id = (uint64_t)slot < (1ull << 32) ? kvc_div((uint32_t)slot, a.block_size, a.block_shift) : (uint64_t)slot / a.block_size;
     if (id >= a.num_blocks || (a.rot && (uint32_t)pos >= a.max_pos)) {
-        if (lane == 0 && u == (uint64_t)tok * per_token)
+        if (lane == 0 && u == tok * per_token)
             atomicAdd(a.status, 1u);
         return;
     }
@@ -515,6 +515,7 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
     a.rot = d->rot_dim;
     a.max_pos = d->max_positions;
     a.block_size = lay->d.block_size;
+    a.block_shift = kvc_shift_of(a.block_size);
     a.num_blocks = lay->d.num_blocks;
     a.status = lay->d_status;
     a.lanes = 1;
