@@ -282,7 +282,7 @@ __device__ __forceinline__ KvcRun kvc_find_run(const KvcAttn &a, uint32_t n_seq)
     __shared__ unsigned long long sums[THREADS / 32][2];
     __shared__ KvcRun found;
     // A sequence to a thread; or, where there are few sequences of many row tiles, one to a warp whose
-    // lanes take its row tiles in turn (one 8192-token prompt: 24 us for one thread, 2 us for a warp).
+    // lanes take its row tiles in turn (one 8192-token prompt: 24 us for one thread, 4 us for a warp).
     const uint32_t lane = threadIdx.x & 31u, w = threadIdx.x >> 5;
     const bool wide = n_seq <= 4u * (THREADS / 32) && (uint64_t)a.n_tokens * a.g >= 4ull * ROWS * n_seq;
     const uint32_t owners = wide ? THREADS / 32 : THREADS, owner = wide ? w : threadIdx.x;

@@ -17,9 +17,13 @@
 //   warp 19         one thread walks the run's pairs and hands them to the others
 // Two row tiles share each K and V tile, and while one is in its softmax the other's products run.  A pair
 // of 128 rows or fewer has one row tile; its scores then alternate between the two score buffers, so that
-// those of the next tile are made while this one is in its softmax (measured on 32 one-token questions
-// about a 32,000-token document: 2.9 us a tile without, 1.6 us with).
-// Bound by the exponentials and the matrix unit alike: 128 x 128 scores take 1024 cycles on each.
+// those of the next tile are made while this one is in its softmax (16 requests of up to 5 drafted tokens
+// behind 16,000, 64 and 8 heads of 128: 243 us with one buffer, 208 us with two).
+// Bound by the exponentials and the matrix unit alike: 128 x 128 scores take 1024 cycles on each.  Measured:
+// an 8192-token prompt (32 and 8 heads of 128, 550 GFLOP) in 580 us = 948 TFLOP/s, either unit busy 45 % of the
+// time; what is left is the chain scores - maximum - weights - products - next scores of either row tile.
+// Moving a part of the exponentials to the multiply-add pipe, smaller key tiles and one softmax thread a
+// row were all slower.
 // O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use: weights are then
 // at most 2^8, which neither type nor the 32-bit sums mind, and almost all tiles skip the rescaling.
 // Every wait is bounded; one that gives up makes all roles leave and is counted.
@@ -35,8 +39,8 @@ constexpr int ROWS = KVC_ATTN_TILE_ROWS;
 constexpr int TK = 128;             // keys of a K or V stage
 constexpr int HK = TK / 2;          // keys of one softmax thread
 constexpr int THREADS = 640;
-constexpr int HEAD = 3;             // what a pair costs besides its units, in units (measured: 13,000 cycles against 3,800)
-constexpr int LEAST = 3;            // units of a run at least
+constexpr int HEAD = 3;             // what a pair costs besides its units, in units (8192-token prompt: 655, 604, 580, 585 us with 1 to 4)
+constexpr int LEAST = 3;            // units of a run at least (64 requests on a 1024-token prefix: 69, 66, 66 us with 2 to 4)
 constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper than the K ring
 
 template <int D>
@@ -360,8 +364,8 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
                                  "r"((uint32_t)__popc(good) * args.box_keys * (uint32_t)D * 2u) : "memory");
                 __syncwarp();
-                // a lane a box: the lanes take turns at the copy unit, but their operands are ready (measured
-                // against one lane in a loop of 16 boxes: 2 us a tile less)
+                // a lane a box: the lanes take turns at the copy unit, but their operands are ready (8192-token
+                // prompt in 16-token blocks: 580 us, and 620 with one lane in a loop of 16 boxes)
                 const uint32_t h = boxes * (D / 64) > lane ? lane / boxes : 0u, i = lane - h * boxes;
                 if (lane < boxes * (D / 64) && (good >> i & 1u))
                     box_load(tile + h * S::HALF + box_at * 128u, map, h * 64u, c.h, boxes > 1 ? 0u : (uint32_t)j0 % a.block_size, id, bar);
