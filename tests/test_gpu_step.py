@@ -581,3 +581,82 @@ def test_a_copy_that_does_not_wait_for_copies_waits_for_a_step():
             kvc.kvc_pack(lay, ids[c * 64: (c + 1) * 64], chunks[c])
         torch.cuda.synchronize()
         assert (chunks.view(BF16) == float(i % 2 + 1)).all()
+
+
+def test_a_whole_step_replayed_from_a_graph_with_other_lengths():
+    """Map, append, attention and attention over a shared prefix captured once, replayed with fewer and more tokens
+    than at capture: lengths are read when the graph runs, and rows behind the last token are left as they were."""
+    hq, hkv, d, block, nb, n, cap = 8, 2, 64, 16, 256, 3, 192
+    g = torch.Generator().manual_seed(3)
+    pool = torch.full((1, 2, nb, block, hkv, d), math.nan, dtype=BF16, device="cuda")
+    lay = make_layout(pool, block)
+    wide = 40
+    tables, free = torch.full((n, wide), -1, dtype=torch.int32, device="cuda"), torch.randperm(nb, generator=g).int().cuda()
+    ctx, new = dev([0, 0, 0]), dev([60, 3, 100])
+    cu, pos = torch.zeros(n + 1, dtype=torch.int32, device="cuda"), torch.zeros(cap, dtype=torch.int32, device="cuda")
+    slots, total = torch.zeros(cap, dtype=torch.int64, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    counts = torch.zeros(3, dtype=torch.int32, device="cuda")
+    x = torch.randn(cap, hq + 2 * hkv, d, generator=g).to(BF16).cuda()
+    q, out, again = (torch.zeros(cap, hq, d, dtype=BF16, device="cuda") for _ in range(3))
+    ws = torch.empty(kvc.kvc_attention_workspace_bytes(lay, cap, n, hq, 1), dtype=torch.uint8, device="cuda")
+    groups, prefix = dev([0, 1]), dev([48])   # the first request alone: its first blocks count as a prefix
+
+    def step():
+        kvc.kvc_map_tokens(lay, ctx, new, free, tables, cu, pos, slots, total_lens=total, counts=counts)
+        kvc.kvc_append(lay, 0, x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:], q, slots, None, None)
+        kvc.kvc_attention(lay, 0, q, out, tables, total, cu, ws, max_q_len=cap)
+        kvc.kvc_attention_shared(lay, 0, q, again, tables, total, cu, groups, prefix, ws, max_q_len=cap)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    held = [[], [], []]
+    taken = 0
+    for lens in ([60, 3, 100], [1, 0, 1], [70, 90, 2], [1, 1, 1]):
+        new.copy_(dev(lens))
+        x.copy_(torch.randn(x.shape, generator=g).to(BF16))
+        for t in (q, out, again):
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        c = cu.tolist()
+        m = c[-1]
+        for r in range(n):
+            held[r].append((x[c[r]: c[r + 1], hq: hq + hkv].cpu(), x[c[r]: c[r + 1], hq + hkv:].cpu()))
+        keys, values = ([torch.cat([a[i] for a in h]) for h in held] for i in range(2))
+        want, wl, weight, slip = ref.attention(q, keys, values, [(c[r], c[r + 1]) for r in range(n)], total.tolist(), d ** -0.5)
+        bound, _ = ref.attention_bounds(BF16, want, wl, weight, slip)
+        for got in (out, again):
+            assert ((got.double().cpu() - want).abs() <= bound)[:m].all() and (got[m:] == 7.0).all()
+        assert (q[m:] == 7.0).all() and torch.equal(q[:m], x[:m, :hq])
+        ctx.copy_(total)
+        taken = int(counts[1])
+        free.copy_(torch.roll(free, -taken))
+    assert kvc.kvc_poll_device_status(lay) == (0, 0)
+
+
+def test_calls_on_two_streams_at_once():
+    """The same handle, two streams, workspaces of their own: the bits of either alone."""
+    sets = [Batch([1900, 40, 700], [1, 1, 1], 8, 2, 128, BF16, 16, seed=31), Batch([900, 300], [200, 70], 8, 2, 128, BF16, 16, seed=32)]
+    lay = sets[0].lay
+    calls = []
+    for b, hint in zip(sets, (1, 200)):
+        ws = b.workspace()
+        calls.append(lambda s, b=b, ws=ws, hint=hint: kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, ws, lse=b.lse,
+                                                                       max_q_len=hint, stream=s))
+    alone = []
+    for b, call in zip(sets, calls):
+        call(None)
+        torch.cuda.synchronize()
+        alone.append((b.out.clone(), b.lse.clone()))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(30):
+        for s, call in zip(streams, calls):
+            call(s)
+    torch.cuda.synchronize()
+    for b, (o, l) in zip(sets, alone):
+        assert torch.equal(b.out, o) and torch.equal(b.lse, l)
+        b.check()
+    assert kvc.kvc_poll_device_status(lay) == (0, 0)
