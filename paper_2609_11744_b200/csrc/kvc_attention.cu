@@ -282,7 +282,7 @@ struct Carver {
     }
 };
 
-// The parts that the kernel for many rows (tiles) or few can leave.  With whole sequences: at most two
+// The parts that the kernel for pairs of `rows` rows can leave.  With whole sequences: at most two
 // a block.  By pair, every pair leaves its parts: run + pair is a slot of its own, since along the
 // order of units each new part has a larger run or a larger pair.
 struct Shape {
@@ -290,10 +290,10 @@ struct Shape {
     uint64_t tokens, requests, groups;
 };
 
-void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, bool tiles, uint64_t sequences, bool by_pair)
+void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, uint32_t rows, uint64_t sequences, bool by_pair)
 {
-    const uint32_t blocks = tiles ? kvc_attn_tiles_blocks(lay) : kvc_attn_rows_blocks(lay, by_pair);
-    const uint32_t rows = tiles ? KVC_ATTN_TILE_ROWS : KVC_ATTN_SMALL_ROWS, head_dim = s.head_dim;
+    const uint32_t blocks = rows == KVC_ATTN_SMALL_ROWS ? kvc_attn_rows_blocks(lay, by_pair) : kvc_attn_tiles_blocks(lay);
+    const uint32_t head_dim = s.head_dim;
     const uint64_t pairs = by_pair ? kvc_max_pairs(sequences, s.tokens, s.g, s.hkv, rows) : 0;
     const uint64_t slots = pairs ? (uint64_t)blocks + pairs : 2ull * blocks;
     memset(&p, 0, sizeof(p));
@@ -311,14 +311,14 @@ void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, bool t
     }
 }
 
-// Bytes of the parts of one phase, for either kernel that may serve it.
+// Bytes of the parts of one phase, for any kernel that may serve it.
 uint64_t phase_bytes(const kvc_layout *lay, const Shape &s, uint64_t sequences, bool pairs)
 {
     uint64_t most = 0;
-    for (const bool tiles : {false, true}) {
+    for (const uint32_t rows : {KVC_ATTN_SMALL_ROWS, KVC_ATTN_TILE_ROWS, KVC_ATTN_MANY_ROWS}) {
         KvcParts p;
         Carver c = {nullptr, 0};
-        carve(c, p, lay, s, tiles, sequences, pairs);
+        carve(c, p, lay, s, rows, sequences, pairs);
         most = std::max(most, c.used);
     }
     return most;
@@ -438,36 +438,40 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     const bool bf16 = d->dtype == KVC_DTYPE_BF16, wide = l.head_dim == 128;
     Carver c = {static_cast<unsigned char *>(d->workspace), 0};
     // Sixteen rows or fewer fit the kernel for few rows, which reads the keys once for them; with more
-    // it would read them once for every sixteen, and the matrix unit takes over.
+    // it would read them once for every sixteen, and the matrix unit takes over.  Up to 128 rows it gets one
+    // row tile and a deeper ring of keys.  (Whatever the lengths turn out to be, any of the three is right.)
     const uint64_t q_len = std::min<uint64_t>(d->max_q_len ? d->max_q_len : d->n_tokens, d->n_tokens);
-    const bool many = q_len * a.g > KVC_ATTN_SMALL_ROWS;
-    const auto launch = [&](bool tiles) {
+    const auto kernel_rows = [&](uint64_t tokens) {
+        const uint64_t rows = tokens * a.g;
+        return rows <= KVC_ATTN_SMALL_ROWS ? KVC_ATTN_SMALL_ROWS : rows <= KVC_ATTN_TILE_ROWS ? KVC_ATTN_TILE_ROWS : KVC_ATTN_MANY_ROWS;
+    };
+    const auto launch = [&]() {
         ++lay->launches;
-        return tiles ? kvc_launch_attn_tiles(a, d->dtype, l.head_dim, a.parts.blocks, st)
-                     : kvc_launch_attn_rows(a, d->dtype, l.head_dim, a.parts.blocks, st);
+        return a.parts.rows == KVC_ATTN_SMALL_ROWS ? kvc_launch_attn_rows(a, d->dtype, l.head_dim, a.parts.blocks, st)
+                                                   : kvc_launch_attn_tiles(a, d->dtype, l.head_dim, a.parts.blocks, st);
     };
     cudaError_t e;
     if (!shared) {
         a.phase = KVC_PHASE_WHOLE;
-        carve(c, a.parts, lay, shape, many, d->n_requests, false);
-        e = launch(many);
+        carve(c, a.parts, lay, shape, kernel_rows(q_len), d->n_requests, false);
+        e = launch();
         if (e == cudaSuccess)
             e = bf16 ? (wide ? join_split<__nv_bfloat16, 128>(a, st) : join_split<__nv_bfloat16, 64>(a, st))
                      : (wide ? join_split<__half, 128>(a, st) : join_split<__half, 64>(a, st));
     } else {
         JoinShared j;
         // a group has at least as many rows as a request, and usually several requests
-        const bool many_prefix = std::max<uint64_t>(q_len, (d->n_tokens + d->n_groups - 1) / d->n_groups) * a.g > KVC_ATTN_SMALL_ROWS;
+        const uint64_t group_len = std::max<uint64_t>(q_len, (d->n_tokens + d->n_groups - 1) / d->n_groups);
         a.phase = KVC_PHASE_PREFIX;
-        carve(c, a.parts, lay, shape, many_prefix, d->n_groups, true);
+        carve(c, a.parts, lay, shape, kernel_rows(group_len), d->n_groups, true);
         j.prefix = a.parts;
-        e = launch(many_prefix);
+        e = launch();
         a.phase = KVC_PHASE_SUFFIX;
         a.beside = 1;  // the two phases share nothing but what they read
-        carve(c, a.parts, lay, shape, many, d->n_requests, true);
+        carve(c, a.parts, lay, shape, kernel_rows(q_len), d->n_requests, true);
         j.suffix = a.parts;
         if (e == cudaSuccess)
-            e = launch(many);
+            e = launch();
         j.a = a;
         if (e == cudaSuccess)
             e = bf16 ? (wide ? join_shared<__nv_bfloat16, 128>(j, st) : join_shared<__nv_bfloat16, 64>(j, st))

@@ -24,7 +24,8 @@
 #include "kvc_internal.h"
 
 #define KVC_ATTN_SMALL_ROWS 16u   // rows of a pair in the kernel for few rows
-#define KVC_ATTN_TILE_ROWS 256u   // and in the kernel for many
+#define KVC_ATTN_TILE_ROWS 128u   // and in the kernel for many, with one row tile
+#define KVC_ATTN_MANY_ROWS 256u   // or two
 
 enum {
     KVC_PHASE_WHOLE = 0,   // sequences are requests, all of their keys

@@ -1,5 +1,5 @@
 // Attention over the paged pool for many query rows (prompts, and the shared prefix of a group): tiles
-// of 256 rows against tiles of 128 keys on the fifth-generation tensor cores.
+// of 256 or 128 rows against tiles of 128 keys on the fifth-generation tensor cores.
 //
 // Per row: s_j = scale * q . k_j, o = sum_j 2^(s_j' - m) v_j / sum_j 2^(s_j' - m), s' in base 2; one pass
 // with the running maximum and sum of a softmax in 32 bits.
@@ -35,7 +35,6 @@
 
 namespace {
 
-constexpr int ROWS = KVC_ATTN_TILE_ROWS;
 constexpr int TK = 128;             // keys of a K or V stage
 constexpr int HK = TK / 2;          // keys of one softmax thread
 constexpr int THREADS = 640;
@@ -43,12 +42,15 @@ constexpr int HEAD = 3;             // what a pair costs besides its units, in u
 constexpr int LEAST = 3;            // units of a run at least (64 requests on a 1024-token prefix: 69, 66, 66 us with 2 to 4)
 constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper than the K ring
 
-template <int D>
+// ROWS is 256, two row tiles a block, or 128, one: half the queries then make room for a third K stage
+// (16 requests of up to 5 drafted tokens behind 16,000: 208 us with 256, 200 us with 128; 32 questions on a
+// 32,000-token document 70 and 68 us).
+template <int D, int ROWS>
 struct Shape {
-    static constexpr int TILE = TK * D * 2;           // a K or V tile; also half of the queries
+    static constexpr int TILE = TK * D * 2;           // a K or V tile; also the queries of a row tile
     static constexpr int HALF = TK * 128;             // 64 elements (128 bytes) of 128 rows
-    static constexpr int KS = D == 128 ? 2 : 4, VS = KS;
-    static constexpr int Q = 0, K = 2 * TILE, V = K + KS * TILE, END = V + VS * TILE;
+    static constexpr int KS = D == 64 ? 4 : ROWS == 128 ? 3 : 2, VS = D == 64 ? 4 : 2;
+    static constexpr int Q = 0, K = ROWS / 128 * TILE, V = K + KS * TILE, END = V + VS * TILE;
     static constexpr int SMEM = END + 1024;           // room to align the stages to the swizzle's 1024 bytes
 };
 
@@ -285,11 +287,11 @@ __device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap *map, u
 // and tiles divide one another; a box's block id is looked up a tile ahead.  What is not a key's may be
 // garbage in K, whose scores are replaced; in V it meets a weight of zero, which infinity or NaN would
 // survive, so a tile of V that is not all keys is copied key by key, with zeros between.
-template <int D, bool KEYS>
+template <int D, int ROWS, bool KEYS>
 __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *segments, uint32_t tiles, Bars *bars,
                                           uint32_t (*there)[4], volatile uint32_t *dead, uint32_t lane)
 {
-    using S = Shape<D>;
+    using S = Shape<D, ROWS>;
     constexpr int STAGES = KEYS ? S::KS : S::VS;
     constexpr int PER = 512 / (D * 2);  // keys per round of 32 lanes
     constexpr uint32_t NONE = ~0u;
@@ -400,10 +402,10 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
             ;
 }
 
-template <typename T, int D>
+template <typename T, int D, int ROWS>
 __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid_constant__ TilesArgs args)
 {
-    using S = Shape<D>;
+    using S = Shape<D, ROWS>;
     const KvcAttn &a = args.a;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Bars bars;
@@ -476,7 +478,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         // of the segment before have been seen, so their operand may go.
         const auto load_queries = [&](const Segment &c) {
             const uint32_t row0 = c.rt * ROWS + sub * 128u, rows_all = (uint32_t)c.q.rows;
-            if (row0 >= rows_all)
+            if (row0 >= rows_all || (ROWS == 128 && sub == 1))
                 return;
             constexpr uint32_t STEP = 256u / (D / 8), TURNS = 128u / STEP;
             const uint32_t at = threadIdx.x & 255u, chunk = at % (D / 8), r0 = at / (D / 8);
@@ -587,8 +589,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 break;
             c = d;
             row0 = c.rt * ROWS + sub * 128u;
-            open = row0 < (uint32_t)c.q.rows;
-            const bool two = (uint32_t)c.q.rows - c.rt * ROWS > 128u;
+            open = row0 < (uint32_t)c.q.rows && (ROWS == 256 || sub == 0);
+            const bool two = ROWS == 256 && (uint32_t)c.q.rows - c.rt * ROWS > 128u;
             if (open) {
                 const int32_t pos = row0 + tid < (uint32_t)c.q.rows ? kvc_row_pos(a, c.q, row0 + tid) : -1;
                 const int32_t old = a.window ? pos - a.window : -1;  // the last key behind the row's window
@@ -710,9 +712,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 17) {
-            load_role<D, true>(args, segments, tiles + S::K, &bars, there, dead, lane);
+            load_role<D, ROWS, true>(args, segments, tiles + S::K, &bars, there, dead, lane);
         } else if (warp == 18) {
-            load_role<D, false>(args, segments, tiles + S::V, &bars, there, dead, lane);
+            load_role<D, ROWS, false>(args, segments, tiles + S::V, &bars, there, dead, lane);
         } else if (warp == 16) {
             // ------------------------------------------------------------ matrix instructions
             // The unit takes few instructions ahead, so what this thread does between them is time that
@@ -761,7 +763,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 p_parity ^= 1u << buf;
             };
             while (reader.next(segments, &bars, c, dead, a.status)) {
-                const bool two = uniform((uint32_t)c.q.rows - c.rt * ROWS > 128u);
+                const bool two = ROWS == 256 && uniform((uint32_t)c.q.rows - c.rt * ROWS > 128u);
                 const uint32_t n = uniform(c.n);
                 if (!wait(BAR(k_full) + k.stage * 8u, k.parity) || !wait(BAR(q_full), q_parity) ||
                     (two && !wait(BAR(q_full) + 8u, q_parity >> 1)))
@@ -898,14 +900,20 @@ bool encode(EncodeTiled fn, CUtensorMap *map, const KvcAttn &a, const unsigned c
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int D>
+template <typename T, int D, int ROWS>
 cudaError_t launch(const TilesArgs &args, uint32_t blocks, cudaStream_t st)
 {
-    const cudaError_t e = cudaFuncSetAttribute(kvc_attn_tiles_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               Shape<D>::SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(kvc_attn_tiles_kernel<T, D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               Shape<D, ROWS>::SMEM);
     if (e != cudaSuccess)
         return e;
-    return kvc_launch_pdl(kvc_attn_tiles_kernel<T, D>, args, dim3(blocks), THREADS, Shape<D>::SMEM, st);
+    return kvc_launch_pdl(kvc_attn_tiles_kernel<T, D, ROWS>, args, dim3(blocks), THREADS, Shape<D, ROWS>::SMEM, st);
+}
+
+template <typename T, int D>
+cudaError_t launch_rows(const TilesArgs &args, uint32_t blocks, cudaStream_t st)
+{
+    return args.a.parts.rows == 128 ? launch<T, D, 128>(args, blocks, st) : launch<T, D, 256>(args, blocks, st);
 }
 
 }  // namespace
@@ -931,6 +939,6 @@ cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t hea
             args.boxes = 0;  // a pool that no map describes
     }
     if (dtype == KVC_DTYPE_BF16)
-        return head_dim == 128 ? launch<__nv_bfloat16, 128>(args, blocks, st) : launch<__nv_bfloat16, 64>(args, blocks, st);
-    return head_dim == 128 ? launch<__half, 128>(args, blocks, st) : launch<__half, 64>(args, blocks, st);
+        return head_dim == 128 ? launch_rows<__nv_bfloat16, 128>(args, blocks, st) : launch_rows<__nv_bfloat16, 64>(args, blocks, st);
+    return head_dim == 128 ? launch_rows<__half, 128>(args, blocks, st) : launch_rows<__half, 64>(args, blocks, st);
 }
