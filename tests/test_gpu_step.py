@@ -660,3 +660,33 @@ def test_calls_on_two_streams_at_once():
         assert torch.equal(b.out, o) and torch.equal(b.lse, l)
         b.check()
     assert kvc.kvc_poll_device_status(lay) == (0, 0)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 70])
+@pytest.mark.parametrize("window,sinks", [(100, 0), (129, 5), (33, 64)])
+def test_attention_does_not_read_what_no_window_reaches(rows, window, sinks):
+    """Keys and values behind every window and all sinks are gone: their slots hold NaN, and the blocks that
+    held nothing else have no entry in the table."""
+    for hq, hkv, d in ((8, 1, 128), (12, 4, 64)):
+        b = Batch([700], [rows], hq, hkv, d, BF16 if d == 128 else FP16, 16, seed=window)
+        first = 700 - rows + 1 - window       # the first key that some window reaches
+        for j in range(sinks, first):
+            for plane in b.planes[2:]:
+                plane[b.tables_np[0, j // 16], j % 16] = math.nan
+        for block in range(-(-sinks // 16), first // 16):
+            b.tables[0, block] = -1
+        kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, b.workspace(), window=window, sinks=sinks, lse=b.lse,
+                          max_q_len=rows)
+        b.check(window, sinks)
+
+
+@pytest.mark.parametrize("rows", [[1, 1, 1], [30, 1, 70]])
+def test_attention_shared_reads_the_prefix_through_the_first_request_only(rows):
+    """The other requests' table entries for the shared blocks may be missing."""
+    for hq, hkv, d in ((8, 2, 128), (12, 1, 64)):
+        prefix = 176
+        b = Batch([300, 290, 280], rows, hq, hkv, d, BF16, 16, seed=3, share=[(0, prefix)] * 3)
+        b.tables[1:, : prefix // 16] = -1
+        kvc.kvc_attention_shared(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, dev([0, 3]), dev([prefix]), b.workspace(1), lse=b.lse,
+                                 max_q_len=max(rows))
+        b.check()
