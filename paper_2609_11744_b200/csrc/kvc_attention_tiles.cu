@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     __shared__ __align__(16) uint32_t there[THERE][4];
     __shared__ uint32_t s_dead, s_tmem;
     __shared__ Segment segments[SEGMENTS];
-    __shared__ float row_top[2][2][128], row_sum[2][2][128];  // [row tile][half][row]
+    __shared__ float row_top[2][2][2][128], row_sum[2][2][128];  // ([tile of keys, odd or even])[row tile][half][row]
     // What touches no memory of the caller's comes before the wait for the stream's previous kernel.
     const uint32_t warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31u;
     const uint32_t tiles = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -630,11 +630,13 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                         for (int e = 0; e < 4; ++e)
                             t[e] = fmaxf(t[e], fmaxf(s[k + e], s[k + 4 + e]));
                     float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-                    // the row's other half.  After this both halves of S have been read, so P may go over them; and
-                    // the next scores come only after both halves' weights, so no value is overwritten unread
-                    row_top[sub][half][tid] = top;
+                    // the row's other half.  After this both halves of S have been read, so P may go over them.
+                    // Odd and even tiles have words of their own: with one row tile the scores of tile i + 1 do not
+                    // wait for the weights of tile i, so a warp may be here again before its partner has read.  Those
+                    // of tile i + 2 do wait for both halves' weights of tile i, and those are made after the reading
+                    row_top[i & 1u][sub][half][tid] = top;
                     meet();
-                    top = fmaxf(top, row_top[sub][half ^ 1u][tid]) * a.scale_log2;
+                    top = fmaxf(top, row_top[i & 1u][sub][half ^ 1u][tid]) * a.scale_log2;
                     if (i == 0) {
                         m = top;
                     } else {
