@@ -466,11 +466,18 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         const uint32_t lanes = (warp & 3u) << 21;  // this warp's 32 rows of tensor memory
         const uint32_t s_col = tmem + COL_S + lanes, o_col = tmem + COL_O + sub * 128u + half * (D / 2) + lanes;
         const uint32_t bar = smem_addr(&bars);
-        // The two warps of the same rows meet here.  One that leaves early, because a wait gave up, arrives
-        // once more for its partner, which can come here once at most before it finds the same: the next scores
-        // need the weights of both, and the end of a segment looks at `dead` first.
+        // The two warps of the same rows meet here: true where one of them is leaving.  A warp that leaves, at its end
+        // or because a wait gave up, meets its partner once more and says so; the partner, wherever it comes to meet,
+        // then leaves without another meeting.  So every meeting has two sides, and no warp waits for one that
+        // is gone, however far apart the two are when a wait gives up.
         const uint32_t meeting = 1u + sub * 4u + (warp & 3u);
-        const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(meeting) : "memory"); };
+        const auto meet = [&](bool leaving) {
+            uint32_t gone;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbar.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                         : "=r"(gone) : "r"(meeting), "r"((uint32_t)leaving) : "memory");
+            return gone != 0;
+        };
+        bool parted = false;  // the partner has left
         SegmentReader reader;
         Segment c, d;
         uint32_t s_parity = 0, o_parity = 0, slot = 0;  // parities: a bit for each barrier of a pair
@@ -524,7 +531,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             if (open) {
                 const bool from_start = c.t == 0, to_end = c.t + c.n == c.r.n, real = row0 + tid < (uint32_t)c.q.rows;
                 row_sum[sub][half][tid] = l;
-                meet();
+                if ((parted = meet(false)))
+                    break;
                 l = row_sum[sub][0][tid] + row_sum[sub][1][tid];
                 if (!__all_sync(~0u, bar_wait(bar + BAR(o_done) + last * 8u, o_parity >> last & 1u ^ 1u, dead, a.status))) {
                     ok = false;
@@ -635,7 +643,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     // wait for the weights of tile i, so a warp may be here again before its partner has read.  Those
                     // of tile i + 2 do wait for both halves' weights of tile i, and those are made after the reading
                     row_top[i & 1u][sub][half][tid] = top;
-                    meet();
+                    if ((parted = meet(false))) {
+                        ok = false;
+                        break;
+                    }
                     top = fmaxf(top, row_top[i & 1u][sub][half ^ 1u][tid]) * a.scale_log2;
                     if (i == 0) {
                         m = top;
@@ -709,8 +720,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             }
             slot = (slot + c.n) % THERE;
         }
-        if (__any_sync(~0u, *dead))
-            asm volatile("bar.arrive %0, 64;" ::"r"(meeting) : "memory");
+        if (!parted)
+            meet(true);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 17) {

@@ -1,0 +1,121 @@
+"""The order of events around one row group of the attention tiles, as a model run under random schedules.
+
+Two softmax warps hold the two halves of a row's keys; a third actor makes scores and products.  The model has the
+rules that the kernel keeps: whose words are written when, what waits for what, and how a warp leaves.  Under them
+no schedule may read a word that is not its tile's, or leave a warp waiting; without any one of them some schedule does."""
+import random
+
+import pytest
+
+
+def run(seed, tiles, buffers, words, farewell, give_up=None):
+    """Errors of one random schedule.  buffers: score buffers of the row tile (scores run that many tiles ahead); words:
+    sets of words that maxima are exchanged through; farewell: a leaving warp meets its partner and says so, else it
+    only arrives once where a wait gave up; give_up = (half, tile): the wait that gives up."""
+    rng = random.Random(seed)
+    scores, weights, products = set(), set(), set()
+    top, errors, dead = {}, set(), [False]
+    meeting = dict(sides=[], turn=0, gone={})
+
+    def side(leaving):
+        turn = meeting["turn"]
+        meeting["sides"].append(leaving)
+        if len(meeting["sides"]) == 2:
+            meeting["gone"][turn] = any(meeting["sides"])
+            meeting["sides"], meeting["turn"] = [], turn + 1
+        return turn
+
+    def meet(leaving=False):
+        turn = side(leaving)
+        while meeting["turn"] == turn:
+            yield "wait"
+        return farewell and meeting["gone"][turn]
+
+    def softmax(half):
+        parted, ok = False, True
+        for i in range(tiles):
+            if give_up == (half, i):
+                dead[0] = True
+            while i not in scores and not dead[0]:
+                yield "wait"
+            if i not in scores or give_up == (half, i):
+                ok = False
+                break
+            yield
+            top[i % words, half] = i
+            yield
+            parted = yield from meet()
+            if parted:
+                ok = False
+                break
+            yield
+            if top.get((i % words, half ^ 1)) != i and not dead[0]:
+                errors.add("maximum of another tile")
+            for _ in range(rng.randint(1, 4)):
+                yield
+            weights.add((i, half))
+        if ok:
+            parted = yield from meet()   # the sums of the segment
+        if farewell:
+            if not parted:
+                yield from meet(True)
+        elif dead[0]:
+            side(True)
+
+    def matrix():
+        for i in range(min(buffers, tiles)):
+            yield
+            scores.add(i)
+        for i in range(tiles):
+            for half in (0, 1):
+                while (i, half) not in weights:
+                    if dead[0]:
+                        return
+                    yield "wait"
+                yield
+            products.add(i)
+            if i + buffers < tiles:
+                yield
+                scores.add(i + buffers)
+
+    actors = [softmax(0), softmax(1), matrix()]
+    rng.shuffle(actors)
+    idle = 0
+    while actors and idle < 300:
+        k = rng.randrange(len(actors)) if rng.random() < 0.5 else 0   # one actor is favoured
+        try:
+            idle = idle + 1 if next(actors[k]) == "wait" else 0
+        except StopIteration:
+            del actors[k]
+            idle = 0
+    if actors:
+        errors.add("a warp waits for ever")
+    return errors
+
+
+def over_schedules(n, **kw):
+    found = set()
+    for seed in range(n):
+        found |= run(seed, 6, **kw)
+    return found
+
+
+@pytest.mark.parametrize("buffers", [1, 2])
+def test_no_schedule_goes_wrong(buffers):
+    assert over_schedules(1500, buffers=buffers, words=2, farewell=True) == set()
+    for half in (0, 1):
+        for at in range(6):
+            assert over_schedules(150, buffers=buffers, words=2, farewell=True, give_up=(half, at)) == set()
+
+
+def test_one_set_of_words_does_for_one_score_buffer_only():
+    assert over_schedules(1500, buffers=1, words=1, farewell=True) == set()
+    assert over_schedules(1500, buffers=2, words=1, farewell=True) == {"maximum of another tile"}
+
+
+def test_a_single_arrival_does_not_release_the_partner_of_a_warp_that_gives_up():
+    found = set()
+    for half in (0, 1):
+        for at in range(6):
+            found |= over_schedules(150, buffers=2, words=2, farewell=False, give_up=(half, at))
+    assert found == {"a warp waits for ever"}
