@@ -674,6 +674,16 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                                     o[k] *= f;
                                 tmem_st32(o_col + q, o);
                             }
+                            // Each half has rescaled its columns of O, and the products of either half's weights add to
+                            // all of them: no weights are released before both halves have got here (they take this
+                            // branch together, having the same rows, maxima and thus votes)
+                            tmem_wait_st();
+                            fence_before();
+                            if ((parted = meet(false))) {
+                                ok = false;
+                                break;
+                            }
+                            fence_after();
                         }
                     }
                     const float base = m == -INFINITY ? 0.f : m;

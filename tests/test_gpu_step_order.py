@@ -36,3 +36,23 @@ def test_halves_of_a_tile_share_one_maximum(hq, hkv, d, dtype):
             first = b.out.clone(), b.lse.clone()
         assert torch.equal(first[0], b.out) and torch.equal(first[1], b.lse)
     b.check()
+
+
+@pytest.mark.parametrize("rows,d,dtype", [(30, 128, BF16), (100, 64, FP16), (120, 128, BF16)])
+def test_results_rescaled_at_every_tile_repeat(rows, d, dtype):
+    """Maxima that grow by more than 2^8 from key tile to key tile, so that both halves of a row rescale their columns
+    of the result again and again while products wait: right, and the same bits each time."""
+    n = 3000
+    b = Batch([n, 1500], [rows, rows], 4, 1, d, dtype, 16, seed=8)
+    b.q.copy_(b.q.abs())
+    for r, m in enumerate((n, 1500)):
+        grow = (torch.arange(m) // 128).float() * (7.0 if r else 9.0) / (0.8 * d ** 0.5)
+        set_keys(b, r, b.keys[r].float() * 0.1 + grow[:, None, None])
+    ws = b.workspace()
+    first = None
+    for _ in range(200):
+        kvc.kvc_attention(b.lay, 1, b.q, b.out, b.tables, b.seq, b.cu, ws, lse=b.lse, max_q_len=rows)
+        if first is None:
+            first = b.out.clone(), b.lse.clone()
+        assert torch.equal(first[0], b.out) and torch.equal(first[1], b.lse)
+    b.check()

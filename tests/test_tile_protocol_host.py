@@ -8,14 +8,16 @@ import random
 import pytest
 
 
-def run(seed, tiles, buffers, words, farewell, give_up=None):
+def run(seed, tiles, buffers, words, farewell, give_up=None, together=True):
     """Errors of one random schedule.  buffers: score buffers of the row tile (scores run that many tiles ahead); words:
     sets of words that maxima are exchanged through; farewell: a leaving warp meets its partner and says so, else it
-    only arrives once where a wait gave up; give_up = (half, tile): the wait that gives up."""
+    only arrives once where a wait gave up; give_up = (half, tile): the wait that gives up; together: the halves
+    meet again after rescaling their columns of the result, which the products of either half's weights add to."""
     rng = random.Random(seed)
     scores, weights, products = set(), set(), set()
     top, errors, dead = {}, set(), [False]
     meeting = dict(sides=[], turn=0, gone={})
+    rescaling = [False, False]
 
     def side(leaving):
         turn = meeting["turn"]
@@ -51,6 +53,21 @@ def run(seed, tiles, buffers, words, farewell, give_up=None):
             yield
             if top.get((i % words, half ^ 1)) != i and not dead[0]:
                 errors.add("maximum of another tile")
+            if i % 3:   # the maximum has moved
+                while buffers == 2 and i - 1 not in products and not dead[0]:
+                    yield "wait"
+                if buffers == 2 and i - 1 not in products:
+                    ok = False
+                    break
+                rescaling[half] = True
+                for _ in range(rng.randint(1, 6)):
+                    yield
+                rescaling[half] = False
+                if together:
+                    parted = yield from meet()
+                    if parted:
+                        ok = False
+                        break
             for _ in range(rng.randint(1, 4)):
                 yield
             weights.add((i, half))
@@ -72,7 +89,10 @@ def run(seed, tiles, buffers, words, farewell, give_up=None):
                     if dead[0]:
                         return
                     yield "wait"
-                yield
+                for _ in range(2):
+                    yield
+                    if any(rescaling):
+                        errors.add("products while columns are rescaled")
             products.add(i)
             if i + buffers < tiles:
                 yield
@@ -119,3 +139,8 @@ def test_a_single_arrival_does_not_release_the_partner_of_a_warp_that_gives_up()
         for at in range(6):
             found |= over_schedules(150, buffers=2, words=2, farewell=False, give_up=(half, at))
     assert found == {"a warp waits for ever"}
+
+
+@pytest.mark.parametrize("buffers", [1, 2])
+def test_products_meet_columns_that_are_being_rescaled_unless_the_halves_meet_again(buffers):
+    assert over_schedules(300, buffers=buffers, words=2, farewell=True, together=False) == {"products while columns are rescaled"}
