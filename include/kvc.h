@@ -166,8 +166,9 @@ typedef struct {
                             of after them.  The caller vouches for the independence: a pack right
                             after an unpack of the same blocks would read stale bytes.  Work of other
                             kinds queued earlier on the stream (copies, waits for events) is
-                            complete either way, and an event recorded after a call still covers
-                            that call and everything before it */
+                            complete either way, an event recorded after a call still covers
+                            that call and everything before it, and a later call of this library
+                            that waits for the last of them has waited for all */
     uint32_t group;      /* BULK: slabs per work item.  0 = default: when a slab is at most half a
                             tile, as many whole slabs as fit one tile (a power of two, at most 16;
                             the default tile is 16 KiB for slabs under 4 KiB)

@@ -118,13 +118,22 @@ __device__ __forceinline__ Item decode(const KvcLaunch &a, uint32_t w, bool coun
 // Without the attribute both instructions do nothing.
 // With overlap != 0 the wait is skipped: the caller has declared that this launch does not touch
 // what the previous kernel of the stream reads or writes, so its blocks may run beside that
-// kernel's last blocks (work that preceded the previous kernel has completed either way, because
-// that kernel could not start before it).
+// kernel's last blocks, and, behind a row of such launches, beside those of several (work of other
+// kinds that was queued before the row has completed: its first kernel could not start before it).
 __device__ __forceinline__ void grid_dependency_wait(uint32_t overlap = 0)
 {
     if (!overlap)
         asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// The end of a kernel.  A later kernel that waits for this one relies on the earlier ones being over too, so a
+// launch that skipped the wait makes up for it here: the grid is not complete before this one thread has
+// seen the previous grid complete, and its blocks that are done leave their SMs all the same.
+__device__ __forceinline__ void grid_dependency_end(uint32_t overlap)
+{
+    if (overlap && blockIdx.x == 0 && threadIdx.x == 0)
+        asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // ------------------------------------------------------------------------------------ VEC
@@ -222,6 +231,7 @@ kvc_vec_kernel(const __grid_constant__ KvcLaunch a)
         cur = nxt;
         w = wn;
     }
+    grid_dependency_end(a.pdl == 2u);
 }
 
 
@@ -299,6 +309,7 @@ kvc_vec_group_kernel(const __grid_constant__ KvcLaunch a)
         cur = nxt;
         w = wn;
     }
+    grid_dependency_end(a.pdl == 2u);
 }
 
 // ------------------------------------------------------------------------------------ BULK
@@ -516,6 +527,7 @@ kvc_bulk_kernel(const __grid_constant__ KvcLaunch a)
         }
         bulk_wait_all();
     }
+    grid_dependency_end(a.pdl == 2u);
 }
 
 
@@ -662,6 +674,7 @@ kvc_bulk_group_kernel(const __grid_constant__ KvcLaunch a)
             (void)mbar_wait(smem_u32(&bars[m % stages]), (m / stages) & 1u);
     }
     bulk_wait_all();
+    grid_dependency_end(a.pdl == 2u);
 }
 
 template <typename K>

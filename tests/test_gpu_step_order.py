@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2609_11744_b200 import kvc
-from test_gpu_step import BF16, FP16, Batch
+from test_gpu_step import BF16, FP16, Batch, dev, make_layout
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +56,81 @@ def test_results_rescaled_at_every_tile_repeat(rows, d, dtype):
             first = b.out.clone(), b.lse.clone()
         assert torch.equal(first[0], b.out) and torch.equal(first[1], b.lse)
     b.check()
+
+
+def copies_then_step(nb=2048, hkv=8, d=128, block=16):
+    pool = torch.zeros(1, 2, nb, block, hkv, d, dtype=BF16, device="cuda")
+    lay = make_layout(pool, block)
+    kvc.kvc_layout_set_tuning(lay, pdl=3, slot_memory=1)
+    return pool, lay, torch.arange(nb, dtype=torch.int32).cuda()
+
+
+@pytest.mark.parametrize("graphed", [False, True])
+@pytest.mark.parametrize("rows", [1, 24])
+def test_attention_behind_copies_that_do_not_wait_reads_what_all_of_them_wrote(graphed, rows):
+    """pdl = 3: a large unpack, two of a single block, then attention over the large one's blocks.  All keys are alike, so
+    the result is the value that every block holds, exactly."""
+    nb, hkv, d, block, n = 2048, 8, 128, 16, 64
+    pool, lay, ids = copies_then_step(nb, hkv, d, block)
+    big = kvc.kvc_layout_chunk_bytes(lay, nb - 2)
+    chunk = torch.empty(big, dtype=torch.uint8, device="cuda")
+    small = torch.zeros(2, kvc.kvc_layout_chunk_bytes(lay, 1), dtype=torch.uint8, device="cuda")
+    tables = torch.arange(n * 31, dtype=torch.int32).view(n, 31).cuda()
+    q = torch.ones(n * rows, hkv, d, dtype=BF16, device="cuda")
+    out = torch.empty_like(q)
+    lens, cu = dev([31 * block] * n), dev([i * rows for i in range(n + 1)])
+    ws = torch.empty(kvc.kvc_attention_workspace_bytes(lay, n * rows, n, hkv), dtype=torch.uint8, device="cuda")
+
+    def call():
+        kvc.kvc_unpack(lay, chunk, ids[: nb - 2])
+        kvc.kvc_unpack(lay, small[0], ids[nb - 2: nb - 1])
+        kvc.kvc_unpack(lay, small[1], ids[nb - 1:])
+        kvc.kvc_attention(lay, 0, q, out, tables, lens, cu, ws, max_q_len=rows)
+
+    call()
+    torch.cuda.synchronize()
+    if graphed:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+    for i in range(20):
+        chunk.view(BF16).fill_(float(i % 3 + 1))
+        torch.cuda.synchronize()
+        graph.replay() if graphed else call()
+        torch.cuda.synchronize()
+        assert (out == float(i % 3 + 1)).all(), i
+    assert kvc.kvc_poll_device_status(lay) == (0, 0)
+
+
+@pytest.mark.parametrize("graphed", [False, True])
+def test_append_behind_copies_that_do_not_wait_leaves_them_what_they_read(graphed):
+    """pdl = 3: a large pack and one of a single block, then an append into the large one's blocks."""
+    nb, hkv, d, block = 2048, 8, 128, 16
+    pool, lay, ids = copies_then_step(nb, hkv, d, block)
+    chunk = torch.empty(kvc.kvc_layout_chunk_bytes(lay, nb - 1), dtype=torch.uint8, device="cuda")
+    small = torch.empty(kvc.kvc_layout_chunk_bytes(lay, 1), dtype=torch.uint8, device="cuda")
+    t = (nb - 1) * block
+    slots = torch.arange(t).cuda()
+    x = torch.empty(t, hkv, d, dtype=BF16, device="cuda")
+
+    def call():
+        kvc.kvc_pack(lay, ids[: nb - 1], chunk)
+        kvc.kvc_pack(lay, ids[nb - 1:], small)
+        kvc.kvc_append(lay, 0, None, x, x, None, slots, None, None)
+
+    call()
+    torch.cuda.synchronize()
+    if graphed:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+    for i in range(20):
+        x.fill_(float(i + 1))
+        pool.fill_(float(i))
+        chunk.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay() if graphed else call()
+        torch.cuda.synchronize()
+        assert (chunk.view(BF16) == float(i)).all(), i
+        assert (pool.view(2, nb, -1)[:, : nb - 1] == float(i + 1)).all(), i
+    assert kvc.kvc_poll_device_status(lay) == (0, 0)
