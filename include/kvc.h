@@ -361,8 +361,9 @@ kvc_status kvc_layout_kernel_time(kvc_layout *layout, uint32_t *launches, double
  *   - calls enqueue kernels on `stream` only and allocate nothing after the handle's first launch, so
  *     they can be captured into a CUDA graph, after one call of the same kind outside a capture;
  *   - results are the same bits every time: no sum depends on the order in which blocks run;
- *   - the first pack or unpack through the same handle after one of these calls waits for it even
- *     with pdl = 3 (kvc_tuning); a copy through another handle with pdl = 3 does not.
+ *   - the first pack or unpack on the same stream after one of these calls waits for it even with
+ *     pdl = 3 (kvc_tuning), through whichever handle; in a graph capture that holds one of these calls
+ *     every pack and unpack behind it waits for the kernel before it.
  * A descriptor's `reserved` must be 0. */
 
 typedef enum { KVC_DTYPE_BF16 = 0, KVC_DTYPE_FP16 = 1 } kvc_dtype;

@@ -100,6 +100,9 @@ enum { KVC_VARIANT_VEC32 = 100, KVC_VARIANT_BULK_GROUP = 101, KVC_VARIANT_VEC_GR
 // Implemented in kvc_kernels.cu.
 cudaError_t kvc_launch_copy(int dir, int variant, const KvcLaunch &a, uint32_t grid,
                             uint32_t smem_bytes, cudaStream_t stream);
+// A step's kernel was launched on the stream: it lets later kernels in early, so the next copy there that would
+// not wait (pdl = 3) waits for it.
+void kvc_step_launched(cudaStream_t stream);
 cudaError_t kvc_kernel_limits(int *sm_count, int *vec_blocks_per_sm, int *max_smem_optin);
 
 // A pinned-host + device pair that carries one batched launch's entry table.
@@ -131,8 +134,6 @@ struct kvc_layout {
     cudaStream_t upload_stream;  // entry tables travel on their own stream
     cudaEvent_t upload_done;
     uint64_t launches;
-    bool after_step;  // a step's kernel (tokens, attention) was launched since the last copy: it lets later
-                      // kernels in early, so a copy that would not wait (pdl = 3) waits for this one
     std::vector<uint32_t> seen;  // scratch for duplicate detection: stamp per pool block
     uint32_t seen_stamp;
     // kernel timing (diagnostic): event pairs around launches not yet collected, and spare events

@@ -28,6 +28,7 @@
 #include <mutex>
 
 #include "kvc_internal.h"
+#include "kvc_step_order.h"
 
 namespace {
 
@@ -757,8 +758,9 @@ cudaError_t launch_one(int variant, const KvcLaunch &a, uint32_t grid, uint32_t 
 
 }  // namespace
 
-cudaError_t kvc_launch_copy(int dir, int variant, const KvcLaunch &a, uint32_t grid,
-                            uint32_t smem_bytes, cudaStream_t stream)
+namespace {
+
+cudaError_t launch_copy(int dir, int variant, const KvcLaunch &a, uint32_t grid, uint32_t smem_bytes, cudaStream_t stream)
 {
     const bool table = a.table != nullptr;
     if (dir == KVC_DIR_PACK)
@@ -766,6 +768,56 @@ cudaError_t kvc_launch_copy(int dir, int variant, const KvcLaunch &a, uint32_t g
                      : launch_one<KVC_DIR_PACK, false>(variant, a, grid, smem_bytes, stream);
     return table ? launch_one<KVC_DIR_UNPACK, true>(variant, a, grid, smem_bytes, stream)
                  : launch_one<KVC_DIR_UNPACK, false>(variant, a, grid, smem_bytes, stream);
+}
+
+// Shared by all handles and host threads of the process.
+std::mutex g_order_mu;
+KvcStepOrder g_order;
+
+struct StreamName {
+    int device;
+    uint64_t stream, capture;
+    explicit StreamName(cudaStream_t st) : device(0), stream((uint64_t)(uintptr_t)st), capture(0)
+    {
+        cudaStreamCaptureStatus status;
+        unsigned long long id = 0;
+        if (cudaGetDevice(&device) != cudaSuccess || cudaStreamGetCaptureInfo(st, &status, &id) != cudaSuccess)
+            (void)cudaGetLastError();  // (a launch on this stream will say so)
+        else if (status != cudaStreamCaptureStatusNone)
+            capture = id;
+    }
+};
+
+}  // namespace
+
+void kvc_step_launched(cudaStream_t stream)
+{
+    const StreamName n(stream);
+    std::lock_guard<std::mutex> lock(g_order_mu);
+    g_order.step(n.device, n.stream, n.capture);
+}
+
+cudaError_t kvc_launch_copy(int dir, int variant, const KvcLaunch &a, uint32_t grid,
+                            uint32_t smem_bytes, cudaStream_t stream)
+{
+    if (a.pdl != 2u)
+        return launch_copy(dir, variant, a, grid, smem_bytes, stream);
+    const StreamName n(stream);
+    bool wait;
+    {
+        std::lock_guard<std::mutex> lock(g_order_mu);
+        wait = g_order.pending(n.device, n.stream, n.capture);
+    }
+    if (!wait)
+        return launch_copy(dir, variant, a, grid, smem_bytes, stream);
+    KvcLaunch b = a;
+    b.pdl = 1u;
+    const cudaError_t e = launch_copy(dir, variant, b, grid, smem_bytes, stream);
+    if (e == cudaSuccess) {
+        std::lock_guard<std::mutex> lock(g_order_mu);
+        g_order.waited(n.device, n.stream, n.capture);
+    }
+    return e;
 }
 
 cudaError_t kvc_kernel_limits(int *sm_count, int *vec_blocks_per_sm, int *max_smem_optin)

@@ -202,9 +202,8 @@ kvc_status kvc_make_plan(kvc_layout *lay, uint64_t n_ent, const void *slot_probe
     // 0 = plain launch, 1 = programmatic dependent launch, 2 = the same without waiting for the
     // previous kernel (only where the launch reads nothing a kernel could have written: the
     // batched calls read a table that an asynchronous copy delivers, which is ordered by an event)
-    // (and the first launch after a step's kernels, which write and read the blocks, always waits)
-    a->pdl = t.pdl == 1 ? 0u : (t.pdl == 3 && !lay->after_step ? 2u : 1u);
-    lay->after_step = false;
+    // (kvc_launch_copy makes the first launch behind a step's kernels, which write and read the blocks, wait)
+    a->pdl = t.pdl == 1 ? 0u : (t.pdl == 3 ? 2u : 1u);
     a->status = lay->d_status;
     uint64_t grid;
     if (t.max_ctas) {
@@ -625,7 +624,6 @@ kvc_status kvc_layout_create(const kvc_layout_desc *d, kvc_layout **out)
     lay->upload_stream = nullptr;
     lay->upload_done = nullptr;
     lay->launches = 0;
-    lay->after_step = false;
     lay->seen_stamp = 0;
     lay->time_kernels = false;
     *out = lay;

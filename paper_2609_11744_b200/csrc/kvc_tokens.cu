@@ -455,7 +455,7 @@ kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *s
         return KVC_ERR_CUDA;
     }
     ++lay->launches;
-    lay->after_step = true;
+    kvc_step_launched((cudaStream_t)stream);
     return KVC_OK;
 }
 
@@ -553,7 +553,7 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
         return KVC_ERR_CUDA;
     }
     ++lay->launches;
-    lay->after_step = true;
+    kvc_step_launched((cudaStream_t)stream);
     return KVC_OK;
 }
 

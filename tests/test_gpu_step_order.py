@@ -134,3 +134,31 @@ def test_append_behind_copies_that_do_not_wait_leaves_them_what_they_read(graphe
         assert (chunk.view(BF16) == float(i)).all(), i
         assert (pool.view(2, nb, -1)[:, : nb - 1] == float(i + 1)).all(), i
     assert kvc.kvc_poll_device_status(lay) == (0, 0)
+
+
+@pytest.mark.parametrize("other_handle", [False, True])
+def test_copies_on_another_stream_do_not_make_the_next_copy_forget_a_step(other_handle):
+    """pdl = 3: kvc_append on stream A, a copy on stream B, then a pack on A of what was appended, through the same
+    handle or another one on the same pool."""
+    nb, hkv, d, block = 1024, 8, 128, 16
+    pool, lay, ids = copies_then_step(nb, hkv, d, block)
+    packer = lay
+    if other_handle:
+        packer = make_layout(pool, block)
+        kvc.kvc_layout_set_tuning(packer, pdl=3, slot_memory=1)
+    side = torch.zeros(kvc.kvc_layout_chunk_bytes(lay, 1), dtype=torch.uint8, device="cuda")
+    chunk = torch.empty(8, kvc.kvc_layout_chunk_bytes(lay, nb // 8), dtype=torch.uint8, device="cuda")
+    slots = torch.arange((nb - 1) * block).cuda()
+    x = torch.empty((nb - 1) * block, hkv, d, dtype=BF16, device="cuda")
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for i in range(30):
+        x.fill_(float(i % 5 + 1))
+        torch.cuda.synchronize()
+        kvc.kvc_append(lay, 0, None, x, x, None, slots, None, None, stream=streams[0])
+        kvc.kvc_pack(lay, ids[nb - 1:], side, stream=streams[1])   # a block that nothing is appended to
+        for c in range(8):
+            kvc.kvc_pack(packer, ids[c * (nb // 8): (c + 1) * (nb // 8)], chunk[c], stream=streams[0])
+        torch.cuda.synchronize()
+        got = chunk.view(BF16).view(8, 2, nb // 8, -1).transpose(1, 2).reshape(nb, -1)
+        assert (got[: nb - 1] == float(i % 5 + 1)).all() and (got[nb - 1] == 0.0).all(), i
+    assert kvc.kvc_poll_device_status(lay) == (0, 0)
