@@ -249,7 +249,9 @@ struct AppendRaw {
 };
 
 // NEIGHBOURS: pairs are (2n, 2n+1), else (n, n + rot/2).  VEC: rows of the cos/sin table are 16-byte aligned.
-template <typename T, bool NEIGHBOURS, bool VEC>
+// PART: some of a head is not rotated (the choice between the two for every pair is 1.5 % of the time, which calls that
+// rotate whole heads need not pay).
+template <typename T, bool NEIGHBOURS, bool VEC, bool PART>
 __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kernel(const AppendArgs a)
 {
     kvc_pdl_wait();
@@ -369,8 +371,11 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
                 float2 ye[2], yo[2];
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    ye[n] = kvc_unpair(kvc_mul2(inv2, kvc_fma2(os[n], o[n], kvc_mul2(ec[n], e[n]))));
-                    yo[n] = kvc_unpair(kvc_mul2(inv2, kvc_fma2(es[n], e[n], kvc_mul2(oc[n], o[n]))));
+                    // (a value outside the rotation takes nothing from its neighbour, not even zero times it, which
+                    // would turn the neighbour's infinity into NaN here, or -0 into 0)
+                    const uint64_t ce = kvc_mul2(ec[n], e[n]), co = kvc_mul2(oc[n], o[n]);
+                    ye[n] = kvc_unpair(kvc_mul2(inv2, !PART || turned ? kvc_fma2(os[n], o[n], ce) : ce));
+                    yo[n] = kvc_unpair(kvc_mul2(inv2, !PART || turned ? kvc_fma2(es[n], e[n], co) : co));
                 }
                 if (NEIGHBOURS) {
                     res.a = make_uint2(kvc_from_float2<T>(ye[0].x, yo[0].x), kvc_from_float2<T>(ye[0].y, yo[0].y));
@@ -538,15 +543,18 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
     const uint32_t grid = (uint32_t)((units + per_block - 1) / per_block);
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
-    const bool vec = aligned(d->cos_sin, 16) && d->cos_sin_stride % 4 == 0;
-    const auto go = [&](auto type, auto neighbours, auto v) {
-        return kvc_launch_pdl(kvc_append_kernel<decltype(type), decltype(neighbours)::value, decltype(v)::value>, a, dim3(grid),
-                              APPEND_THREADS, 0, st);
+    const bool vec = aligned(d->cos_sin, 16) && d->cos_sin_stride % 4 == 0, part = d->rot_dim < dim;
+    const auto go = [&](auto type, auto neighbours, auto v, auto p) {
+        return kvc_launch_pdl(kvc_append_kernel<decltype(type), decltype(neighbours)::value, decltype(v)::value, decltype(p)::value>, a,
+                              dim3(grid), APPEND_THREADS, 0, st);
     };
-    const auto pick = [&](auto type) {
-        return d->interleaved ? (vec ? go(type, std::true_type(), std::true_type()) : go(type, std::true_type(), std::false_type()))
-                              : (vec ? go(type, std::false_type(), std::true_type()) : go(type, std::false_type(), std::false_type()));
+    const auto go2 = [&](auto type, auto neighbours) {
+        const std::true_type yes;
+        const std::false_type no;
+        return vec ? (part ? go(type, neighbours, yes, yes) : go(type, neighbours, yes, no))
+                   : (part ? go(type, neighbours, no, yes) : go(type, neighbours, no, no));
     };
+    const auto pick = [&](auto type) { return d->interleaved ? go2(type, std::true_type()) : go2(type, std::false_type()); };
     e = d->dtype == KVC_DTYPE_BF16 ? pick(__nv_bfloat16()) : pick(__half());
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
