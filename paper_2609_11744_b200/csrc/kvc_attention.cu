@@ -478,7 +478,7 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
                      : (wide ? join_shared<__half, 128>(j, st) : join_shared<__half, 64>(j, st));
     }
     ++lay->launches;
-    kvc_step_launched(st);
+    kvc_step_launched(lay->device, st);
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return KVC_ERR_CUDA;

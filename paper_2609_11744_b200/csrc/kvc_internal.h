@@ -102,7 +102,7 @@ cudaError_t kvc_launch_copy(int dir, int variant, const KvcLaunch &a, uint32_t g
                             uint32_t smem_bytes, cudaStream_t stream);
 // A step's kernel was launched on the stream: it lets later kernels in early, so the next copy there that would
 // not wait (pdl = 3) waits for it.
-void kvc_step_launched(cudaStream_t stream);
+void kvc_step_launched(int device, cudaStream_t stream);
 cudaError_t kvc_kernel_limits(int *sm_count, int *vec_blocks_per_sm, int *max_smem_optin);
 
 // A pinned-host + device pair that carries one batched launch's entry table.

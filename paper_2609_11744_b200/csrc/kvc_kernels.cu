@@ -777,11 +777,11 @@ KvcStepOrder g_order;
 struct StreamName {
     int device;
     uint64_t stream, capture;
-    explicit StreamName(cudaStream_t st) : device(0), stream((uint64_t)(uintptr_t)st), capture(0)
+    StreamName(int dev, cudaStream_t st) : device(dev), stream((uint64_t)(uintptr_t)st), capture(0)
     {
         cudaStreamCaptureStatus status;
         unsigned long long id = 0;
-        if (cudaGetDevice(&device) != cudaSuccess || cudaStreamGetCaptureInfo(st, &status, &id) != cudaSuccess)
+        if (cudaStreamGetCaptureInfo(st, &status, &id) != cudaSuccess)
             (void)cudaGetLastError();  // (a launch on this stream will say so)
         else if (status != cudaStreamCaptureStatusNone)
             capture = id;
@@ -790,9 +790,9 @@ struct StreamName {
 
 }  // namespace
 
-void kvc_step_launched(cudaStream_t stream)
+void kvc_step_launched(int device, cudaStream_t stream)
 {
-    const StreamName n(stream);
+    const StreamName n(device, stream);
     std::lock_guard<std::mutex> lock(g_order_mu);
     g_order.step(n.device, n.stream, n.capture);
 }
@@ -802,7 +802,11 @@ cudaError_t kvc_launch_copy(int dir, int variant, const KvcLaunch &a, uint32_t g
 {
     if (a.pdl != 2u)
         return launch_copy(dir, variant, a, grid, smem_bytes, stream);
-    const StreamName n(stream);
+    int device = 0;
+    const cudaError_t current = cudaGetDevice(&device);
+    if (current != cudaSuccess)
+        return current;
+    const StreamName n(device, stream);
     bool wait;
     {
         std::lock_guard<std::mutex> lock(g_order_mu);

@@ -460,7 +460,7 @@ kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *s
         return KVC_ERR_CUDA;
     }
     ++lay->launches;
-    kvc_step_launched((cudaStream_t)stream);
+    kvc_step_launched(lay->device, (cudaStream_t)stream);
     return KVC_OK;
 }
 
@@ -561,7 +561,7 @@ kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
         return KVC_ERR_CUDA;
     }
     ++lay->launches;
-    kvc_step_launched((cudaStream_t)stream);
+    kvc_step_launched(lay->device, (cudaStream_t)stream);
     return KVC_OK;
 }
 
