@@ -389,8 +389,9 @@ typedef enum { KVC_DTYPE_BF16 = 0, KVC_DTYPE_FP16 = 1 } kvc_dtype;
  *     table row or the free list was too short   (optional)
  * The row of a table may be longer than max_blocks (table_stride entries apart).  At most
  * KVC_MAP_MAX_REQUESTS requests (TOO_LARGE).  One kernel.  The layout gives block size and pool size
- * only; its pool is not touched.  Outputs must not overlap inputs or one another, except that
- * block_tables is both.
+ * only; its pool is not touched.  Outputs must not overlap inputs or one another (INVALID_ARG), except
+ * that block_tables is both: total_lens in particular is another array than context_lens, and the two
+ * may change places from step to step.
  * Errors: INVALID_ARG, TOO_LARGE, ALIGNMENT (a pointer not a multiple of its element), CUDA. */
 typedef struct {
     const int32_t *context_lens; /* [n_requests] */

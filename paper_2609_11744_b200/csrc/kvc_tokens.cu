@@ -399,6 +399,31 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
 
 inline bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
+struct Span {
+    const void *at;  // or NULL
+    uint64_t bytes;
+};
+inline bool overlap(const Span &a, const Span &b)
+{
+    const uint64_t x = (uint64_t)(uintptr_t)a.at, y = (uint64_t)(uintptr_t)b.at;
+    return x && y && a.bytes && b.bytes && (x < y ? y - x < a.bytes : x - y < b.bytes);
+}
+// Rows of a table, `stride` bytes apart; what lies between them is not the table's.
+struct Rows {
+    Span first;
+    uint64_t stride, n;
+};
+inline bool overlap(const Span &a, const Rows &b)
+{
+    const uint64_t x = (uint64_t)(uintptr_t)a.at, y = (uint64_t)(uintptr_t)b.first.at;
+    if (b.n == 0 || x <= y || b.n == 1)
+        return b.n && overlap(a, b.first);
+    // the row at whose place `a` begins, and the one behind it
+    const uint64_t row = b.stride ? (x - y) / b.stride : 0, off = (x - y) - row * b.stride;
+    return a.at && b.first.at && a.bytes && b.first.bytes &&
+           ((row < b.n && off < b.first.bytes) || (row + 1 < b.n && a.bytes > b.stride - off));
+}
+
 }  // namespace
 
 extern "C" {
@@ -418,6 +443,25 @@ kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *s
         !aligned(d->free_blocks, 4) || !aligned(d->block_tables, 4) || !aligned(d->positions, 4) ||
         !aligned(d->slots, 8) || !aligned(d->token_request, 4) || !aligned(d->total_lens, 4) || !aligned(d->counts, 4))
         return KVC_ERR_ALIGNMENT;
+    // Every block reads the lengths, and those that finish early write beside blocks that have not read yet
+    const uint64_t r = d->n_requests, t = d->token_capacity;
+    const Span outs[] = {{d->cu_tokens, 4 * (r + 1)}, {d->positions, 4 * t}, {d->slots, 8 * t}, {d->token_request, 4 * t},
+                         {d->total_lens, 4 * r}, {d->counts, 12}};
+    const Span ins[] = {{d->context_lens, 4 * r}, {d->new_lens, 4 * r}, {d->free_blocks, 4ull * d->n_free}};
+    const Rows tables = {{d->block_tables, 4ull * d->max_blocks}, 4 * d->table_stride, r};
+    for (const Span &o : outs) {
+        for (const Span &x : ins)
+            if (overlap(o, x))
+                return KVC_ERR_INVALID_ARG;
+        for (const Span *x = outs; x != &o; ++x)
+            if (overlap(o, *x))
+                return KVC_ERR_INVALID_ARG;
+        if (overlap(o, tables))
+            return KVC_ERR_INVALID_ARG;
+    }
+    for (const Span &x : ins)
+        if (overlap(x, tables))
+            return KVC_ERR_INVALID_ARG;
     kvc_status s = kvc_ensure_device(lay);
     if (s != KVC_OK)
         return s;

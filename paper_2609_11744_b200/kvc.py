@@ -673,7 +673,8 @@ def kvc_map_tokens(layout, context_lens, new_lens, free_blocks, block_tables, cu
 
     context_lens, new_lens [R] and free_blocks [F] are int32; block_tables [R, max_blocks] int32 is
     completed in place; cu_tokens [R + 1] int32, positions [T] int32, slots [T] int64 and, if given,
-    token_request [T], total_lens [R] and counts [3] int32 are written."""
+    token_request [T], total_lens [R] and counts [3] int32 are written.  No output may share memory with another
+    tensor of the call: total_lens is not context_lens."""
     t, dev, L = _step_call()
     i32, n, cap, free = t.i32, context_lens.numel(), positions.numel(), free_blocks.numel()
     tab, stride, wide = _table(block_tables, n, i32, dev)
