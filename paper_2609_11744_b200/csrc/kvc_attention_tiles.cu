@@ -442,10 +442,12 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             asm volatile("prefetch.tensormap [%0];" ::"l"(&args.v_map) : "memory");
         }
     }
+    kvc_pdl_begin(a.beside);
+    // Tensor memory is not held while waiting for the kernel before: one that lets this one in early, and allocates
+    // on the same SM after that, would wait for this block for ever.
     if (warp == 16)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(COLS) : "memory");
     fence_before();
-    kvc_pdl_begin(a.beside);
 
     const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
     const KvcRun run = kvc_find_run<ROWS, TK, HEAD, LEAST, THREADS>(a, n_seq);  // (has block-wide barriers)

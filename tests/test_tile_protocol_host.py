@@ -3,6 +3,7 @@
 Two softmax warps hold the two halves of a row's keys; a third actor makes scores and products.  The model has the
 rules that the kernel keeps: whose words are written when, what waits for what, and how a warp leaves.  Under them
 no schedule may read a word that is not its tile's, or leave a warp waiting; without any one of them some schedule does."""
+import os
 import random
 
 import pytest
@@ -144,3 +145,12 @@ def test_a_single_arrival_does_not_release_the_partner_of_a_warp_that_gives_up()
 @pytest.mark.parametrize("buffers", [1, 2])
 def test_products_meet_columns_that_are_being_rescaled_unless_the_halves_meet_again(buffers):
     assert over_schedules(300, buffers=buffers, words=2, farewell=True, together=False) == {"products while columns are rescaled"}
+
+
+def test_tensor_memory_is_not_held_while_waiting_for_the_kernel_before():
+    """Where two kernels overlap on an SM, one that waits for the other to end must not hold what the other may still
+    ask for."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "paper_2609_11744_b200", "csrc", "kvc_attention_tiles.cu")) as f:
+        kernel = f.read().split("kvc_attn_tiles_kernel(const __grid_constant__", 1)[1]
+    assert 0 < kernel.index("kvc_pdl_begin(") < kernel.index("tcgen05.alloc")
