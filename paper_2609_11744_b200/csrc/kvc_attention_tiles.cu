@@ -214,10 +214,12 @@ __device__ __forceinline__ float exp2_fast(float x)
 __device__ __forceinline__ uint32_t low_bits(int32_t n) { return n <= 0 ? 0u : n > 31 ? ~0u : (1u << n) - 1u; }
 
 struct Bars {
-    // [row tile, or score buffer where there is one row tile], p_full: and half of the keys.  o_done: a
-    // row tile's last product of a segment; with one row tile, the products of even and of odd tiles, so that a
-    // warp that looks one product late is never two phases behind
-    uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];
+    // q_full: [row tile].  p_full: [score buffer][half of the keys].  s_full, o_done: scores made, and a row tile's
+    // last products of a segment, [0] and [1] of either row tile; with one row tile [0] and [2], scores in either buffer
+    // and the products of even and of odd tiles (so that a warp that looks one product late is never two phases
+    // behind).  [1] belongs to the second row tile alone: nothing waits for its warps while there is one row tile, and
+    // a parity does not tell a warp that comes late how many phases it has missed.
+    uint64_t q_full[2], s_full[3], p_full[2][2], o_done[3];
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
     uint64_t seg_full[4], seg_empty[4], drained;
 };
@@ -422,9 +424,11 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         s_dead = 0;
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_addr(&bars.q_full[i]), 8);
-            bar_init(smem_addr(&bars.s_full[i]), 1);
             bar_init(smem_addr(&bars.p_full[i][0]), 128);
             bar_init(smem_addr(&bars.p_full[i][1]), 128);
+        }
+        for (int i = 0; i < 3; ++i) {
+            bar_init(smem_addr(&bars.s_full[i]), 1);
             bar_init(smem_addr(&bars.o_done[i]), 1);
         }
         for (int i = 0; i < 4; ++i) {
@@ -482,7 +486,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         bool parted = false;  // the partner has left
         SegmentReader reader;
         Segment c, d;
-        uint32_t s_parity = 0, o_parity = 0, slot = 0;  // parities: a bit for each barrier of a pair
+        uint32_t s_parity = 0, o_parity = 0, slot = 0;  // parities: a bit for each barrier, of those that this warp waits for
         // Queries of a segment: 16 bytes a thread and turn, rows of 128 bytes in the swizzle.  All scores
         // of the segment before have been seen, so their operand may go.
         const auto load_queries = [&](const Segment &c) {
@@ -609,10 +613,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
 #pragma unroll 1
                 for (uint32_t i = 0; i < c.n; ++i) {
                     const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + i) * TK + half * HK);
-                    const uint32_t buf = two ? sub : i & 1u, s_at = s_col + buf * 128u;
-                    if (!(ok = __all_sync(~0u, bar_wait(bar + BAR(s_full) + buf * 8u, s_parity >> buf & 1u, dead, a.status))))
+                    const uint32_t buf = two ? sub : i & 1u, at = two ? sub : buf * 2u, s_at = s_col + buf * 128u;
+                    if (!(ok = __all_sync(~0u, bar_wait(bar + BAR(s_full) + at * 8u, s_parity >> at & 1u, dead, a.status))))
                         break;
-                    s_parity ^= 1u << buf;
+                    s_parity ^= 1u << at;
                     fence_after();
                     float s[HK];
                     tmem_ld32(s, s_at + half * HK);
@@ -662,7 +666,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                             // the products so far have to be in O.  With two row tiles these scores were issued after
                             // them; with one, only the product before the last is known to be there
                             if (!two) {
-                                if (!(ok = __all_sync(~0u, bar_wait(bar + BAR(o_done) + (buf ^ 1u) * 8u, o_parity >> (buf ^ 1u) & 1u ^ 1u, dead, a.status))))
+                                if (!(ok = __all_sync(~0u, bar_wait(bar + BAR(o_done) + (at ^ 2u) * 8u, o_parity >> (at ^ 2u) & 1u ^ 1u, dead, a.status))))
                                     break;
                                 fence_after();
                             }
@@ -709,26 +713,13 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     fence_before();
                     bar_arrive(bar + BAR(p_full) + (buf * 2 + half) * 8u);
                     if (!two)
-                        o_parity ^= 1u << buf;
+                        o_parity ^= 1u << at;
                 }
                 if (!ok)
                     break;
-                last = two ? sub : (c.n - 1) & 1u;
-            } else {
-                // the single row tile uses the other row tile's barriers too.  Their phases are waited for one by
-                // one: a warp that skipped two could not tell a later one by its parity
-                for (uint32_t i = 1; i < c.n && ok; i += 2) {
-                    ok = __all_sync(~0u, bar_wait(bar + BAR(s_full) + 8u, s_parity >> 1, dead, a.status));
-                    s_parity ^= 2u;
-                    o_parity ^= 2u;
-                }
-                if (!ok)
-                    break;
-            }
-            if (two) {  // (warps of rows 128 up never look at the first barriers, and need not count them)
-                o_parity ^= 3u;
-                if (sub == 0)
-                    s_parity ^= (c.n & 1u) << 1;
+                last = two ? sub : (c.n - 1) % 2u * 2u;
+                if (two)
+                    o_parity ^= 1u << sub;
             }
             slot = (slot + c.n) % THERE;
         }
@@ -760,7 +751,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 if (elect_one())
                     mma_commit(bar + at);
             };
-            const auto scores = [&](uint32_t sub, uint32_t buf) {
+            const auto scores = [&](uint32_t sub, uint32_t buf, uint32_t at) {
                 const uint32_t qa = q_at + sub * (S::TILE >> 4), ka = k_at + k.stage * (S::TILE >> 4), d = tmem + COL_S + buf * 128u;
                 if (elect_one()) {
 #pragma unroll
@@ -768,7 +759,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                         const uint32_t at = ((i >> 2) * S::HALF + (i & 3) * 32) >> 4;
                         mma_ss(d, qa + at, ka + at, KIND_S, i > 0);
                     }
-                    mma_commit(bar + BAR(s_full) + buf * 8u);
+                    mma_commit(bar + BAR(s_full) + at * 8u);
                 }
             };
             // O of row tile `sub` += P V, P from score buffer `buf`, in two halves as they come
@@ -799,9 +790,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 for (uint32_t i = 0; i < min(ahead, n); ++i) {
                     if (i > 0 && !wait(BAR(k_full) + k.stage * 8u, k.parity))
                         break;
-                    scores(0, i);
+                    scores(0, i, i * 2u);
                     if (two)
-                        scores(1, 1);
+                        scores(1, 1, 1);
                     commit(BAR(k_empty) + k.stage * 8u);
                     k.next();
                 }
@@ -825,7 +816,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                             if (more) {  // these scores' barrier stands for the products before them too
                                 if (sub == 0 && !wait(BAR(k_full) + k.stage * 8u, k.parity))
                                     break;
-                                scores(sub, sub);
+                                scores(sub, sub, sub);
                             }
                         }
                     } else {
@@ -833,10 +824,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                         products(0, buf, i == 0);
                         if (!ok)
                             break;
-                        commit(BAR(o_done) + buf * 8u);
+                        commit(BAR(o_done) + buf * 16u);
                         commit(BAR(v_empty) + v.stage * 8u);
                         if (more && wait(BAR(k_full) + k.stage * 8u, k.parity))
-                            scores(0, buf);
+                            scores(0, buf, buf * 2u);
                     }
                     if (!ok)
                         break;

@@ -147,6 +147,55 @@ def test_products_meet_columns_that_are_being_rescaled_unless_the_halves_meet_ag
     assert over_schedules(300, buffers=buffers, words=2, farewell=True, together=False) == {"products while columns are rescaled"}
 
 
+def follow(seed, kinds, own):
+    """Segments of one row tile (1) or two (2) in turn; whether the second row tile's warp gets through them.  It waits for
+    phases of its scores' barrier by their parity.  own: that barrier has no phases but its own; else the odd key
+    tiles of a single row tile use it too, which nobody waits for it to see, and it follows them one by one."""
+    rng = random.Random(seed)
+    done, ready, answered = [0], [0], [0]   # phases of the barrier; segments that the second row tile has come to; phases it saw
+
+    def matrix():
+        for i, kind in enumerate(kinds):
+            while kind == 2 and ready[0] <= i:
+                yield "wait"
+            for tile in range(5):
+                yield
+                if kind == 2 or (tile % 2 and not own):
+                    done[0] += 1
+                    seen = done[0]
+                    while kind == 2 and answered[0] < seen:
+                        yield "wait"
+
+    def second():
+        parity = 0
+        for i, kind in enumerate(kinds):
+            ready[0] = i + 1
+            for _ in range(rng.randint(0, 12)):   # writes its last result, or is held up
+                yield
+            for tile in range(5):
+                if kind == 2 or (tile % 2 and not own):
+                    while done[0] % 2 == parity:   # the phase of this parity is not over
+                        yield "wait"
+                    parity ^= 1
+                    answered[0] = max(answered[0], done[0])
+
+    actors, idle = [matrix(), second()], 0
+    while actors and idle < 200:
+        k = rng.randrange(len(actors))
+        try:
+            idle = idle + 1 if next(actors[k]) == "wait" else 0
+        except StopIteration:
+            del actors[k]
+            idle = 0
+    return not actors
+
+
+def test_a_warp_that_nobody_waits_for_cannot_follow_phases_by_their_parity():
+    kinds = [2, 1, 2, 1, 1, 2]
+    assert all(follow(seed, kinds, own=True) for seed in range(2000))
+    assert not all(follow(seed, kinds, own=False) for seed in range(2000))
+
+
 def test_tensor_memory_is_not_held_while_waiting_for_the_kernel_before():
     """Where two kernels overlap on an SM, one that waits for the other to end must not hold what the other may still
     ask for."""
