@@ -423,7 +423,8 @@ kvc_status kvc_map_tokens(kvc_layout *layout, const kvc_map_tokens_desc *desc, v
  * slot's place in planes K (0) and V (1) of `layer`.  Computed in 32 bits, rounded once.
  * Rows with slots[t] < 0 are skipped: neither q_out nor the pool is touched.  So are rows whose slot
  * lies behind the pool, or whose position lies outside the cos_sin table (with rot_dim > 0); those
- * are counted.  Two rows with the same slot: either one's keys and values.
+ * are counted.  Two rows with the same slot: every element there is one row's or the other's, and
+ * neighbours need not be the same row's.
  * Layout: kv_planes = 2, elem_bytes = 2, head_dim a multiple of 8 up to 256; rot_dim a multiple of 16
  * up to head_dim, or 0 (positions and cos_sin are then unused).  Strides are in elements; elements
  * of a head are adjacent.  Pointers of q, k, v, q_out and the weights, and all strides in bytes, are

@@ -70,3 +70,16 @@ def test_append_norm_of_a_head_with_an_infinity(dtype):
     rest = torch.ones(t, hkv, dtype=torch.bool)
     rest[4, 1] = False
     assert torch.equal(got[0][rest.cuda()], got[1][rest.cuda()])
+
+
+def test_append_of_two_rows_to_one_slot_leaves_elements_of_either():
+    """And what other slots get is not touched by it."""
+    t, hkv, d, block = 64, 2, 128, 16
+    pool = torch.zeros(1, 2, 8, block, hkv, d, dtype=BF16, device="cuda")
+    x = torch.arange(1, t + 1, device="cuda")[:, None, None].expand(t, hkv, d).to(BF16).contiguous()
+    slots = torch.arange(t).cuda()
+    slots[32:] = slots[:32].flip(0)   # rows i and 63 - i
+    kvc.kvc_append(make_layout(pool, block), 0, None, x, -x, None, slots, None, None)
+    for got, sign in zip(pool.view(2, -1, hkv, d), (1.0, -1.0)):
+        first, second = x[:32] * sign, x[32:].flip(0) * sign
+        assert ((got[:32] == first) | (got[:32] == second)).all() and (got[32:] == 0).all()
