@@ -131,22 +131,4 @@ __device__ __forceinline__ uint32_t kvc_from_float2<__half>(float lo, float hi)
     return v;
 }
 
-template <typename T>
-__device__ __forceinline__ void kvc_unpack8(const uint4 &v, float (&x)[8])
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = kvc_to_float2<T>(w[i]);
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-    }
-}
-template <typename T>
-__device__ __forceinline__ uint4 kvc_pack8(const float (&x)[8])
-{
-    return make_uint4(kvc_from_float2<T>(x[0], x[1]), kvc_from_float2<T>(x[2], x[3]),
-                      kvc_from_float2<T>(x[4], x[5]), kvc_from_float2<T>(x[6], x[7]));
-}
-
 #endif
