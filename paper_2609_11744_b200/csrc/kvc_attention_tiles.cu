@@ -18,14 +18,20 @@
 // Two row tiles share each K and V tile, and while one is in its softmax the other's products run.  A pair
 // of 128 rows or fewer has one row tile; its scores then alternate between the two score buffers, so that
 // those of the next tile are made while this one is in its softmax (16 requests of up to 5 drafted tokens
-// behind 16,000, 64 and 8 heads of 128: 243 us with one buffer, 208 us with two).
+// behind 16,000, 64 and 8 heads of 128: a sixth less time than with one buffer, 204 us).
 // Bound by the exponentials and the matrix unit alike: 128 x 128 scores take 1024 cycles on each.  Measured:
-// an 8192-token prompt (32 and 8 heads of 128, 550 GFLOP) in 580 us = 948 TFLOP/s, either unit busy 45 % of the
-// time; what is left is the chain scores - maximum - weights - products - next scores of either row tile.
+// an 8192-token prompt (32 and 8 heads of 128, 550 GFLOP) in 600 us = 916 TFLOP/s in runs of five, and in 666 us =
+// 825 TFLOP/s in a loop of seconds, where the power limit holds the clock at 1.76 GHz; either unit is busy 45 % of the
+// time.  What is left is the chain scores - maximum - weights - products - next scores of either row tile, two
+// meetings of the warps of a row in it, and some spills (96 registers a thread, 224 bytes read back).
 // Moving a part of the exponentials to the multiply-add pipe, smaller key tiles and one softmax thread a
 // row were all slower.
-// O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use: weights are then
-// at most 2^8, which neither type nor the 32-bit sums mind, and almost all tiles skip the rescaling.
+// O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use (a published refinement of the
+// online softmax of Milakov and Gimelshein, 2018): weights are then at most 2^8, which neither type nor the 32-bit sums
+// mind, and almost all tiles skip the rescaling.
+// Weights are rounded to the pool's type, since the matrix unit takes 16-bit operands of one type; a second product
+// for what the rounding leaves would be half as much tensor work again.  Against 64 bits the result is off by 0.0021 to
+// 0.0023 in bf16 (0.0017 with weights in 32 bits: the result's own rounding) and 0.0003 in fp16 (0.0002).
 // Every wait is bounded; one that gives up makes all roles leave and is counted.
 #include <cuda.h>
 #include <stddef.h>
@@ -38,13 +44,13 @@ namespace {
 constexpr int TK = 128;             // keys of a K or V stage
 constexpr int HK = TK / 2;          // keys of one softmax thread
 constexpr int THREADS = 640;
-constexpr int HEAD = 3;             // what a pair costs besides its units, in units (8192-token prompt: 655, 604, 580, 585 us with 1 to 4)
-constexpr int LEAST = 3;            // units of a run at least (64 requests on a 1024-token prefix: 69, 66, 66 us with 2 to 4)
+constexpr int HEAD = 3;             // what a pair costs besides its units, in units (8192-token prompt: 670, 621, 601, 607 us with 1 to 4)
+constexpr int LEAST = 3;            // units of a run at least (64 requests on a 1024-token prefix: 76, 71, 72 us with 2 to 4)
 constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper than the K ring
 
-// ROWS is 256, two row tiles a block, or 128, one: half the queries then make room for a third K stage
-// (16 requests of up to 5 drafted tokens behind 16,000: 208 us with 256, 200 us with 128; 32 questions on a
-// 32,000-token document 70 and 68 us).
+// ROWS is 256, two row tiles a block, or 128, one: half the queries then make room for a third K stage, which long
+// runs of keys gain by (one request of drafted tokens behind 80,000: 85.4 us with 256, 83.6 with 128; 32 questions on a
+// 32,000-token document 71.2 and 69.5; but 16 requests of drafted tokens behind 16,000 202.4 and 204.5).
 template <int D, int ROWS>
 struct Shape {
     static constexpr int TILE = TK * D * 2;           // a K or V tile; also the queries of a row tile
@@ -369,7 +375,7 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
                                  "r"((uint32_t)__popc(good) * args.box_keys * (uint32_t)D * 2u) : "memory");
                 __syncwarp();
                 // a lane a box: the lanes take turns at the copy unit, but their operands are ready (8192-token
-                // prompt in 16-token blocks: 580 us, and 620 with one lane in a loop of 16 boxes)
+                // prompt in 16-token blocks: 7 % more with one lane in a loop of 16 boxes)
                 const uint32_t h = boxes * (D / 64) > lane ? lane / boxes : 0u, i = lane - h * boxes;
                 if (lane < boxes * (D / 64) && (good >> i & 1u))
                     box_load(tile + h * S::HALF + box_at * 128u, map, h * 64u, c.h, boxes > 1 ? 0u : (uint32_t)j0 % a.block_size, id, bar);
