@@ -47,7 +47,7 @@ TRAFFIC_8B_80K = {
     "bytes": 20_920_170_000.0,
     "source": "profiles/kvc_bulk_kernel_8b_80k_dram_traffic.md",
     "kernel_file": "paper_2609_11744_b200/csrc/kvc_kernels.cu",
-    "kernel_file_sha256_at_last_check": "372d51959538a4b208716ac5e245c751f5d2247fb86df750d1a596d13a7471f7",
+    "kernel_file_sha256_at_last_check": "365e72c6f40b7e3c0415adc2df5af2e2ede3a38c457971f4999e23294679cb57",
 }
 
 
