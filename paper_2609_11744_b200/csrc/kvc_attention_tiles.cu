@@ -22,8 +22,8 @@
 // Bound by the exponentials and the matrix unit alike: 128 x 128 scores take 1024 cycles on each.  Measured:
 // an 8192-token prompt (32 and 8 heads of 128, 550 GFLOP) in 600 us = 916 TFLOP/s in runs of five, and in 666 us =
 // 825 TFLOP/s in a loop of seconds, where the power limit holds the clock at 1.76 GHz; either unit is busy 45 % of the
-// time.  What is left is the chain scores - maximum - weights - products - next scores of either row tile, two
-// meetings of the warps of a row in it, and some spills (96 registers a thread, 224 bytes read back).
+// time.  What is left is the chain scores - maximum - weights - products - next scores of either row tile, with a
+// meeting of the two warps of a row in it, and some spills (96 registers a thread, 224 bytes read back).
 // Moving a part of the exponentials to the multiply-add pipe, smaller key tiles and one softmax thread a
 // row were all slower.
 // O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use (a published refinement of the

@@ -162,3 +162,43 @@ def test_copies_on_another_stream_do_not_make_the_next_copy_forget_a_step(other_
         got = chunk.view(BF16).view(8, 2, nb // 8, -1).transpose(1, 2).reshape(nb, -1)
         assert (got[: nb - 1] == float(i % 5 + 1)).all() and (got[nb - 1] == 0.0).all(), i
     assert kvc.kvc_poll_device_status(lay) == (0, 0)
+
+
+def test_copies_captured_behind_a_step_wait_for_it():
+    """pdl = 3: kvc_append and packs of what was appended in one graph; a capture takes nothing from the next copy outside it."""
+    nb, hkv, d, block = 1024, 8, 128, 16
+    pool, lay, ids = copies_then_step(nb, hkv, d, block)
+    chunk = torch.empty(8, kvc.kvc_layout_chunk_bytes(lay, nb // 8), dtype=torch.uint8, device="cuda")
+    slots = torch.arange(nb * block).cuda()
+    x = torch.empty(nb * block, hkv, d, dtype=BF16, device="cuda")
+
+    def packs():
+        for c in range(8):
+            kvc.kvc_pack(lay, ids[c * (nb // 8): (c + 1) * (nb // 8)], chunk[c])
+
+    def step():
+        kvc.kvc_append(lay, 0, None, x, x, None, slots, None, None)
+
+    step()
+    packs()
+    torch.cuda.synchronize()
+    both = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(both):
+        step()
+        packs()
+    for i in range(20):
+        x.fill_(float(i + 1))
+        torch.cuda.synchronize()
+        if i % 2:
+            both.replay()
+        else:
+            step()
+            if i % 4:
+                packs()
+            else:
+                with torch.cuda.graph(torch.cuda.CUDAGraph()):   # captured, not run, between the step and the copies
+                    packs()
+                packs()
+        torch.cuda.synchronize()
+        assert (chunk.view(BF16) == float(i + 1)).all(), i
+    assert kvc.kvc_poll_device_status(lay) == (0, 0)
