@@ -518,6 +518,78 @@ kvc_status kvc_attention_workspace_bytes(kvc_layout *layout, uint32_t n_tokens, 
 kvc_status kvc_attention(kvc_layout *layout, const kvc_attention_desc *desc, void *stream);
 kvc_status kvc_attention_shared(kvc_layout *layout, const kvc_attention_desc *desc, void *stream);
 
+/* ------------------------------------------------------------------ positions with several axes, a pool held in 4 bits
+ *
+ * The same conventions as above. */
+
+/* kvc_append for tokens whose position has several axes (time, height and width of a picture's patches,
+ * say): pair n of a head turns by the angle at the position on axis pair_axis[n],
+ *   cos = cos_sin[positions[pair_axis[n] * axis_stride + t]][n], sin likewise,
+ * so sections of a head, axes in turns, and any other split of the pairs are one table.  Text tokens
+ * have the same position on every axis.  `token` is kvc_append's descriptor with all its rules;
+ * token.positions is [n_axes][axis_stride], 1 <= n_axes <= KVC_MAX_AXES, axis_stride >= n_tokens.  A row
+ * with a position outside the table on any axis, a pair's or not, is skipped and counted once.
+ * pair_axis entries of pairs 0 .. rot_dim/2-1 must be below n_axes (INVALID_ARG); others are not read.
+ * One kernel.  Errors: as kvc_append. */
+#define KVC_MAX_AXES 4u
+#define KVC_MAX_PAIRS 128u
+typedef struct {
+    kvc_append_desc token;
+    uint64_t axis_stride;        /* entries of `positions` between axes */
+    uint32_t n_axes;
+    uint32_t reserved;
+    uint8_t pair_axis[KVC_MAX_PAIRS];
+} kvc_append_axes_desc;
+kvc_status kvc_append_axes(kvc_layout *layout, const kvc_append_axes_desc *desc, void *stream);
+
+/* A pool held in 4 bits.  A row -- one token of one KV head in one plane -- is head_dim values in groups of
+ * KVC_Q4_GROUP.  With x the values as a 16-bit pool would hold them (rounded to the dtype), a group has
+ *   offset = min x,  step = (max x - min x) / 15 rounded towards zero to the dtype,
+ *   code = (x - offset) / step rounded to the nearest integer, ties to even, at most 15 (0 where step = 0)
+ * and its values stand for offset + step * code, off by at most (max x - min x) / 30, or by 15 of the dtype's
+ * smallest numbers where the step is not a normal one.  A group that holds an infinity or a NaN, or whose range is
+ * none of a 32-bit float's, stands for NaN.
+ * In the slab of a block the rows of a KV head lie together, heads in order:
+ *   codes  [token][head_dim / 2]                         low half of a byte first
+ *   scales [token][head_dim / KVC_Q4_GROUP]{step, offset}  16 bits each
+ * so to the layout, and to every call that moves blocks, a row is KVC_Q4_ROW_BYTES(head_dim) elements of
+ * one byte: elem_bytes = 1, head_dim = KVC_Q4_ROW_BYTES(64) or (128), kv_planes = 2, and a KV head's rows of a
+ * block a multiple of 16 bytes (ALIGNMENT: with heads of 64 the block size is even).  The calls that follow
+ * refuse other layouts (INVALID_ARG).  All calls on a pool take the same dtype: the scales have it. */
+#define KVC_Q4_GROUP 32u
+#define KVC_Q4_ROW_BYTES(head_dim) ((head_dim) / 2u + (head_dim) / 8u)
+
+/* kvc_append_axes into a pool held in 4 bits: queries as there, keys (behind norm and rotation) and values
+ * in codes.  One position for each token: n_axes = 1 and pair_axis of zeros.  One kernel.
+ * Errors: as kvc_append. */
+kvc_status kvc_append_q4(kvc_layout *layout, const kvc_append_axes_desc *desc, void *stream);
+
+/* Tokens of a pool held in 4 bits, as values of the dtype (offset + step * code, rounded once): k_out[t][h],
+ * v_out[t][h] = the row of slot slots[t].  Either output may be NULL.  Rows with slots[t] < 0 are left as
+ * they are; so are rows whose slot lies behind the pool, which are counted.  Strides in elements; pointers
+ * and strides in bytes are multiples of 16 bytes.  One kernel.
+ * Errors: INVALID_ARG, ALIGNMENT, TOO_LARGE (over 2^31 thread blocks), CUDA. */
+typedef struct {
+    uint32_t layer;
+    uint32_t dtype;              /* kvc_dtype: of the outputs and of the pool's scales */
+    void *k_out, *v_out;         /* [n_tokens][num_kv_heads][head_dim] */
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const int64_t *slots;        /* [n_tokens] */
+    uint32_t n_tokens;
+    uint32_t reserved;
+} kvc_read_q4_desc;
+kvc_status kvc_read_q4(kvc_layout *layout, const kvc_read_q4_desc *desc, void *stream);
+
+/* kvc_attention and kvc_attention_shared over a pool held in 4 bits, with the same descriptor and rules: masks,
+ * lengths, clamps, groups, workspaces.  Products with keys and values are taken in the dtype with 32-bit sums: in the
+ * kernel for few rows the codes of a key are exact and the steps multiply the sums, elsewhere a value is
+ * rounded to the dtype before its product, as a 16-bit pool would hold it.  With many query rows any block
+ * size is as fast as another.  The workspace comes from kvc_attention_q4_workspace_bytes. */
+kvc_status kvc_attention_q4_workspace_bytes(kvc_layout *layout, uint32_t n_tokens, uint32_t n_requests,
+                                            uint32_t n_q_heads, uint32_t n_groups, uint64_t *bytes);
+kvc_status kvc_attention_q4(kvc_layout *layout, const kvc_attention_desc *desc, void *stream);
+kvc_status kvc_attention_q4_shared(kvc_layout *layout, const kvc_attention_desc *desc, void *stream);
+
 /* ------------------------------------------------------------------ staging ring (Sec. 6.4) */
 
 typedef struct kvc_ring kvc_ring;

@@ -8,7 +8,7 @@ INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libkvc.so")
 SOURCES = ["kvc_kernels.cu", "kvc_layout.cu", "kvc_ring.cu", "kvc_noalloc.cu", "kvc_copy_engine.cu", "kvc_store.cpp", "kvc_pipeline.cpp", "kvc_slot_pool.cpp",
            "kvc_host_transfer.cpp", "kvc_tokens.cu", "kvc_attention.cu", "kvc_attention_rows.cu",
-           "kvc_attention_tiles.cu"]
+           "kvc_attention_tiles.cu", "kvc_attention_q4_rows.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-Wall", "-cudart", "static"]
 

@@ -1,5 +1,5 @@
-// Entry points of attention over the paged pool (kvc_attention, kvc_attention_shared), the layout of
-// their workspace, and the kernels that join the parts of a pair.
+// Entry points of attention over the paged pool (kvc_attention, kvc_attention_shared, and the same over a
+// pool held in 4 bits), the layout of their workspace, and the kernels that join the parts of a pair.
 #include <string.h>
 
 #include <algorithm>
@@ -288,11 +288,14 @@ struct Carver {
 struct Shape {
     uint32_t head_dim, hkv, g;
     uint64_t tokens, requests, groups;
+    bool q4;
 };
 
 void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, uint32_t rows, uint64_t sequences, bool by_pair)
 {
-    const uint32_t blocks = rows == KVC_ATTN_SMALL_ROWS ? kvc_attn_rows_blocks(lay, by_pair) : kvc_attn_tiles_blocks(lay);
+    const uint32_t blocks = rows > KVC_ATTN_SMALL_ROWS ? kvc_attn_tiles_blocks(lay)
+                            : s.q4                     ? kvc_attn_q4_rows_blocks(lay, rows)
+                                                       : kvc_attn_rows_blocks(lay, by_pair);
     const uint32_t head_dim = s.head_dim;
     const uint64_t pairs = by_pair ? kvc_max_pairs(sequences, s.tokens, s.g, s.hkv, rows) : 0;
     const uint64_t slots = pairs ? (uint64_t)blocks + pairs : 2ull * blocks;
@@ -315,7 +318,9 @@ void carve(Carver &c, KvcParts &p, const kvc_layout *lay, const Shape &s, uint32
 uint64_t phase_bytes(const kvc_layout *lay, const Shape &s, uint64_t sequences, bool pairs)
 {
     uint64_t most = 0;
-    for (const uint32_t rows : {KVC_ATTN_SMALL_ROWS, KVC_ATTN_TILE_ROWS, KVC_ATTN_MANY_ROWS}) {
+    for (const uint32_t rows : {KVC_ATTN_FEW_ROWS, KVC_ATTN_SMALL_ROWS, KVC_ATTN_TILE_ROWS, KVC_ATTN_MANY_ROWS}) {
+        if (rows == KVC_ATTN_FEW_ROWS && !s.q4)
+            continue;
         KvcParts p;
         Carver c = {nullptr, 0};
         carve(c, p, lay, s, rows, sequences, pairs);
@@ -330,12 +335,13 @@ uint64_t workspace_bytes(const kvc_layout *lay, const Shape &s)
                     : phase_bytes(lay, s, s.requests, false);
 }
 
-kvc_status check(const kvc_layout *lay, const kvc_attention_desc *d)
+kvc_status check(const kvc_layout *lay, const kvc_attention_desc *d, bool q4)
 {
     if (!lay || !d || d->reserved != 0)
         return KVC_ERR_INVALID_ARG;
     const kvc_layout_desc &l = lay->d;
-    if (d->layer >= l.num_layers || l.kv_planes != 2 || l.elem_bytes != 2 || (l.head_dim != 64 && l.head_dim != 128) ||
+    if (d->layer >= l.num_layers || l.kv_planes != 2 ||
+        (q4 ? kvc_q4_head_dim(lay) == 0 : l.elem_bytes != 2 || (l.head_dim != 64 && l.head_dim != 128)) ||
         (d->dtype != KVC_DTYPE_BF16 && d->dtype != KVC_DTYPE_FP16))
         return KVC_ERR_INVALID_ARG;
     if (d->n_q_heads == 0 || d->n_q_heads % l.num_kv_heads || !(d->scale > 0.f) || d->scale > 3.0e38f ||
@@ -343,13 +349,13 @@ kvc_status check(const kvc_layout *lay, const kvc_attention_desc *d)
         return KVC_ERR_INVALID_ARG;
     if ((uint64_t)d->n_tokens * (d->n_q_heads / l.num_kv_heads) > 0x7FFFFFFFull)
         return KVC_ERR_TOO_LARGE;
-    return KVC_OK;
+    return q4 && !kvc_q4_aligned(lay) ? KVC_ERR_ALIGNMENT : KVC_OK;
 }
 
 template <typename T, int D>
 cudaError_t join_split(const KvcAttn &a, cudaStream_t st)
 {
-    if (a.parts.rows == KVC_ATTN_SMALL_ROWS)  // few rows, possibly of many parts: a block to a row
+    if (a.parts.rows <= KVC_ATTN_SMALL_ROWS)  // few rows, possibly of many parts: a block to a row
         return kvc_launch_pdl(kvc_join_split_kernel<T, D, JOIN_WARPS>, a, dim3(a.parts.blocks - 1, 4), JOIN_WARPS * 32, 0, st);
     return kvc_launch_pdl(kvc_join_split_kernel<T, D, 1>, a, dim3(a.parts.blocks - 1, 16), JOIN_WARPS * 32, 0, st);
 }
@@ -367,9 +373,9 @@ cudaError_t join_shared(const JoinShared &j, cudaStream_t st)
                           JOIN_WARPS * 32, 0, st);
 }
 
-kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, void *stream)
+kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, bool q4, void *stream)
 {
-    kvc_status s = check(lay, d);
+    kvc_status s = check(lay, d, q4);
     if (s != KVC_OK)
         return s;
     if (shared ? (d->window != 0 || d->sinks != 0 || d->n_groups == 0 || d->n_groups > d->n_requests)
@@ -389,8 +395,10 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     if (s != KVC_OK)
         return s;
     const kvc_layout_desc &l = lay->d;
+    const uint32_t head_dim = q4 ? kvc_q4_head_dim(lay) : l.head_dim;
     Shape shape;
-    shape.head_dim = l.head_dim;
+    shape.q4 = q4;
+    shape.head_dim = head_dim;
     shape.hkv = l.num_kv_heads;
     shape.g = d->n_q_heads / l.num_kv_heads;
     shape.tokens = d->n_tokens;
@@ -435,20 +443,24 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     a.status = lay->d_status;
 
     cudaStream_t st = (cudaStream_t)stream;
-    const bool bf16 = d->dtype == KVC_DTYPE_BF16, wide = l.head_dim == 128;
+    const bool bf16 = d->dtype == KVC_DTYPE_BF16, wide = head_dim == 128;
     Carver c = {static_cast<unsigned char *>(d->workspace), 0};
     // Sixteen rows or fewer fit the kernel for few rows, which reads the keys once for them; with more
     // it would read them once for every sixteen, and the matrix unit takes over.  Up to 128 rows it gets one
     // row tile and a deeper ring of keys.  (Whatever the lengths turn out to be, any of the three is right.)
+    // Over a pool held in 4 bits eight rows or fewer are one tile of columns, which leaves registers for a fourth block a SM.
     const uint64_t q_len = std::min<uint64_t>(d->max_q_len ? d->max_q_len : d->n_tokens, d->n_tokens);
     const auto kernel_rows = [&](uint64_t tokens) {
         const uint64_t rows = tokens * a.g;
+        if (q4 && rows <= KVC_ATTN_FEW_ROWS)
+            return KVC_ATTN_FEW_ROWS;
         return rows <= KVC_ATTN_SMALL_ROWS ? KVC_ATTN_SMALL_ROWS : rows <= KVC_ATTN_TILE_ROWS ? KVC_ATTN_TILE_ROWS : KVC_ATTN_MANY_ROWS;
     };
     const auto launch = [&]() {
         ++lay->launches;
-        return a.parts.rows == KVC_ATTN_SMALL_ROWS ? kvc_launch_attn_rows(a, d->dtype, l.head_dim, a.parts.blocks, st)
-                                                   : kvc_launch_attn_tiles(a, d->dtype, l.head_dim, a.parts.blocks, st);
+        const bool few = a.parts.rows <= KVC_ATTN_SMALL_ROWS;
+        return (q4 ? (few ? kvc_launch_attn_q4_rows : kvc_launch_attn_q4_tiles) : few ? kvc_launch_attn_rows : kvc_launch_attn_tiles)(
+            a, d->dtype, head_dim, a.parts.blocks, st);
     };
     cudaError_t e;
     if (!shared) {
@@ -486,12 +498,8 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     return KVC_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-kvc_status kvc_attention_workspace_bytes(kvc_layout *lay, uint32_t n_tokens, uint32_t n_requests, uint32_t n_q_heads,
-                                         uint32_t n_groups, uint64_t *bytes)
+kvc_status workspace(kvc_layout *lay, uint32_t n_tokens, uint32_t n_requests, uint32_t n_q_heads, uint32_t n_groups, bool q4,
+                     uint64_t *bytes)
 {
     if (!lay || !bytes)
         return KVC_ERR_INVALID_ARG;
@@ -502,7 +510,7 @@ kvc_status kvc_attention_workspace_bytes(kvc_layout *lay, uint32_t n_tokens, uin
     d.n_requests = n_requests;
     d.n_q_heads = n_q_heads;
     d.scale = 1.f;
-    kvc_status s = check(lay, &d);
+    kvc_status s = check(lay, &d, q4);
     if (s != KVC_OK)
         return s;
     if (n_groups > n_requests)
@@ -511,7 +519,8 @@ kvc_status kvc_attention_workspace_bytes(kvc_layout *lay, uint32_t n_tokens, uin
     if (s != KVC_OK)
         return s;
     Shape shape;
-    shape.head_dim = lay->d.head_dim;
+    shape.q4 = q4;
+    shape.head_dim = q4 ? kvc_q4_head_dim(lay) : lay->d.head_dim;
     shape.hkv = lay->d.num_kv_heads;
     shape.g = n_q_heads / lay->d.num_kv_heads;
     shape.tokens = n_tokens;
@@ -521,14 +530,40 @@ kvc_status kvc_attention_workspace_bytes(kvc_layout *lay, uint32_t n_tokens, uin
     return KVC_OK;
 }
 
+}  // namespace
+
+extern "C" {
+
+kvc_status kvc_attention_workspace_bytes(kvc_layout *lay, uint32_t n_tokens, uint32_t n_requests, uint32_t n_q_heads,
+                                         uint32_t n_groups, uint64_t *bytes)
+{
+    return workspace(lay, n_tokens, n_requests, n_q_heads, n_groups, false, bytes);
+}
+
 kvc_status kvc_attention(kvc_layout *lay, const kvc_attention_desc *d, void *stream)
 {
-    return attention(lay, d, false, stream);
+    return attention(lay, d, false, false, stream);
 }
 
 kvc_status kvc_attention_shared(kvc_layout *lay, const kvc_attention_desc *d, void *stream)
 {
-    return attention(lay, d, true, stream);
+    return attention(lay, d, true, false, stream);
+}
+
+kvc_status kvc_attention_q4_workspace_bytes(kvc_layout *lay, uint32_t n_tokens, uint32_t n_requests, uint32_t n_q_heads,
+                                            uint32_t n_groups, uint64_t *bytes)
+{
+    return workspace(lay, n_tokens, n_requests, n_q_heads, n_groups, true, bytes);
+}
+
+kvc_status kvc_attention_q4(kvc_layout *lay, const kvc_attention_desc *d, void *stream)
+{
+    return attention(lay, d, false, true, stream);
+}
+
+kvc_status kvc_attention_q4_shared(kvc_layout *lay, const kvc_attention_desc *d, void *stream)
+{
+    return attention(lay, d, true, true, stream);
 }
 
 }  // extern "C"

@@ -23,7 +23,8 @@
 #include "kvc_device.h"
 #include "kvc_internal.h"
 
-#define KVC_ATTN_SMALL_ROWS 16u   // rows of a pair in the kernel for few rows
+#define KVC_ATTN_FEW_ROWS 8u      // rows of a pair in the kernel for few rows of a pool in 4 bits, with one tile of columns
+#define KVC_ATTN_SMALL_ROWS 16u   // rows of a pair in the kernels for few rows
 #define KVC_ATTN_TILE_ROWS 128u   // and in the kernel for many, with one row tile
 #define KVC_ATTN_MANY_ROWS 256u   // or two
 
@@ -90,6 +91,10 @@ uint32_t kvc_attn_rows_blocks(const kvc_layout *lay, bool shared);
 cudaError_t kvc_launch_attn_rows(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
 uint32_t kvc_attn_tiles_blocks(const kvc_layout *lay);
 cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
+// The same for a pool held in 4 bits: kvc_attention_q4_rows.cu (pairs of 8 or 16 rows), kvc_attention_tiles.cu.
+uint32_t kvc_attn_q4_rows_blocks(const kvc_layout *lay, uint32_t rows);
+cudaError_t kvc_launch_attn_q4_rows(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
+cudaError_t kvc_launch_attn_q4_tiles(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st);
 
 #ifdef __CUDACC__
 

@@ -1,0 +1,552 @@
+// Attention over a pool held in 4 bits for few query rows (decode): at most 16 rows share a KV head's keys.
+//
+// The mathematics of kvc_attention_rows.cu: one pass with the running maximum and sum of a softmax, in 32 bits and base
+// 2.  What differs is where the values come from.  With codes c, step s and offset f of each group of 32,
+//     q . k = sum over groups of (s * sum_d q_d c_d + f * sum_d q_d):
+// the codes are exact in the model's 16-bit type, so the first product runs on them, and the steps and offsets
+// multiply its 32-bit sums, four a key.  Values cannot be taken apart like that -- their sum is over keys, each
+// with its own step -- so they become f + s * c in that type (rounded once, as a 16-bit pool would hold them).
+//
+// Keys are the rows of the matrix instruction and queries its columns (16 x 8), since a KV head has 4 or 8 queries where
+// one token is decoded: no half of a product is wasted, and a code made into a number serves all columns.  Any order of
+// the head's values does for a product as long as both operands have it, so a word of eight codes is taken as
+// the pairs (0,4) (1,5) (2,6) (3,7) that its two halves hold side by side: a shift and a merge for two codes.  For
+// values the pairs are two keys, from the halves of two keys' words.  Scores go from accumulator to operand
+// through a transposition of 8 x 8 in registers.
+//
+// A block is four warps, each with its own 32 keys of every 128-key unit and its own ring of stages filled by
+// asynchronous copies; the run of units that a block has, parts and joins are kvc_attention.h's.
+#include "kvc_q4_device.h"
+
+namespace {
+
+constexpr int WARPS = 4;
+constexpr int THREADS = WARPS * 32;
+constexpr int WK = 32;             // keys per warp and unit
+constexpr int TK = WK * WARPS;     // keys per unit
+constexpr int KT = WK / 16;        // key tiles of the matrix instruction
+constexpr int HEAD = 1;            // what a pair costs besides its units, in units
+constexpr int LEAST = 1;           // units of a run at least
+
+template <int D, int NT>
+struct Shape {
+    static constexpr int ROWS = 8 * NT;
+    static constexpr int GROUPS = D / 32;
+    static constexpr int CODES = D / 2;              // bytes of a key's codes
+    static constexpr int SCALES = D / 8;             // and of its steps and offsets, which lie behind them
+    static constexpr int PITCH = D == 128 ? 80 : 48;  // of a key in shared memory: eight keys' words in different banks
+    static constexpr int STAGE = 2 * WK * PITCH;     // K and V of one warp's share of a unit
+    static constexpr int STAGES = D == 128 ? 2 : 3;
+    static constexpr int MERGE = 2 * ROWS * D * 4;   // two warps' sums
+    static constexpr int SMEM = WARPS * STAGES * STAGE + MERGE;
+    static constexpr int MT = D / 16;                // tiles of the second product
+    static constexpr int WORDS = D / 64;             // of codes that a lane takes of a value
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t dst, const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds(uint32_t at)
+{
+    uint32_t r;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(at) : "memory");
+    return r;
+}
+template <int N>
+__device__ __forceinline__ void lds_words(uint32_t (&r)[N], uint32_t at)
+{
+    if (N == 4)
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1 % N]), "=r"(r[2 % N]), "=r"(r[3 % N]) : "r"(at) : "memory");
+    else if (N == 2)
+        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1 % N]) : "r"(at) : "memory");
+    else
+        r[0] = lds(at);
+}
+
+template <typename T>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// 8 x 8 of 16-bit elements: a lane's two are row lane / 4, columns 2 * (lane % 4) and the next, before and after.
+__device__ __forceinline__ uint32_t transpose(uint32_t x)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Where this lane's key of the cursor's unit lies.
+template <int D>
+__device__ __forceinline__ KvcQ4Key look_up(const KvcAttn &a, const KvcCursor &c, uint32_t warp, uint32_t lane)
+{
+    const int32_t j = (int32_t)(kvc_tile(c.r, c.t) * TK + warp * WK + lane);
+    KvcQ4Key k;
+    k.codes = -1;
+    k.scales = 0;
+    if (j < c.r.hi && (j >= c.r.lo || j < c.r.sink_end)) {
+        k = kvc_q4_key<D>(a, c.q.table, j, c.h);
+        if (k.codes < 0)
+            atomicAdd(a.status, 1u);
+    }
+    return k;
+}
+
+// Issues the copies of this warp's keys of one unit; returns which of the 32 are there.  Keys that are not
+// become zeros, steps and offsets too.
+template <int D, int NT>
+__device__ __forceinline__ uint32_t load_unit(const KvcAttn &a, const KvcQ4Key &key, uint32_t lane, uint32_t stage)
+{
+    using S = Shape<D, NT>;
+    constexpr uint32_t CHUNKS = S::CODES / 16, PER = 32 / CHUNKS;  // pieces of a key's codes, keys per round
+    const uint32_t chunk = lane % CHUNKS, sub = lane / CHUNKS;
+#pragma unroll
+    for (uint32_t i = 0; i < WK / PER; ++i) {
+        const uint32_t row = i * PER + sub;
+        const int64_t o = __shfl_sync(~0u, key.codes, row);
+        const uint32_t bytes = o >= 0 ? 16u : 0u, dst = stage + row * S::PITCH + chunk * 16u;
+        const uint64_t at = (o >= 0 ? (uint64_t)o : 0ull) + chunk * 16u;
+        copy16(dst, a.k + at, bytes);
+        copy16(dst + WK * S::PITCH, a.v + at, bytes);
+    }
+    const uint32_t dst = stage + lane * S::PITCH + S::CODES;
+    const uint64_t at = key.codes >= 0 ? (uint64_t)key.codes + key.scales : 0ull;
+    if (S::SCALES == 16) {
+        copy16(dst, a.k + at, key.codes >= 0 ? 16u : 0u);
+        copy16(dst + WK * S::PITCH, a.v + at, key.codes >= 0 ? 16u : 0u);
+    } else {
+        copy8(dst, a.k + at, key.codes >= 0 ? 8u : 0u);
+        copy8(dst + WK * S::PITCH, a.v + at, key.codes >= 0 ? 8u : 0u);
+    }
+    return __ballot_sync(~0u, key.codes >= 0);
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_kernel(const KvcAttn a)
+{
+    using S = Shape<D, NT>;
+    constexpr int ROWS = S::ROWS, G = S::GROUPS;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint32_t s_there[WARPS][S::STAGES];
+    __shared__ float s_m[WARPS][ROWS], s_l[WARPS][ROWS];
+    kvc_pdl_begin(a.beside);
+
+    const uint32_t n_seq = a.phase == KVC_PHASE_PREFIX ? a.n_groups : a.n_requests;
+    const KvcRun run = kvc_find_run<ROWS, TK, HEAD, LEAST, THREADS>(a, n_seq);
+    if (!run.any) {
+        kvc_pdl_end(a.beside);
+        return;
+    }
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t ring = smem_addr(smem) + warp * S::STAGES * S::STAGE;
+    float *merge = reinterpret_cast<float *>(smem + WARPS * S::STAGES * S::STAGE);
+    const uint32_t gr = lane >> 2, gc = lane & 3u;  // row and column pair of an accumulator
+
+    KvcCursor ld = run.at, c = run.at;
+    unsigned long long ld_at = run.units_at, units_at = run.units_at;  // where their pairs' units lie on the line
+    uint32_t pair = run.pair;
+    // the load cursor's unit, if it is in the run, and one step on; places are looked up a unit ahead
+    bool more = true;
+    KvcQ4Key key = look_up<D>(a, ld, warp, lane);
+    const auto load = [&](uint32_t stage) {
+        if (more) {
+            const KvcQ4Key now = key;
+            const uint32_t n = ld.r.n;
+            kvc_next<ROWS, TK>(a, n_seq, ld);
+            if (ld.t == 0)
+                ld_at += n + HEAD;
+            more = ld.s < n_seq && ld_at + ld.t < run.end;
+            if (more)
+                key = look_up<D>(a, ld, warp, lane);
+            const uint32_t there = load_unit<D, NT>(a, now, lane, ring + stage * S::STAGE);
+            if (lane == 0)
+                s_there[warp][stage] = there;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll 1
+    for (uint32_t i = 0; i < S::STAGES - 1; ++i)
+        load(i);
+    uint32_t stage = 0;
+
+    for (uint32_t n_units; c.s < n_seq && (n_units = run.count(c, units_at)) != 0;) {
+        // ---- a new pair (or the rest of one): its queries as matrix operands, D x 8 NT
+        const uint32_t row0 = c.rt * ROWS, rows = min((uint32_t)ROWS, (uint32_t)c.q.rows - row0);
+        uint32_t qf[NT][2 * G][2];
+        float qs[NT][G][2];  // sums of a query's groups, of the two columns of an accumulator
+        int32_t pos[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t i = n * 8 + gr;
+            const bool real = i < rows;
+            const unsigned char *src = a.q;
+            if (real) {
+                const uint32_t row = row0 + i, tok = kvc_div_g(a, row);
+                src += (int64_t)(c.q.qa + (int32_t)tok) * a.q_tok + (int64_t)(c.h * a.g + (row - tok * a.g)) * a.q_head;
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (real)
+                    x = *reinterpret_cast<const uint4 *>(src + g * 64 + gc * 16);
+                qf[n][2 * g][0] = kvc_lows(x.x, x.z);
+                qf[n][2 * g][1] = kvc_highs(x.x, x.z);
+                qf[n][2 * g + 1][0] = kvc_lows(x.y, x.w);
+                qf[n][2 * g + 1][1] = kvc_highs(x.y, x.w);
+                const float2 p = kvc_to_float2<T>(x.x), q = kvc_to_float2<T>(x.y), u = kvc_to_float2<T>(x.z), v = kvc_to_float2<T>(x.w);
+                float sum = ((p.x + p.y) + (q.x + q.y)) + ((u.x + u.y) + (v.x + v.y));
+                sum += __shfl_xor_sync(~0u, sum, 1);
+                sum += __shfl_xor_sync(~0u, sum, 2);
+                qs[n][g][0] = __shfl_sync(~0u, sum, gc * 8);
+                qs[n][g][1] = __shfl_sync(~0u, sum, gc * 8 + 4);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t col = n * 8 + gc * 2 + e;  // (a column of no row sees all: it holds up no check)
+                pos[n][e] = col < rows ? kvc_row_pos(a, c.q, row0 + col) : 0x7FFFFFFF;
+            }
+        }
+        float o[NT][S::MT][4];
+        float m[NT][2], l[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int t = 0; t < S::MT; ++t)
+                o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
+            m[n][0] = m[n][1] = -INFINITY;
+            l[n][0] = l[n][1] = 0.f;
+        }
+        const bool from_start = c.t == 0;
+        const bool to_end = c.t + n_units == c.r.n;
+
+        for (uint32_t i = 0; i < n_units; ++i) {
+            // the stage that the previous unit used is free once every lane is past its reads
+            __syncwarp();
+            load(stage == 0 ? S::STAGES - 1 : stage - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
+            __syncwarp();
+
+            const uint32_t kb = ring + stage * S::STAGE, vb = kb + WK * S::PITCH;
+            const uint32_t there = s_there[warp][stage];
+            const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + i) * TK + warp * WK);
+            if (there != 0) {
+                float s[KT][NT][4];
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
+                    const uint32_t at = kb + (t * 16 + gr) * S::PITCH;
+                    uint32_t sc[2][G];
+                    lds_words<G>(sc[0], at + S::CODES);
+                    lds_words<G>(sc[1], at + 8 * S::PITCH + S::CODES);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const uint32_t w0 = lds(at + g * 16 + gc * 4), w1 = lds(at + 8 * S::PITCH + g * 16 + gc * 4);
+                        float acc[NT][4];
+                        constexpr bool BIASED = std::is_same<T, __nv_bfloat16>::value;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            // bf16: the bias of the codes is taken off beforehand, in the 32-bit sums (2^-17 of it is what
+                            // they lose); fp16's is 8 times as large and comes off the codes
+                            acc[n][0] = acc[n][2] = BIASED ? -KvcQ4<T>::BIAS * qs[n][g][0] : 0.f;
+                            acc[n][1] = acc[n][3] = BIASED ? -KvcQ4<T>::BIAS * qs[n][g][1] : 0.f;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            uint32_t f[4] = {kvc_q4_biased<T>(w0 >> (8 * k)), kvc_q4_biased<T>(w1 >> (8 * k)),
+                                             kvc_q4_biased<T>(w0 >> (8 * k + 4)), kvc_q4_biased<T>(w1 >> (8 * k + 4))};
+                            if (!BIASED)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    f[e] = kvc_q4_plain<T>(f[e]);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+                                mma<T>(acc[n], f, qf[n][2 * g + k][0], qf[n][2 * g + k][1]);
+                        }
+                        const float2 x0 = kvc_to_float2<T>(sc[0][g]), x1 = kvc_to_float2<T>(sc[1][g]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float2 x = e < 2 ? x0 : x1;
+                                s[t][n][e] = fmaf(x.x, acc[n][e], fmaf(x.y, qs[n][g][e & 1], s[t][n][e]));
+                            }
+                    }
+                }
+                // scores in base 2; where some row does not see all of the warp's keys, those it does not become -inf
+                bool all = there == ~0u;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        all = all && j0 + WK - 1 <= pos[n][e] && (a.window == 0 || pos[n][e] - j0 < a.window || j0 + WK <= a.sinks);
+                all = __all_sync(~0u, all);
+                float top[NT][2];
+                bool moved = false;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[t][n][e] *= a.scale_log2;
+                            if (!all) {
+                                const int k = t * 16 + (e >> 1) * 8 + (int)gr;
+                                if (!((there >> k & 1u) && kvc_sees(a, pos[n][e & 1], j0 + k)))
+                                    s[t][n][e] = -INFINITY;
+                            }
+                        }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float x = fmaxf(s[0][n][e], s[0][n][e + 2]);
+#pragma unroll
+                        for (int t = 1; t < KT; ++t)
+                            x = fmaxf(x, fmaxf(s[t][n][e], s[t][n][e + 2]));
+                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                        top[n][e] = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                        moved |= top[n][e] > m[n][e];
+                    }
+                }
+                if (__any_sync(~0u, moved)) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float now = fmaxf(m[n][e], top[n][e]);
+                            const float f = m[n][e] == -INFINITY ? 0.f : exp2_fast(m[n][e] - now);
+                            m[n][e] = now;
+                            l[n][e] *= f;
+#pragma unroll
+                            for (int t = 0; t < S::MT; ++t) {
+                                o[n][t][e] *= f;
+                                o[n][t][e + 2] *= f;
+                            }
+                        }
+                }
+                uint32_t p[KT][NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float base0 = m[n][0] == -INFINITY ? 0.f : m[n][0], base1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
+#pragma unroll
+                    for (int t = 0; t < KT; ++t) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[t][n][e] = exp2_fast(s[t][n][e] - (e & 1 ? base1 : base0));
+                            l[n][e & 1] += s[t][n][e];
+                        }
+                        p[t][n][0] = transpose(kvc_from_float2<T>(s[t][n][0], s[t][n][1]));
+                        p[t][n][1] = transpose(kvc_from_float2<T>(s[t][n][2], s[t][n][3]));
+                    }
+                }
+                // ---- values: of keys 2 gc, 2 gc + 1 and the same + 8, the codes of words WORDS * gr ..
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    uint32_t w[4][S::WORDS], sc[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t at = vb + (t * 16 + gc * 2 + (r & 1) + (r >> 1) * 8) * S::PITCH;
+                        lds_words<S::WORDS>(w[r], at + gr * (4 * S::WORDS));
+                        sc[r] = lds(at + S::CODES + gr * S::WORDS / 4 * 4);
+                    }
+                    const uint32_t step0 = kvc_lows(sc[0], sc[1]), off0 = kvc_highs(sc[0], sc[1]);
+                    const uint32_t step1 = kvc_lows(sc[2], sc[3]), off1 = kvc_highs(sc[2], sc[3]);
+#pragma unroll
+                    for (int u = 0; u < S::WORDS; ++u) {
+                        const uint32_t x0 = kvc_lows(w[0][u], w[1][u]), y0 = kvc_highs(w[0][u], w[1][u]);
+                        const uint32_t x1 = kvc_lows(w[2][u], w[3][u]), y1 = kvc_highs(w[2][u], w[3][u]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t f[4] = {
+                                kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(x0 >> (4 * k))), step0, off0),
+                                kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(y0 >> (4 * k))), step0, off0),
+                                kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(x1 >> (4 * k))), step1, off1),
+                                kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(y1 >> (4 * k))), step1, off1)};
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+                                mma<T>(o[n][u * 4 + k], f, p[t][n][0], p[t][n][1]);
+                        }
+                    }
+                }
+            }
+            stage = stage == S::STAGES - 1 ? 0 : stage + 1;
+        }
+
+        // ---- end of the pair, or of the run: join the four warps' parts
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                l[n][e] += __shfl_xor_sync(~0u, l[n][e], 4);
+                l[n][e] += __shfl_xor_sync(~0u, l[n][e], 8);
+                l[n][e] += __shfl_xor_sync(~0u, l[n][e], 16);
+            }
+        __syncthreads();  // the join before this one is over
+        if (gr == 0)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    s_m[warp][n * 8 + gc * 2 + e] = m[n][e];
+                    s_l[warp][n * 8 + gc * 2 + e] = l[n][e];
+                }
+        __syncthreads();
+        float tm[NT][2], tl[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t col = n * 8 + gc * 2 + e;
+                tm[n][e] = s_m[0][col];
+#pragma unroll
+                for (int w = 1; w < WARPS; ++w)
+                    tm[n][e] = fmaxf(tm[n][e], s_m[w][col]);
+                const float ref = tm[n][e] == -INFINITY ? 0.f : tm[n][e];
+                tl[n][e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w)
+                    tl[n][e] += s_l[w][col] * exp2f(s_m[w][col] - ref);
+                const float f = exp2f(m[n][e] - ref);
+#pragma unroll
+                for (int t = 0; t < S::MT; ++t) {
+                    o[n][t][e] *= f;
+                    o[n][t][e + 2] *= f;
+                }
+            }
+        // 3 + 2 -> 1 + 0 -> 0, each lane reading back the places that its partner's lane wrote
+#pragma unroll
+        for (uint32_t step = 2; step; step /= 2) {
+            if (warp >= step && warp < 2 * step) {
+                float4 *dst = reinterpret_cast<float4 *>(merge) + (warp - step) * (ROWS * D / 4) + lane;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int t = 0; t < S::MT; ++t)
+                        dst[(n * S::MT + t) * 32] = make_float4(o[n][t][0], o[n][t][1], o[n][t][2], o[n][t][3]);
+            }
+            __syncthreads();
+            if (warp < step) {
+                const float4 *src = reinterpret_cast<const float4 *>(merge) + warp * (ROWS * D / 4) + lane;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int t = 0; t < S::MT; ++t) {
+                        const float4 v = src[(n * S::MT + t) * 32];
+                        o[n][t][0] += v.x;
+                        o[n][t][1] += v.y;
+                        o[n][t][2] += v.z;
+                        o[n][t][3] += v.w;
+                    }
+            }
+            if (step > 1)
+                __syncthreads();
+        }
+        if (warp == 0) {
+            const bool whole = a.phase == KVC_PHASE_WHOLE && from_start && to_end;
+            const bool room = a.phase == KVC_PHASE_WHOLE || pair < a.parts.max_pairs;
+            const uint64_t slot = a.phase == KVC_PHASE_WHOLE ? 2ull * blockIdx.x + (from_start ? 1 : 0) : (uint64_t)blockIdx.x + pair;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t col = n * 8 + gc * 2 + e;
+                    if (col >= rows)
+                        continue;
+                    // words WORDS * gr ..: value k of a word is in tile k, row gr, value 4 + k in row gr + 8
+                    if (whole) {
+                        const uint32_t row = row0 + col, t = kvc_div_g(a, row);
+                        const int64_t tok = c.q.qa + (int32_t)t;
+                        const uint32_t head = c.h * a.g + (row - t * a.g);
+                        const float inv = tl[n][e] == 0.f ? 0.f : 1.f / tl[n][e];  // a row that sees nothing: zeros
+                        unsigned char *dst = a.out + tok * a.o_tok + (int64_t)head * a.o_head + gr * (16 * S::WORDS);
+#pragma unroll
+                        for (int u = 0; u < S::WORDS; ++u) {
+                            const auto x = [&](int k) { return o[n][u * 4 + (k & 3)][e + (k >> 2) * 2] * inv; };
+                            *reinterpret_cast<uint4 *>(dst + u * 16) =
+                                make_uint4(kvc_from_float2<T>(x(0), x(1)), kvc_from_float2<T>(x(2), x(3)),
+                                           kvc_from_float2<T>(x(4), x(5)), kvc_from_float2<T>(x(6), x(7)));
+                        }
+                        if (a.lse && gr == 0)
+                            a.lse[tok * a.hq + head] = (tm[n][e] + log2f(tl[n][e])) * 0.693147180559945309f;
+                    } else if (room) {
+                        const uint64_t at = slot * ROWS + col;
+                        float *dst = a.parts.o + at * D + gr * (8 * S::WORDS);
+#pragma unroll
+                        for (int u = 0; u < S::WORDS; ++u) {
+                            const auto x = [&](int k) { return o[n][u * 4 + (k & 3)][e + (k >> 2) * 2]; };
+                            *reinterpret_cast<float4 *>(dst + u * 8) = make_float4(x(0), x(1), x(2), x(3));
+                            *reinterpret_cast<float4 *>(dst + u * 8 + 4) = make_float4(x(4), x(5), x(6), x(7));
+                        }
+                        if (gr == 0)
+                            a.parts.ml[at] = make_float2(tm[n][e], tl[n][e]);
+                    }
+                }
+            if (a.phase != KVC_PHASE_WHOLE && room && from_start && lane == 0)
+                a.parts.range[pair] = make_ulonglong2(units_at, units_at + c.r.n);
+        }
+        if (to_end) {
+            units_at += c.r.n + HEAD;
+            ++pair;
+        }
+        c.t += n_units - 1;
+        kvc_next<ROWS, TK>(a, n_seq, c);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    kvc_pdl_end(a.beside);
+}
+
+template <typename T, int D, int NT>
+cudaError_t launch(const KvcAttn &a, uint32_t blocks, cudaStream_t st)
+{
+    using S = Shape<D, NT>;
+    const cudaError_t e = cudaFuncSetAttribute(kvc_attn_q4_rows_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    if (e != cudaSuccess)
+        return e;
+    return kvc_launch_pdl(kvc_attn_q4_rows_kernel<T, D, NT>, a, dim3(blocks), THREADS, S::SMEM, st);
+}
+
+template <typename T>
+cudaError_t launch_type(const KvcAttn &a, uint32_t head_dim, uint32_t blocks, cudaStream_t st)
+{
+    if (a.parts.rows == KVC_ATTN_FEW_ROWS)
+        return head_dim == 128 ? launch<T, 128, 1>(a, blocks, st) : launch<T, 64, 1>(a, blocks, st);
+    return head_dim == 128 ? launch<T, 128, 2>(a, blocks, st) : launch<T, 64, 2>(a, blocks, st);
+}
+
+}  // namespace
+
+// As many blocks as are resident.
+uint32_t kvc_attn_q4_rows_blocks(const kvc_layout *lay, uint32_t rows) { return (rows == KVC_ATTN_FEW_ROWS ? 4u : 3u) * (uint32_t)lay->sm_count; }
+
+cudaError_t kvc_launch_attn_q4_rows(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st)
+{
+    return dtype == KVC_DTYPE_BF16 ? launch_type<__nv_bfloat16>(a, head_dim, blocks, st) : launch_type<__half>(a, head_dim, blocks, st);
+}

@@ -37,7 +37,7 @@
 #include <stddef.h>
 #include <string.h>
 
-#include "kvc_attention.h"
+#include "kvc_q4_device.h"
 
 namespace {
 
@@ -51,13 +51,21 @@ constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper t
 // ROWS is 256, two row tiles a block, or 128, one: half the queries then make room for a third K stage, which long
 // runs of keys gain by (one request of drafted tokens behind 80,000: 85.4 us with 256, 83.6 with 128; 32 questions on a
 // 32,000-token document 71.2 and 69.5; but 16 requests of drafted tokens behind 16,000 202.4 and 204.5).
-template <int D, int ROWS>
+//
+// Q4: a pool held in 4 bits.  Its keys pass through a ring of parts (32 keys as they lie in the pool) on their way to a stage.
+// With 256 rows one warp makes a tile of values of them, K or V, and with 128, where the softmax warps of the
+// second row tile have none, four do: its pace is that of the loads then, not of the softmax.
+template <int D, int ROWS, bool Q4>
 struct Shape {
     static constexpr int TILE = TK * D * 2;           // a K or V tile; also the queries of a row tile
     static constexpr int HALF = TK * 128;             // 64 elements (128 bytes) of 128 rows
-    static constexpr int KS = D == 64 ? 4 : ROWS == 128 ? 3 : 2, VS = D == 64 ? 4 : 2;
-    static constexpr int Q = 0, K = ROWS / 128 * TILE, V = K + KS * TILE, END = V + VS * TILE;
+    static constexpr int KS = D == 64 ? 4 : ROWS == 128 && !Q4 ? 3 : 2, VS = D == 64 ? 4 : 2;
+    static constexpr int WARPS = ROWS == 128 ? 4 : 1, PARTS = ROWS == 128 ? 3 : 5;  // Q4: that load K, and V; parts of each
+    static constexpr int PITCH = D == 128 ? 80 : 48, PART = 32 * PITCH;              // Q4: of a key, bytes of a part
+    static constexpr int RAW_BYTES = Q4 ? 2 * WARPS * PARTS * PART : 0;
+    static constexpr int Q = 0, K = ROWS / 128 * TILE, V = K + KS * TILE, RAW = V + VS * TILE, END = RAW + RAW_BYTES;
     static constexpr int SMEM = END + 1024;           // room to align the stages to the swizzle's 1024 bytes
+    static_assert(SMEM + (ROWS == 128 ? 5 : 8) * 1024 <= 227 * 1024, "with the kernel's own variables");
 };
 
 // tensor memory columns
@@ -299,7 +307,7 @@ template <int D, int ROWS, bool KEYS>
 __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *segments, uint32_t tiles, Bars *bars,
                                           uint32_t (*there)[4], volatile uint32_t *dead, uint32_t lane)
 {
-    using S = Shape<D, ROWS>;
+    using S = Shape<D, ROWS, false>;
     constexpr int STAGES = KEYS ? S::KS : S::VS;
     constexpr int PER = 512 / (D * 2);  // keys per round of 32 lanes
     constexpr uint32_t NONE = ~0u;
@@ -410,17 +418,151 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
             ;
 }
 
-template <typename T, int D, int ROWS>
+// One of the warps that load K or V of a pool held in 4 bits: all tiles of the block's run, 32 keys at a time.  Codes
+// and scales are copied as they lie, PARTS - 1 ahead and across segments; a lane then makes one key's values,
+// offset + step * code in the model's type, and writes them where the matrix unit reads them.  What is no key's comes as
+// zeros and stays zeros.  A word of eight codes gives the pairs (0,4) (1,5) (2,6) (3,7); K keeps that order, which
+// the queries are given too, and V's is put right.
+template <typename T, int D, int ROWS, bool KEYS>
+__device__ __forceinline__ void load_role_q4(const KvcAttn &a, const Segment *segments, uint32_t tiles, uint32_t raw, uint32_t *raw_there,
+                                             Bars *bars, uint32_t (*there)[4], volatile uint32_t *dead, uint32_t sub, uint32_t lane)
+{
+    using S = Shape<D, ROWS, true>;
+    constexpr int STAGES = KEYS ? S::KS : S::VS, GROUPS = D / 32;
+    constexpr uint32_t CHUNKS = D / 32, PER = 32 / CHUNKS;  // 16-byte pieces of a key's codes, keys per round of copies
+    constexpr uint32_t LAST = 4 - S::WARPS;                 // a warp takes parts sub, sub + WARPS, ..
+    const uint32_t full = smem_addr(KEYS ? bars->k_full : bars->v_full), empty = smem_addr(KEYS ? bars->k_empty : bars->v_empty);
+    const unsigned char *plane = KEYS ? a.k : a.v;
+    SegmentReader reader;
+    Segment c;
+    bool more = reader.next(segments, bars, c, dead, a.status);
+    uint32_t u = 0, part = 0;  // of the next part that is loaded: tile, place in it
+    KvcQ4Key key;
+    const auto look = [&]() {
+        const int32_t j = (int32_t)(kvc_tile(c.r, c.t + u) * TK + (part + sub) * 32u + lane);
+        key.codes = -1;
+        key.scales = 0;
+        if (j < c.r.hi && (j >= c.r.lo || j < c.r.sink_end)) {
+            key = kvc_q4_key<D>(a, c.q.table, j, c.h);
+            if (KEYS && key.codes < 0)
+                atomicAdd(a.status, 1u);
+        }
+    };
+    if (more)
+        look();
+    uint32_t loaded = 0, used = 0, to = 0, from = 0;  // parts, and their places in the ring
+    const auto load = [&]() {
+        if (more) {
+            const uint32_t dst = raw + to * S::PART;
+            const uint32_t chunk = lane % CHUNKS, row0 = lane / CHUNKS;
+#pragma unroll
+            for (uint32_t i = 0; i < 32 / PER; ++i) {
+                const uint32_t row = i * PER + row0;
+                const int64_t o = __shfl_sync(~0u, key.codes, row);
+                copy16(dst + row * S::PITCH + chunk * 16u, plane + (o >= 0 ? o : 0) + chunk * 16u, o >= 0 ? 16u : 0u);
+            }
+            const bool is = key.codes >= 0;
+            const unsigned char *src = plane + (is ? key.codes + key.scales : 0);
+            const uint32_t at = dst + lane * S::PITCH + D / 2;
+            if (D == 128)
+                copy16(at, src, is ? 16u : 0u);
+            else
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(at), "l"(src), "r"(is ? 8u : 0u) : "memory");
+            if (KEYS) {
+                const uint32_t w = __ballot_sync(~0u, is);
+                if (lane == 0)
+                    raw_there[to] = w;
+            }
+            // the next part, whose place is looked up while this one is on its way
+            ++loaded;
+            part += S::WARPS;
+            if (part > LAST) {
+                part = 0;
+                if (++u == c.n) {
+                    u = 0;
+                    more = reader.next(segments, bars, c, dead, a.status);
+                }
+            }
+            if (more)
+                look();
+            to = to == S::PARTS - 1 ? 0 : to + 1;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll 1
+    for (int i = 0; i < S::PARTS - 1; ++i)
+        load();
+    Ring<STAGES> ring;
+    uint32_t slot = 0, at = 0;  // at: place of the used part in its tile
+#pragma unroll 1
+    for (;;) {
+        load();
+        if (used == loaded)
+            break;
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::PARTS - 1) : "memory");
+        __syncwarp();
+        if (at == 0 && !__all_sync(~0u, bar_wait(empty + ring.stage * 8u, ring.parity ^ 1u, dead, a.status)))
+            break;
+        if (KEYS && lane == 0)
+            there[slot][at + sub] = raw_there[from];
+        const uint32_t src = raw + from * S::PART + lane * S::PITCH, row = (at + sub) * 32u + lane;
+        const uint32_t dst = tiles + ring.stage * S::TILE + row * 128u;
+        uint32_t sc[4];
+        if (D == 128)
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(sc[0]), "=r"(sc[1]), "=r"(sc[2]), "=r"(sc[3]) : "r"(src + D / 2) : "memory");
+        else
+            asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(src + D / 2) : "memory");
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src + g * 16u) : "memory");
+            const uint32_t step = kvc_lows(sc[g], sc[g]), offset = kvc_highs(sc[g], sc[g]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[e] = kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(w[k] >> (4 * e))), step, offset);
+                const uint32_t chunk = g * 4 + k, to = dst + (chunk >> 3) * S::HALF + (((chunk & 7u) ^ (lane & 7u)) << 4);
+                if (KEYS)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                else
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(kvc_lows(x[0], x[1])), "r"(kvc_lows(x[2], x[3])),
+                                 "r"(kvc_highs(x[0], x[1])), "r"(kvc_highs(x[2], x[3])) : "memory");
+            }
+        }
+        ++used;
+        from = from == S::PARTS - 1 ? 0 : from + 1;
+        at += S::WARPS;
+        if (at > LAST) {
+            at = 0;
+            fence_async();
+            __syncwarp();
+            if (lane == 0)
+                bar_arrive(full + ring.stage * 8u);
+            ring.next();
+            slot = (slot + 1) % THERE;
+        }
+        __syncwarp();  // all have read the part, whose place the next copies take
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+template <typename T, int D, int ROWS, bool Q4>
 __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid_constant__ TilesArgs args)
 {
-    using S = Shape<D, ROWS>;
+    using S = Shape<D, ROWS, Q4>;
+    constexpr bool HELPED = Q4 && ROWS == 128;  // warps 8-15 load
+    constexpr uint32_t READERS = HELPED ? SEGMENT_READERS - 2 : SEGMENT_READERS;
+    constexpr uint32_t LOADERS = Q4 ? S::WARPS : 1;
     const KvcAttn &a = args.a;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Bars bars;
     __shared__ __align__(16) uint32_t there[THERE][4];
     __shared__ uint32_t s_dead, s_tmem;
     __shared__ Segment segments[SEGMENTS];
-    __shared__ float row_top[2][2][2][128], row_sum[2][2][128];  // ([tile of keys, odd or even])[row tile][half][row]
+    __shared__ uint32_t raw_there[S::WARPS][S::PARTS];
+    __shared__ float row_top[2][ROWS / 128][2][128], row_sum[ROWS / 128][2][128];  // ([tile of keys, odd or even])[row tile][half][row]
     // What touches no memory of the caller's comes before the wait for the stream's previous kernel.
     const uint32_t warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31u;
     const uint32_t tiles = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -438,16 +580,16 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             bar_init(smem_addr(&bars.o_done[i]), 1);
         }
         for (int i = 0; i < 4; ++i) {
-            bar_init(smem_addr(&bars.k_full[i]), 1);
+            bar_init(smem_addr(&bars.k_full[i]), LOADERS);
             bar_init(smem_addr(&bars.k_empty[i]), 1);
-            bar_init(smem_addr(&bars.v_full[i]), 1);
+            bar_init(smem_addr(&bars.v_full[i]), LOADERS);
             bar_init(smem_addr(&bars.v_empty[i]), 1);
             bar_init(smem_addr(&bars.seg_full[i]), 1);
-            bar_init(smem_addr(&bars.seg_empty[i]), SEGMENT_READERS);
+            bar_init(smem_addr(&bars.seg_empty[i]), READERS);
         }
         bar_init(smem_addr(&bars.drained), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        if (args.boxes) {
+        if (!Q4 && args.boxes) {
             asm volatile("prefetch.tensormap [%0];" ::"l"(&args.k_map) : "memory");
             asm volatile("prefetch.tensormap [%0];" ::"l"(&args.v_map) : "memory");
         }
@@ -473,6 +615,14 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     if (warp < 16) {
         // registers: 512 x 104 + 128 x 64 = 640 x 96 of the launch
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    }
+    if (HELPED && warp >= 8 && warp < 16) {
+        const uint32_t w = warp & 3u, raw = tiles + S::RAW + w * (S::PARTS * S::PART);
+        if (warp < 12)
+            load_role_q4<T, D, ROWS, true>(a, segments, tiles + S::K, raw, raw_there[w % S::WARPS], &bars, there, dead, w, lane);
+        else
+            load_role_q4<T, D, ROWS, false>(a, segments, tiles + S::V, raw + S::WARPS * S::PARTS * S::PART, nullptr, &bars, there, dead, w, lane);
+    } else if (warp < 16) {
         // ---------------------------------------------------------------- softmax
         const uint32_t sub = warp >> 3, half = warp >> 2 & 1u, tid = threadIdx.x & 127u;  // tid: the row
         const uint32_t lanes = (warp & 3u) << 21;  // this warp's 32 rows of tensor memory
@@ -521,6 +671,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
 #pragma unroll
             for (uint32_t e = 0; e < TURNS; ++e) {
                 const uint32_t r = r0 + e * STEP;
+                if (Q4)  // the order that the keys' values come in
+                    x[e] = make_uint4(kvc_lows(x[e].x, x[e].z), kvc_highs(x[e].x, x[e].z), kvc_lows(x[e].y, x[e].w), kvc_highs(x[e].y, x[e].w));
                 *reinterpret_cast<uint4 *>(dst + r * 128u + (((chunk & 7u) ^ (r & 7u)) << 4)) = x[e];
             }
             fence_async();
@@ -734,9 +886,15 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 17) {
-            load_role<D, ROWS, true>(args, segments, tiles + S::K, &bars, there, dead, lane);
+            if constexpr (!Q4)
+                load_role<D, ROWS, true>(args, segments, tiles + S::K, &bars, there, dead, lane);
+            else if constexpr (!HELPED)
+                load_role_q4<T, D, ROWS, true>(a, segments, tiles + S::K, tiles + S::RAW, raw_there[0], &bars, there, dead, 0, lane);
         } else if (warp == 18) {
-            load_role<D, ROWS, false>(args, segments, tiles + S::V, &bars, there, dead, lane);
+            if constexpr (!Q4)
+                load_role<D, ROWS, false>(args, segments, tiles + S::V, &bars, there, dead, lane);
+            else if constexpr (!HELPED)
+                load_role_q4<T, D, ROWS, false>(a, segments, tiles + S::V, tiles + S::RAW + S::PARTS * S::PART, nullptr, &bars, there, dead, 0, lane);
         } else if (warp == 16) {
             // ------------------------------------------------------------ matrix instructions
             // The unit takes few instructions ahead, so what this thread does between them is time that
@@ -922,20 +1080,28 @@ bool encode(EncodeTiled fn, CUtensorMap *map, const KvcAttn &a, const unsigned c
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int D, int ROWS>
+template <typename T, int D, int ROWS, bool Q4>
 cudaError_t launch(const TilesArgs &args, uint32_t blocks, cudaStream_t st)
 {
-    const cudaError_t e = cudaFuncSetAttribute(kvc_attn_tiles_kernel<T, D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               Shape<D, ROWS>::SMEM);
+    using S = Shape<D, ROWS, Q4>;
+    const cudaError_t e = cudaFuncSetAttribute(kvc_attn_tiles_kernel<T, D, ROWS, Q4>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     if (e != cudaSuccess)
         return e;
-    return kvc_launch_pdl(kvc_attn_tiles_kernel<T, D, ROWS>, args, dim3(blocks), THREADS, Shape<D, ROWS>::SMEM, st);
+    return kvc_launch_pdl(kvc_attn_tiles_kernel<T, D, ROWS, Q4>, args, dim3(blocks), THREADS, S::SMEM, st);
 }
 
-template <typename T, int D>
+template <bool Q4, typename T, int D>
 cudaError_t launch_rows(const TilesArgs &args, uint32_t blocks, cudaStream_t st)
 {
-    return args.a.parts.rows == 128 ? launch<T, D, 128>(args, blocks, st) : launch<T, D, 256>(args, blocks, st);
+    return args.a.parts.rows == 128 ? launch<T, D, 128, Q4>(args, blocks, st) : launch<T, D, 256, Q4>(args, blocks, st);
+}
+
+template <bool Q4>
+cudaError_t launch_type(const TilesArgs &args, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st)
+{
+    if (dtype == KVC_DTYPE_BF16)
+        return head_dim == 128 ? launch_rows<Q4, __nv_bfloat16, 128>(args, blocks, st) : launch_rows<Q4, __nv_bfloat16, 64>(args, blocks, st);
+    return head_dim == 128 ? launch_rows<Q4, __half, 128>(args, blocks, st) : launch_rows<Q4, __half, 64>(args, blocks, st);
 }
 
 }  // namespace
@@ -960,7 +1126,13 @@ cudaError_t kvc_launch_attn_tiles(const KvcAttn &a, uint32_t dtype, uint32_t hea
             !encode(fn, &args.v_map, a, a.v, dtype, head_dim, args.box_keys))
             args.boxes = 0;  // a pool that no map describes
     }
-    if (dtype == KVC_DTYPE_BF16)
-        return head_dim == 128 ? launch_rows<__nv_bfloat16, 128>(args, blocks, st) : launch_rows<__nv_bfloat16, 64>(args, blocks, st);
-    return head_dim == 128 ? launch_rows<__half, 128>(args, blocks, st) : launch_rows<__half, 64>(args, blocks, st);
+    return launch_type<false>(args, dtype, head_dim, blocks, st);
+}
+
+cudaError_t kvc_launch_attn_q4_tiles(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st)
+{
+    TilesArgs args;
+    memset(&args, 0, sizeof(args));
+    args.a = a;
+    return launch_type<true>(args, dtype, head_dim, blocks, st);
 }

@@ -154,6 +154,16 @@ inline const unsigned char *kvc_plane_ptr(const kvc_layout *lay, uint32_t l, uin
            (uint64_t)p * lay->d.plane_stride;
 }
 
+// Pools held in 4 bits: the head dimension that a layout's rows are of (0: it is none of theirs), and whether a KV
+// head's rows of a block end on 16 bytes.
+inline uint32_t kvc_q4_head_dim(const kvc_layout *lay)
+{
+    if (lay->d.kv_planes != 2 || lay->d.elem_bytes != 1)
+        return 0;
+    return lay->d.head_dim == KVC_Q4_ROW_BYTES(128) ? 128u : lay->d.head_dim == KVC_Q4_ROW_BYTES(64) ? 64u : 0u;
+}
+inline bool kvc_q4_aligned(const kvc_layout *lay) { return (uint64_t)lay->d.block_size * lay->d.head_dim % 16 == 0; }
+
 // Launches the copy kernel; with kernel timing on, between two events on the same stream.
 kvc_status kvc_launch_timed(kvc_layout *lay, int dir, int variant, const KvcLaunch &a, uint32_t grid,
                             uint32_t smem, cudaStream_t st);

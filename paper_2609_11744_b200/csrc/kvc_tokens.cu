@@ -1,5 +1,6 @@
 // The step's tokens: block tables and slots built from request lengths (kvc_map_tokens), and the
-// per-head norm, rotation and cache write of their queries, keys and values (kvc_append).
+// per-head norm, rotation and cache write of their queries, keys and values (kvc_append, kvc_append_axes;
+// into a pool held in 4 bits kvc_append_q4, and back kvc_read_q4).
 #include <string.h>
 
 #include <algorithm>
@@ -234,6 +235,13 @@ struct AppendArgs {
     uint32_t *status;
 };
 
+// Positions with several axes: which axis turns each pair, a byte a pair.
+struct AppendAxes : AppendArgs {
+    int64_t axis_stride;
+    uint32_t n_axes;
+    uint32_t axis[KVC_MAX_PAIRS / 4];
+};
+
 #define APPEND_THREADS 64u
 // Small blocks, 16 a SM: a block's warps go through the same chain (slot, angles, heads) at the same time, and
 // small ones start and end more evenly (16384 tokens of 64 + 16 heads: 153 us with 256 threads, 141 with 128,
@@ -242,24 +250,118 @@ struct AppendArgs {
 #define APPEND_BLOCKS 16
 #define APPEND_UNROLL 4
 #define APPEND_CHUNK 2
+#define APPEND_Q4_BLOCKS 12
 
 // A lane's eight values as two words of either piece, and as two pairs of floats an operand.
 struct AppendRaw {
     uint2 a, b;
 };
 
+// ---- the 4-bit form (kvc_append_q4): a lane's eight values make one word of codes, four lanes a group.
+
+// A head's values from pieces of the two halves of its rotated part to eight neighbours a lane; the lanes behind
+// the `turned` ones hold theirs already.
+__device__ __forceinline__ AppendRaw append_natural(const AppendRaw &r, uint32_t lane, uint32_t l, uint32_t turned)
+{
+    const bool moves = l < turned, upper = l >= turned / 2;
+    const uint32_t from = moves ? lane - l + 2 * l - (upper ? turned : 0u) : lane, next = moves ? from + 1 : lane;
+    const uint2 a0 = make_uint2(__shfl_sync(~0u, r.a.x, from), __shfl_sync(~0u, r.a.y, from));
+    const uint2 a1 = make_uint2(__shfl_sync(~0u, r.a.x, next), __shfl_sync(~0u, r.a.y, next));
+    const uint2 b0 = make_uint2(__shfl_sync(~0u, r.b.x, from), __shfl_sync(~0u, r.b.y, from));
+    const uint2 b1 = make_uint2(__shfl_sync(~0u, r.b.x, next), __shfl_sync(~0u, r.b.y, next));
+    AppendRaw n;
+    n.a = !moves ? r.a : upper ? b0 : a0;
+    n.b = !moves ? r.b : upper ? b1 : a1;
+    return n;
+}
+
+__device__ __forceinline__ float min_nan(float x, float y)
+{
+    float z;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+__device__ __forceinline__ float max_nan(float x, float y)
+{
+    float z;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+
+// x rounded towards zero to the type (x >= 0), and its value.
+template <typename T>
+__device__ __forceinline__ uint32_t down_bits(float x, float &value);
+template <>
+__device__ __forceinline__ uint32_t down_bits<__nv_bfloat16>(float x, float &value)
+{
+    const __nv_bfloat16 r = __float2bfloat16_rz(x);
+    value = __bfloat162float(r);
+    return __bfloat16_as_ushort(r);
+}
+template <>
+__device__ __forceinline__ uint32_t down_bits<__half>(float x, float &value)
+{
+    const __half r = __float2half_rz(x);
+    value = __half2float(r);
+    return __half_as_ushort(r);
+}
+
+// Codes of the lane's eight values (natural order), and the group's step and offset.  The quotient (x - offset) / step
+// is rounded exactly: its product with the reciprocal is off by 2^-20 at most, so only the choice between two neighbours can
+// be wrong, and the remainder, which fma gives without rounding, decides it.
+template <typename T>
+__device__ __forceinline__ uint32_t append_quantise(const AppendRaw &r, uint32_t &scale)
+{
+    const float2 p = kvc_to_float2<T>(r.a.x), q = kvc_to_float2<T>(r.a.y), u = kvc_to_float2<T>(r.b.x), v = kvc_to_float2<T>(r.b.y);
+    const float x[8] = {p.x, p.y, q.x, q.y, u.x, u.y, v.x, v.y};
+    float low = x[0], high = x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        low = min_nan(low, x[i]);
+        high = max_nan(high, x[i]);
+    }
+#pragma unroll
+    for (int n = 1; n < 4; n *= 2) {
+        low = min_nan(low, __shfl_xor_sync(~0u, low, n));
+        high = max_nan(high, __shfl_xor_sync(~0u, high, n));
+    }
+    float step;
+    scale = down_bits<T>(__fdiv_rn(high - low, 15.f), step) | kvc_from_float2<T>(0.f, low);
+    // (steps whose reciprocal is none are taken 2^64 times as large, like the differences)
+    const float up = step < 0x1p-100f ? 0x1p64f : 1.f;
+    step *= up;
+    const float inv = step > 0.f ? __frcp_rn(step) : 0.f, half = 0.5f * step;
+    float c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float d = (x[i] - low) * up;
+        float n = rintf(d * inv);
+        const float rest = fmaf(-n, step, d);
+        const bool odd = rintf(0.5f * n) != 0.5f * n;
+        if (rest > half || (rest == half && odd))
+            n += 1.f;
+        else if (rest < -half || (rest == -half && odd))
+            n -= 1.f;
+        c[i] = step > 0.f ? fminf(fmaxf(n, 0.f), 15.f) : 0.f;
+    }
+    const float lo = fmaf(4096.f, c[3], fmaf(256.f, c[2], fmaf(16.f, c[1], c[0])));
+    const float hi = fmaf(4096.f, c[7], fmaf(256.f, c[6], fmaf(16.f, c[5], c[4])));
+    return __float2uint_rn(lo) | __float2uint_rn(hi) << 16;
+}
+
 // NEIGHBOURS: pairs are (2n, 2n+1), else (n, n + rot/2).  VEC: rows of the cos/sin table are 16-byte aligned.
 // PART: some of a head is not rotated (the choice between the two for every pair is 1.5 % of the time, which calls that
-// rotate whole heads need not pay).
-template <typename T, bool NEIGHBOURS, bool VEC, bool PART>
-__global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kernel(const AppendArgs a)
+// rotate whole heads need not pay).  Args: AppendAxes where a position has several axes.  Q4: keys and values in 4 bits.
+template <typename T, bool NEIGHBOURS, bool VEC, bool PART, typename Args, bool Q4>
+__global__ void __launch_bounds__(APPEND_THREADS, Q4 ? APPEND_Q4_BLOCKS : APPEND_BLOCKS) kvc_append_kernel(const Args a)
 {
+    constexpr bool AXES = std::is_same<Args, AppendAxes>::value;
     kvc_pdl_wait();
     const uint32_t lane = threadIdx.x & 31u;
     const uint32_t team = lane / a.lanes, teams = 32u / a.lanes, l = lane % a.lanes;
     const bool on = l * 8u < a.d, turned = l * 8u < a.rot;
     // first elements of the lane's two pieces of four
-    const uint32_t ea = !NEIGHBOURS && turned ? 4u * l : 8u * l, eb = !NEIGHBOURS && turned ? a.rot / 2 + 4u * l : 8u * l + 4u;
+    uint32_t ea = !NEIGHBOURS && turned ? 4u * l : 8u * l, eb = !NEIGHBOURS && turned ? a.rot / 2 + 4u * l : 8u * l + 4u;
     const uint32_t per_token = a.q_chunks + 2 * a.kv_chunks;
     const uint32_t u = blockIdx.x * (APPEND_THREADS / 32u) + (threadIdx.x >> 5);  // (two warps in 2^31 blocks)
     const uint32_t tok = u / per_token;
@@ -272,6 +374,10 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
         if (part >= a.kv_chunks) {
             part -= a.kv_chunks;
             kind = 2;
+            if (Q4) {  // nothing turns: a lane's values as they lie, which is how they are quantised
+                ea = 8u * l;
+                eb = 8u * l + 4u;
+            }
         }
     }
     const uint32_t h0 = part * a.chunk, h1 = min(h0 + a.chunk, a.heads[kind != 0]);
@@ -294,24 +400,53 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
     const int64_t slot = a.slots[tok];
     if (slot < 0)
         return;  // a row without a token
-    const int32_t pos = a.rot ? a.positions[tok] : 0;
+    int32_t pos = 0;  // (several axes: a lane an axis)
+    bool far = false;
+    if constexpr (AXES) {
+        if (a.rot && lane < a.n_axes)
+            pos = a.positions[lane * a.axis_stride + tok];
+        far = __any_sync(~0u, a.rot && (uint32_t)pos >= a.max_pos);
+    } else {
+        pos = a.rot ? a.positions[tok] : 0;
+        far = a.rot && (uint32_t)pos >= a.max_pos;
+    }
     const uint64_t id = (uint64_t)slot < (1ull << 32) ? kvc_div((uint32_t)slot, a.block_size, a.block_shift) : (uint64_t)slot / a.block_size;
-    if (id >= a.num_blocks || (a.rot && (uint32_t)pos >= a.max_pos)) {
+    if (id >= a.num_blocks || far) {
         if (lane == 0 && u == tok * per_token)
             atomicAdd(a.status, 1u);
         return;
     }
+    const uint32_t in_block = (uint32_t)((uint64_t)slot - id * a.block_size);
     unsigned char *dst = kind == 0 ? a.q_out + tok * a.o_tok
                                    : (kind == 1 ? a.k_plane : a.v_plane) + id * a.block_stride +
-                                         ((uint64_t)slot - id * a.block_size) * a.heads[1] * a.d * sizeof(T);
-    const int64_t dst_head = kind == 0 ? a.o_head : (int64_t)(a.d * sizeof(T));
+                                         (Q4 ? 0 : (uint64_t)in_block * a.heads[1] * a.d * sizeof(T));
+    const int64_t dst_head = kind == 0 ? a.o_head : (int64_t)(Q4 ? a.block_size * KVC_Q4_ROW_BYTES(a.d) : a.d * sizeof(T));
     // w_e c, -w_o s, w_o c, w_e s of the lane's four pairs
     uint64_t ec[2], os[2], oc[2], es[2];
     const void *weight = kind < 2 ? a.weight[kind] : nullptr;
     if (kind < 2) {
         float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f}, we[4] = {1.f, 1.f, 1.f, 1.f}, wo[4] = {1.f, 1.f, 1.f, 1.f};
-        if (turned) {
-            const float *row = a.cos_sin + (int64_t)pos * a.cs_stride + 4u * l;
+        const float *row = a.cos_sin + 4u * l;
+        bool apart = false;  // the lane's pairs turn by positions of different axes
+        if constexpr (AXES) {
+            const uint32_t of = turned ? a.axis[l] : 0u, x = of & 0xFFu;
+            apart = of != x * 0x01010101u;
+            const int32_t p0 = __shfl_sync(~0u, pos, x);
+            if (__any_sync(~0u, apart)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t p = __shfl_sync(~0u, pos, of >> (8 * i) & 0xFFu);
+                    if (apart) {
+                        c[i] = row[(int64_t)p * a.cs_stride + i];
+                        s[i] = row[(int64_t)p * a.cs_stride + a.rot / 2 + i];
+                    }
+                }
+            }
+            row += (int64_t)p0 * a.cs_stride;
+        } else {
+            row += (int64_t)pos * a.cs_stride;
+        }
+        if (turned && !apart) {
             if (VEC) {
                 const float4 x = *reinterpret_cast<const float4 *>(row), y = *reinterpret_cast<const float4 *>(row + a.rot / 2);
                 c[0] = x.x, c[1] = x.y, c[2] = x.z, c[3] = x.w;
@@ -385,6 +520,21 @@ __global__ void __launch_bounds__(APPEND_THREADS, APPEND_BLOCKS) kvc_append_kern
                     res.b = make_uint2(kvc_from_float2<T>(yo[0].x, yo[0].y), kvc_from_float2<T>(yo[1].x, yo[1].y));
                 }
             }
+            if constexpr (Q4) {
+                if (kind != 0) {
+                    if (kind == 1 && !NEIGHBOURS && a.rot)
+                        res = append_natural(res, lane, l, a.rot / 8u);
+                    uint32_t scale;
+                    const uint32_t codes = append_quantise<T>(res, scale);
+                    if (h < h1) {
+                        unsigned char *row = dst + h * dst_head;
+                        __stcs(reinterpret_cast<uint32_t *>(row + in_block * (a.d / 2u) + l * 4u), codes);
+                        if (l % 4u == 0)
+                            __stcs(reinterpret_cast<uint32_t *>(row + a.block_size * (a.d / 2u) + in_block * (a.d / 8u) + l), scale);
+                    }
+                    continue;
+                }
+            }
             if (h < h1 && on) {
                 __stcs(reinterpret_cast<uint2 *>(dst + h * dst_head + ea * 2u), res.a);
                 __stcs(reinterpret_cast<uint2 *>(dst + h * dst_head + eb * 2u), res.b);
@@ -422,6 +572,202 @@ inline bool overlap(const Span &a, const Rows &b)
     const uint64_t row = b.stride ? (x - y) / b.stride : 0, off = (x - y) - row * b.stride;
     return a.at && b.first.at && a.bytes && b.first.bytes &&
            ((row < b.n && off < b.first.bytes) || (row + 1 < b.n && a.bytes > b.stride - off));
+}
+
+// The calls that write a step's tokens: kvc_append (x NULL), kvc_append_axes, kvc_append_q4 (q4).
+kvc_status append(kvc_layout *lay, const kvc_append_desc *d, const kvc_append_axes_desc *x, bool q4, void *stream)
+{
+    if (!lay || !d || d->reserved != 0)
+        return KVC_ERR_INVALID_ARG;
+    const uint32_t hkv = lay->d.num_kv_heads, dim = q4 ? kvc_q4_head_dim(lay) : lay->d.head_dim;
+    if (d->layer >= lay->d.num_layers || lay->d.kv_planes != 2 || (q4 ? dim == 0 : lay->d.elem_bytes != 2) ||
+        (d->dtype != KVC_DTYPE_BF16 && d->dtype != KVC_DTYPE_FP16))
+        return KVC_ERR_INVALID_ARG;
+    if (dim % 8 || dim > 256 || d->rot_dim > dim || d->rot_dim % 16 || d->interleaved > 1u ||
+        !(d->eps >= 0.f) || d->n_tokens > 0x7FFFFFFFu || d->n_q_heads > 0x10000u)
+        return KVC_ERR_INVALID_ARG;
+    if (x) {
+        if (x->reserved != 0 || x->n_axes == 0 || x->n_axes > KVC_MAX_AXES || (d->rot_dim && x->n_axes > 1 && x->axis_stride < d->n_tokens) ||
+            x->axis_stride > (1ull << 60))
+            return KVC_ERR_INVALID_ARG;
+        for (uint32_t i = 0; i < d->rot_dim / 2; ++i)
+            if (x->pair_axis[i] >= x->n_axes)
+                return KVC_ERR_INVALID_ARG;
+    }
+    if (q4 && !kvc_q4_aligned(lay))
+        return KVC_ERR_ALIGNMENT;
+    if (d->n_tokens == 0)
+        return KVC_OK;
+    if (!d->k || !d->v || !d->slots || (d->n_q_heads && (!d->q || !d->q_out)) ||
+        (d->rot_dim && (!d->positions || !d->cos_sin || d->cos_sin_stride < d->rot_dim)))
+        return KVC_ERR_INVALID_ARG;
+    if (!aligned(d->k, 16) || !aligned(d->v, 16) || !aligned(d->q, 16) || !aligned(d->q_out, 16) ||
+        !aligned(d->q_weight, 16) || !aligned(d->k_weight, 16) || !aligned(d->slots, 8) ||
+        !aligned(d->positions, 4) || !aligned(d->cos_sin, 4))
+        return KVC_ERR_ALIGNMENT;
+    if ((d->q_token_stride | d->q_head_stride | d->k_token_stride | d->k_head_stride | d->v_token_stride |
+         d->v_head_stride | d->out_token_stride | d->out_head_stride) % 8)
+        return KVC_ERR_ALIGNMENT;
+    kvc_status s = kvc_ensure_device(lay);
+    if (s != KVC_OK)
+        return s;
+    AppendAxes a;
+    a.src[0] = static_cast<const unsigned char *>(d->q);
+    a.src[1] = static_cast<const unsigned char *>(d->k);
+    a.src[2] = static_cast<const unsigned char *>(d->v);
+    const int64_t tok[3] = {d->q_token_stride, d->k_token_stride, d->v_token_stride};
+    const int64_t head[3] = {d->q_head_stride, d->k_head_stride, d->v_head_stride};
+    for (int i = 0; i < 3; ++i) {
+        a.src_tok[i] = 2 * tok[i];
+        a.src_head[i] = 2 * head[i];
+    }
+    a.q_out = static_cast<unsigned char *>(d->q_out);
+    a.k_plane = const_cast<unsigned char *>(kvc_plane_ptr(lay, d->layer, 0));
+    a.v_plane = const_cast<unsigned char *>(kvc_plane_ptr(lay, d->layer, 1));
+    a.o_tok = 2 * d->out_token_stride;
+    a.o_head = 2 * d->out_head_stride;
+    a.block_stride = lay->block_stride;
+    a.slots = d->slots;
+    a.positions = d->positions;
+    a.cos_sin = d->cos_sin;
+    a.cs_stride = (int64_t)d->cos_sin_stride;
+    a.weight[0] = d->q_weight;
+    a.weight[1] = d->k_weight;
+    a.eps = d->eps;
+    a.n_tokens = d->n_tokens;
+    a.heads[0] = d->n_q_heads;
+    a.heads[1] = hkv;
+    a.d = dim;
+    a.rot = d->rot_dim;
+    a.max_pos = d->max_positions;
+    a.block_size = lay->d.block_size;
+    a.block_shift = kvc_shift_of(a.block_size);
+    a.num_blocks = lay->d.num_blocks;
+    a.status = lay->d_status;
+    a.lanes = 1;
+    while (a.lanes * 8 < dim)
+        a.lanes *= 2;
+    // Heads per warp: the fewest that fill the machine's warps once -- a warp that serves more heads
+    // of its token fetches the table row once for them, one that serves fewer spreads a small call
+    // over more SMs.
+    const uint32_t heads = d->n_q_heads + 2 * hkv, teams = 32 / a.lanes;
+    const uint64_t warps = (uint64_t)lay->sm_count * APPEND_BLOCKS * (APPEND_THREADS / 32);
+    uint64_t chunk = (uint64_t)d->n_tokens * heads / warps;
+    chunk = std::max<uint64_t>((chunk + teams - 1) / teams * teams, teams);
+    a.chunk = (uint32_t)std::min<uint64_t>(chunk, (uint64_t)APPEND_CHUNK * APPEND_UNROLL * teams);
+    a.q_chunks = (d->n_q_heads + a.chunk - 1) / a.chunk;
+    a.kv_chunks = (hkv + a.chunk - 1) / a.chunk;
+    const uint64_t units = (uint64_t)d->n_tokens * (a.q_chunks + 2 * a.kv_chunks);
+    const uint32_t per_block = APPEND_THREADS / 32;
+    if ((units + per_block - 1) / per_block > 0x7FFFFFFFull)
+        return KVC_ERR_TOO_LARGE;
+    const uint32_t grid = (uint32_t)((units + per_block - 1) / per_block);
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e;
+    const bool vec = aligned(d->cos_sin, 16) && d->cos_sin_stride % 4 == 0, part = d->rot_dim < dim;
+    // Several axes: one position a token where they are one.
+    const bool axes = x && x->n_axes > 1 && d->rot_dim;
+    if (axes) {
+        a.axis_stride = (int64_t)x->axis_stride;
+        a.n_axes = x->n_axes;
+        memset(a.axis, 0, sizeof(a.axis));
+        memcpy(a.axis, x->pair_axis, d->rot_dim / 2);  // (whole words: rot_dim is a multiple of 16)
+    }
+    const std::true_type yes;
+    const std::false_type no;
+    const auto go = [&](auto type, auto neighbours, auto v, auto p, auto many, auto bits) {
+        typedef std::conditional_t<decltype(many)::value, AppendAxes, AppendArgs> Args;
+        return kvc_launch_pdl(kvc_append_kernel<decltype(type), decltype(neighbours)::value, decltype(v)::value, decltype(p)::value, Args,
+                                                decltype(bits)::value>,
+                              static_cast<const Args &>(a), dim3(grid), APPEND_THREADS, 0, st);
+    };
+    // (the calls with several axes or 4 bits do not tell whole heads from parts: half as many kernels)
+    const auto go2 = [&](auto type, auto neighbours, auto v) {
+        if (q4)
+            return axes ? go(type, neighbours, v, yes, yes, yes) : go(type, neighbours, v, yes, no, yes);
+        if (axes)
+            return go(type, neighbours, v, yes, yes, no);
+        return part ? go(type, neighbours, v, yes, no, no) : go(type, neighbours, v, no, no, no);
+    };
+    const auto go3 = [&](auto type, auto neighbours) { return vec ? go2(type, neighbours, yes) : go2(type, neighbours, no); };
+    const auto pick = [&](auto type) { return d->interleaved ? go3(type, yes) : go3(type, no); };
+    e = d->dtype == KVC_DTYPE_BF16 ? pick(__nv_bfloat16()) : pick(__half());
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return KVC_ERR_CUDA;
+    }
+    ++lay->launches;
+    kvc_step_launched(lay->device, (cudaStream_t)stream);
+    return KVC_OK;
+}
+
+// ------------------------------------------------------------------------------------ read_q4
+//
+// offset + step * code, rounded once.  Bound by memory, most of it the 16-bit result: a lane takes one word of codes, eight
+// values, and writes 16 bytes; a warp takes the heads of one token and plane.
+struct ReadArgs {
+    const unsigned char *plane[2];
+    unsigned char *out[2];
+    int64_t out_tok[2], out_head[2];  // bytes
+    uint64_t block_stride;
+    const int64_t *slots;
+    uint32_t n_tokens, heads, block_size, block_shift, num_blocks;
+    uint32_t planes, parts;  // units: token, plane, part of its heads
+    uint32_t *status;
+};
+
+#define READ_THREADS 128u
+#define READ_UNROLL 4u
+
+template <typename T, int D>
+__global__ void __launch_bounds__(READ_THREADS) kvc_read_q4_kernel(const ReadArgs a)
+{
+    constexpr uint32_t LANES = D / 8, TEAMS = 32 / LANES;
+    kvc_pdl_wait();
+    const uint32_t lane = threadIdx.x & 31u, l = lane % LANES, team = lane / LANES;
+    const uint64_t u = (uint64_t)blockIdx.x * (READ_THREADS / 32u) + (threadIdx.x >> 5);
+    const uint32_t per_token = a.planes * a.parts;
+    const uint64_t t64 = u / per_token;
+    if (t64 >= a.n_tokens)
+        return;
+    const uint32_t tok = (uint32_t)t64, in_token = (uint32_t)(u - t64 * per_token);
+    const uint32_t p = in_token / a.parts, part = in_token - p * a.parts;
+    const int64_t slot = a.slots[tok];
+    if (slot < 0)
+        return;
+    const uint64_t id = (uint64_t)slot < (1ull << 32) ? kvc_div((uint32_t)slot, a.block_size, a.block_shift) : (uint64_t)slot / a.block_size;
+    if (id >= a.num_blocks) {
+        if (lane == 0 && in_token == 0)
+            atomicAdd(a.status, 1u);
+        return;
+    }
+    const uint32_t in_block = (uint32_t)((uint64_t)slot - id * a.block_size);
+    const unsigned char *block = (p ? a.plane[1] : a.plane[0]) + id * a.block_stride;
+    unsigned char *dst = (p ? a.out[1] : a.out[0]) + tok * (p ? a.out_tok[1] : a.out_tok[0]) + l * 16u;
+    const int64_t dst_head = p ? a.out_head[1] : a.out_head[0];
+    const uint32_t h0 = part * (TEAMS * READ_UNROLL) + team;
+    uint32_t w[READ_UNROLL], scale[READ_UNROLL];
+#pragma unroll
+    for (uint32_t i = 0; i < READ_UNROLL; ++i) {
+        const uint32_t h = h0 + i * TEAMS;
+        if (h < a.heads) {
+            const unsigned char *row = block + (uint64_t)h * a.block_size * KVC_Q4_ROW_BYTES(D);
+            w[i] = *reinterpret_cast<const uint32_t *>(row + in_block * (D / 2u) + l * 4u);
+            scale[i] = *reinterpret_cast<const uint32_t *>(row + a.block_size * (D / 2u) + in_block * (D / 8u) + l / 4u * 4u);
+        }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < READ_UNROLL; ++i) {
+        const uint32_t h = h0 + i * TEAMS;
+        if (h < a.heads) {
+            const float2 s = kvc_to_float2<T>(scale[i]);  // step, offset
+            uint32_t r[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                r[k] = kvc_from_float2<T>(fmaf((float)(w[i] >> (8 * k) & 15u), s.x, s.y), fmaf((float)(w[i] >> (8 * k + 4) & 15u), s.x, s.y));
+            *reinterpret_cast<uint4 *>(dst + h * dst_head) = make_uint4(r[0], r[1], r[2], r[3]);
+        }
+    }
 }
 
 }  // namespace
@@ -510,102 +856,77 @@ kvc_status kvc_map_tokens(kvc_layout *lay, const kvc_map_tokens_desc *d, void *s
 
 kvc_status kvc_append(kvc_layout *lay, const kvc_append_desc *d, void *stream)
 {
+    return append(lay, d, nullptr, false, stream);
+}
+
+kvc_status kvc_append_axes(kvc_layout *lay, const kvc_append_axes_desc *d, void *stream)
+{
+    return d ? append(lay, &d->token, d, false, stream) : KVC_ERR_INVALID_ARG;
+}
+
+kvc_status kvc_append_q4(kvc_layout *lay, const kvc_append_axes_desc *d, void *stream)
+{
+    return d ? append(lay, &d->token, d, true, stream) : KVC_ERR_INVALID_ARG;
+}
+
+kvc_status kvc_read_q4(kvc_layout *lay, const kvc_read_q4_desc *d, void *stream)
+{
     if (!lay || !d || d->reserved != 0)
         return KVC_ERR_INVALID_ARG;
-    const uint32_t hkv = lay->d.num_kv_heads, dim = lay->d.head_dim;
-    if (d->layer >= lay->d.num_layers || lay->d.kv_planes != 2 || lay->d.elem_bytes != 2 ||
-        (d->dtype != KVC_DTYPE_BF16 && d->dtype != KVC_DTYPE_FP16))
+    const uint32_t dim = kvc_q4_head_dim(lay);
+    if (d->layer >= lay->d.num_layers || dim == 0 || (d->dtype != KVC_DTYPE_BF16 && d->dtype != KVC_DTYPE_FP16) ||
+        d->n_tokens > 0x7FFFFFFFu)
         return KVC_ERR_INVALID_ARG;
-    if (dim % 8 || dim > 256 || d->rot_dim > dim || d->rot_dim % 16 || d->interleaved > 1u ||
-        !(d->eps >= 0.f) || d->n_tokens > 0x7FFFFFFFu || d->n_q_heads > 0x10000u)
-        return KVC_ERR_INVALID_ARG;
-    if (d->n_tokens == 0)
+    if (!kvc_q4_aligned(lay))
+        return KVC_ERR_ALIGNMENT;
+    if (d->n_tokens == 0 || (!d->k_out && !d->v_out))
         return KVC_OK;
-    if (!d->k || !d->v || !d->slots || (d->n_q_heads && (!d->q || !d->q_out)) ||
-        (d->rot_dim && (!d->positions || !d->cos_sin || d->cos_sin_stride < d->rot_dim)))
+    if (!d->slots)
         return KVC_ERR_INVALID_ARG;
-    if (!aligned(d->k, 16) || !aligned(d->v, 16) || !aligned(d->q, 16) || !aligned(d->q_out, 16) ||
-        !aligned(d->q_weight, 16) || !aligned(d->k_weight, 16) || !aligned(d->slots, 8) ||
-        !aligned(d->positions, 4) || !aligned(d->cos_sin, 4))
+    if (!aligned(d->k_out, 16) || !aligned(d->v_out, 16) || !aligned(d->slots, 8) ||
+        (d->k_token_stride | d->k_head_stride | d->v_token_stride | d->v_head_stride) % 8)
         return KVC_ERR_ALIGNMENT;
-    if ((d->q_token_stride | d->q_head_stride | d->k_token_stride | d->k_head_stride | d->v_token_stride |
-         d->v_head_stride | d->out_token_stride | d->out_head_stride) % 8)
-        return KVC_ERR_ALIGNMENT;
-    kvc_status s = kvc_ensure_device(lay);
+    const kvc_status s = kvc_ensure_device(lay);
     if (s != KVC_OK)
         return s;
-    AppendArgs a;
-    a.src[0] = static_cast<const unsigned char *>(d->q);
-    a.src[1] = static_cast<const unsigned char *>(d->k);
-    a.src[2] = static_cast<const unsigned char *>(d->v);
-    const int64_t tok[3] = {d->q_token_stride, d->k_token_stride, d->v_token_stride};
-    const int64_t head[3] = {d->q_head_stride, d->k_head_stride, d->v_head_stride};
-    for (int i = 0; i < 3; ++i) {
-        a.src_tok[i] = 2 * tok[i];
-        a.src_head[i] = 2 * head[i];
-    }
-    a.q_out = static_cast<unsigned char *>(d->q_out);
-    a.k_plane = const_cast<unsigned char *>(kvc_plane_ptr(lay, d->layer, 0));
-    a.v_plane = const_cast<unsigned char *>(kvc_plane_ptr(lay, d->layer, 1));
-    a.o_tok = 2 * d->out_token_stride;
-    a.o_head = 2 * d->out_head_stride;
+    ReadArgs a;
+    memset(&a, 0, sizeof(a));
+    void *const out[2] = {d->k_out, d->v_out};
+    const int64_t tok[2] = {d->k_token_stride, d->v_token_stride}, head[2] = {d->k_head_stride, d->v_head_stride};
+    uint32_t planes = 0;
+    for (uint32_t p = 0; p < 2; ++p)
+        if (out[p]) {
+            a.plane[planes] = kvc_plane_ptr(lay, d->layer, p);
+            a.out[planes] = static_cast<unsigned char *>(out[p]);
+            a.out_tok[planes] = 2 * tok[p];
+            a.out_head[planes] = 2 * head[p];
+            ++planes;
+        }
     a.block_stride = lay->block_stride;
     a.slots = d->slots;
-    a.positions = d->positions;
-    a.cos_sin = d->cos_sin;
-    a.cs_stride = (int64_t)d->cos_sin_stride;
-    a.weight[0] = d->q_weight;
-    a.weight[1] = d->k_weight;
-    a.eps = d->eps;
     a.n_tokens = d->n_tokens;
-    a.heads[0] = d->n_q_heads;
-    a.heads[1] = hkv;
-    a.d = dim;
-    a.rot = d->rot_dim;
-    a.max_pos = d->max_positions;
+    a.heads = lay->d.num_kv_heads;
     a.block_size = lay->d.block_size;
     a.block_shift = kvc_shift_of(a.block_size);
     a.num_blocks = lay->d.num_blocks;
     a.status = lay->d_status;
-    a.lanes = 1;
-    while (a.lanes * 8 < dim)
-        a.lanes *= 2;
-    // Heads per warp: the fewest that fill the machine's warps once -- a warp that serves more heads
-    // of its token fetches the table row once for them, one that serves fewer spreads a small call
-    // over more SMs.
-    const uint32_t heads = d->n_q_heads + 2 * hkv, teams = 32 / a.lanes;
-    const uint64_t warps = (uint64_t)lay->sm_count * APPEND_BLOCKS * (APPEND_THREADS / 32);
-    uint64_t chunk = (uint64_t)d->n_tokens * heads / warps;
-    chunk = std::max<uint64_t>((chunk + teams - 1) / teams * teams, teams);
-    a.chunk = (uint32_t)std::min<uint64_t>(chunk, (uint64_t)APPEND_CHUNK * APPEND_UNROLL * teams);
-    a.q_chunks = (d->n_q_heads + a.chunk - 1) / a.chunk;
-    a.kv_chunks = (hkv + a.chunk - 1) / a.chunk;
-    const uint64_t units = (uint64_t)d->n_tokens * (a.q_chunks + 2 * a.kv_chunks);
-    const uint32_t per_block = APPEND_THREADS / 32;
-    if ((units + per_block - 1) / per_block > 0x7FFFFFFFull)
+    const uint32_t per_warp = 32u / (dim / 8u) * READ_UNROLL;
+    a.parts = (a.heads + per_warp - 1) / per_warp;
+    a.planes = planes;
+    const uint64_t units = (uint64_t)d->n_tokens * planes * a.parts, blocks = (units + READ_THREADS / 32 - 1) / (READ_THREADS / 32);
+    if (blocks > 0x7FFFFFFFull)
         return KVC_ERR_TOO_LARGE;
-    const uint32_t grid = (uint32_t)((units + per_block - 1) / per_block);
     cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t e;
-    const bool vec = aligned(d->cos_sin, 16) && d->cos_sin_stride % 4 == 0, part = d->rot_dim < dim;
-    const auto go = [&](auto type, auto neighbours, auto v, auto p) {
-        return kvc_launch_pdl(kvc_append_kernel<decltype(type), decltype(neighbours)::value, decltype(v)::value, decltype(p)::value>, a,
-                              dim3(grid), APPEND_THREADS, 0, st);
-    };
-    const auto go2 = [&](auto type, auto neighbours) {
-        const std::true_type yes;
-        const std::false_type no;
-        return vec ? (part ? go(type, neighbours, yes, yes) : go(type, neighbours, yes, no))
-                   : (part ? go(type, neighbours, no, yes) : go(type, neighbours, no, no));
-    };
-    const auto pick = [&](auto type) { return d->interleaved ? go2(type, std::true_type()) : go2(type, std::false_type()); };
-    e = d->dtype == KVC_DTYPE_BF16 ? pick(__nv_bfloat16()) : pick(__half());
+    const auto go = [&](auto kernel) { return kvc_launch_pdl(kernel, a, dim3((uint32_t)blocks), READ_THREADS, 0, st); };
+    const bool bf16 = d->dtype == KVC_DTYPE_BF16;
+    const cudaError_t e = dim == 128 ? (bf16 ? go(kvc_read_q4_kernel<__nv_bfloat16, 128>) : go(kvc_read_q4_kernel<__half, 128>))
+                                     : (bf16 ? go(kvc_read_q4_kernel<__nv_bfloat16, 64>) : go(kvc_read_q4_kernel<__half, 64>));
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return KVC_ERR_CUDA;
     }
     ++lay->launches;
-    kvc_step_launched(lay->device, (cudaStream_t)stream);
+    kvc_step_launched(lay->device, st);
     return KVC_OK;
 }
 

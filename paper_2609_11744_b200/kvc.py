@@ -131,6 +131,25 @@ class kvc_append_desc(ctypes.Structure):
                [("reserved", ctypes.c_uint64)]
 
 
+KVC_MAX_AXES, KVC_MAX_PAIRS, KVC_Q4_GROUP = 4, 128, 32
+
+
+def KVC_Q4_ROW_BYTES(head_dim: int) -> int:
+    """Bytes of a row of a pool held in 4 bits."""
+    return head_dim // 2 + head_dim // 8
+
+
+class kvc_append_axes_desc(ctypes.Structure):
+    _fields_ = [("token", kvc_append_desc), ("axis_stride", ctypes.c_uint64), ("n_axes", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32), ("pair_axis", ctypes.c_uint8 * KVC_MAX_PAIRS)]
+
+
+class kvc_read_q4_desc(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_uint32), ("dtype", ctypes.c_uint32), ("k_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p)] + \
+               [(k, ctypes.c_int64) for k in ("k_token_stride", "k_head_stride", "v_token_stride", "v_head_stride")] + \
+               [("slots", ctypes.c_void_p), ("n_tokens", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
 class kvc_attention_desc(ctypes.Structure):
     _fields_ = [("layer", ctypes.c_uint32), ("dtype", ctypes.c_uint32)] + \
                [(k, ctypes.c_void_p) for k in ("q", "out", "lse")] + \
@@ -208,6 +227,12 @@ def lib() -> ctypes.CDLL:
                                         P(ctypes.c_double)]),
         "kvc_map_tokens": (ci, [vp, vp, vp]),
         "kvc_append": (ci, [vp, vp, vp]),
+        "kvc_append_axes": (ci, [vp, vp, vp]),
+        "kvc_append_q4": (ci, [vp, vp, vp]),
+        "kvc_read_q4": (ci, [vp, vp, vp]),
+        "kvc_attention_q4_workspace_bytes": (ci, [vp, u32, u32, u32, u32, P(u64)]),
+        "kvc_attention_q4": (ci, [vp, vp, vp]),
+        "kvc_attention_q4_shared": (ci, [vp, vp, vp]),
         "kvc_attention_workspace_bytes": (ci, [vp, u32, u32, u32, u32, P(u64)]),
         "kvc_attention": (ci, [vp, vp, vp]),
         "kvc_attention_shared": (ci, [vp, vp, vp]),
@@ -387,6 +412,17 @@ def kvc_layout_create_dense(pool, num_layers, kv_planes, num_blocks, block_size,
     out = ctypes.c_void_p()
     _check(lib().kvc_layout_create(ctypes.byref(d), ctypes.byref(out)), "kvc_layout_create")
     return LayoutHandle(out.value, [pool], (num_kv_heads, head_dim))
+
+
+def kvc_layout_create_q4(pool, num_layers, num_blocks, block_size, num_kv_heads, head_dim, chunk_tokens,
+                         chunk_order: int = 0) -> LayoutHandle:
+    """Layout over one dense allocation of a pool held in 4 bits, [L][K|V][NB][slab] with slabs of
+    block_size * num_kv_heads * KVC_Q4_ROW_BYTES(head_dim) bytes: to pack, unpack and the rest a layout of
+    one-byte elements."""
+    if head_dim not in (64, 128):
+        raise ValueError("a pool held in 4 bits has heads of 64 or 128, not %d" % head_dim)
+    return kvc_layout_create_dense(pool, num_layers, 2, num_blocks, block_size, num_kv_heads,
+                                   KVC_Q4_ROW_BYTES(head_dim), 1, chunk_tokens, chunk_order)
 
 
 def kvc_layout_destroy(layout: LayoutHandle) -> None:
@@ -608,9 +644,13 @@ _torch = None
 _MAP_DESC = struct.Struct("@4PQ4I6PQ")
 _APPEND_DESC = struct.Struct("@2I4P8q3PQ2Pf5IQ")
 _ATTENTION_DESC = struct.Struct("@2I3P4q3PQ5If2I2P2IPQ")
+_APPEND_AXES_DESC = struct.Struct(_APPEND_DESC.format + "Q2I128s")
+_READ_Q4_DESC = struct.Struct("@2I2P4qP2I")
 assert _MAP_DESC.size == ctypes.sizeof(kvc_map_tokens_desc)
 assert _APPEND_DESC.size == ctypes.sizeof(kvc_append_desc)
 assert _ATTENTION_DESC.size == ctypes.sizeof(kvc_attention_desc)
+assert _APPEND_AXES_DESC.size == ctypes.sizeof(kvc_append_axes_desc)
+assert _READ_Q4_DESC.size == ctypes.sizeof(kvc_read_q4_desc)
 
 
 def _step_call():
@@ -698,14 +738,21 @@ def kvc_append(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, q_
     q, q_out [T, Hq, D] (or both None), k, v [T, Hkv, D]: bf16 or fp16, any token and head strides;
     slots [T] int64; positions [T] int32 and cos_sin [max_positions, rot_dim] float32 (or both None:
     no rotation); q_weight, k_weight [D] of the type of k, or None: no norm."""
+    _append("kvc_append", layout, layout.heads, layer, q, k, v, q_out, slots, positions, cos_sin, None, q_weight, k_weight, eps,
+            interleaved, stream)
+
+
+def _append(name, layout, heads, layer, q, k, v, q_out, slots, positions, cos_sin, axes, q_weight, k_weight, eps, interleaved,
+            stream):
+    """axes: None, or (axes of `positions`, bytes that name each pair's)."""
     t, dev, L = _step_call()
     dt = k.dtype
     kind = t.kv.get(dt)
     if kind is None:
         raise TypeError("k must be torch.bfloat16 or torch.float16, not %s" % dt)
     n, hkv, dim = k.shape
-    if (hkv, dim) != layout.heads:
-        raise ValueError("k has %d heads of %d, the layout %d of %d" % ((hkv, dim) + layout.heads))
+    if (hkv, dim) != heads:
+        raise ValueError("k has %d heads of %d, the layout %d of %d" % ((hkv, dim) + heads))
     if (q is None) != (q_out is None) or (positions is None) != (cos_sin is None):
         raise TypeError("q and q_out, and positions and cos_sin, go together")
     qp = qt = qh = op = ot = oh = hq = 0
@@ -718,15 +765,82 @@ def kvc_append(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, q_
     rot = rows = cs = pos = 0
     if cos_sin is not None:
         rows, rot = cos_sin.shape
-        pos = _arg(positions, "positions", t.i32, n, dev)
+        pos = _arg(positions, "positions", t.i32, n if axes is None else n * axes[0], dev)
         cs = _arg(cos_sin, "cos_sin", t.f32, rows * rot, dev)
-    d = _APPEND_DESC.pack(layer, kind, qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, _arg(slots, "slots", t.i64, n, dev), pos, cs, rot,
-                          0 if q_weight is None else _arg(q_weight, "q_weight", dt, dim, dev),
-                          0 if k_weight is None else _arg(k_weight, "k_weight", dt, dim, dev), eps, n, hq, rot, rows,
-                          1 if interleaved else 0, 0)
-    status = L.kvc_append(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
+    desc = (layer, kind, qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, _arg(slots, "slots", t.i64, n, dev), pos, cs, rot,
+            0 if q_weight is None else _arg(q_weight, "q_weight", dt, dim, dev),
+            0 if k_weight is None else _arg(k_weight, "k_weight", dt, dim, dev), eps, n, hq, rot, rows,
+            1 if interleaved else 0, 0)
+    if axes is None:
+        d = _APPEND_DESC.pack(*desc)
+    else:
+        if len(axes[1]) != rot // 2:
+            raise ValueError("pair_axis names the axes of %d pairs, a head has %d" % (len(axes[1]), rot // 2))
+        d = _APPEND_AXES_DESC.pack(*desc, n, axes[0], 0, axes[1])
+    status = getattr(L, name)(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
     if status:
-        raise KvcError(status, "kvc_append")
+        raise KvcError(status, name)
+
+
+def kvc_pair_axes(sections: Sequence[int], in_turns: bool = False) -> bytes:
+    """The pair_axis of the calls below.  sections[a]: how many pairs turn by axis a, one axis behind the
+    other; in_turns: they take turns instead (0, 1, 2, 0, 1, 2, ..), an axis being left out once its pairs
+    are used up."""
+    if not in_turns:
+        return b"".join(bytes([a]) * n for a, n in enumerate(sections))
+    return bytes(a for i in range(max(sections)) for a, n in enumerate(sections) if i < n)
+
+
+def _positions_of(positions, pair_axis, rot: int):
+    """The `axes` of _append for positions [T] or [A, T]."""
+    many = positions is not None and positions.dim() == 2
+    if pair_axis is None:
+        if many and positions.shape[0] != 1:
+            raise TypeError("positions with several axes need pair_axis")
+        pair_axis = bytes(rot // 2)
+    return (positions.shape[0] if many else 1, bytes(pair_axis))
+
+
+def kvc_append_axes(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, pair_axis, q_weight=None,
+                    k_weight=None, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """kvc_append for positions with several axes: positions [A, T] int32, pair_axis: bytes of length
+    rot_dim / 2, the axis that turns each pair (see kvc_pair_axes)."""
+    _append("kvc_append_axes", layout, layout.heads, layer, q, k, v, q_out, slots, positions, cos_sin,
+            _positions_of(positions, pair_axis, 0 if cos_sin is None else cos_sin.shape[1]), q_weight, k_weight, eps, interleaved,
+            stream)
+
+
+def _q4_heads(layout) -> Tuple[int, int]:
+    """(KV heads, values of a head) of a pool held in 4 bits."""
+    return layout.heads[0], layout.heads[1] * 8 // 5
+
+
+def kvc_append_q4(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, pair_axis=None, q_weight=None,
+                  k_weight=None, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """kvc_append into a pool held in 4 bits (kvc_layout_create_q4).  positions [T], or [A, T] with pair_axis."""
+    _append("kvc_append_q4", layout, _q4_heads(layout), layer, q, k, v, q_out, slots, positions, cos_sin,
+            _positions_of(positions, pair_axis, 0 if cos_sin is None else cos_sin.shape[1]), q_weight, k_weight, eps, interleaved,
+            stream)
+
+
+def kvc_read_q4(layout, layer: int, k_out, v_out, slots, stream=None) -> None:
+    """Tokens of a pool held in 4 bits as 16-bit values: k_out, v_out [T, Hkv, D] bf16 or fp16 (the type that
+    was appended), any token and head strides, either None; slots [T] int64."""
+    t, dev, L = _step_call()
+    some = k_out if k_out is not None else v_out
+    if some is None:
+        raise TypeError("k_out and v_out are both missing")
+    dt, n = some.dtype, slots.numel()
+    kind = t.kv.get(dt)
+    if kind is None:
+        raise TypeError("the outputs must be torch.bfloat16 or torch.float16, not %s" % dt)
+    hkv, dim = _q4_heads(layout)
+    kp, kt, kh = (0, 0, 0) if k_out is None else _heads(k_out, "k_out", dt, n, hkv, dim, dev)
+    vp, vt, vh = (0, 0, 0) if v_out is None else _heads(v_out, "v_out", dt, n, hkv, dim, dev)
+    d = _READ_Q4_DESC.pack(layer, kind, kp, vp, kt, kh, vt, vh, _arg(slots, "slots", t.i64, n, dev), n, 0)
+    status = L.kvc_read_q4(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
+    if status:
+        raise KvcError(status, "kvc_read_q4")
 
 
 def kvc_attention_workspace_bytes(layout, n_tokens: int, n_requests: int, n_q_heads: int, n_groups: int = 0) -> int:
@@ -737,7 +851,15 @@ def kvc_attention_workspace_bytes(layout, n_tokens: int, n_requests: int, n_q_he
     return out.value
 
 
-def _attention(name, layout, layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, window, sinks, lse,
+def kvc_attention_q4_workspace_bytes(layout, n_tokens: int, n_requests: int, n_q_heads: int, n_groups: int = 0) -> int:
+    """kvc_attention_workspace_bytes for a pool held in 4 bits."""
+    out = ctypes.c_uint64()
+    _check(lib().kvc_attention_q4_workspace_bytes(layout.handle, n_tokens, n_requests, n_q_heads, n_groups,
+                                                  ctypes.byref(out)), "kvc_attention_q4_workspace_bytes")
+    return out.value
+
+
+def _attention(name, layout, head_dim, layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, window, sinks, lse,
                max_q_len, group_starts, prefix_lens, stream):
     t, dev, L = _step_call()
     i32, dt = t.i32, q.dtype
@@ -745,8 +867,8 @@ def _attention(name, layout, layer, q, out, block_tables, seq_lens, cu_tokens, w
     if kind is None:
         raise TypeError("q must be torch.bfloat16 or torch.float16, not %s" % dt)
     n, hq, dim = q.shape
-    if dim != layout.heads[1]:
-        raise ValueError("q has heads of %d, the layout of %d" % (dim, layout.heads[1]))
+    if dim != head_dim:
+        raise ValueError("q has heads of %d, the layout of %d" % (dim, head_dim))
     r = seq_lens.numel()
     tab, stride, wide = _table(block_tables, r, i32, dev)
     qp, qt, qh = _heads(q, "q", dt, n, hq, dim, dev)
@@ -776,7 +898,7 @@ def kvc_attention(layout, layer: int, q, out, block_tables, seq_lens, cu_tokens,
     int32; lse [T, Hq] float32 or None; workspace: a tensor of at least
     kvc_attention_workspace_bytes.  scale defaults to D ** -0.5; max_q_len is a hint, the most query
     rows of one request (0: unknown)."""
-    _attention("kvc_attention", layout, layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, window,
+    _attention("kvc_attention", layout, layout.heads[1], layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, window,
                sinks, lse, max_q_len, None, None, stream)
 
 
@@ -784,8 +906,23 @@ def kvc_attention_shared(layout, layer: int, q, out, block_tables, seq_lens, cu_
                          workspace, scale=None, lse=None, max_q_len: int = 0, stream=None) -> None:
     """kvc_attention for groups of requests with a common prefix, whose keys and values are read once
     per group: group_starts [G + 1] and prefix_lens [G] int32."""
-    _attention("kvc_attention_shared", layout, layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale, 0, 0,
-               lse, max_q_len, group_starts, prefix_lens, stream)
+    _attention("kvc_attention_shared", layout, layout.heads[1], layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale,
+               0, 0, lse, max_q_len, group_starts, prefix_lens, stream)
+
+
+def kvc_attention_q4(layout, layer: int, q, out, block_tables, seq_lens, cu_tokens, workspace, scale=None, window: int = 0,
+                     sinks: int = 0, lse=None, max_q_len: int = 0, stream=None) -> None:
+    """kvc_attention over a pool held in 4 bits (kvc_layout_create_q4); workspace: at least
+    kvc_attention_q4_workspace_bytes."""
+    _attention("kvc_attention_q4", layout, _q4_heads(layout)[1], layer, q, out, block_tables, seq_lens, cu_tokens, workspace, scale,
+               window, sinks, lse, max_q_len, None, None, stream)
+
+
+def kvc_attention_q4_shared(layout, layer: int, q, out, block_tables, seq_lens, cu_tokens, group_starts, prefix_lens,
+                            workspace, scale=None, lse=None, max_q_len: int = 0, stream=None) -> None:
+    """kvc_attention_shared over a pool held in 4 bits."""
+    _attention("kvc_attention_q4_shared", layout, _q4_heads(layout)[1], layer, q, out, block_tables, seq_lens, cu_tokens, workspace,
+               scale, 0, 0, lse, max_q_len, group_starts, prefix_lens, stream)
 
 
 # ------------------------------------------------------------------ staging ring
