@@ -103,20 +103,10 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
-// Where this lane's key of the cursor's unit lies.
-template <int D>
-__device__ __forceinline__ KvcQ4Key look_up(const KvcAttn &a, const KvcCursor &c, uint32_t warp, uint32_t lane)
+// This lane's key of the cursor's unit.
+__device__ __forceinline__ KvcQ4Next look_up(const KvcAttn &a, const KvcCursor &c, uint32_t warp, uint32_t lane)
 {
-    const int32_t j = (int32_t)(kvc_tile(c.r, c.t) * TK + warp * WK + lane);
-    KvcQ4Key k;
-    k.codes = -1;
-    k.scales = 0;
-    if (j < c.r.hi && (j >= c.r.lo || j < c.r.sink_end)) {
-        k = kvc_q4_key<D>(a, c.q.table, j, c.h);
-        if (k.codes < 0)
-            atomicAdd(a.status, 1u);
-    }
-    return k;
+    return kvc_q4_look(a, c.q, c.r, (int32_t)(kvc_tile(c.r, c.t) * TK + warp * WK + lane));
 }
 
 // Issues the copies of this warp's keys of one unit; returns which of the 32 are there.  Keys that are not
@@ -174,18 +164,24 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
     uint32_t pair = run.pair;
     // the load cursor's unit, if it is in the run, and one step on; places are looked up a unit ahead
     bool more = true;
-    KvcQ4Key key = look_up<D>(a, ld, warp, lane);
+    KvcQ4Next next = look_up(a, ld, warp, lane);
+    uint32_t next_head = ld.h;
     const auto load = [&](uint32_t stage) {
         if (more) {
-            const KvcQ4Key now = key;
-            const uint32_t n = ld.r.n;
+            const KvcQ4Next now = next;
+            const uint32_t head = next_head, n = ld.r.n;
             kvc_next<ROWS, TK>(a, n_seq, ld);
             if (ld.t == 0)
                 ld_at += n + HEAD;
             more = ld.s < n_seq && ld_at + ld.t < run.end;
-            if (more)
-                key = look_up<D>(a, ld, warp, lane);
-            const uint32_t there = load_unit<D, NT>(a, now, lane, ring + stage * S::STAGE);
+            if (more) {
+                next = look_up(a, ld, warp, lane);
+                next_head = ld.h;
+            }
+            const KvcQ4Key key = kvc_q4_key<D>(a, now, head);
+            if (now.asked && key.codes < 0)
+                atomicAdd(a.status, 1u);
+            const uint32_t there = load_unit<D, NT>(a, key, lane, ring + stage * S::STAGE);
             if (lane == 0)
                 s_there[warp][stage] = there;
         }

@@ -52,17 +52,14 @@ constexpr uint32_t THERE = 8;  // ring of "which keys are there" words, deeper t
 // runs of keys gain by (one request of drafted tokens behind 80,000: 85.4 us with 256, 83.6 with 128; 32 questions on a
 // 32,000-token document 71.2 and 69.5; but 16 requests of drafted tokens behind 16,000 202.4 and 204.5).
 //
-// Q4: a pool held in 4 bits.  Its keys pass through a ring of parts (32 keys as they lie in the pool) on their way to a stage.
-// With 256 rows one warp makes a tile of values of them, K or V, and with 128, where the softmax warps of the
-// second row tile have none, four do: its pace is that of the loads then, not of the softmax.
+// Q4: a pool held in 4 bits.  Its keys pass through a ring of raw parts on their way to a stage, a quarter of a tile each, K and V.
 template <int D, int ROWS, bool Q4>
 struct Shape {
     static constexpr int TILE = TK * D * 2;           // a K or V tile; also the queries of a row tile
     static constexpr int HALF = TK * 128;             // 64 elements (128 bytes) of 128 rows
     static constexpr int KS = D == 64 ? 4 : ROWS == 128 && !Q4 ? 3 : 2, VS = D == 64 ? 4 : 2;
-    static constexpr int WARPS = ROWS == 128 ? 4 : 1, PARTS = ROWS == 128 ? 3 : 5;  // Q4: that load K, and V; parts of each
-    static constexpr int PITCH = D == 128 ? 80 : 48, PART = 32 * PITCH;              // Q4: of a key, bytes of a part
-    static constexpr int RAW_BYTES = Q4 ? 2 * WARPS * PARTS * PART : 0;
+    static constexpr int PARTS = ROWS == 128 ? 12 : 5, PART = 32 * KVC_Q4_ROW_BYTES(D);  // Q4: raw parts, bytes of K's or V's
+    static constexpr int RAW_BYTES = Q4 ? 2 * PARTS * PART : 0;
     static constexpr int Q = 0, K = ROWS / 128 * TILE, V = K + KS * TILE, RAW = V + VS * TILE, END = RAW + RAW_BYTES;
     static constexpr int SMEM = END + 1024;           // room to align the stages to the swizzle's 1024 bytes
     static_assert(SMEM + (ROWS == 128 ? 5 : 8) * 1024 <= 227 * 1024, "with the kernel's own variables");
@@ -418,124 +415,242 @@ __device__ __forceinline__ void load_role(const TilesArgs &args, const Segment *
             ;
 }
 
-// One of the warps that load K or V of a pool held in 4 bits: all tiles of the block's run, 32 keys at a time.  Codes
-// and scales are copied as they lie, PARTS - 1 ahead and across segments; a lane then makes one key's values,
-// offset + step * code in the model's type, and writes them where the matrix unit reads them.  What is no key's comes as
-// zeros and stays zeros.  A word of eight codes gives the pairs (0,4) (1,5) (2,6) (3,7); K keeps that order, which
-// the queries are given too, and V's is put right.
+// ---- a pool held in 4 bits: its keys come in parts of 32, K and V, through a ring of raw parts.  One or two warps copy
+// them there as they lie, others make them the values that the stages hold.
+
+// Bytes as they lie, counted by the barrier.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const unsigned char *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+struct RawBars {
+    uint64_t full[12], empty[12];
+    uint32_t there[12];  // which of a part's 32 keys are there
+};
+
+// Blocks of 4 to 32 keys, a power of two: a part is a row of blocks as they lie, codes and scales; else all codes, then all
+// scales.
+__device__ __forceinline__ bool raw_images(const KvcAttn &a) { return a.block_shift >= 2u && a.block_shift <= 5u; }
+
+// A warp that copies parts first, first + 1, .. (PER of each tile's four) of the block's run.  A lane takes the keys of a part that
+// lie in one block, of K or of V; block ids are looked up ahead, by tile where parts are rows of blocks (a lane a block), else
+// by part.  `between` is called once a segment.
+template <int D, int ROWS, typename Between>
+__device__ __forceinline__ void raw_role(const KvcAttn &a, const Segment *segments, uint32_t raw, RawBars *rb, Bars *bars, uint32_t first,
+                                         volatile uint32_t *dead, uint32_t lane, const Between &between)
+{
+    using S = Shape<D, ROWS, true>;
+    constexpr uint32_t CODES = D / 2, SCALES = D / 8, ROW = CODES + SCALES, PER = ROWS == 128 ? 2 : 4;
+    constexpr uint32_t NONE = ~0u;
+    const bool images = raw_images(a);
+    const uint32_t shift = images ? a.block_shift : 0u;
+    SegmentReader reader;
+    Segment c;
+    uint32_t slot = ROWS == 128 ? first : 0u, parity = 1, issued = 0;
+    bool ok = true;
+#pragma unroll 1
+    while (ok && reader.next(segments, bars, c, dead, a.status)) {
+        between();
+        const int32_t *table = a.tables + (int64_t)c.q.table * a.table_stride;
+        const uint64_t head_at = (uint64_t)c.h * a.block_size * ROW;
+        const auto wanted_of = [&](int32_t j0) { return low_bits(c.r.hi - j0) & (~low_bits(c.r.lo - j0) | low_bits(c.r.sink_end - j0)); };
+        // the id of this lane's block of a tile, or NONE where none of its keys is wanted
+        const auto look_tile = [&](uint32_t u) {
+            const int32_t j = (int32_t)(kvc_tile(c.r, c.t + u) * TK + (lane << shift)), e = j + (int32_t)a.block_size;
+            const bool some = lane << shift < (uint32_t)TK && j < c.r.hi && (e > c.r.lo || j < c.r.sink_end);
+            return some ? min((uint32_t)table[(uint32_t)j >> shift], NONE - 1u) : NONE;  // (an entry may be any number)
+        };
+        // this lane's stretch of a part: its first key in the part, keys, place in its block, the block's id
+        uint32_t begin = 0, keys = 0, in_block = 0, id = NONE;
+        const auto look_part = [&](int32_t j0, uint32_t wanted) {
+            const uint32_t b = kvc_div((uint32_t)j0, a.block_size, a.block_shift) + lane;
+            const int64_t at = (int64_t)b * a.block_size - j0;  // where that block begins, from the part's beginning
+            begin = (uint32_t)min(max(at, (int64_t)0), (int64_t)32);
+            keys = (uint32_t)min(at + (int64_t)a.block_size, (int64_t)32) - begin;
+            in_block = begin - (uint32_t)at;
+            id = NONE;
+            if (keys && (wanted >> begin & low_bits((int32_t)keys)))
+                id = (uint32_t)table[b];
+            else
+                keys = 0;
+        };
+        uint32_t next = images ? look_tile(0) : NONE;
+#pragma unroll 1
+        for (uint32_t u = 0; ok && u < c.n; ++u) {
+            const uint32_t tile_id = next;
+            if (images && u + 1 < c.n)
+                next = look_tile(u + 1);
+            const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + u) * TK + first * 32u);
+#pragma unroll 1
+            for (uint32_t p = 0; p < PER; ++p) {
+                const uint32_t wanted = wanted_of(j0 + (int32_t)p * 32);
+                if (images) {
+                    // blocks of the part, first those of K and then of V
+                    const uint32_t n = 32u >> shift, i = lane & (n - 1u);
+                    id = __shfl_sync(~0u, tile_id, (first + p) * n + i);
+                    begin = i << shift;
+                    keys = id == NONE ? 0u : a.block_size;
+                    in_block = 0;
+                } else {
+                    look_part(j0 + (int32_t)p * 32, wanted);
+                }
+                const uint32_t mine = low_bits((int32_t)keys) << begin;
+                const bool good = keys && id < a.num_blocks;
+                if (keys && !good && (!images || lane < 32u >> shift))
+                    atomicAdd(a.status, (uint32_t)__popc(mine & wanted));
+                const uint32_t is = __reduce_or_sync(~0u, good ? mine : 0u);
+                const uint32_t bar = smem_addr(&rb->full[slot]), dst = raw + slot * (2u * S::PART);
+                if (!(ok = __all_sync(~0u, bar_wait(smem_addr(&rb->empty[slot]), parity, dead, a.status))))
+                    break;
+                if (lane == 0) {
+                    rb->there[slot] = is & wanted;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)__popc(is) * 2u * ROW) : "memory");
+                }
+                __syncwarp();
+                const uint64_t at = (uint64_t)id * a.block_stride + head_at;
+                if (images) {
+                    const bool values = lane >= 32u >> shift;
+                    if (good && lane < 64u >> shift)
+                        bulk_load(dst + (values ? S::PART : 0u) + begin * ROW, (values ? a.v : a.k) + at, a.block_size * ROW, bar);
+                } else if (good) {
+                    const uint64_t codes = at + in_block * CODES, scales = at + (uint64_t)a.block_size * CODES + in_block * SCALES;
+                    bulk_load(dst + begin * CODES, a.k + codes, keys * CODES, bar);
+                    bulk_load(dst + 32u * CODES + begin * SCALES, a.k + scales, keys * SCALES, bar);
+                    bulk_load(dst + S::PART + begin * CODES, a.v + codes, keys * CODES, bar);
+                    bulk_load(dst + S::PART + 32u * CODES + begin * SCALES, a.v + scales, keys * SCALES, bar);
+                }
+                ++issued;
+                if (ROWS == 128 && (slot & 3u) != first + PER - 1) {
+                    ++slot;
+                } else {
+                    slot += ROWS == 128 ? 5u - PER : 1u;
+                    if (slot >= (uint32_t)S::PARTS) {
+                        slot -= S::PARTS;
+                        parity ^= 1u;
+                    }
+                }
+            }
+        }
+    }
+    // no copy of ours runs on when the block ends, on no way out: the last parts' barriers have had their bytes
+#pragma unroll 1
+    for (uint32_t n = 0; n < min(issued, (uint32_t)S::PARTS / 4u * PER + (ROWS == 128 ? 0u : 1u)); ++n) {
+        // a step back
+        if (ROWS == 128 && (slot & 3u) != first) {
+            --slot;
+        } else {
+            const uint32_t step = ROWS == 128 ? 5u - PER : 1u;
+            if (slot < step) {
+                slot += S::PARTS;
+                parity ^= 1u;
+            }
+            slot -= step;
+        }
+        // (`parity` is that of the empty barrier's phase before the use, the opposite of the full one's)
+#pragma unroll 1
+        for (uint32_t i = 0; i < KVC_WAIT_LIMIT && !bar_try(smem_addr(&rb->full[slot]), parity ^ 1u); ++i)
+            ;
+    }
+}
+
+// A warp that makes values of raw parts: K or V, part `sub` of every tile with four warps, all parts with one.  A lane
+// makes one key's values, offset + step * code in the model's type, and writes them where the matrix unit reads
+// them; what is no key becomes zeros.  A word of eight codes gives the pairs (0,4) (1,5) (2,6) (3,7): K keeps that
+// order, which the queries are given too, and V's is put right.  Lanes take the groups of their keys in
+// different orders, which keeps their reads and writes in different banks.
 template <typename T, int D, int ROWS, bool KEYS>
-__device__ __forceinline__ void load_role_q4(const KvcAttn &a, const Segment *segments, uint32_t tiles, uint32_t raw, uint32_t *raw_there,
-                                             Bars *bars, uint32_t (*there)[4], volatile uint32_t *dead, uint32_t sub, uint32_t lane)
+__device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segments, uint32_t tiles, uint32_t raw, RawBars *rb, Bars *bars,
+                                           uint32_t (*there)[4], uint32_t sub, volatile uint32_t *dead, uint32_t lane)
 {
     using S = Shape<D, ROWS, true>;
     constexpr int STAGES = KEYS ? S::KS : S::VS, GROUPS = D / 32;
-    constexpr uint32_t CHUNKS = D / 32, PER = 32 / CHUNKS;  // 16-byte pieces of a key's codes, keys per round of copies
-    constexpr uint32_t LAST = 4 - S::WARPS;                 // a warp takes parts sub, sub + WARPS, ..
+    constexpr uint32_t CODES = D / 2, SCALES = D / 8, PER = ROWS == 128 ? 1 : 4;
     const uint32_t full = smem_addr(KEYS ? bars->k_full : bars->v_full), empty = smem_addr(KEYS ? bars->k_empty : bars->v_empty);
-    const unsigned char *plane = KEYS ? a.k : a.v;
+    // this lane's key in a raw part
+    const bool images = raw_images(a);
+    const uint32_t shift = images ? a.block_shift : 0u, block = lane >> shift, in = lane - (block << shift);
+    const uint32_t base = raw + (KEYS ? 0u : (uint32_t)S::PART);
+    const uint32_t code_at = base + (images ? (block << shift) * (CODES + SCALES) + in * CODES : lane * CODES);
+    const uint32_t scale_at = base + (images ? ((block + 1u) << shift) * CODES + (block << shift) * SCALES + in * SCALES
+                                             : 32u * CODES + lane * SCALES);
+    // (D = 64: a row of the stage is all of a key, and its two groups in the same order suit the writes)
+    const uint32_t turn = D == 128 ? (lane >> 1) + (lane >> 3) : lane >> 4, swap = (lane & 7u) << 4;
     SegmentReader reader;
     Segment c;
-    bool more = reader.next(segments, bars, c, dead, a.status);
-    uint32_t u = 0, part = 0;  // of the next part that is loaded: tile, place in it
-    KvcQ4Key key;
-    const auto look = [&]() {
-        const int32_t j = (int32_t)(kvc_tile(c.r, c.t + u) * TK + (part + sub) * 32u + lane);
-        key.codes = -1;
-        key.scales = 0;
-        if (j < c.r.hi && (j >= c.r.lo || j < c.r.sink_end)) {
-            key = kvc_q4_key<D>(a, c.q.table, j, c.h);
-            if (KEYS && key.codes < 0)
-                atomicAdd(a.status, 1u);
-        }
-    };
-    if (more)
-        look();
-    uint32_t loaded = 0, used = 0, to = 0, from = 0;  // parts, and their places in the ring
-    const auto load = [&]() {
-        if (more) {
-            const uint32_t dst = raw + to * S::PART;
-            const uint32_t chunk = lane % CHUNKS, row0 = lane / CHUNKS;
+    Ring<STAGES> ring;
+    uint32_t slot = 0, from = sub, parity = 0;
+    bool ok = true;
+#pragma unroll 1
+    while (ok && reader.next(segments, bars, c, dead, a.status)) {
+        const uint32_t tiles_n = c.n;
+#pragma unroll 1
+        for (uint32_t u = 0; u < tiles_n; ++u) {
+            if (!(ok = __all_sync(~0u, bar_wait(empty + ring.stage * 8u, ring.parity ^ 1u, dead, a.status))))
+                break;
+#pragma unroll 1
+            for (uint32_t p = 0; p < PER; ++p) {
+                if (!(ok = __all_sync(~0u, bar_wait(smem_addr(&rb->full[from]), parity, dead, a.status))))
+                    break;
+                const uint32_t is = rb->there[from];
+                if (KEYS && lane == 0)
+                    there[slot][sub + p] = is;
+                const uint32_t codes = code_at + from * (2u * S::PART), scales = scale_at + from * (2u * S::PART);
+                const uint32_t dst = tiles + ring.stage * S::TILE + ((sub + p) * 32u + lane) * 128u;
+                const uint32_t keep = is >> lane & 1u ? ~0u : 0u;
+                // not unrolled: a warp that shares its instruction cache with the softmax runs a short loop at several times
+                // the pace of a long stretch.  Each group's codes are read a turn ahead
+                uint32_t w[4], sc, g = turn % GROUPS;
+                const auto read = [&] {
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(codes + g * 16u));
+                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc) : "r"(scales + g * 4u));
+                };
+                read();
+#pragma unroll 1
+                for (int i = 0; i < GROUPS; ++i) {
+                    const uint32_t now[4] = {w[0], w[1], w[2], w[3]};
+                    const uint32_t step = kvc_lows(sc, sc) & keep, offset = kvc_highs(sc, sc) & keep;
+                    const uint32_t to = dst + (g >> 1) * S::HALF + (((g & 1u) << 6) ^ swap);
+                    g = (g + 1u) % GROUPS;
+                    read();  // (the last turn reads the first group again)
+                    // step by step over all sixteen pairs: a step's instructions do not wait for one another
+                    uint32_t x[4][4];
 #pragma unroll
-            for (uint32_t i = 0; i < 32 / PER; ++i) {
-                const uint32_t row = i * PER + row0;
-                const int64_t o = __shfl_sync(~0u, key.codes, row);
-                copy16(dst + row * S::PITCH + chunk * 16u, plane + (o >= 0 ? o : 0) + chunk * 16u, o >= 0 ? 16u : 0u);
-            }
-            const bool is = key.codes >= 0;
-            const unsigned char *src = plane + (is ? key.codes + key.scales : 0);
-            const uint32_t at = dst + lane * S::PITCH + D / 2;
-            if (D == 128)
-                copy16(at, src, is ? 16u : 0u);
-            else
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(at), "l"(src), "r"(is ? 8u : 0u) : "memory");
-            if (KEYS) {
-                const uint32_t w = __ballot_sync(~0u, is);
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[k][e] = kvc_q4_biased<T>(now[k] >> (4 * e));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[k][e] = kvc_q4_plain<T>(x[k][e]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[k][e] = kvc_q4_value<T>(x[k][e], step, offset);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (KEYS)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to ^ (k << 4)), "r"(x[k][0]), "r"(x[k][1]), "r"(x[k][2]), "r"(x[k][3]));
+                        else
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to ^ (k << 4)), "r"(kvc_lows(x[k][0], x[k][1])),
+                                         "r"(kvc_lows(x[k][2], x[k][3])), "r"(kvc_highs(x[k][0], x[k][1])), "r"(kvc_highs(x[k][2], x[k][3])));
+                    }
+                }
+                __syncwarp();
                 if (lane == 0)
-                    raw_there[to] = w;
-            }
-            // the next part, whose place is looked up while this one is on its way
-            ++loaded;
-            part += S::WARPS;
-            if (part > LAST) {
-                part = 0;
-                if (++u == c.n) {
-                    u = 0;
-                    more = reader.next(segments, bars, c, dead, a.status);
+                    bar_arrive(smem_addr(&rb->empty[from]));
+                from += ROWS == 128 ? 4u : 1u;
+                if (from >= (uint32_t)S::PARTS) {
+                    from -= S::PARTS;
+                    parity ^= 1u;
                 }
             }
-            if (more)
-                look();
-            to = to == S::PARTS - 1 ? 0 : to + 1;
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-#pragma unroll 1
-    for (int i = 0; i < S::PARTS - 1; ++i)
-        load();
-    Ring<STAGES> ring;
-    uint32_t slot = 0, at = 0;  // at: place of the used part in its tile
-#pragma unroll 1
-    for (;;) {
-        load();
-        if (used == loaded)
-            break;
-        asm volatile("cp.async.wait_group %0;" ::"n"(S::PARTS - 1) : "memory");
-        __syncwarp();
-        if (at == 0 && !__all_sync(~0u, bar_wait(empty + ring.stage * 8u, ring.parity ^ 1u, dead, a.status)))
-            break;
-        if (KEYS && lane == 0)
-            there[slot][at + sub] = raw_there[from];
-        const uint32_t src = raw + from * S::PART + lane * S::PITCH, row = (at + sub) * 32u + lane;
-        const uint32_t dst = tiles + ring.stage * S::TILE + row * 128u;
-        uint32_t sc[4];
-        if (D == 128)
-            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(sc[0]), "=r"(sc[1]), "=r"(sc[2]), "=r"(sc[3]) : "r"(src + D / 2) : "memory");
-        else
-            asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(src + D / 2) : "memory");
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            uint32_t w[4];
-            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src + g * 16u) : "memory");
-            const uint32_t step = kvc_lows(sc[g], sc[g]), offset = kvc_highs(sc[g], sc[g]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    x[e] = kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(w[k] >> (4 * e))), step, offset);
-                const uint32_t chunk = g * 4 + k, to = dst + (chunk >> 3) * S::HALF + (((chunk & 7u) ^ (lane & 7u)) << 4);
-                if (KEYS)
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
-                else
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(kvc_lows(x[0], x[1])), "r"(kvc_lows(x[2], x[3])),
-                                 "r"(kvc_highs(x[0], x[1])), "r"(kvc_highs(x[2], x[3])) : "memory");
-            }
-        }
-        ++used;
-        from = from == S::PARTS - 1 ? 0 : from + 1;
-        at += S::WARPS;
-        if (at > LAST) {
-            at = 0;
+            if (!ok)
+                break;
             fence_async();
             __syncwarp();
             if (lane == 0)
@@ -543,25 +658,23 @@ __device__ __forceinline__ void load_role_q4(const KvcAttn &a, const Segment *se
             ring.next();
             slot = (slot + 1) % THERE;
         }
-        __syncwarp();  // all have read the part, whose place the next copies take
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 template <typename T, int D, int ROWS, bool Q4>
 __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid_constant__ TilesArgs args)
 {
     using S = Shape<D, ROWS, Q4>;
-    constexpr bool HELPED = Q4 && ROWS == 128;  // warps 8-15 load
-    constexpr uint32_t READERS = HELPED ? SEGMENT_READERS - 2 : SEGMENT_READERS;
-    constexpr uint32_t LOADERS = Q4 ? S::WARPS : 1;
+    constexpr bool HELPED = Q4 && ROWS == 128;  // warps 8-15 make values
+    constexpr uint32_t READERS = Q4 && !HELPED ? SEGMENT_READERS + 1 : SEGMENT_READERS;
+    constexpr uint32_t LOADERS = HELPED ? 4 : 1;
     const KvcAttn &a = args.a;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Bars bars;
     __shared__ __align__(16) uint32_t there[THERE][4];
     __shared__ uint32_t s_dead, s_tmem;
     __shared__ Segment segments[SEGMENTS];
-    __shared__ uint32_t raw_there[S::WARPS][S::PARTS];
+    __shared__ RawBars raw;  // (Q4)
     __shared__ float row_top[2][ROWS / 128][2][128], row_sum[ROWS / 128][2][128];  // ([tile of keys, odd or even])[row tile][half][row]
     // What touches no memory of the caller's comes before the wait for the stream's previous kernel.
     const uint32_t warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31u;
@@ -588,6 +701,11 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             bar_init(smem_addr(&bars.seg_empty[i]), READERS);
         }
         bar_init(smem_addr(&bars.drained), 1);
+        if (Q4)
+            for (int i = 0; i < S::PARTS; ++i) {
+                bar_init(smem_addr(&raw.full[i]), 1);
+                bar_init(smem_addr(&raw.empty[i]), 2);
+            }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (!Q4 && args.boxes) {
             asm volatile("prefetch.tensormap [%0];" ::"l"(&args.k_map) : "memory");
@@ -612,17 +730,21 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     }
     const uint32_t tmem = uniform(s_tmem);
 
-    if (warp < 16) {
+    const auto make_values = [&](auto keys, uint32_t sub) {
+        constexpr bool KEYS = decltype(keys)::value;
+        value_role<T, D, ROWS, KEYS>(a, segments, tiles + (KEYS ? S::K : S::V), tiles + S::RAW, &raw, &bars, there, sub, dead, lane);
+    };
+    if (HELPED && warp >= 8 && warp < 16) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        if constexpr (HELPED) {
+            if (warp < 12)
+                make_values(std::true_type(), warp & 3u);
+            else
+                make_values(std::false_type(), warp & 3u);
+        }
+    } else if (warp < 16) {
         // registers: 512 x 104 + 128 x 64 = 640 x 96 of the launch
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-    }
-    if (HELPED && warp >= 8 && warp < 16) {
-        const uint32_t w = warp & 3u, raw = tiles + S::RAW + w * (S::PARTS * S::PART);
-        if (warp < 12)
-            load_role_q4<T, D, ROWS, true>(a, segments, tiles + S::K, raw, raw_there[w % S::WARPS], &bars, there, dead, w, lane);
-        else
-            load_role_q4<T, D, ROWS, false>(a, segments, tiles + S::V, raw + S::WARPS * S::PARTS * S::PART, nullptr, &bars, there, dead, w, lane);
-    } else if (warp < 16) {
         // ---------------------------------------------------------------- softmax
         const uint32_t sub = warp >> 3, half = warp >> 2 & 1u, tid = threadIdx.x & 127u;  // tid: the row
         const uint32_t lanes = (warp & 3u) << 21;  // this warp's 32 rows of tensor memory
@@ -888,13 +1010,17 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         if (warp == 17) {
             if constexpr (!Q4)
                 load_role<D, ROWS, true>(args, segments, tiles + S::K, &bars, there, dead, lane);
-            else if constexpr (!HELPED)
-                load_role_q4<T, D, ROWS, true>(a, segments, tiles + S::K, tiles + S::RAW, raw_there[0], &bars, there, dead, 0, lane);
+            else if constexpr (HELPED)
+                raw_role<D, ROWS>(a, segments, tiles + S::RAW, &raw, &bars, 0, dead, lane, [] {});
+            else
+                make_values(std::true_type(), 0);
         } else if (warp == 18) {
             if constexpr (!Q4)
                 load_role<D, ROWS, false>(args, segments, tiles + S::V, &bars, there, dead, lane);
-            else if constexpr (!HELPED)
-                load_role_q4<T, D, ROWS, false>(a, segments, tiles + S::V, tiles + S::RAW + S::PARTS * S::PART, nullptr, &bars, there, dead, 0, lane);
+            else if constexpr (HELPED)
+                raw_role<D, ROWS>(a, segments, tiles + S::RAW, &raw, &bars, 2, dead, lane, [] {});
+            else
+                make_values(std::false_type(), 0);
         } else if (warp == 16) {
             // ------------------------------------------------------------ matrix instructions
             // The unit takes few instructions ahead, so what this thread does between them is time that
@@ -1010,14 +1136,17 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             for (uint32_t i = 0; i < KVC_WAIT_LIMIT && !bar_try(smem_addr(&bars.drained), 0); ++i)
                 ;
         }
-        if (warp == 19 && lane == 0) {
+        if (warp == 19) {
             // ------------------------------------------------------------ the run, pair by pair
             KvcCursor c = run.at;
-            uint32_t slot = 0, parity = 1, pair = run.pair, n;
+            uint32_t slot = 0, parity = 1, pair = run.pair, n = 1;
             unsigned long long units_at = run.units_at;
-            do {
-                if (!bar_wait(smem_addr(&bars.seg_empty[slot]), parity, dead, a.status))
-                    break;
+            // Hands on the next segment (the last has no tiles); one thread calls it.
+            const auto hand_on = [&] {
+                if (!bar_wait(smem_addr(&bars.seg_empty[slot]), parity, dead, a.status)) {
+                    n = 0;
+                    return;
+                }
                 n = c.s < n_seq ? run.count(c, units_at) : 0u;
                 Segment &s = segments[slot];
                 s.n = n;
@@ -1038,7 +1167,21 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 ++pair;
                 c.t = c.r.n - 1;
                 kvc_next<ROWS, TK>(a, n_seq, c);
-            } while (n != 0);
+            };
+            if constexpr (Q4 && !HELPED) {
+                // two ahead of the parts that this warp copies
+                const auto next = [&] {
+                    if (lane == 0 && n != 0)
+                        hand_on();
+                    __syncwarp();
+                };
+                next();
+                raw_role<D, ROWS>(a, segments, tiles + S::RAW, &raw, &bars, 0, dead, lane, next);
+            } else if (lane == 0) {
+                do
+                    hand_on();
+                while (n != 0);
+            }
         }
         __syncwarp();
     }

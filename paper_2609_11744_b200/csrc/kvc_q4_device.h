@@ -4,6 +4,25 @@
 
 #include "kvc_attention.h"
 
+// A key that is on its way: its position and its block's id, which nothing looks at until the copies are issued, so
+// that the table's latency passes meanwhile.
+struct KvcQ4Next {
+    int32_t j;
+    uint32_t id;
+    bool asked;  // whether j is a key of the pair at all
+};
+
+__device__ __forceinline__ KvcQ4Next kvc_q4_look(const KvcAttn &a, const KvcSeq &q, const KvcRange &r, int32_t j)
+{
+    KvcQ4Next n;
+    n.j = j;
+    n.id = ~0u;
+    n.asked = j < r.hi && (j >= r.lo || j < r.sink_end);
+    if (n.asked)
+        n.id = (uint32_t)a.tables[(int64_t)q.table * a.table_stride + kvc_div((uint32_t)j, a.block_size, a.block_shift)];
+    return n;
+}
+
 // A key's codes relative to its plane's base (negative: not there), and its scales relative to them.
 struct KvcQ4Key {
     int64_t codes;
@@ -11,15 +30,14 @@ struct KvcQ4Key {
 };
 
 template <int D>
-__device__ __forceinline__ KvcQ4Key kvc_q4_key(const KvcAttn &a, uint32_t table, int32_t j, uint32_t h)
+__device__ __forceinline__ KvcQ4Key kvc_q4_key(const KvcAttn &a, const KvcQ4Next &n, uint32_t h)
 {
-    const uint32_t b = kvc_div(j, a.block_size, a.block_shift), in = (uint32_t)j - b * a.block_size;
-    const uint32_t id = (uint32_t)a.tables[(int64_t)table * a.table_stride + b];
     KvcQ4Key k;
     k.codes = -1;
     k.scales = 0;
-    if (id < a.num_blocks) {
-        k.codes = (int64_t)((uint64_t)id * a.block_stride + (uint64_t)h * a.block_size * KVC_Q4_ROW_BYTES(D) + in * (D / 2u));
+    if (n.id < a.num_blocks) {
+        const uint32_t in = (uint32_t)n.j - kvc_div((uint32_t)n.j, a.block_size, a.block_shift) * a.block_size;
+        k.codes = (int64_t)((uint64_t)n.id * a.block_stride + (uint64_t)h * a.block_size * KVC_Q4_ROW_BYTES(D) + in * (D / 2u));
         k.scales = a.block_size * (D / 2u) - in * (D / 2u - D / 8u);
     }
     return k;
