@@ -112,31 +112,73 @@ __device__ __forceinline__ KvcQ4Next look_up(const KvcAttn &a, const KvcCursor &
 // Issues the copies of this warp's keys of one unit; returns which of the 32 are there.  Keys that are not
 // become zeros, steps and offsets too.
 template <int D, int NT>
-__device__ __forceinline__ uint32_t load_unit(const KvcAttn &a, const KvcQ4Key &key, uint32_t lane, uint32_t stage)
+__device__ __forceinline__ uint32_t load_unit(const KvcAttn &a, const KvcQ4Next &key, uint32_t head, uint32_t lane, uint32_t stage)
 {
     using S = Shape<D, NT>;
     constexpr uint32_t CHUNKS = S::CODES / 16, PER = 32 / CHUNKS;  // pieces of a key's codes, keys per round
     const uint32_t chunk = lane % CHUNKS, sub = lane / CHUNKS;
+    const uint32_t there = __ballot_sync(~0u, key.id < a.num_blocks);
+    const uint32_t in = (uint32_t)key.j - kvc_div((uint32_t)key.j, a.block_size, a.block_shift) * a.block_size;
+    const uint64_t head_at = (uint64_t)head * a.block_size * KVC_Q4_ROW_BYTES(D);
+    const unsigned char *k = a.k + head_at, *v = a.v + head_at;
+    const uint32_t dst = stage + sub * S::PITCH + chunk * 16u, scale_dst = stage + lane * S::PITCH + S::CODES;
+    const uint32_t scale_in = a.block_size * S::CODES + in * S::SCALES;
+    const auto scales = [&](uint64_t at, uint32_t bytes) {
+        if (S::SCALES == 16) {
+            copy16(scale_dst, k + at, bytes);
+            copy16(scale_dst + WK * S::PITCH, v + at, bytes);
+        } else {
+            copy8(scale_dst, k + at, bytes);
+            copy8(scale_dst + WK * S::PITCH, v + at, bytes);
+        }
+    };
+    if (there == ~0u) {
 #pragma unroll
-    for (uint32_t i = 0; i < WK / PER; ++i) {
-        const uint32_t row = i * PER + sub;
-        const int64_t o = __shfl_sync(~0u, key.codes, row);
-        const uint32_t bytes = o >= 0 ? 16u : 0u, dst = stage + row * S::PITCH + chunk * 16u;
-        const uint64_t at = (o >= 0 ? (uint64_t)o : 0ull) + chunk * 16u;
-        copy16(dst, a.k + at, bytes);
-        copy16(dst + WK * S::PITCH, a.v + at, bytes);
-    }
-    const uint32_t dst = stage + lane * S::PITCH + S::CODES;
-    const uint64_t at = key.codes >= 0 ? (uint64_t)key.codes + key.scales : 0ull;
-    if (S::SCALES == 16) {
-        copy16(dst, a.k + at, key.codes >= 0 ? 16u : 0u);
-        copy16(dst + WK * S::PITCH, a.v + at, key.codes >= 0 ? 16u : 0u);
+        for (uint32_t i = 0; i < WK / PER; ++i) {
+            const uint32_t row = i * PER + sub;
+            const uint64_t at = (uint64_t)__shfl_sync(~0u, key.id, row) * a.block_stride + (__shfl_sync(~0u, in, row) * S::CODES + chunk * 16u);
+            copy16(dst + i * PER * S::PITCH, k + at, 16);
+            copy16(dst + (i * PER + WK) * S::PITCH, v + at, 16);
+        }
+        scales((uint64_t)key.id * a.block_stride + scale_in, S::SCALES);
     } else {
-        copy8(dst, a.k + at, key.codes >= 0 ? 8u : 0u);
-        copy8(dst + WK * S::PITCH, a.v + at, key.codes >= 0 ? 8u : 0u);
+        const uint64_t mine = key.id < a.num_blocks ? (uint64_t)key.id * a.block_stride : 0ull;
+#pragma unroll 1
+        for (uint32_t i = 0; i < WK / PER; ++i) {
+            const uint32_t row = i * PER + sub, bytes = there >> row & 1u ? 16u : 0u;
+            const uint64_t at = __shfl_sync(~0u, mine, row) + (__shfl_sync(~0u, in, row) * S::CODES + chunk * 16u);
+            copy16(dst + i * PER * S::PITCH, bytes ? k + at : a.k, bytes);
+            copy16(dst + (i * PER + WK) * S::PITCH, bytes ? v + at : a.v, bytes);
+        }
+        const bool is = there >> lane & 1u;
+        scales(is ? mine + scale_in : 0ull, is ? (uint32_t)S::SCALES : 0u);
     }
-    return __ballot_sync(~0u, key.codes >= 0);
+    return there;
 }
+
+// Powers of two that queries take with them into the first product, so that products with codes as numbers as they
+// stand (bf16: 2^-133 each) are none of the smallest: QUERY, and 1 / QUERY / (what a code in the low bits is worth).
+template <typename T>
+struct Scaling;
+template <>
+struct Scaling<__nv_bfloat16> {
+    static constexpr uint32_t QUERY = 0x5F805F80u, QUERY_HIGH = 0x5D805D80u;  // 2^64, 2^60
+    static constexpr float BACK = 0x1p69f;                                    // 2^(133 - 64)
+    static constexpr float SUM = 1.f;
+    static __device__ __forceinline__ uint32_t times(uint32_t x, uint32_t f) { return kvc_mul_bf16x2(x, f); }
+};
+template <>
+struct Scaling<__half> {
+    static constexpr uint32_t QUERY = 0x3C003C00u, QUERY_HIGH = 0x2C002C00u;  // 1, 2^-4
+    static constexpr float BACK = 0x1p24f;
+    static constexpr float SUM = 0x1p-6f;  // of a query's sums, which may leave the type's range
+    static __device__ __forceinline__ uint32_t times(uint32_t x, uint32_t f)
+    {
+        uint32_t r;
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(f));
+        return r;
+    }
+};
 
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_kernel(const KvcAttn a)
@@ -178,10 +220,9 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                 next = look_up(a, ld, warp, lane);
                 next_head = ld.h;
             }
-            const KvcQ4Key key = kvc_q4_key<D>(a, now, head);
-            if (now.asked && key.codes < 0)
+            if (now.asked && now.id >= a.num_blocks)
                 atomicAdd(a.status, 1u);
-            const uint32_t there = load_unit<D, NT>(a, key, lane, ring + stage * S::STAGE);
+            const uint32_t there = load_unit<D, NT>(a, now, head, lane, ring + stage * S::STAGE);
             if (lane == 0)
                 s_there[warp][stage] = there;
         }
@@ -195,8 +236,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
     for (uint32_t n_units; c.s < n_seq && (n_units = run.count(c, units_at)) != 0;) {
         // ---- a new pair (or the rest of one): its queries as matrix operands, D x 8 NT
         const uint32_t row0 = c.rt * ROWS, rows = min((uint32_t)ROWS, (uint32_t)c.q.rows - row0);
-        uint32_t qf[NT][2 * G][2];
-        float qs[NT][G][2];  // sums of a query's groups, of the two columns of an accumulator
+        uint32_t qf[NT][2 * G][2], qs[NT][2];
         int32_t pos[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -207,22 +247,34 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                 const uint32_t row = row0 + i, tok = kvc_div_g(a, row);
                 src += (int64_t)(c.q.qa + (int32_t)tok) * a.q_tok + (int64_t)(c.h * a.g + (row - tok * a.g)) * a.q_head;
             }
+            float sums[G];
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 uint4 x = make_uint4(0, 0, 0, 0);
                 if (real)
                     x = *reinterpret_cast<const uint4 *>(src + g * 64 + gc * 16);
-                qf[n][2 * g][0] = kvc_lows(x.x, x.z);
-                qf[n][2 * g][1] = kvc_highs(x.x, x.z);
-                qf[n][2 * g + 1][0] = kvc_lows(x.y, x.w);
-                qf[n][2 * g + 1][1] = kvc_highs(x.y, x.w);
+                using F = Scaling<T>;
+                qf[n][2 * g][0] = F::times(kvc_lows(x.x, x.z), F::QUERY);
+                qf[n][2 * g][1] = F::times(kvc_highs(x.x, x.z), F::QUERY_HIGH);
+                qf[n][2 * g + 1][0] = F::times(kvc_lows(x.y, x.w), F::QUERY);
+                qf[n][2 * g + 1][1] = F::times(kvc_highs(x.y, x.w), F::QUERY_HIGH);
                 const float2 p = kvc_to_float2<T>(x.x), q = kvc_to_float2<T>(x.y), u = kvc_to_float2<T>(x.z), v = kvc_to_float2<T>(x.w);
                 float sum = ((p.x + p.y) + (q.x + q.y)) + ((u.x + u.y) + (v.x + v.y));
                 sum += __shfl_xor_sync(~0u, sum, 1);
-                sum += __shfl_xor_sync(~0u, sum, 2);
-                qs[n][g][0] = __shfl_sync(~0u, sum, gc * 8);
-                qs[n][g][1] = __shfl_sync(~0u, sum, gc * 8 + 4);
+                sums[g] = (sum + __shfl_xor_sync(~0u, sum, 2)) * Scaling<T>::SUM;
             }
+            // The product of offsets and a query's sums: places 0-3 of the operand take the groups' sums rounded to the type, 4-7
+            // and 8-11 what that leaves, twice over: all 24 bits.  This lane holds places 2 gc, 2 gc + 1 and the same + 8.
+            const float s0 = G == 4 && (gc & 1u) ? sums[G / 2] : sums[0], s1 = G == 4 && (gc & 1u) ? sums[G - 1] : sums[1];
+            const uint32_t first = kvc_from_float2<T>(s0, s1);
+            float2 left = kvc_to_float2<T>(first);
+            left = make_float2(s0 - left.x, s1 - left.y);
+            const uint32_t second = kvc_from_float2<T>(left.x, left.y);
+            const float2 then = kvc_to_float2<T>(second);
+            const uint32_t third = kvc_from_float2<T>(left.x - then.x, left.y - then.y);
+            const bool has = G == 4 || (gc & 1u) == 0;  // (two groups: every second pair of places is empty)
+            qs[n][0] = !has ? 0u : gc < 2 ? first : second;
+            qs[n][1] = !has || gc >= 2 ? 0u : third;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const uint32_t col = n * 8 + gc * 2 + e;  // (a column of no row sees all: it holds up no check)
@@ -256,48 +308,50 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                 float s[KT][NT][4];
 #pragma unroll
                 for (int t = 0; t < KT; ++t) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
                     const uint32_t at = kb + (t * 16 + gr) * S::PITCH;
                     uint32_t sc[2][G];
                     lds_words<G>(sc[0], at + S::CODES);
                     lds_words<G>(sc[1], at + 8 * S::PITCH + S::CODES);
+                    uint32_t f[4];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        f[r] = f[r + 2] = G == 4 && (gc & 1u) ? kvc_highs(sc[r][G / 2], sc[r][G - 1]) : kvc_highs(sc[r][0], sc[r][1]);
+                    float codes[NT][4];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
+                        codes[n][0] = codes[n][1] = codes[n][2] = codes[n][3] = 0.f;
+                        mma<T>(s[t][n], f, qs[n][0], qs[n][1]);
+                    }
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
                         const uint32_t w0 = lds(at + g * 16 + gc * 4), w1 = lds(at + 8 * S::PITCH + g * 16 + gc * 4);
                         float acc[NT][4];
-                        constexpr bool BIASED = std::is_same<T, __nv_bfloat16>::value;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            // bf16: the bias of the codes is taken off beforehand, in the 32-bit sums (2^-17 of it is what
-                            // they lose); fp16's is 8 times as large and comes off the codes
-                            acc[n][0] = acc[n][2] = BIASED ? -KvcQ4<T>::BIAS * qs[n][g][0] : 0.f;
-                            acc[n][1] = acc[n][3] = BIASED ? -KvcQ4<T>::BIAS * qs[n][g][1] : 0.f;
-                        }
+                        for (int n = 0; n < NT; ++n)
+                            acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
-                            uint32_t f[4] = {kvc_q4_biased<T>(w0 >> (8 * k)), kvc_q4_biased<T>(w1 >> (8 * k)),
-                                             kvc_q4_biased<T>(w0 >> (8 * k + 4)), kvc_q4_biased<T>(w1 >> (8 * k + 4))};
-                            if (!BIASED)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    f[e] = kvc_q4_plain<T>(f[e]);
+                            const uint32_t y0 = k ? w0 >> 8 : w0, y1 = k ? w1 >> 8 : w1;
+                            const uint32_t f[4] = {kvc_q4_low(y0), kvc_q4_low(y1), kvc_q4_high(y0), kvc_q4_high(y1)};
 #pragma unroll
                             for (int n = 0; n < NT; ++n)
                                 mma<T>(acc[n], f, qf[n][2 * g + k][0], qf[n][2 * g + k][1]);
                         }
-                        const float2 x0 = kvc_to_float2<T>(sc[0][g]), x1 = kvc_to_float2<T>(sc[1][g]);
+                        const float x0 = kvc_to_float2<T>(sc[0][g]).x, x1 = kvc_to_float2<T>(sc[1][g]).x;
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float2 x = e < 2 ? x0 : x1;
-                                s[t][n][e] = fmaf(x.x, acc[n][e], fmaf(x.y, qs[n][g][e & 1], s[t][n][e]));
-                            }
+                            for (int e = 0; e < 4; ++e)
+                                codes[n][e] = fmaf(e < 2 ? x0 : x1, acc[n][e], codes[n][e]);
                     }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[t][n][e] = fmaf(codes[n][e], Scaling<T>::BACK, Scaling<T>::SUM == 1.f ? s[t][n][e] : s[t][n][e] * (1.f / Scaling<T>::SUM));
                 }
-                // scores in base 2; where some row does not see all of the warp's keys, those it does not become -inf
+                // where some row does not see all of the warp's keys, the scores of those it does not become -inf
                 bool all = there == ~0u;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -313,7 +367,6 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                     for (int t = 0; t < KT; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            s[t][n][e] *= a.scale_log2;
                             if (!all) {
                                 const int k = t * 16 + (e >> 1) * 8 + (int)gr;
                                 if (!((there >> k & 1u) && kvc_sees(a, pos[n][e & 1], j0 + k)))
@@ -338,7 +391,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const float now = fmaxf(m[n][e], top[n][e]);
-                            const float f = m[n][e] == -INFINITY ? 0.f : exp2_fast(m[n][e] - now);
+                            const float f = m[n][e] == -INFINITY ? 0.f : exp2_fast((m[n][e] - now) * a.scale_log2);
                             m[n][e] = now;
                             l[n][e] *= f;
 #pragma unroll
@@ -351,12 +404,12 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                 uint32_t p[KT][NT][2];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const float base0 = m[n][0] == -INFINITY ? 0.f : m[n][0], base1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
+                    const float base0 = m[n][0] == -INFINITY ? 0.f : -m[n][0] * a.scale_log2, base1 = m[n][1] == -INFINITY ? 0.f : -m[n][1] * a.scale_log2;
 #pragma unroll
                     for (int t = 0; t < KT; ++t) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            s[t][n][e] = exp2_fast(s[t][n][e] - (e & 1 ? base1 : base0));
+                            s[t][n][e] = exp2_fast(fmaf(s[t][n][e], a.scale_log2, e & 1 ? base1 : base0));
                             l[n][e & 1] += s[t][n][e];
                         }
                         p[t][n][0] = transpose(kvc_from_float2<T>(s[t][n][0], s[t][n][1]));
@@ -373,23 +426,26 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                         lds_words<S::WORDS>(w[r], at + gr * (4 * S::WORDS));
                         sc[r] = lds(at + S::CODES + gr * S::WORDS / 4 * 4);
                     }
-                    const uint32_t step0 = kvc_lows(sc[0], sc[1]), off0 = kvc_highs(sc[0], sc[1]);
-                    const uint32_t step1 = kvc_lows(sc[2], sc[3]), off1 = kvc_highs(sc[2], sc[3]);
+                    const uint32_t step0 = kvc_q4_step<T>(kvc_lows(sc[0], sc[1])), off0 = kvc_highs(sc[0], sc[1]);
+                    const uint32_t step1 = kvc_q4_step<T>(kvc_lows(sc[2], sc[3])), off1 = kvc_highs(sc[2], sc[3]);
 #pragma unroll
                     for (int u = 0; u < S::WORDS; ++u) {
                         const uint32_t x0 = kvc_lows(w[0][u], w[1][u]), y0 = kvc_highs(w[0][u], w[1][u]);
                         const uint32_t x1 = kvc_lows(w[2][u], w[3][u]), y1 = kvc_highs(w[2][u], w[3][u]);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t f[4] = {
-                                kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(x0 >> (4 * k))), step0, off0),
-                                kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(y0 >> (4 * k))), step0, off0),
-                                kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(x1 >> (4 * k))), step1, off1),
-                                kvc_q4_value<T>(kvc_q4_plain<T>(kvc_q4_biased<T>(y1 >> (4 * k))), step1, off1)};
+                        const auto tile = [&](auto high, uint32_t far, int k) {
+                            constexpr bool HIGH = decltype(high)::value;
+                            const uint32_t f[4] = {kvc_q4_value<T>(kvc_q4_code<T, HIGH>(x0 >> far), step0, off0),
+                                                   kvc_q4_value<T>(kvc_q4_code<T, HIGH>(y0 >> far), step0, off0),
+                                                   kvc_q4_value<T>(kvc_q4_code<T, HIGH>(x1 >> far), step1, off1),
+                                                   kvc_q4_value<T>(kvc_q4_code<T, HIGH>(y1 >> far), step1, off1)};
 #pragma unroll
                             for (int n = 0; n < NT; ++n)
                                 mma<T>(o[n][u * 4 + k], f, p[t][n][0], p[t][n][1]);
-                        }
+                        };
+                        tile(std::false_type(), 0, 0);
+                        tile(std::true_type(), 0, 1);
+                        tile(std::false_type(), 8, 2);
+                        tile(std::true_type(), 8, 3);
                     }
                 }
             }
@@ -405,6 +461,12 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                 l[n][e] += __shfl_xor_sync(~0u, l[n][e], 8);
                 l[n][e] += __shfl_xor_sync(~0u, l[n][e], 16);
             }
+        // (a maximum is a score so far: from here on in base 2)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                m[n][e] *= a.scale_log2;
         __syncthreads();  // the join before this one is over
         if (gr == 0)
 #pragma unroll

@@ -610,22 +610,20 @@ __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segm
 #pragma unroll 1
                 for (int i = 0; i < GROUPS; ++i) {
                     const uint32_t now[4] = {w[0], w[1], w[2], w[3]};
-                    const uint32_t step = kvc_lows(sc, sc) & keep, offset = kvc_highs(sc, sc) & keep;
+                    const uint32_t step = kvc_q4_step<T>(kvc_lows(sc, sc) & keep), offset = kvc_highs(sc, sc) & keep;
                     const uint32_t to = dst + (g >> 1) * S::HALF + (((g & 1u) << 6) ^ swap);
                     g = (g + 1u) % GROUPS;
                     read();  // (the last turn reads the first group again)
                     // step by step over all sixteen pairs: a step's instructions do not wait for one another
                     uint32_t x[4][4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[k][e] = kvc_q4_biased<T>(now[k] >> (4 * e));
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[k][e] = kvc_q4_plain<T>(x[k][e]);
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t far = now[k] >> 8;
+                        x[k][0] = kvc_q4_code<T, false>(now[k]);
+                        x[k][1] = kvc_q4_code<T, true>(now[k]);
+                        x[k][2] = kvc_q4_code<T, false>(far);
+                        x[k][3] = kvc_q4_code<T, true>(far);
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll

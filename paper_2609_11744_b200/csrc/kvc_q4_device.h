@@ -23,41 +23,6 @@ __device__ __forceinline__ KvcQ4Next kvc_q4_look(const KvcAttn &a, const KvcSeq 
     return n;
 }
 
-// A key's codes relative to its plane's base (negative: not there), and its scales relative to them.
-struct KvcQ4Key {
-    int64_t codes;
-    uint32_t scales;
-};
-
-template <int D>
-__device__ __forceinline__ KvcQ4Key kvc_q4_key(const KvcAttn &a, const KvcQ4Next &n, uint32_t h)
-{
-    KvcQ4Key k;
-    k.codes = -1;
-    k.scales = 0;
-    if (n.id < a.num_blocks) {
-        const uint32_t in = (uint32_t)n.j - kvc_div((uint32_t)n.j, a.block_size, a.block_shift) * a.block_size;
-        k.codes = (int64_t)((uint64_t)n.id * a.block_stride + (uint64_t)h * a.block_size * KVC_Q4_ROW_BYTES(D) + in * (D / 2u));
-        k.scales = a.block_size * (D / 2u) - in * (D / 2u - D / 8u);
-    }
-    return k;
-}
-
-// Codes as numbers.  The low four bits of either half of a word, put under an exponent whose last place is one, are
-// that power of two (BIAS) plus the code: two codes an instruction.  (bf16's 7 bits behind the point reach to 128.)
-template <typename T>
-struct KvcQ4;
-template <>
-struct KvcQ4<__nv_bfloat16> {
-    static constexpr uint32_t EXPONENT = 0x43004300u;
-    static constexpr float BIAS = 128.f;
-};
-template <>
-struct KvcQ4<__half> {
-    static constexpr uint32_t EXPONENT = 0x64006400u;
-    static constexpr float BIAS = 1024.f;
-};
-
 __device__ __forceinline__ uint32_t kvc_bytes(uint32_t a, uint32_t b, uint32_t which)
 {
     uint32_t r;
@@ -68,39 +33,69 @@ __device__ __forceinline__ uint32_t kvc_bytes(uint32_t a, uint32_t b, uint32_t w
 __device__ __forceinline__ uint32_t kvc_lows(uint32_t a, uint32_t b) { return kvc_bytes(a, b, 0x5410u); }
 __device__ __forceinline__ uint32_t kvc_highs(uint32_t a, uint32_t b) { return kvc_bytes(a, b, 0x7632u); }
 
-// BIAS + code of the low four bits of either half.
+// Codes as numbers, two a word.  Bits that lie in the lowest eight of a 16-bit float are a number as they stand: that many of
+// the type's smallest, the step from the subnormal numbers to the first binade included.  So the codes in bits 0-3 of either
+// half are that many times TINY, and those in bits 4-7 sixteen times as much: one instruction, and the matrix
+// instructions, which take subnormal numbers for what they are, can have them.  A word's third and fourth pair are
+// eight bits further up.
+__device__ __forceinline__ uint32_t kvc_q4_low(uint32_t x) { return x & 0x000F000Fu; }
+__device__ __forceinline__ uint32_t kvc_q4_high(uint32_t x) { return x & 0x00F000F0u; }
+
+// And as values: offset + step * code, rounded once.  The codes are brought into the type's range first -- bf16: times a
+// power of two, fp16 (whose range is too small for the step to make up for TINY): under an exponent that makes them 1024 + code
+// or 64 + code / 16, less that -- which is exact, then fma.  `step` is kvc_q4_step's.
 template <typename T>
-__device__ __forceinline__ uint32_t kvc_q4_biased(uint32_t x)
-{
-    uint32_t r;
-    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(r) : "r"(x), "n"(KvcQ4<T>::EXPONENT));
-    return r;
-}
-// Without the bias: exact.
-template <typename T>
-__device__ __forceinline__ uint32_t kvc_q4_plain(uint32_t biased);
-template <>
-__device__ __forceinline__ uint32_t kvc_q4_plain<__nv_bfloat16>(uint32_t biased)
-{
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(KvcQ4<__nv_bfloat16>::EXPONENT));
-    return r;
-}
-template <>
-__device__ __forceinline__ uint32_t kvc_q4_plain<__half>(uint32_t biased)
-{
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(KvcQ4<__half>::EXPONENT));
-    return r;
-}
-// offset + step * code, rounded once.
+__device__ __forceinline__ uint32_t kvc_q4_step(uint32_t step);
+template <typename T, bool HIGH>
+__device__ __forceinline__ uint32_t kvc_q4_code(uint32_t x);
 template <typename T>
 __device__ __forceinline__ uint32_t kvc_q4_value(uint32_t code, uint32_t step, uint32_t offset);
+
+__device__ __forceinline__ uint32_t kvc_mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <>
+__device__ __forceinline__ uint32_t kvc_q4_step<__nv_bfloat16>(uint32_t step)
+{
+    return kvc_mul_bf16x2(step, 0x42804280u);  // 2^6
+}
+template <>
+__device__ __forceinline__ uint32_t kvc_q4_code<__nv_bfloat16, false>(uint32_t x)
+{
+    return kvc_mul_bf16x2(kvc_q4_low(x), 0x7F007F00u);  // 2^127 * 2^-133
+}
+template <>
+__device__ __forceinline__ uint32_t kvc_q4_code<__nv_bfloat16, true>(uint32_t x)
+{
+    return kvc_mul_bf16x2(kvc_q4_high(x), 0x7D007D00u);  // 2^123 * 2^-129
+}
 template <>
 __device__ __forceinline__ uint32_t kvc_q4_value<__nv_bfloat16>(uint32_t code, uint32_t step, uint32_t offset)
 {
     uint32_t r;
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(code), "r"(step), "r"(offset));
+    return r;
+}
+template <>
+__device__ __forceinline__ uint32_t kvc_q4_step<__half>(uint32_t step)
+{
+    return step;
+}
+template <>
+__device__ __forceinline__ uint32_t kvc_q4_code<__half, false>(uint32_t x)
+{
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(kvc_q4_low(x) | 0x64006400u), "r"(0x64006400u));
+    return r;
+}
+template <>
+__device__ __forceinline__ uint32_t kvc_q4_code<__half, true>(uint32_t x)
+{
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(kvc_q4_high(x) | 0x64006400u), "r"(0x2C002C00u), "r"(0xD400D400u));
     return r;
 }
 template <>
