@@ -426,18 +426,15 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                         lds_words<S::WORDS>(w[r], at + gr * (4 * S::WORDS));
                         sc[r] = lds(at + S::CODES + gr * S::WORDS / 4 * 4);
                     }
-                    const uint32_t step0 = kvc_q4_step<T>(kvc_lows(sc[0], sc[1])), off0 = kvc_highs(sc[0], sc[1]);
-                    const uint32_t step1 = kvc_q4_step<T>(kvc_lows(sc[2], sc[3])), off1 = kvc_highs(sc[2], sc[3]);
+                    const KvcQ4Values<T> v0(kvc_lows(sc[0], sc[1]), kvc_highs(sc[0], sc[1])), v1(kvc_lows(sc[2], sc[3]), kvc_highs(sc[2], sc[3]));
 #pragma unroll
                     for (int u = 0; u < S::WORDS; ++u) {
                         const uint32_t x0 = kvc_lows(w[0][u], w[1][u]), y0 = kvc_highs(w[0][u], w[1][u]);
                         const uint32_t x1 = kvc_lows(w[2][u], w[3][u]), y1 = kvc_highs(w[2][u], w[3][u]);
                         const auto tile = [&](auto high, uint32_t far, int k) {
                             constexpr bool HIGH = decltype(high)::value;
-                            const uint32_t f[4] = {kvc_q4_value<T>(kvc_q4_code<T, HIGH>(x0 >> far), step0, off0),
-                                                   kvc_q4_value<T>(kvc_q4_code<T, HIGH>(y0 >> far), step0, off0),
-                                                   kvc_q4_value<T>(kvc_q4_code<T, HIGH>(x1 >> far), step1, off1),
-                                                   kvc_q4_value<T>(kvc_q4_code<T, HIGH>(y1 >> far), step1, off1)};
+                            const uint32_t f[4] = {v0.template of<HIGH>(x0 >> far), v0.template of<HIGH>(y0 >> far),
+                                                   v1.template of<HIGH>(x1 >> far), v1.template of<HIGH>(y1 >> far)};
 #pragma unroll
                             for (int n = 0; n < NT; ++n)
                                 mma<T>(o[n][u * 4 + k], f, p[t][n][0], p[t][n][1]);
@@ -492,7 +489,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
 #pragma unroll
                 for (int w = 0; w < WARPS; ++w)
                     tl[n][e] += s_l[w][col] * exp2f(s_m[w][col] - ref);
-                const float f = exp2f(m[n][e] - ref);
+                const float f = exp2f(m[n][e] - ref) * (1.f / KvcQ4Values<T>::SCALE);
 #pragma unroll
                 for (int t = 0; t < S::MT; ++t) {
                     o[n][t][e] *= f;

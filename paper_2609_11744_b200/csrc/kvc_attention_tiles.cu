@@ -555,7 +555,7 @@ __device__ __forceinline__ void raw_role(const KvcAttn &a, const Segment *segmen
     }
 }
 
-// A warp that makes values of raw parts: K or V, part `sub` of every tile with four warps, all parts with one.  A lane
+// A warp that makes values (SCALE of them) of raw parts: K or V, part `sub` of every tile with four warps, all parts with one.  A lane
 // makes one key's values, offset + step * code in the model's type, and writes them where the matrix unit reads
 // them; what is no key becomes zeros.  A word of eight codes gives the pairs (0,4) (1,5) (2,6) (3,7): K keeps that
 // order, which the queries are given too, and V's is put right.  Lanes take the groups of their keys in
@@ -610,25 +610,19 @@ __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segm
 #pragma unroll 1
                 for (int i = 0; i < GROUPS; ++i) {
                     const uint32_t now[4] = {w[0], w[1], w[2], w[3]};
-                    const uint32_t step = kvc_q4_step<T>(kvc_lows(sc, sc) & keep), offset = kvc_highs(sc, sc) & keep;
+                    const KvcQ4Values<T> values(kvc_lows(sc, sc) & keep, kvc_highs(sc, sc) & keep);
                     const uint32_t to = dst + (g >> 1) * S::HALF + (((g & 1u) << 6) ^ swap);
                     g = (g + 1u) % GROUPS;
                     read();  // (the last turn reads the first group again)
-                    // step by step over all sixteen pairs: a step's instructions do not wait for one another
                     uint32_t x[4][4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const uint32_t far = now[k] >> 8;
-                        x[k][0] = kvc_q4_code<T, false>(now[k]);
-                        x[k][1] = kvc_q4_code<T, true>(now[k]);
-                        x[k][2] = kvc_q4_code<T, false>(far);
-                        x[k][3] = kvc_q4_code<T, true>(far);
+                        x[k][0] = values.template of<false>(now[k]);
+                        x[k][1] = values.template of<true>(now[k]);
+                        x[k][2] = values.template of<false>(far);
+                        x[k][3] = values.template of<true>(far);
                     }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[k][e] = kvc_q4_value<T>(x[k][e], step, offset);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         if (KEYS)
@@ -830,7 +824,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 const bool room = a.phase == KVC_PHASE_WHOLE || c.pair < a.parts.max_pairs;
                 const uint64_t slot_row = (a.phase == KVC_PHASE_WHOLE ? 2ull * blockIdx.x + (from_start ? 1 : 0)
                                                                       : (uint64_t)blockIdx.x + c.pair) * ROWS + sub * 128u;
-                const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
+                constexpr float BACK = Q4 ? 1.f / KvcQ4Values<T>::SCALE : 1.f;  // values that are SCALE of what they are
+                const float inv = l == 0.f ? 0.f : BACK / l;  // a row that sees nothing: zeros
 #pragma unroll 1
                 for (uint32_t rows16 = 0; rows16 < 32; rows16 += 16) {
                     unsigned char *dst[2];
@@ -861,7 +856,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                                     *reinterpret_cast<uint32_t *>(dst[e] + (q + k * 8) * 2) =
                                         f[e] == 0.f ? 0u : kvc_from_float2<T>(x * f[e], y * f[e]);
                                 else
-                                    *reinterpret_cast<float2 *>(dst[e] + (q + k * 8) * 4) = make_float2(x, y);
+                                    *reinterpret_cast<float2 *>(dst[e] + (q + k * 8) * 4) = make_float2(x * BACK, y * BACK);
                             }
                     }
                 }
@@ -1275,5 +1270,6 @@ cudaError_t kvc_launch_attn_q4_tiles(const KvcAttn &a, uint32_t dtype, uint32_t 
     TilesArgs args;
     memset(&args, 0, sizeof(args));
     args.a = a;
+    args.a.scale_log2 *= 1.f / (dtype == KVC_DTYPE_BF16 ? KvcQ4Values<__nv_bfloat16>::SCALE : KvcQ4Values<__half>::SCALE);
     return launch_type<true>(args, dtype, head_dim, blocks, st);
 }

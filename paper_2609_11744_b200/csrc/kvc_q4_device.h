@@ -41,69 +41,54 @@ __device__ __forceinline__ uint32_t kvc_highs(uint32_t a, uint32_t b) { return k
 __device__ __forceinline__ uint32_t kvc_q4_low(uint32_t x) { return x & 0x000F000Fu; }
 __device__ __forceinline__ uint32_t kvc_q4_high(uint32_t x) { return x & 0x00F000F0u; }
 
-// And as values: offset + step * code, rounded once.  The codes are brought into the type's range first -- bf16: times a
-// power of two, fp16 (whose range is too small for the step to make up for TINY): under an exponent that makes them 1024 + code
-// or 64 + code / 16, less that -- which is exact, then fma.  `step` is kvc_q4_step's.
-template <typename T>
-__device__ __forceinline__ uint32_t kvc_q4_step(uint32_t step);
-template <typename T, bool HIGH>
-__device__ __forceinline__ uint32_t kvc_q4_code(uint32_t x);
-template <typename T>
-__device__ __forceinline__ uint32_t kvc_q4_value(uint32_t code, uint32_t step, uint32_t offset);
-
 __device__ __forceinline__ uint32_t kvc_mul_bf16x2(uint32_t a, uint32_t b)
 {
     uint32_t r;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+// And as values: offset + step * code, rounded once, of two groups a word.
+// bf16: as many TINYs times a step that makes up for them, by fma: two instructions for two values.  The step has to stay
+// in the type's range, so the values come out as SCALE of what they are, which their product's sums, of 32 bits, do
+// not mind (values above 2^60 are none then, and differences below 2^-69 are lost).
+// fp16's range is too small for that: the codes go under an exponent that makes them 1024 + code or 64 + code / 16, less that,
+// which is exact, then fma.
+template <typename T>
+struct KvcQ4Values;
 template <>
-__device__ __forceinline__ uint32_t kvc_q4_step<__nv_bfloat16>(uint32_t step)
-{
-    return kvc_mul_bf16x2(step, 0x42804280u);  // 2^6
-}
+struct KvcQ4Values<__nv_bfloat16> {
+    static constexpr float SCALE = 0x1p-64f;
+    uint32_t low, high, offset;
+    __device__ __forceinline__ KvcQ4Values(uint32_t step, uint32_t off)
+        : low(kvc_mul_bf16x2(step, 0x62006200u)),    // 2^(133 - 64)
+          high(kvc_mul_bf16x2(step, 0x60006000u)),   // 2^(129 - 64)
+          offset(kvc_mul_bf16x2(off, 0x1F801F80u))   // 2^-64
+    {
+    }
+    template <bool HIGH>
+    __device__ __forceinline__ uint32_t of(uint32_t x) const
+    {
+        uint32_t r;
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(HIGH ? kvc_q4_high(x) : kvc_q4_low(x)), "r"(HIGH ? high : low), "r"(offset));
+        return r;
+    }
+};
 template <>
-__device__ __forceinline__ uint32_t kvc_q4_code<__nv_bfloat16, false>(uint32_t x)
-{
-    return kvc_mul_bf16x2(kvc_q4_low(x), 0x7F007F00u);  // 2^127 * 2^-133
-}
-template <>
-__device__ __forceinline__ uint32_t kvc_q4_code<__nv_bfloat16, true>(uint32_t x)
-{
-    return kvc_mul_bf16x2(kvc_q4_high(x), 0x7D007D00u);  // 2^123 * 2^-129
-}
-template <>
-__device__ __forceinline__ uint32_t kvc_q4_value<__nv_bfloat16>(uint32_t code, uint32_t step, uint32_t offset)
-{
-    uint32_t r;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(code), "r"(step), "r"(offset));
-    return r;
-}
-template <>
-__device__ __forceinline__ uint32_t kvc_q4_step<__half>(uint32_t step)
-{
-    return step;
-}
-template <>
-__device__ __forceinline__ uint32_t kvc_q4_code<__half, false>(uint32_t x)
-{
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(kvc_q4_low(x) | 0x64006400u), "r"(0x64006400u));
-    return r;
-}
-template <>
-__device__ __forceinline__ uint32_t kvc_q4_code<__half, true>(uint32_t x)
-{
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(kvc_q4_high(x) | 0x64006400u), "r"(0x2C002C00u), "r"(0xD400D400u));
-    return r;
-}
-template <>
-__device__ __forceinline__ uint32_t kvc_q4_value<__half>(uint32_t code, uint32_t step, uint32_t offset)
-{
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(code), "r"(step), "r"(offset));
-    return r;
-}
+struct KvcQ4Values<__half> {
+    static constexpr float SCALE = 1.f;
+    uint32_t step, offset;
+    __device__ __forceinline__ KvcQ4Values(uint32_t s, uint32_t off) : step(s), offset(off) {}
+    template <bool HIGH>
+    __device__ __forceinline__ uint32_t of(uint32_t x) const
+    {
+        uint32_t r;
+        if (HIGH)
+            asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(kvc_q4_high(x) | 0x64006400u), "r"(0x2C002C00u), "r"(0xD400D400u));
+        else
+            asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(kvc_q4_low(x) | 0x64006400u), "r"(0x64006400u));
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(r), "r"(step), "r"(offset));
+        return r;
+    }
+};
 
 #endif
