@@ -25,8 +25,8 @@ constexpr int THREADS = WARPS * 32;
 constexpr int WK = 32;             // keys per warp and unit
 constexpr int TK = WK * WARPS;     // keys per unit
 constexpr int KT = WK / 16;        // key tiles of the matrix instruction
-constexpr int HEAD = 1;            // what a pair costs besides its units, in units
-constexpr int LEAST = 1;           // units of a run at least
+constexpr int HEAD = 2;            // what a pair costs besides its units, in units
+constexpr int LEAST = 2;           // units of a run at least
 
 template <int D, int NT>
 struct Shape {
@@ -36,7 +36,8 @@ struct Shape {
     static constexpr int SCALES = D / 8;             // and of its steps and offsets, which lie behind them
     static constexpr int PITCH = D == 128 ? 80 : 48;  // of a key in shared memory: eight keys' words in different banks
     static constexpr int STAGE = 2 * WK * PITCH;     // K and V of one warp's share of a unit
-    static constexpr int STAGES = D == 128 ? 2 : 3;
+    static constexpr int STAGES = 3;                 // one that is loaded, one whose keys are used, one whose values are
+    static constexpr int BLOCKS = (NT == 1 ? 3 : 2) + (D == 64 ? 1 : 0);  // a SM
     static constexpr int MERGE = 2 * ROWS * D * 4;   // two warps' sums
     static constexpr int SMEM = WARPS * STAGES * STAGE + MERGE;
     static constexpr int MT = D / 16;                // tiles of the second product
@@ -54,21 +55,20 @@ __device__ __forceinline__ void copy8(uint32_t dst, const void *src, uint32_t by
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-__device__ __forceinline__ uint32_t lds(uint32_t at)
-{
-    uint32_t r;
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(at) : "memory");
-    return r;
-}
+// Words of shared memory.
+__device__ __forceinline__ uint32_t word(const unsigned char *at) { return *reinterpret_cast<const uint32_t *>(at); }
 template <int N>
-__device__ __forceinline__ void lds_words(uint32_t (&r)[N], uint32_t at)
+__device__ __forceinline__ void words(uint32_t (&r)[N], const unsigned char *at)
 {
-    if (N == 4)
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1 % N]), "=r"(r[2 % N]), "=r"(r[3 % N]) : "r"(at) : "memory");
-    else if (N == 2)
-        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1 % N]) : "r"(at) : "memory");
-    else
-        r[0] = lds(at);
+    if constexpr (N == 4) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(at);
+        r[0] = x.x, r[1] = x.y, r[2] = x.z, r[3] = x.w;
+    } else if constexpr (N == 2) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(at);
+        r[0] = x.x, r[1] = x.y;
+    } else {
+        r[0] = word(at);
+    }
 }
 
 template <typename T>
@@ -76,14 +76,14 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
 template <>
 __device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <>
 __device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -103,55 +103,55 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
-// This lane's key of the cursor's unit.
-__device__ __forceinline__ KvcQ4Next look_up(const KvcAttn &a, const KvcCursor &c, uint32_t warp, uint32_t lane)
-{
-    return kvc_q4_look(a, c.q, c.r, (int32_t)(kvc_tile(c.r, c.t) * TK + warp * WK + lane));
-}
-
 // Issues the copies of this warp's keys of one unit; returns which of the 32 are there.  Keys that are not
-// become zeros, steps and offsets too.
+// become zeros, steps and offsets too.  `k`: where the head's rows begin in the plane's first block.  `near`: every place of
+// the plane is fewer than 2^32 steps of 16 bytes from its beginning, so a place is one register until its address is
+// made, by one multiply-add.
 template <int D, int NT>
-__device__ __forceinline__ uint32_t load_unit(const KvcAttn &a, const KvcQ4Next &key, uint32_t head, uint32_t lane, uint32_t stage)
+__device__ __forceinline__ uint32_t load_unit(const KvcAttn &a, int32_t j, uint32_t id, bool asked, const unsigned char *k, bool near,
+                                              uint32_t lane, uint32_t stage)
 {
     using S = Shape<D, NT>;
     constexpr uint32_t CHUNKS = S::CODES / 16, PER = 32 / CHUNKS;  // pieces of a key's codes, keys per round
     const uint32_t chunk = lane % CHUNKS, sub = lane / CHUNKS;
-    const uint32_t there = __ballot_sync(~0u, key.id < a.num_blocks);
-    const uint32_t in = (uint32_t)key.j - kvc_div((uint32_t)key.j, a.block_size, a.block_shift) * a.block_size;
-    const uint64_t head_at = (uint64_t)head * a.block_size * KVC_Q4_ROW_BYTES(D);
-    const unsigned char *k = a.k + head_at, *v = a.v + head_at;
+    const uint32_t there = __ballot_sync(~0u, id < a.num_blocks);
+    const uint32_t in = a.block_shift != KVC_NO_SHIFT ? (uint32_t)j & (a.block_size - 1u) : (uint32_t)j % a.block_size;
+    const int64_t to_v = a.v - a.k;
     const uint32_t dst = stage + sub * S::PITCH + chunk * 16u, scale_dst = stage + lane * S::PITCH + S::CODES;
-    const uint32_t scale_in = a.block_size * S::CODES + in * S::SCALES;
-    const auto scales = [&](uint64_t at, uint32_t bytes) {
+    const auto scales = [&](const unsigned char *at, uint32_t bytes) {
         if (S::SCALES == 16) {
-            copy16(scale_dst, k + at, bytes);
-            copy16(scale_dst + WK * S::PITCH, v + at, bytes);
+            copy16(scale_dst, at, bytes);
+            copy16(scale_dst + WK * S::PITCH, at + to_v, bytes);
         } else {
-            copy8(scale_dst, k + at, bytes);
-            copy8(scale_dst + WK * S::PITCH, v + at, bytes);
+            copy8(scale_dst, at, bytes);
+            copy8(scale_dst + WK * S::PITCH, at + to_v, bytes);
         }
     };
-    if (there == ~0u) {
+    const uint32_t to_scales = a.block_size * S::CODES - in * (S::CODES - S::SCALES);
+    if (there == ~0u && near) {
+        const uint32_t mine = id * (uint32_t)(a.block_stride >> 4) + in * (S::CODES / 16);
+        const unsigned char *kc = k + chunk * 16u, *vc = kc + to_v;
 #pragma unroll
         for (uint32_t i = 0; i < WK / PER; ++i) {
-            const uint32_t row = i * PER + sub;
-            const uint64_t at = (uint64_t)__shfl_sync(~0u, key.id, row) * a.block_stride + (__shfl_sync(~0u, in, row) * S::CODES + chunk * 16u);
-            copy16(dst + i * PER * S::PITCH, k + at, 16);
-            copy16(dst + (i * PER + WK) * S::PITCH, v + at, 16);
+            const uint32_t at = __shfl_sync(~0u, mine, i * PER + sub);
+            copy16(dst + i * PER * S::PITCH, kc + (uint64_t)at * 16u, 16);
+            copy16(dst + (i * PER + WK) * S::PITCH, vc + (uint64_t)at * 16u, 16);
         }
-        scales((uint64_t)key.id * a.block_stride + scale_in, S::SCALES);
+        scales(k + (uint64_t)mine * 16u + to_scales, S::SCALES);
     } else {
-        const uint64_t mine = key.id < a.num_blocks ? (uint64_t)key.id * a.block_stride : 0ull;
+        if (asked && id >= a.num_blocks)
+            atomicAdd(a.status, 1u);
+        const uint64_t mine = id < a.num_blocks ? (uint64_t)id * a.block_stride + (uint64_t)in * S::CODES : 0ull;
 #pragma unroll 1
         for (uint32_t i = 0; i < WK / PER; ++i) {
             const uint32_t row = i * PER + sub, bytes = there >> row & 1u ? 16u : 0u;
-            const uint64_t at = __shfl_sync(~0u, mine, row) + (__shfl_sync(~0u, in, row) * S::CODES + chunk * 16u);
-            copy16(dst + i * PER * S::PITCH, bytes ? k + at : a.k, bytes);
-            copy16(dst + (i * PER + WK) * S::PITCH, bytes ? v + at : a.v, bytes);
+            const uint64_t at = __shfl_sync(~0u, mine, row);
+            const unsigned char *src = bytes ? k + at + chunk * 16u : a.k;
+            copy16(dst + i * PER * S::PITCH, src, bytes);
+            copy16(dst + (i * PER + WK) * S::PITCH, src + to_v, bytes);
         }
         const bool is = there >> lane & 1u;
-        scales(is ? mine + scale_in : 0ull, is ? (uint32_t)S::SCALES : 0u);
+        scales(is ? k + mine + to_scales : a.k, is ? (uint32_t)S::SCALES : 0u);
     }
     return there;
 }
@@ -181,7 +181,7 @@ struct Scaling<__half> {
 };
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_kernel(const KvcAttn a)
+__global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) kvc_attn_q4_rows_kernel(const KvcAttn a)
 {
     using S = Shape<D, NT>;
     constexpr int ROWS = S::ROWS, G = S::GROUPS;
@@ -204,33 +204,57 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
     KvcCursor ld = run.at, c = run.at;
     unsigned long long ld_at = run.units_at, units_at = run.units_at;  // where their pairs' units lie on the line
     uint32_t pair = run.pair;
-    // the load cursor's unit, if it is in the run, and one step on; places are looked up a unit ahead
-    bool more = true;
-    KvcQ4Next next = look_up(a, ld, warp, lane);
-    uint32_t next_head = ld.h;
+    const bool near = a.block_stride < (1ull << 36) && ((uint64_t)a.num_blocks * (a.block_stride >> 4)) >> 32 == 0;
+    // The next unit to load is one of a stretch of key tiles that follow one another; what they have in common is found
+    // once a stretch.  `left`: of the stretch, that one among them (0: the run has no more).
+    uint32_t left = 0, tiles = 0;
+    int32_t ld_j = 0;                // this lane's key
+    uint32_t ld_id = ~0u;            // the id of its block, looked up a unit ahead, so that the table's latency passes meanwhile
+    bool ld_asked = false;           // whether it is a key of the pair at all
+    const int32_t *ld_table = a.tables;
+    const unsigned char *ld_k = a.k;
+    const auto look = [&] {
+        ld_asked = ld_j < ld.r.hi && (ld_j >= ld.r.lo || ld_j < ld.r.sink_end);
+        ld_id = ~0u;
+        if (ld_asked)
+            ld_id = (uint32_t)ld_table[kvc_div((uint32_t)ld_j, a.block_size, a.block_shift)];
+    };
+    const auto stretch = [&] {  // from the unit at `ld`
+        tiles = left = 0;
+        if (ld.s < n_seq)
+            tiles = left = min(run.count(ld, ld_at), (ld.t < ld.r.sink_tiles ? ld.r.sink_tiles : ld.r.n) - ld.t);
+        if (left) {
+            ld_j = (int32_t)(kvc_tile(ld.r, ld.t) * TK + warp * WK + lane);
+            ld_table = a.tables + (int64_t)ld.q.table * a.table_stride;
+            ld_k = a.k + (uint64_t)ld.h * a.block_size * KVC_Q4_ROW_BYTES(D);
+            look();
+        }
+    };
+    stretch();
     const auto load = [&](uint32_t stage) {
-        if (more) {
-            const KvcQ4Next now = next;
-            const uint32_t head = next_head, n = ld.r.n;
-            kvc_next<ROWS, TK>(a, n_seq, ld);
-            if (ld.t == 0)
-                ld_at += n + HEAD;
-            more = ld.s < n_seq && ld_at + ld.t < run.end;
-            if (more) {
-                next = look_up(a, ld, warp, lane);
-                next_head = ld.h;
+        if (left) {
+            const int32_t j = ld_j;
+            const uint32_t id = ld_id;
+            const bool asked = ld_asked;
+            const unsigned char *k = ld_k;
+            if (--left) {
+                ld_j += TK;
+                look();
+            } else {
+                const uint32_t n = ld.r.n;
+                ld.t += tiles - 1;
+                kvc_next<ROWS, TK>(a, n_seq, ld);
+                if (ld.t == 0)
+                    ld_at += n + HEAD;
+                stretch();
             }
-            if (now.asked && now.id >= a.num_blocks)
-                atomicAdd(a.status, 1u);
-            const uint32_t there = load_unit<D, NT>(a, now, head, lane, ring + stage * S::STAGE);
+            const uint32_t there = load_unit<D, NT>(a, j, id, asked, k, near, lane, ring + stage * S::STAGE);
             if (lane == 0)
                 s_there[warp][stage] = there;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-#pragma unroll 1
-    for (uint32_t i = 0; i < S::STAGES - 1; ++i)
-        load(i);
+    load(0);
     uint32_t stage = 0;
 
     for (uint32_t n_units; c.s < n_seq && (n_units = run.count(c, units_at)) != 0;) {
@@ -282,172 +306,186 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
             }
         }
         float o[NT][S::MT][4];
-        float m[NT][2], l[NT][2];
+        float m[NT][2], l[NT][2], limit[NT][2];  // the maximum in use, base 2; the sum; the score that would move the maximum
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int t = 0; t < S::MT; ++t)
                 o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
-            m[n][0] = m[n][1] = -INFINITY;
+            m[n][0] = m[n][1] = limit[n][0] = limit[n][1] = -INFINITY;
             l[n][0] = l[n][1] = 0.f;
         }
         const bool from_start = c.t == 0;
         const bool to_end = c.t + n_units == c.r.n;
 
+        // The weights of one unit and where its values are: their product is made beside the next unit's scores, which have
+        // nothing to do with one another, so that the instructions of either fill the waits of the other.
+        uint32_t p[KT][NT][2];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                p[t][n][0] = p[t][n][1] = 0;
+        const auto products = [&](const unsigned char *vb) {
+            // ---- values: of keys 2 gc, 2 gc + 1 and the same + 8, the codes of words WORDS * gr ..
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                uint32_t w[4][S::WORDS], sc[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const unsigned char *at = vb + (t * 16 + gc * 2 + (r & 1) + (r >> 1) * 8) * S::PITCH;
+                    words<S::WORDS>(w[r], at + gr * (4 * S::WORDS));
+                    sc[r] = word(at + S::CODES + gr * S::WORDS / 4 * 4);
+                }
+                const KvcQ4Values<T> v0(kvc_lows(sc[0], sc[1]), kvc_highs(sc[0], sc[1])), v1(kvc_lows(sc[2], sc[3]), kvc_highs(sc[2], sc[3]));
+#pragma unroll
+                for (int u = 0; u < S::WORDS; ++u) {
+                    const uint32_t x0 = kvc_lows(w[0][u], w[1][u]), y0 = kvc_highs(w[0][u], w[1][u]);
+                    const uint32_t x1 = kvc_lows(w[2][u], w[3][u]), y1 = kvc_highs(w[2][u], w[3][u]);
+                    const auto tile = [&](auto high, uint32_t far, int k) {
+                        constexpr bool HIGH = decltype(high)::value;
+                        const uint32_t f[4] = {v0.template of<HIGH>(x0 >> far), v0.template of<HIGH>(y0 >> far),
+                                               v1.template of<HIGH>(x1 >> far), v1.template of<HIGH>(y1 >> far)};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            mma<T>(o[n][u * 4 + k], f, p[t][n][0], p[t][n][1]);
+                    };
+                    tile(std::false_type(), 0, 0);
+                    tile(std::true_type(), 0, 1);
+                    tile(std::false_type(), 8, 2);
+                    tile(std::true_type(), 8, 3);
+                }
+            }
+        };
+        uint32_t before = stage;  // (the first unit's own values, with weights of zero)
         for (uint32_t i = 0; i < n_units; ++i) {
-            // the stage that the previous unit used is free once every lane is past its reads
+            // the stage of the unit before the last is free once every lane is past its reads
             __syncwarp();
-            load(stage == 0 ? S::STAGES - 1 : stage - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
+            load(stage == S::STAGES - 1 ? 0 : stage + 1);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncwarp();
 
-            const uint32_t kb = ring + stage * S::STAGE, vb = kb + WK * S::PITCH;
+            const unsigned char *kb = smem + (warp * S::STAGES + stage) * S::STAGE;
             const uint32_t there = s_there[warp][stage];
             const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + i) * TK + warp * WK);
-            if (there != 0) {
-                float s[KT][NT][4];
+            float s[KT][NT][4];
 #pragma unroll
-                for (int t = 0; t < KT; ++t) {
-                    const uint32_t at = kb + (t * 16 + gr) * S::PITCH;
-                    uint32_t sc[2][G];
-                    lds_words<G>(sc[0], at + S::CODES);
-                    lds_words<G>(sc[1], at + 8 * S::PITCH + S::CODES);
-                    uint32_t f[4];
+            for (int t = 0; t < KT; ++t) {
+                const unsigned char *at = kb + (t * 16 + gr) * S::PITCH;
+                uint32_t sc[2][G];
+                words<G>(sc[0], at + S::CODES);
+                words<G>(sc[1], at + 8 * S::PITCH + S::CODES);
+                uint32_t f[4];
 #pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        f[r] = f[r + 2] = G == 4 && (gc & 1u) ? kvc_highs(sc[r][G / 2], sc[r][G - 1]) : kvc_highs(sc[r][0], sc[r][1]);
-                    float codes[NT][4];
+                for (int r = 0; r < 2; ++r)
+                    f[r] = f[r + 2] = G == 4 && (gc & 1u) ? kvc_highs(sc[r][G / 2], sc[r][G - 1]) : kvc_highs(sc[r][0], sc[r][1]);
+                float codes[NT][4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
-                        codes[n][0] = codes[n][1] = codes[n][2] = codes[n][3] = 0.f;
-                        mma<T>(s[t][n], f, qs[n][0], qs[n][1]);
-                    }
+                for (int n = 0; n < NT; ++n) {
+                    s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
+                    codes[n][0] = codes[n][1] = codes[n][2] = codes[n][3] = 0.f;
+                    mma<T>(s[t][n], f, qs[n][0], qs[n][1]);
+                }
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        const uint32_t w0 = lds(at + g * 16 + gc * 4), w1 = lds(at + 8 * S::PITCH + g * 16 + gc * 4);
-                        float acc[NT][4];
+                for (int g = 0; g < G; ++g) {
+                    const uint32_t w0 = word(at + g * 16 + gc * 4), w1 = word(at + 8 * S::PITCH + g * 16 + gc * 4);
+                    float acc[NT][4];
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+                    for (int n = 0; n < NT; ++n)
+                        acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const uint32_t y0 = k ? w0 >> 8 : w0, y1 = k ? w1 >> 8 : w1;
-                            const uint32_t f[4] = {kvc_q4_low(y0), kvc_q4_low(y1), kvc_q4_high(y0), kvc_q4_high(y1)};
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-                                mma<T>(acc[n], f, qf[n][2 * g + k][0], qf[n][2 * g + k][1]);
-                        }
-                        const float x0 = kvc_to_float2<T>(sc[0][g]).x, x1 = kvc_to_float2<T>(sc[1][g]).x;
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t y0 = k ? w0 >> 8 : w0, y1 = k ? w1 >> 8 : w1;
+                        const uint32_t f[4] = {kvc_q4_low(y0), kvc_q4_low(y1), kvc_q4_high(y0), kvc_q4_high(y1)};
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                codes[n][e] = fmaf(e < 2 ? x0 : x1, acc[n][e], codes[n][e]);
+                            mma<T>(acc[n], f, qf[n][2 * g + k][0], qf[n][2 * g + k][1]);
                     }
+                    const float x0 = kvc_to_float2<T>(sc[0][g]).x, x1 = kvc_to_float2<T>(sc[1][g]).x;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            s[t][n][e] = fmaf(codes[n][e], Scaling<T>::BACK, Scaling<T>::SUM == 1.f ? s[t][n][e] : s[t][n][e] * (1.f / Scaling<T>::SUM));
+                            codes[n][e] = fmaf(e < 2 ? x0 : x1, acc[n][e], codes[n][e]);
                 }
-                // where some row does not see all of the warp's keys, the scores of those it does not become -inf
-                bool all = there == ~0u;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        all = all && j0 + WK - 1 <= pos[n][e] && (a.window == 0 || pos[n][e] - j0 < a.window || j0 + WK <= a.sinks);
-                all = __all_sync(~0u, all);
-                float top[NT][2];
-                bool moved = false;
+                    for (int e = 0; e < 4; ++e)
+                        s[t][n][e] = fmaf(codes[n][e], Scaling<T>::BACK, Scaling<T>::SUM == 1.f ? s[t][n][e] : s[t][n][e] * (1.f / Scaling<T>::SUM));
+            }
+            products(smem + (warp * S::STAGES + before) * S::STAGE + WK * S::PITCH);
+            before = stage;
+            // where some row does not see all of the warp's keys, the scores of those it does not become -inf
+            bool all = there == ~0u;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int t = 0; t < KT; ++t)
+                for (int e = 0; e < 2; ++e)
+                    all = all && j0 + WK - 1 <= pos[n][e] && (a.window == 0 || pos[n][e] - j0 < a.window || j0 + WK <= a.sinks);
+            all = __all_sync(~0u, all);
+            // The maximum in use need not be the largest score: it moves when a score is more than 2^8 times its weight, which
+            // neither type nor the sums mind, and else the lanes of a row have nothing to tell one another
+            float top[NT][2];
+            bool move = false;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (!all) {
-                                const int k = t * 16 + (e >> 1) * 8 + (int)gr;
-                                if (!((there >> k & 1u) && kvc_sees(a, pos[n][e & 1], j0 + k)))
-                                    s[t][n][e] = -INFINITY;
-                            }
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!all) {
+                            const int k = t * 16 + (e >> 1) * 8 + (int)gr;
+                            if (!((there >> k & 1u) && kvc_sees(a, pos[n][e & 1], j0 + k)))
+                                s[t][n][e] = -INFINITY;
                         }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = fmaxf(s[0][n][e], s[0][n][e + 2]);
+#pragma unroll
+                    for (int t = 1; t < KT; ++t)
+                        x = fmaxf(x, fmaxf(s[t][n][e], s[t][n][e + 2]));
+                    top[n][e] = x;
+                    move |= x > limit[n][e];
+                }
+            }
+            if (__any_sync(~0u, move)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float x = fmaxf(s[0][n][e], s[0][n][e + 2]);
-#pragma unroll
-                        for (int t = 1; t < KT; ++t)
-                            x = fmaxf(x, fmaxf(s[t][n][e], s[t][n][e + 2]));
-                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                        float x = fmaxf(top[n][e], __shfl_xor_sync(~0u, top[n][e], 4));
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
-                        top[n][e] = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                        moved |= top[n][e] > m[n][e];
-                    }
-                }
-                if (__any_sync(~0u, moved)) {
+                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                        const float now = fmaxf(m[n][e], x * a.scale_log2);
+                        const float f = m[n][e] == -INFINITY ? 0.f : exp2_fast(m[n][e] - now);
+                        m[n][e] = now;
+                        limit[n][e] = now == -INFINITY ? -INFINITY : (now + 8.f) * (1.f / a.scale_log2);
+                        l[n][e] *= f;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float now = fmaxf(m[n][e], top[n][e]);
-                            const float f = m[n][e] == -INFINITY ? 0.f : exp2_fast((m[n][e] - now) * a.scale_log2);
-                            m[n][e] = now;
-                            l[n][e] *= f;
-#pragma unroll
-                            for (int t = 0; t < S::MT; ++t) {
-                                o[n][t][e] *= f;
-                                o[n][t][e + 2] *= f;
-                            }
+                        for (int t = 0; t < S::MT; ++t) {
+                            o[n][t][e] *= f;
+                            o[n][t][e + 2] *= f;
                         }
-                }
-                uint32_t p[KT][NT][2];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float base0 = m[n][0] == -INFINITY ? 0.f : -m[n][0] * a.scale_log2, base1 = m[n][1] == -INFINITY ? 0.f : -m[n][1] * a.scale_log2;
-#pragma unroll
-                    for (int t = 0; t < KT; ++t) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            s[t][n][e] = exp2_fast(fmaf(s[t][n][e], a.scale_log2, e & 1 ? base1 : base0));
-                            l[n][e & 1] += s[t][n][e];
-                        }
-                        p[t][n][0] = transpose(kvc_from_float2<T>(s[t][n][0], s[t][n][1]));
-                        p[t][n][1] = transpose(kvc_from_float2<T>(s[t][n][2], s[t][n][3]));
                     }
-                }
-                // ---- values: of keys 2 gc, 2 gc + 1 and the same + 8, the codes of words WORDS * gr ..
+            }
+            #pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float base0 = m[n][0] == -INFINITY ? 0.f : -m[n][0], base1 = m[n][1] == -INFINITY ? 0.f : -m[n][1];
 #pragma unroll
                 for (int t = 0; t < KT; ++t) {
-                    uint32_t w[4][S::WORDS], sc[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const uint32_t at = vb + (t * 16 + gc * 2 + (r & 1) + (r >> 1) * 8) * S::PITCH;
-                        lds_words<S::WORDS>(w[r], at + gr * (4 * S::WORDS));
-                        sc[r] = lds(at + S::CODES + gr * S::WORDS / 4 * 4);
+                    for (int e = 0; e < 4; ++e) {
+                        s[t][n][e] = exp2_fast(fmaf(s[t][n][e], a.scale_log2, e & 1 ? base1 : base0));
+                        l[n][e & 1] += s[t][n][e];
                     }
-                    const KvcQ4Values<T> v0(kvc_lows(sc[0], sc[1]), kvc_highs(sc[0], sc[1])), v1(kvc_lows(sc[2], sc[3]), kvc_highs(sc[2], sc[3]));
-#pragma unroll
-                    for (int u = 0; u < S::WORDS; ++u) {
-                        const uint32_t x0 = kvc_lows(w[0][u], w[1][u]), y0 = kvc_highs(w[0][u], w[1][u]);
-                        const uint32_t x1 = kvc_lows(w[2][u], w[3][u]), y1 = kvc_highs(w[2][u], w[3][u]);
-                        const auto tile = [&](auto high, uint32_t far, int k) {
-                            constexpr bool HIGH = decltype(high)::value;
-                            const uint32_t f[4] = {v0.template of<HIGH>(x0 >> far), v0.template of<HIGH>(y0 >> far),
-                                                   v1.template of<HIGH>(x1 >> far), v1.template of<HIGH>(y1 >> far)};
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-                                mma<T>(o[n][u * 4 + k], f, p[t][n][0], p[t][n][1]);
-                        };
-                        tile(std::false_type(), 0, 0);
-                        tile(std::true_type(), 0, 1);
-                        tile(std::false_type(), 8, 2);
-                        tile(std::true_type(), 8, 3);
-                    }
+                    p[t][n][0] = transpose(kvc_from_float2<T>(s[t][n][0], s[t][n][1]));
+                    p[t][n][1] = transpose(kvc_from_float2<T>(s[t][n][2], s[t][n][3]));
                 }
             }
             stage = stage == S::STAGES - 1 ? 0 : stage + 1;
         }
+        products(smem + (warp * S::STAGES + before) * S::STAGE + WK * S::PITCH);
 
         // ---- end of the pair, or of the run: join the four warps' parts
 #pragma unroll
@@ -458,12 +496,6 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 3) kvc_attn_q4_rows_ker
                 l[n][e] += __shfl_xor_sync(~0u, l[n][e], 8);
                 l[n][e] += __shfl_xor_sync(~0u, l[n][e], 16);
             }
-        // (a maximum is a score so far: from here on in base 2)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                m[n][e] *= a.scale_log2;
         __syncthreads();  // the join before this one is over
         if (gr == 0)
 #pragma unroll
@@ -599,7 +631,12 @@ cudaError_t launch_type(const KvcAttn &a, uint32_t head_dim, uint32_t blocks, cu
 }  // namespace
 
 // As many blocks as are resident.
-uint32_t kvc_attn_q4_rows_blocks(const kvc_layout *lay, uint32_t rows) { return (rows == KVC_ATTN_FEW_ROWS ? 4u : 3u) * (uint32_t)lay->sm_count; }
+uint32_t kvc_attn_q4_rows_blocks(const kvc_layout *lay, uint32_t rows)
+{
+    const int few = kvc_q4_head_dim(lay) == 128 ? Shape<128, 1>::BLOCKS : Shape<64, 1>::BLOCKS;
+    const int more = kvc_q4_head_dim(lay) == 128 ? Shape<128, 2>::BLOCKS : Shape<64, 2>::BLOCKS;
+    return (uint32_t)(rows == KVC_ATTN_FEW_ROWS ? few : more) * (uint32_t)lay->sm_count;
+}
 
 cudaError_t kvc_launch_attn_q4_rows(const KvcAttn &a, uint32_t dtype, uint32_t head_dim, uint32_t blocks, cudaStream_t st)
 {

@@ -4,25 +4,6 @@
 
 #include "kvc_attention.h"
 
-// A key that is on its way: its position and its block's id, which nothing looks at until the copies are issued, so
-// that the table's latency passes meanwhile.
-struct KvcQ4Next {
-    int32_t j;
-    uint32_t id;
-    bool asked;  // whether j is a key of the pair at all
-};
-
-__device__ __forceinline__ KvcQ4Next kvc_q4_look(const KvcAttn &a, const KvcSeq &q, const KvcRange &r, int32_t j)
-{
-    KvcQ4Next n;
-    n.j = j;
-    n.id = ~0u;
-    n.asked = j < r.hi && (j >= r.lo || j < r.sink_end);
-    if (n.asked)
-        n.id = (uint32_t)a.tables[(int64_t)q.table * a.table_stride + kvc_div((uint32_t)j, a.block_size, a.block_shift)];
-    return n;
-}
-
 __device__ __forceinline__ uint32_t kvc_bytes(uint32_t a, uint32_t b, uint32_t which)
 {
     uint32_t r;
