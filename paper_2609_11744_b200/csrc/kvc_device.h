@@ -97,6 +97,16 @@ __device__ __forceinline__ uint64_t kvc_mul2(uint64_t a, uint64_t b)
     return r;
 }
 
+__device__ __forceinline__ uint32_t kvc_bytes(uint32_t a, uint32_t b, uint32_t which)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(which));
+    return r;
+}
+// The low and the high halves of two words.
+__device__ __forceinline__ uint32_t kvc_lows(uint32_t a, uint32_t b) { return kvc_bytes(a, b, 0x5410u); }
+__device__ __forceinline__ uint32_t kvc_highs(uint32_t a, uint32_t b) { return kvc_bytes(a, b, 0x7632u); }
+
 // Two 16-bit elements <-> two floats.
 template <typename T>
 __device__ __forceinline__ float2 kvc_to_float2(uint32_t v);

@@ -4,16 +4,6 @@
 
 #include "kvc_attention.h"
 
-__device__ __forceinline__ uint32_t kvc_bytes(uint32_t a, uint32_t b, uint32_t which)
-{
-    uint32_t r;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(which));
-    return r;
-}
-// The low and the high halves of two words.
-__device__ __forceinline__ uint32_t kvc_lows(uint32_t a, uint32_t b) { return kvc_bytes(a, b, 0x5410u); }
-__device__ __forceinline__ uint32_t kvc_highs(uint32_t a, uint32_t b) { return kvc_bytes(a, b, 0x7632u); }
-
 // Codes as numbers, two a word.  Bits that lie in the lowest eight of a 16-bit float are a number as they stand: that many of
 // the type's smallest, the step from the subnormal numbers to the first binade included.  So the codes in bits 0-3 of either
 // half are that many times TINY, and those in bits 4-7 sixteen times as much: one instruction, and the matrix

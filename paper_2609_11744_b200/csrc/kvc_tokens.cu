@@ -250,7 +250,7 @@ struct AppendAxes : AppendArgs {
 #define APPEND_BLOCKS 16
 #define APPEND_UNROLL 4
 #define APPEND_CHUNK 2
-#define APPEND_Q4_BLOCKS 12
+#define APPEND_Q4_BLOCKS 16
 
 // A lane's eight values as two words of either piece, and as two pairs of floats an operand.
 struct AppendRaw {
@@ -335,18 +335,17 @@ __device__ __forceinline__ uint32_t append_quantise(const AppendRaw &r, uint32_t
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float d = (x[i] - low) * up;
-        float n = rintf(d * inv);
-        const float rest = fmaf(-n, step, d);
-        const bool odd = rintf(0.5f * n) != 0.5f * n;
-        if (rest > half || (rest == half && odd))
-            n += 1.f;
-        else if (rest < -half || (rest == -half && odd))
-            n -= 1.f;
+        // (sums with 3 * 2^22 end on an integer, whose last bit is the sum's)
+        const float t = fmaf(d, inv, 12582912.f);
+        float n = t - 12582912.f;
+        const float rest = fmaf(-n, step, d), off = fabsf(rest);
+        if (off > half || (off == half && (__float_as_uint(t) & 1u)))
+            n += copysignf(1.f, rest);
         c[i] = step > 0.f ? fminf(fmaxf(n, 0.f), 15.f) : 0.f;
     }
     const float lo = fmaf(4096.f, c[3], fmaf(256.f, c[2], fmaf(16.f, c[1], c[0])));
     const float hi = fmaf(4096.f, c[7], fmaf(256.f, c[6], fmaf(16.f, c[5], c[4])));
-    return __float2uint_rn(lo) | __float2uint_rn(hi) << 16;
+    return kvc_lows(__float_as_uint(lo + 8388608.f), __float_as_uint(hi + 8388608.f));
 }
 
 // NEIGHBOURS: pairs are (2n, 2n+1), else (n, n + rot/2).  VEC: rows of the cos/sin table are 16-byte aligned.
