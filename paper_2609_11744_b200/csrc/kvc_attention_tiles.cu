@@ -32,6 +32,20 @@
 // Weights are rounded to the pool's type, since the matrix unit takes 16-bit operands of one type; a second product
 // for what the rounding leaves would be half as much tensor work again.  Against 64 bits the result is off by 0.0021 to
 // 0.0023 in bf16 (0.0017 with weights in 32 bits: the result's own rounding) and 0.0003 in fp16 (0.0002).
+//
+// Over a pool held in 4 bits (Q4) the matrix unit gets values, offset + step * code in the pool's 16-bit type (as a 16-bit pool
+// would hold them, but for a power of two: kvc_q4_device.h); the rest is the same.  Its keys come in raw parts, a quarter of a
+// tile of K and V each, which are copied as they lie (5/16 of the bytes) and made into values by other warps:
+//   256 rows  warp 19 walks the pairs and copies, warps 17 and 18 make values of K and of V
+//   128 rows  warps 17 and 18 copy, warps 8-15, which have no rows, make values: four of K, four of V
+// Measured: the 8192-token prompt in 692 us = 794 TFLOP/s in runs of thirty (16-bit pool: 588).  What bounds it is the pace
+// of the three warps beside the softmax: 1100 cycles for the values of a part and 1500 to copy one, against 1220 that the
+// softmax of 256 rows takes a part.  Such a warp runs at 3.4 cycles an instruction in straight lines, whose code the
+// softmax keeps driving out of the instruction cache, so its loops are short: 916 us with the value loop unrolled, 778
+// without, 724 with the steps of sixteen pairs side by side, 692 with two instructions a pair.  The softmax must keep its 104
+// registers (with 96 the 16-bit prompt takes 1330 us), which leaves none for more warps.  With few rows in tiles of 128
+// (32 requests of up to 5 drafted tokens behind 8000: 231 us) the softmax' chain is the bound, as over a 16-bit pool.  Against
+// 64 bits the result is off by 0.0029 in bf16 (keys and values rounded too) and 0.0004 in fp16.
 // Every wait is bounded; one that gives up makes all roles leave and is counted.
 #include <cuda.h>
 #include <stddef.h>

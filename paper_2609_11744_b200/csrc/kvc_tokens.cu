@@ -235,7 +235,9 @@ struct AppendArgs {
     uint32_t *status;
 };
 
-// Positions with several axes: which axis turns each pair, a byte a pair.
+// Positions with several axes: which axis turns each pair, a byte a pair.  A lane's four pairs usually turn by one axis, whose
+// row's angles are two vectors as ever; where they do not, their angles are fetched one by one (16384 tokens of 64 + 16
+// heads, three axes in sections: 142 us, like one axis).
 struct AppendAxes : AppendArgs {
     int64_t axis_stride;
     uint32_t n_axes;
@@ -258,6 +260,9 @@ struct AppendRaw {
 };
 
 // ---- the 4-bit form (kvc_append_q4): a lane's eight values make one word of codes, four lanes a group.
+// Measured: 16384 tokens of 64 + 16 heads of 128 in 163 us, against 141 for the write in 16 bits: 55 MB less to write, but a
+// key's or value's head is some 150 instructions more (200 us with 12 blocks a SM and roundings by conversions, 175
+// with 16 blocks, 163 with roundings by sums).  Keys whose pairs are halves of a head change lanes first.
 
 // A head's values from pieces of the two halves of its rotated part to eight neighbours a lane; the lanes behind
 // the `turned` ones hold theirs already.
@@ -703,7 +708,8 @@ kvc_status append(kvc_layout *lay, const kvc_append_desc *d, const kvc_append_ax
 // ------------------------------------------------------------------------------------ read_q4
 //
 // offset + step * code, rounded once.  Bound by memory, most of it the 16-bit result: a lane takes one word of codes, eight
-// values, and writes 16 bytes; a warp takes the heads of one token and plane.
+// values, and writes 16 bytes; a warp takes the heads of one token and plane.  Measured: 16384 tokens of 8 heads of 128, 88 MB,
+// in 15.5 us = 5.7 TB/s.
 struct ReadArgs {
     const unsigned char *plane[2];
     unsigned char *out[2];

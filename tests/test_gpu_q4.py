@@ -551,6 +551,37 @@ def test_blocks_past_four_gigabytes_and_long_contexts():
     c.check(c.run(hint=0, window=50000, sinks=2), c.want(50000, 2))
 
 
+def test_planes_past_64_gigabytes():
+    """Blocks 7 GiB apart: a place in the plane is more than 2^32 steps of 16 bytes from its beginning."""
+    d, hkv, block, nb, gap = 128, 2, 16, 11, 7 << 30
+    slab = block * hkv * q4.row_bytes(d)
+    if torch.cuda.mem_get_info()[0] < nb * gap + (4 << 30):
+        pytest.skip("needs 81 GB")
+    base = torch.empty((nb - 1) * gap + 2 * slab, dtype=torch.uint8, device="cuda")
+    lay = kvc.kvc_layout_create(1, 2, nb, block, hkv, q4.row_bytes(d), 1, block, plane_ptrs=[base, base[slab:]], block_stride=gap)
+    gen = torch.Generator().manual_seed(8)
+    n = nb * block - 5
+    x = torch.randn(2, n, hkv, d, generator=gen).to(BF16).cuda()
+    table = torch.randperm(nb, generator=gen).to(torch.int32)[None].contiguous()
+    j = torch.arange(n)
+    slots = (table[0, j // block].long() * block + j % block).cuda()
+    kvc.kvc_append_q4(lay, 0, None, x[0], x[1], None, slots, None, None)
+    back = torch.zeros_like(x)
+    kvc.kvc_read_q4(lay, 0, back[0], back[1], slots)
+    want = q4.quantise(x)
+    assert torch.equal(back, q4.values(*want).float().to(BF16))
+    parts = [[y[p].view(-1, 1, *y.shape[2:]) for y in want] for p in range(2)]         # one key a block, in order
+    for new in (1, 70):
+        q = torch.randn(new, 8, d, generator=gen).to(BF16).cuda()
+        out = torch.zeros_like(q)
+        ws = torch.empty(kvc.kvc_attention_q4_workspace_bytes(lay, new, 1, 8), dtype=torch.uint8, device="cuda")
+        kvc.kvc_attention_q4(lay, 0, q, out, table.cuda(), torch.tensor([n], **I32), torch.tensor([0, new], **I32), ws)
+        w = q4.attention(q, parts, torch.arange(n, dtype=torch.int32)[None], [(0, new)], [n], 1, d ** -0.5)
+        assert ((out.double() - w[0]).abs() <= q4.bounds(BF16, *w)[0]).all()
+    del base, lay
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------ a step of them together
 @pytest.mark.parametrize("dtype,d,hq,hkv", [(BF16, 128, 8, 2), (FP16, 64, 6, 6)])
 def test_a_step_with_pack_and_unpack(dtype, d, hq, hkv):
