@@ -349,6 +349,8 @@ kvc_status check(const kvc_layout *lay, const kvc_attention_desc *d, bool q4)
         return KVC_ERR_INVALID_ARG;
     if ((uint64_t)d->n_tokens * (d->n_q_heads / l.num_kv_heads) > 0x7FFFFFFFull)
         return KVC_ERR_TOO_LARGE;
+    if (q4 && d->scale > KVC_Q4_MAX_SCALE)
+        return KVC_ERR_INVALID_ARG;
     return q4 && !kvc_q4_aligned(lay) ? KVC_ERR_ALIGNMENT : KVC_OK;
 }
 

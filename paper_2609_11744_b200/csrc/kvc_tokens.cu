@@ -412,18 +412,17 @@ __global__ void __launch_bounds__(APPEND_THREADS, Q4 ? APPEND_Q4_BLOCKS : APPEND
         far = __any_sync(~0u, a.rot && (uint32_t)pos >= a.max_pos);
     } else {
         pos = a.rot ? a.positions[tok] : 0;
-        far = a.rot && (uint32_t)pos >= a.max_pos;
     }
     const uint64_t id = (uint64_t)slot < (1ull << 32) ? kvc_div((uint32_t)slot, a.block_size, a.block_shift) : (uint64_t)slot / a.block_size;
-    if (id >= a.num_blocks || far) {
+    if (id >= a.num_blocks || (AXES ? far : a.rot && (uint32_t)pos >= a.max_pos)) {
         if (lane == 0 && u == tok * per_token)
             atomicAdd(a.status, 1u);
         return;
     }
-    const uint32_t in_block = (uint32_t)((uint64_t)slot - id * a.block_size);
+    const uint64_t in_block = (uint64_t)slot - id * a.block_size;
     unsigned char *dst = kind == 0 ? a.q_out + tok * a.o_tok
                                    : (kind == 1 ? a.k_plane : a.v_plane) + id * a.block_stride +
-                                         (Q4 ? 0 : (uint64_t)in_block * a.heads[1] * a.d * sizeof(T));
+                                         (Q4 ? 0 : in_block * a.heads[1] * a.d * sizeof(T));
     const int64_t dst_head = kind == 0 ? a.o_head : (int64_t)(Q4 ? a.block_size * KVC_Q4_ROW_BYTES(a.d) : a.d * sizeof(T));
     // w_e c, -w_o s, w_o c, w_e s of the lane's four pairs
     uint64_t ec[2], os[2], oc[2], es[2];
@@ -532,7 +531,7 @@ __global__ void __launch_bounds__(APPEND_THREADS, Q4 ? APPEND_Q4_BLOCKS : APPEND
                     const uint32_t codes = append_quantise<T>(res, scale);
                     if (h < h1) {
                         unsigned char *row = dst + h * dst_head;
-                        __stcs(reinterpret_cast<uint32_t *>(row + in_block * (a.d / 2u) + l * 4u), codes);
+                        __stcs(reinterpret_cast<uint32_t *>(row + (uint32_t)in_block * (a.d / 2u) + l * 4u), codes);
                         if (l % 4u == 0)
                             __stcs(reinterpret_cast<uint32_t *>(row + a.block_size * (a.d / 2u) + in_block * (a.d / 8u) + l), scale);
                     }

@@ -644,12 +644,12 @@ _torch = None
 _MAP_DESC = struct.Struct("@4PQ4I6PQ")
 _APPEND_DESC = struct.Struct("@2I4P8q3PQ2Pf5IQ")
 _ATTENTION_DESC = struct.Struct("@2I3P4q3PQ5If2I2P2IPQ")
-_APPEND_AXES_DESC = struct.Struct(_APPEND_DESC.format + "Q2I128s")
+_AXES_DESC = struct.Struct("@Q2I128s")  # behind an _APPEND_DESC
 _READ_Q4_DESC = struct.Struct("@2I2P4qP2I")
 assert _MAP_DESC.size == ctypes.sizeof(kvc_map_tokens_desc)
 assert _APPEND_DESC.size == ctypes.sizeof(kvc_append_desc)
 assert _ATTENTION_DESC.size == ctypes.sizeof(kvc_attention_desc)
-assert _APPEND_AXES_DESC.size == ctypes.sizeof(kvc_append_axes_desc)
+assert _APPEND_DESC.size + _AXES_DESC.size == ctypes.sizeof(kvc_append_axes_desc)
 assert _READ_Q4_DESC.size == ctypes.sizeof(kvc_read_q4_desc)
 
 
@@ -732,27 +732,22 @@ def kvc_map_tokens(layout, context_lens, new_lens, free_blocks, block_tables, cu
 
 
 def kvc_append(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, q_weight=None, k_weight=None,
-               eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+               eps: float = 1e-6, interleaved: bool = False, stream=None, _other=None) -> None:
     """Norm and rotate queries and keys, write queries to q_out and keys and values to the pool's slots.
 
     q, q_out [T, Hq, D] (or both None), k, v [T, Hkv, D]: bf16 or fp16, any token and head strides;
     slots [T] int64; positions [T] int32 and cos_sin [max_positions, rot_dim] float32 (or both None:
-    no rotation); q_weight, k_weight [D] of the type of k, or None: no norm."""
-    _append("kvc_append", layout, layout.heads, layer, q, k, v, q_out, slots, positions, cos_sin, None, q_weight, k_weight, eps,
-            interleaved, stream)
-
-
-def _append(name, layout, heads, layer, q, k, v, q_out, slots, positions, cos_sin, axes, q_weight, k_weight, eps, interleaved,
-            stream):
-    """axes: None, or (axes of `positions`, bytes that name each pair's)."""
+    no rotation); q_weight, k_weight [D] of the type of k, or None: no norm.
+    (_other: the calls below that take the same and more: their name, the pool's heads, axes and bytes of pair_axis.)"""
     t, dev, L = _step_call()
     dt = k.dtype
     kind = t.kv.get(dt)
     if kind is None:
         raise TypeError("k must be torch.bfloat16 or torch.float16, not %s" % dt)
     n, hkv, dim = k.shape
-    if (hkv, dim) != heads:
-        raise ValueError("k has %d heads of %d, the layout %d of %d" % ((hkv, dim) + heads))
+    have = layout.heads if _other is None else _other[1]
+    if (hkv, dim) != have:
+        raise ValueError("k has %d heads of %d, the layout %d of %d" % ((hkv, dim) + have))
     if (q is None) != (q_out is None) or (positions is None) != (cos_sin is None):
         raise TypeError("q and q_out, and positions and cos_sin, go together")
     qp = qt = qh = op = ot = oh = hq = 0
@@ -765,19 +760,22 @@ def _append(name, layout, heads, layer, q, k, v, q_out, slots, positions, cos_si
     rot = rows = cs = pos = 0
     if cos_sin is not None:
         rows, rot = cos_sin.shape
-        pos = _arg(positions, "positions", t.i32, n if axes is None else n * axes[0], dev)
+        pos = _arg(positions, "positions", t.i32, n if _other is None else n * _other[2], dev)
         cs = _arg(cos_sin, "cos_sin", t.f32, rows * rot, dev)
-    desc = (layer, kind, qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, _arg(slots, "slots", t.i64, n, dev), pos, cs, rot,
-            0 if q_weight is None else _arg(q_weight, "q_weight", dt, dim, dev),
-            0 if k_weight is None else _arg(k_weight, "k_weight", dt, dim, dev), eps, n, hq, rot, rows,
-            1 if interleaved else 0, 0)
-    if axes is None:
-        d = _APPEND_DESC.pack(*desc)
-    else:
-        if len(axes[1]) != rot // 2:
-            raise ValueError("pair_axis names the axes of %d pairs, a head has %d" % (len(axes[1]), rot // 2))
-        d = _APPEND_AXES_DESC.pack(*desc, n, axes[0], 0, axes[1])
-    status = getattr(L, name)(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
+    d = _APPEND_DESC.pack(layer, kind, qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, _arg(slots, "slots", t.i64, n, dev), pos, cs, rot,
+                          0 if q_weight is None else _arg(q_weight, "q_weight", dt, dim, dev),
+                          0 if k_weight is None else _arg(k_weight, "k_weight", dt, dim, dev), eps, n, hq, rot, rows,
+                          1 if interleaved else 0, 0)
+    if _other is None:
+        status = L.kvc_append(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
+        if status:
+            raise KvcError(status, "kvc_append")
+        return
+    name, _, axes, pair_axis = _other
+    if len(pair_axis) != rot // 2:
+        raise ValueError("pair_axis names the axes of %d pairs, a head has %d" % (len(pair_axis), rot // 2))
+    status = getattr(L, name)(layout.handle, d + _AXES_DESC.pack(n, axes, 0, pair_axis),
+                              t.stream(dev) if stream is None else _stream(stream))
     if status:
         raise KvcError(status, name)
 
@@ -791,23 +789,22 @@ def kvc_pair_axes(sections: Sequence[int], in_turns: bool = False) -> bytes:
     return bytes(a for i in range(max(sections)) for a, n in enumerate(sections) if i < n)
 
 
-def _positions_of(positions, pair_axis, rot: int):
-    """The `axes` of _append for positions [T] or [A, T]."""
+def _with_axes(name: str, heads, positions, pair_axis, cos_sin):
+    """kvc_append's _other for positions [T] or [A, T]."""
     many = positions is not None and positions.dim() == 2
     if pair_axis is None:
         if many and positions.shape[0] != 1:
             raise TypeError("positions with several axes need pair_axis")
-        pair_axis = bytes(rot // 2)
-    return (positions.shape[0] if many else 1, bytes(pair_axis))
+        pair_axis = bytes(0 if cos_sin is None else cos_sin.shape[1] // 2)
+    return name, heads, positions.shape[0] if many else 1, bytes(pair_axis)
 
 
 def kvc_append_axes(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, pair_axis, q_weight=None,
                     k_weight=None, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
     """kvc_append for positions with several axes: positions [A, T] int32, pair_axis: bytes of length
     rot_dim / 2, the axis that turns each pair (see kvc_pair_axes)."""
-    _append("kvc_append_axes", layout, layout.heads, layer, q, k, v, q_out, slots, positions, cos_sin,
-            _positions_of(positions, pair_axis, 0 if cos_sin is None else cos_sin.shape[1]), q_weight, k_weight, eps, interleaved,
-            stream)
+    kvc_append(layout, layer, q, k, v, q_out, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, stream,
+               _with_axes("kvc_append_axes", layout.heads, positions, pair_axis, cos_sin))
 
 
 def _q4_heads(layout) -> Tuple[int, int]:
@@ -818,9 +815,8 @@ def _q4_heads(layout) -> Tuple[int, int]:
 def kvc_append_q4(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, pair_axis=None, q_weight=None,
                   k_weight=None, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
     """kvc_append into a pool held in 4 bits (kvc_layout_create_q4).  positions [T], or [A, T] with pair_axis."""
-    _append("kvc_append_q4", layout, _q4_heads(layout), layer, q, k, v, q_out, slots, positions, cos_sin,
-            _positions_of(positions, pair_axis, 0 if cos_sin is None else cos_sin.shape[1]), q_weight, k_weight, eps, interleaved,
-            stream)
+    kvc_append(layout, layer, q, k, v, q_out, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, stream,
+               _with_axes("kvc_append_q4", _q4_heads(layout), positions, pair_axis, cos_sin))
 
 
 def kvc_read_q4(layout, layer: int, k_out, v_out, slots, stream=None) -> None:

@@ -98,7 +98,7 @@ def test_nothing_to_read_is_no_error():
 
 
 @pytest.mark.parametrize("want,kw", BAD_ATTENTION + [
-    (INVALID, dict(n_groups=1)), (INVALID, dict(group_starts=A)), (INVALID, dict(prefix_lens=A)), (INVALID, dict(window=(1 << 30) + 1)), (INVALID, dict(sinks=1 << 31))])
+    (INVALID, dict(n_groups=1)), (INVALID, dict(group_starts=A)), (INVALID, dict(prefix_lens=A)), (INVALID, dict(window=(1 << 30) + 1)), (INVALID, dict(sinks=1 << 31)), (INVALID, dict(scale=2e18))])
 def test_attention_refuses(want, kw):
     assert status("kvc_attention_q4", q4_layout(), attention_desc(**kw)) == want
 
