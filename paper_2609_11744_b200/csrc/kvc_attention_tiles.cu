@@ -38,14 +38,16 @@
 // tile of K and V each, which are copied as they lie (5/16 of the bytes) and made into values by other warps:
 //   256 rows  warp 19 walks the pairs and copies, warps 17 and 18 make values of K and of V
 //   128 rows  warps 17 and 18 copy, warps 8-15, which have no rows, make values: four of K, four of V
-// Measured: the 8192-token prompt in 692 us = 794 TFLOP/s in runs of thirty (16-bit pool: 588).  What bounds it is the pace
-// of the three warps beside the softmax: 1100 cycles for the values of a part and 1500 to copy one, against 1220 that the
-// softmax of 256 rows takes a part.  Such a warp runs at 3.4 cycles an instruction in straight lines, whose code the
-// softmax keeps driving out of the instruction cache, so its loops are short: 916 us with the value loop unrolled, 778
-// without, 724 with the steps of sixteen pairs side by side, 692 with two instructions a pair.  The softmax must keep its 104
-// registers (with 96 the 16-bit prompt takes 1330 us), which leaves none for more warps.  With few rows in tiles of 128
-// (32 requests of up to 5 drafted tokens behind 8000: 231 us) the softmax' chain is the bound, as over a 16-bit pool.  Against
-// 64 bits the result is off by 0.0029 in bf16 (keys and values rounded too) and 0.0004 in fp16.
+// Measured: the 8192-token prompt in 653 us = 842 TFLOP/s in runs of thirty (16-bit pool: 588).  What bounds it is the pace
+// of the three warps beside the softmax, which hold it up: some 1300 cycles for a part, to copy it (half of them waits
+// and copies' issue) and for its keys or values, against 1220 that the softmax of 256 rows takes a part.  Such a
+// warp runs at 3.4 cycles an instruction in straight lines, whose code the softmax keeps driving out of the instruction
+// cache, so its loops are short: 916 us with the value loop unrolled, 778 without, 724 with the steps of sixteen pairs side by
+// side, 692 with two instructions a pair, 675 with parts of whole blocks in a loop of their own and two groups a turn, 653
+// with results put in order instead of values.  The softmax must keep its 104 registers (with 96 the 16-bit prompt takes
+// 1330 us), which leaves none for more warps.  With few rows in tiles of 128 (32 requests of up to 5 drafted tokens behind
+// 8000: 214 us) the softmax' chain is the bound, as over a 16-bit pool.  Against 64 bits the result is off by 0.0029 in bf16 (keys
+// and values rounded too) and 0.0004 in fp16.
 // Every wait is bounded; one that gives up makes all roles leave and is counted.
 #include <cuda.h>
 #include <stddef.h>
@@ -74,6 +76,10 @@ struct Shape {
     static constexpr int KS = D == 64 ? 4 : ROWS == 128 && !Q4 ? 3 : 2, VS = D == 64 ? 4 : 2;
     static constexpr int PARTS = ROWS == 128 ? 12 : 5, PART = 32 * KVC_Q4_ROW_BYTES(D);  // Q4: raw parts, bytes of K's or V's
     static constexpr int RAW_BYTES = Q4 ? 2 * PARTS * PART : 0;
+    // Q4: V's values stay in the order that words of codes give them in, and a result's columns are put right where it is
+    // written.  It pays where values bind (8192-token prompt 675 -> 654 us) and not where results are many for their keys
+    // (ragged prompts of heads of 64: 123 -> 127).
+    static constexpr bool APART = Q4 && D == 128 && ROWS == 256;
     static constexpr int Q = 0, K = ROWS / 128 * TILE, V = K + KS * TILE, RAW = V + VS * TILE, END = RAW + RAW_BYTES;
     static constexpr int SMEM = END + 1024;           // room to align the stages to the swizzle's 1024 bytes
     static_assert(SMEM + (ROWS == 128 ? 5 : 8) * 1024 <= 227 * 1024, "with the kernel's own variables");
@@ -459,10 +465,33 @@ __device__ __forceinline__ void raw_role(const KvcAttn &a, const Segment *segmen
     constexpr uint32_t CODES = D / 2, SCALES = D / 8, ROW = CODES + SCALES, PER = ROWS == 128 ? 2 : 4;
     constexpr uint32_t NONE = ~0u;
     const bool images = raw_images(a);
-    const uint32_t shift = images ? a.block_shift : 0u;
     SegmentReader reader;
     Segment c;
     uint32_t slot = ROWS == 128 ? first : 0u, parity = 1, issued = 0;
+    // A place of the ring for the next part: waits until it is free, says which keys there will be and how many bytes come.
+    const auto open_part = [&](uint32_t there, uint32_t copied) {
+        if (!__all_sync(~0u, bar_wait(smem_addr(&rb->empty[slot]), parity, dead, a.status)))
+            return false;
+        if (lane == 0) {
+            rb->there[slot] = there;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(&rb->full[slot])),
+                         "r"((uint32_t)__popc(copied) * 2u * ROW) : "memory");
+        }
+        __syncwarp();
+        return true;
+    };
+    const auto next_part = [&] {
+        ++issued;
+        if (ROWS == 128 && (slot & 3u) != first + PER - 1) {
+            ++slot;
+        } else {
+            slot += ROWS == 128 ? 5u - PER : 1u;
+            if (slot >= (uint32_t)S::PARTS) {
+                slot -= S::PARTS;
+                parity ^= 1u;
+            }
+        }
+    };
     bool ok = true;
 #pragma unroll 1
     while (ok && reader.next(segments, bars, c, dead, a.status)) {
@@ -470,81 +499,75 @@ __device__ __forceinline__ void raw_role(const KvcAttn &a, const Segment *segmen
         const int32_t *table = a.tables + (int64_t)c.q.table * a.table_stride;
         const uint64_t head_at = (uint64_t)c.h * a.block_size * ROW;
         const auto wanted_of = [&](int32_t j0) { return low_bits(c.r.hi - j0) & (~low_bits(c.r.lo - j0) | low_bits(c.r.sink_end - j0)); };
-        // the id of this lane's block of a tile, or NONE where none of its keys is wanted
-        const auto look_tile = [&](uint32_t u) {
-            const int32_t j = (int32_t)(kvc_tile(c.r, c.t + u) * TK + (lane << shift)), e = j + (int32_t)a.block_size;
-            const bool some = lane << shift < (uint32_t)TK && j < c.r.hi && (e > c.r.lo || j < c.r.sink_end);
-            return some ? min((uint32_t)table[(uint32_t)j >> shift], NONE - 1u) : NONE;  // (an entry may be any number)
-        };
-        // this lane's stretch of a part: its first key in the part, keys, place in its block, the block's id
-        uint32_t begin = 0, keys = 0, in_block = 0, id = NONE;
-        const auto look_part = [&](int32_t j0, uint32_t wanted) {
-            const uint32_t b = kvc_div((uint32_t)j0, a.block_size, a.block_shift) + lane;
-            const int64_t at = (int64_t)b * a.block_size - j0;  // where that block begins, from the part's beginning
-            begin = (uint32_t)min(max(at, (int64_t)0), (int64_t)32);
-            keys = (uint32_t)min(at + (int64_t)a.block_size, (int64_t)32) - begin;
-            in_block = begin - (uint32_t)at;
-            id = NONE;
-            if (keys && (wanted >> begin & low_bits((int32_t)keys)))
-                id = (uint32_t)table[b];
-            else
-                keys = 0;
-        };
-        uint32_t next = images ? look_tile(0) : NONE;
+        if (images) {
+            const uint32_t shift = a.block_shift, begin = lane << shift;  // this lane's block of a tile
+            // its id, or NONE where none of its keys is wanted
+            const auto look = [&](uint32_t u) {
+                const int32_t j = (int32_t)(kvc_tile(c.r, c.t + u) * TK + begin), e = j + (int32_t)a.block_size;
+                const bool some = begin < (uint32_t)TK && j < c.r.hi && (e > c.r.lo || j < c.r.sink_end);
+                return some ? min((uint32_t)table[(uint32_t)j >> shift], NONE - 1u) : NONE;  // (an entry may be any number)
+            };
+            uint32_t next = look(0);
 #pragma unroll 1
-        for (uint32_t u = 0; ok && u < c.n; ++u) {
-            const uint32_t tile_id = next;
-            if (images && u + 1 < c.n)
-                next = look_tile(u + 1);
-            const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + u) * TK + first * 32u);
+            for (uint32_t u = 0; ok && u < c.n; ++u) {
+                const uint32_t id = next;
+                const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + u) * TK);
+                if (u + 1 < c.n)
+                    next = look(u + 1);
+                const bool mine = begin >> 5 >= first && begin >> 5 < first + PER;
+                if (mine && id != NONE && id >= a.num_blocks)
+                    atomicAdd(a.status, (uint32_t)__popc(low_bits((int32_t)a.block_size) & wanted_of(j0 + (int32_t)begin)));
+                // lane p: the keys of part p whose block is there, and those of them that are wanted
+                const uint32_t blocks = __ballot_sync(~0u, id < a.num_blocks) >> (lane & 3u) * (32u >> shift);
+                uint32_t copied = 0;
 #pragma unroll 1
-            for (uint32_t p = 0; p < PER; ++p) {
-                const uint32_t wanted = wanted_of(j0 + (int32_t)p * 32);
-                if (images) {
-                    // blocks of the part, first those of K and then of V
-                    const uint32_t n = 32u >> shift, i = lane & (n - 1u);
-                    id = __shfl_sync(~0u, tile_id, (first + p) * n + i);
-                    begin = i << shift;
-                    keys = id == NONE ? 0u : a.block_size;
-                    in_block = 0;
-                } else {
-                    look_part(j0 + (int32_t)p * 32, wanted);
+                for (uint32_t i = 0; i < 32u; i += a.block_size)
+                    copied |= blocks >> (i >> shift) & 1u ? low_bits((int32_t)a.block_size) << i : 0u;
+                const uint32_t there = copied & wanted_of(j0 + (int32_t)(lane & 3u) * 32);
+                const uint64_t at = (uint64_t)id * a.block_stride + head_at;
+#pragma unroll 1
+                for (uint32_t p = first; p < first + PER; ++p) {
+                    if (!(ok = open_part(__shfl_sync(~0u, there, p), __shfl_sync(~0u, copied, p))))
+                        break;
+                    if (begin >> 5 == p && id < a.num_blocks) {
+                        const uint32_t dst = raw + slot * (2u * S::PART) + (begin & 31u) * ROW, bar = smem_addr(&rb->full[slot]);
+                        bulk_load(dst, a.k + at, a.block_size * ROW, bar);
+                        bulk_load(dst + S::PART, a.v + at, a.block_size * ROW, bar);
+                    }
+                    next_part();
                 }
+            }
+        } else {
+#pragma unroll 1
+            for (uint32_t n = 0; ok && n < c.n * PER; ++n) {
+                const int32_t j0 = (int32_t)(kvc_tile(c.r, c.t + n / PER) * TK + (first + n % PER) * 32u);
+                const uint32_t wanted = wanted_of(j0), b = kvc_div((uint32_t)j0, a.block_size, a.block_shift) + lane;
+                // this lane's stretch of the part: its first key in the part, keys, place in its block, the block's id
+                const int64_t from = (int64_t)b * a.block_size - j0;  // where that block begins, from the part's beginning
+                const uint32_t begin = (uint32_t)min(max(from, (int64_t)0), (int64_t)32);
+                uint32_t keys = (uint32_t)min(from + (int64_t)a.block_size, (int64_t)32) - begin, id = NONE;
+                const uint32_t in_block = begin - (uint32_t)from;
+                if (keys && (wanted >> begin & low_bits((int32_t)keys)))
+                    id = (uint32_t)table[b];
+                else
+                    keys = 0;
                 const uint32_t mine = low_bits((int32_t)keys) << begin;
                 const bool good = keys && id < a.num_blocks;
-                if (keys && !good && (!images || lane < 32u >> shift))
+                if (keys && !good)
                     atomicAdd(a.status, (uint32_t)__popc(mine & wanted));
-                const uint32_t is = __reduce_or_sync(~0u, good ? mine : 0u);
-                const uint32_t bar = smem_addr(&rb->full[slot]), dst = raw + slot * (2u * S::PART);
-                if (!(ok = __all_sync(~0u, bar_wait(smem_addr(&rb->empty[slot]), parity, dead, a.status))))
+                const uint32_t copied = __reduce_or_sync(~0u, good ? mine : 0u);
+                if (!(ok = open_part(copied & wanted, copied)))
                     break;
-                if (lane == 0) {
-                    rb->there[slot] = is & wanted;
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)__popc(is) * 2u * ROW) : "memory");
-                }
-                __syncwarp();
-                const uint64_t at = (uint64_t)id * a.block_stride + head_at;
-                if (images) {
-                    const bool values = lane >= 32u >> shift;
-                    if (good && lane < 64u >> shift)
-                        bulk_load(dst + (values ? S::PART : 0u) + begin * ROW, (values ? a.v : a.k) + at, a.block_size * ROW, bar);
-                } else if (good) {
-                    const uint64_t codes = at + in_block * CODES, scales = at + (uint64_t)a.block_size * CODES + in_block * SCALES;
+                if (good) {
+                    const uint64_t codes = (uint64_t)id * a.block_stride + head_at + in_block * CODES;
+                    const uint64_t scales = codes + (uint64_t)a.block_size * CODES - in_block * (CODES - SCALES);
+                    const uint32_t dst = raw + slot * (2u * S::PART), bar = smem_addr(&rb->full[slot]);
                     bulk_load(dst + begin * CODES, a.k + codes, keys * CODES, bar);
                     bulk_load(dst + 32u * CODES + begin * SCALES, a.k + scales, keys * SCALES, bar);
                     bulk_load(dst + S::PART + begin * CODES, a.v + codes, keys * CODES, bar);
                     bulk_load(dst + S::PART + 32u * CODES + begin * SCALES, a.v + scales, keys * SCALES, bar);
                 }
-                ++issued;
-                if (ROWS == 128 && (slot & 3u) != first + PER - 1) {
-                    ++slot;
-                } else {
-                    slot += ROWS == 128 ? 5u - PER : 1u;
-                    if (slot >= (uint32_t)S::PARTS) {
-                        slot -= S::PARTS;
-                        parity ^= 1u;
-                    }
-                }
+                next_part();
             }
         }
     }
@@ -571,8 +594,8 @@ __device__ __forceinline__ void raw_role(const KvcAttn &a, const Segment *segmen
 
 // A warp that makes values (SCALE of them) of raw parts: K or V, part `sub` of every tile with four warps, all parts with one.  A lane
 // makes one key's values, offset + step * code in the model's type, and writes them where the matrix unit reads
-// them; what is no key becomes zeros.  A word of eight codes gives the pairs (0,4) (1,5) (2,6) (3,7): K keeps that
-// order, which the queries are given too, and V's is put right.  Lanes take the groups of their keys in
+// them; what is no key becomes zeros.  A word of eight codes gives the pairs (0,4) (1,5) (2,6) (3,7): K keeps that order, which
+// the queries are given too, and so does V, or it is put right (APART).  Lanes take the groups of their keys in
 // different orders, which keeps their reads and writes in different banks.
 template <typename T, int D, int ROWS, bool KEYS>
 __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segments, uint32_t tiles, uint32_t raw, RawBars *rb, Bars *bars,
@@ -621,7 +644,7 @@ __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segm
                     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc) : "r"(scales + g * 4u));
                 };
                 read();
-#pragma unroll 1
+#pragma unroll 2
                 for (int i = 0; i < GROUPS; ++i) {
                     const uint32_t now[4] = {w[0], w[1], w[2], w[3]};
                     const KvcQ4Values<T> values(kvc_lows(sc, sc) & keep, kvc_highs(sc, sc) & keep);
@@ -639,7 +662,7 @@ __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segm
                     }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        if (KEYS)
+                        if (KEYS || S::APART)
                             asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to ^ (k << 4)), "r"(x[k][0]), "r"(x[k][1]), "r"(x[k][2]), "r"(x[k][3]));
                         else
                             asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to ^ (k << 4)), "r"(kvc_lows(x[k][0], x[k][1])),
@@ -864,6 +887,22 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 const float x = o[k * 4 + e * 2], y = o[k * 4 + e * 2 + 1];
+                                if constexpr (S::APART) {  // (lane % 4 has columns lane % 4 and the same + 4 of eight)
+                                    const uint32_t from = (lane & ~3u) | (2u * lane & 3u);
+                                    if (whole) {
+                                        const uint32_t w = f[e] == 0.f ? 0u : kvc_from_float2<T>(x * f[e], y * f[e]);
+                                        const uint32_t w0 = __shfl_sync(~0u, w, from), w1 = __shfl_sync(~0u, w, from + 1u);
+                                        if (write[e])
+                                            *reinterpret_cast<uint32_t *>(dst[e] + (q + k * 8) * 2) = lane & 2u ? kvc_highs(w0, w1) : kvc_lows(w0, w1);
+                                    } else {
+                                        const float x0 = __shfl_sync(~0u, x, from), y0 = __shfl_sync(~0u, y, from);
+                                        const float x1 = __shfl_sync(~0u, x, from + 1u), y1 = __shfl_sync(~0u, y, from + 1u);
+                                        if (write[e])
+                                            *reinterpret_cast<float2 *>(dst[e] + (q + k * 8) * 4) =
+                                                lane & 2u ? make_float2(y0 * BACK, y1 * BACK) : make_float2(x0 * BACK, x1 * BACK);
+                                    }
+                                    continue;
+                                }
                                 if (!write[e])
                                     continue;
                                 if (whole)
