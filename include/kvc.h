@@ -583,10 +583,10 @@ kvc_status kvc_read_q4(kvc_layout *layout, const kvc_read_q4_desc *desc, void *s
 
 /* kvc_attention and kvc_attention_shared over a pool held in 4 bits, with the same descriptor and rules: masks,
  * lengths, clamps, groups, workspaces.  Products with keys and values are taken in the dtype with 32-bit sums: in the
- * kernel for few rows the codes of a key are exact and the steps multiply the sums, elsewhere a value is
- * rounded to the dtype before its product, as a 16-bit pool would hold it.  With many query rows blocks of 4, 8, 16 or
- * 32 tokens are the fast ones, and larger powers of two nearly so.  In bf16 queries and values above 2^60 are not taken for
- * what they are.  scale is at most KVC_Q4_MAX_SCALE (INVALID_ARG).  The workspace comes from
+ * kernel for few rows the codes of a key are exact and the steps multiply the sums, elsewhere a
+ * key is rounded to 11 bits.  A value is rounded to the dtype, as a 16-bit pool would hold it.  With many query rows blocks of
+ * 4, 8, 16 or 32 tokens are the fast ones, and larger powers of two nearly so.  In bf16 values above 2^60 are not taken for
+ * what they are, nor queries and keys above 65504 (with few query rows: queries above 2^60).  scale is at most KVC_Q4_MAX_SCALE (INVALID_ARG).  The workspace comes from
  * kvc_attention_q4_workspace_bytes. */
 #define KVC_Q4_MAX_SCALE 1e18f
 kvc_status kvc_attention_q4_workspace_bytes(kvc_layout *layout, uint32_t n_tokens, uint32_t n_requests,

@@ -33,21 +33,21 @@
 // for what the rounding leaves would be half as much tensor work again.  Against 64 bits the result is off by 0.0021 to
 // 0.0023 in bf16 (0.0017 with weights in 32 bits: the result's own rounding) and 0.0003 in fp16 (0.0002).
 //
-// Over a pool held in 4 bits (Q4) the matrix unit gets values, offset + step * code in the pool's 16-bit type (as a 16-bit pool
-// would hold them, but for a power of two: kvc_q4_device.h); the rest is the same.  Its keys come in raw parts, a quarter of a
+// Over a pool held in 4 bits (Q4) the matrix unit gets offset + step * code, rounded to fp16 for keys (first_operand) and to the
+// pool's type for values (as a 16-bit pool would hold them, but for a power of two: kvc_q4_device.h); the rest is the same.  Its keys come in raw parts, a quarter of a
 // tile of K and V each, which are copied as they lie (5/16 of the bytes) and made into values by other warps:
 //   256 rows  warp 19 walks the pairs and copies, warps 17 and 18 make values of K and of V
 //   128 rows  warps 17 and 18 copy, warps 8-15, which have no rows, make values: four of K, four of V
-// Measured: the 8192-token prompt in 653 us = 842 TFLOP/s in runs of thirty (16-bit pool: 588).  What bounds it is the pace
-// of the three warps beside the softmax, which hold it up: some 1300 cycles for a part, to copy it (half of them waits
-// and copies' issue) and for its keys or values, against 1220 that the softmax of 256 rows takes a part.  Such a
+// Measured: the 8192-token prompt in 720 us = 764 TFLOP/s in runs of thirty (16-bit pool: 588).  What bounds it is the pace
+// of the three warps beside the softmax, which hold it up: some 1450 cycles a part for its keys (three instructions a
+// pair), 1300 for its values or to copy it (half of them waits and copies' issue), against 1220 that the softmax of 256 rows takes.  Such a
 // warp runs at 3.4 cycles an instruction in straight lines, whose code the softmax keeps driving out of the instruction
 // cache, so its loops are short: 916 us with the value loop unrolled, 778 without, 724 with the steps of sixteen pairs side by
 // side, 692 with two instructions a pair, 675 with parts of whole blocks in a loop of their own and two groups a turn, 653
-// with results put in order instead of values.  The softmax must keep its 104 registers (with 96 the 16-bit prompt takes
+// with results put in order instead of values; with keys of 11 bits 737, 720 with a key's scales masked before they are apart.  The softmax must keep its 104 registers (with 96 the 16-bit prompt takes
 // 1330 us), which leaves none for more warps.  With few rows in tiles of 128 (32 requests of up to 5 drafted tokens behind
-// 8000: 214 us) the softmax' chain is the bound, as over a 16-bit pool.  Against 64 bits the result is off by 0.0029 in bf16 (keys
-// and values rounded too) and 0.0004 in fp16.
+// 8000: 216 us) the softmax' chain is the bound, as over a 16-bit pool.  Against 64 bits the result is off by 0.0027 in bf16
+// (weights and values rounded) and 0.0004 in fp16.
 // Every wait is bounded; one that gives up makes all roles leave and is counted.
 #include <cuda.h>
 #include <stddef.h>
@@ -592,7 +592,21 @@ __device__ __forceinline__ void raw_role(const KvcAttn &a, const Segment *segmen
     }
 }
 
-// A warp that makes values (SCALE of them) of raw parts: K or V, part `sub` of every tile with four warps, all parts with one.  A lane
+// The first product over a pool in 4 bits is fp16's whatever the model's type: a key, offset + step * code, is rounded to 11 bits
+// and not to 8, which the log-sum-exp would show (of the 8192-token prompt off by 2e-7 of it, 1e-5 with 8; of fewer keys by
+// more).  Queries and keys of bf16 so end at 65504, and below 2^-14 they are off by 2^-25.
+template <typename T>
+__device__ __forceinline__ uint32_t first_operand(uint32_t x)
+{
+    if constexpr (std::is_same<T, __half>::value) {
+        return x;
+    } else {
+        const float2 v = kvc_to_float2<T>(x);
+        return kvc_from_float2<__half>(v.x, v.y);
+    }
+}
+
+// A warp that makes values (keys: first operands, else SCALE of them) of raw parts: K or V, part `sub` of every tile with four warps, all parts with one.  A lane
 // makes one key's values, offset + step * code in the model's type, and writes them where the matrix unit reads
 // them; what is no key becomes zeros.  A word of eight codes gives the pairs (0,4) (1,5) (2,6) (3,7): K keeps that order, which
 // the queries are given too, and so does V, or it is put right (APART).  Lanes take the groups of their keys in
@@ -636,7 +650,7 @@ __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segm
                 const uint32_t codes = code_at + from * (2u * S::PART), scales = scale_at + from * (2u * S::PART);
                 const uint32_t dst = tiles + ring.stage * S::TILE + ((sub + p) * 32u + lane) * 128u;
                 const uint32_t keep = is >> lane & 1u ? ~0u : 0u;
-                // not unrolled: a warp that shares its instruction cache with the softmax runs a short loop at several times
+                // little unrolled (one turn is best for tiles of 128 rows, 216 us against 223, two for 256, 720 against 757): a warp that shares its instruction cache with the softmax runs a short loop at several times
                 // the pace of a long stretch.  Each group's codes are read a turn ahead
                 uint32_t w[4], sc, g = turn % GROUPS;
                 const auto read = [&] {
@@ -644,10 +658,11 @@ __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segm
                     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc) : "r"(scales + g * 4u));
                 };
                 read();
-#pragma unroll 2
+#pragma unroll (ROWS == 128 ? 1 : 2)
                 for (int i = 0; i < GROUPS; ++i) {
                     const uint32_t now[4] = {w[0], w[1], w[2], w[3]};
-                    const KvcQ4Values<T> values(kvc_lows(sc, sc) & keep, kvc_highs(sc, sc) & keep);
+                    const uint32_t scale = KEYS ? first_operand<T>(sc & keep) : sc & keep;
+                    const KvcQ4Values<std::conditional_t<KEYS, __half, T>> values(kvc_lows(scale, scale), kvc_highs(scale, scale));
                     const uint32_t to = dst + (g >> 1) * S::HALF + (((g & 1u) << 6) ^ swap);
                     g = (g + 1u) % GROUPS;
                     read();  // (the last turn reads the first group again)
@@ -822,8 +837,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
 #pragma unroll
             for (uint32_t e = 0; e < TURNS; ++e) {
                 const uint32_t r = r0 + e * STEP;
-                if (Q4)  // the order that the keys' values come in
+                if constexpr (Q4) {  // the order that the keys' values come in
+                    x[e] = make_uint4(first_operand<T>(x[e].x), first_operand<T>(x[e].y), first_operand<T>(x[e].z), first_operand<T>(x[e].w));
                     x[e] = make_uint4(kvc_lows(x[e].x, x[e].z), kvc_highs(x[e].x, x[e].z), kvc_lows(x[e].y, x[e].w), kvc_highs(x[e].y, x[e].w));
+                }
                 *reinterpret_cast<uint4 *>(dst + r * 128u + (((chunk & 7u) ^ (r & 7u)) << 4)) = x[e];
             }
             fence_async();
@@ -1071,7 +1088,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             // ------------------------------------------------------------ matrix instructions
             // The unit takes few instructions ahead, so what this thread does between them is time that
             // the unit may stand still: addresses and parities live in registers.
-            constexpr uint32_t KIND_S = kind<T>(TK, false), KIND_O = kind<T>(D, true);
+            constexpr uint32_t KIND_S = kind<std::conditional_t<Q4, __half, T>>(TK, false), KIND_O = kind<T>(D, true);
             const uint32_t q_at = operand(tiles + S::Q, 16), k_at = operand(tiles + S::K, 16), v_at = operand(tiles + S::V, S::HALF);
             const uint32_t bar = smem_addr(&bars);
             SegmentReader reader;
@@ -1323,6 +1340,5 @@ cudaError_t kvc_launch_attn_q4_tiles(const KvcAttn &a, uint32_t dtype, uint32_t 
     TilesArgs args;
     memset(&args, 0, sizeof(args));
     args.a = a;
-    args.a.scale_log2 *= 1.f / (dtype == KVC_DTYPE_BF16 ? KvcQ4Values<__nv_bfloat16>::SCALE : KvcQ4Values<__half>::SCALE);
     return launch_type<true>(args, dtype, head_dim, blocks, st);
 }

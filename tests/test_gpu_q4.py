@@ -478,6 +478,45 @@ def test_extreme_scores():
             c.check(c.run(hint=new), c.want())
 
 
+@pytest.mark.parametrize("q_power,k_power", [(0, 0), (12, 0), (0, 10), (-6, -9)])
+@pytest.mark.parametrize("lens,new,h", [([300, 129, 64], [100, 60, 3], 4), ([40, 33], [40, 33], 6), ([2000], [9], 7)])
+def test_keys_of_bf16_keep_eleven_bits(q_power, k_power, lens, new, h):
+    """Over many rows a key is rounded to 11 bits whatever the type, and queries and keys may be large or small: half a step
+    is 2^-12 of a key, and what is below fp16's normal range is off by 2^-25."""
+    hq, hkv = heads(h)
+    c = Case(BF16, lens, new, hq, hkv, 128, 16, seed=3)
+    c.q *= 2.0**q_power
+    for i in (1, 2):
+        c.parts[0][i] *= 2.0**k_power
+    for p in range(2):
+        c.pool[1, p] = q4.pack_slabs(*c.parts[p])
+    scale = 2.0 ** (-q_power - k_power) * 128**-0.5
+    want = c.want(scale=scale)
+    got = c.run(hint=max(new), scale=scale)
+    c.check(got, want)
+    products = want[3][1] / (2.0**-8 + 136 * 2.0**-23)                 # the largest scale * sum_d |q_d k_d|
+    most_q, most_k = c.q.double().abs().max(), q4.values(*c.parts[0]).abs().max()
+    slip = products * (2.0**-12 + 136 * 2.0**-23) + scale * 128 * 2.0**-25 * (most_q + most_k)
+    assert ((got[1].double() - want[1]).abs() <= slip + 2.0**-18 + want[1].abs() * 2.0**-21).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("lens,new,h,window,sinks", [
+    ([2, 1, 5], [2, 1, 5], 7, 0, 0), ([100, 128, 3], [1, 6, 2], 7, 0, 0), ([900, 40], [6, 5], 7, 100, 28), ([1000], [4], 6, 1, 0)])
+def test_rows_that_see_few_keys_take_them_for_what_they_are(dtype, lens, new, h, window, sinks):
+    hq, hkv = heads(h)
+    c = Case(dtype, lens, new, hq, hkv, 64, 16, seed=5)
+    want = c.want(window, sinks)
+    c.check(c.run(window, sinks, hint=max(new), tail=2), want, few=True)
+
+
+@pytest.mark.parametrize("new,window,sinks", [(30, 0, 0), (64, 0, 0), (300, 1, 0), (300, 20, 44)])
+def test_many_rows_of_fp16_that_see_few_keys(new, window, sinks):
+    c = Case(FP16, [new, 7], [new, 7], 12, 2, 128, 8, seed=6)
+    want = c.want(window, sinks)
+    c.check(c.run(window, sinks, hint=new, tail=2), want, few=True)
+
+
 def test_strides_and_layers():
     """Queries and results as parts of wider rows, head-major and token-major."""
     c = Case(FP16, [400, 90], [3, 90], 6, 2, 64, 16, seed=8)
