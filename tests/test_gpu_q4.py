@@ -510,9 +510,9 @@ def test_rows_that_see_few_keys_take_them_for_what_they_are(dtype, lens, new, h,
     c.check(c.run(window, sinks, hint=max(new), tail=2), want, few=True)
 
 
-@pytest.mark.parametrize("new,window,sinks", [(30, 0, 0), (64, 0, 0), (300, 1, 0), (300, 20, 44)])
-def test_many_rows_of_fp16_that_see_few_keys(new, window, sinks):
-    c = Case(FP16, [new, 7], [new, 7], 12, 2, 128, 8, seed=6)
+@pytest.mark.parametrize("dtype,new,window,sinks", [(FP16, 30, 0, 0), (FP16, 64, 0, 0), (FP16, 300, 1, 0), (FP16, 300, 20, 44), (BF16, 300, 1, 4), (BF16, 300, 16, 0)])
+def test_many_rows_that_see_few_keys(dtype, new, window, sinks):
+    c = Case(dtype, [new, 7], [new, 7], 12, 2, 128, 8, seed=6)
     want = c.want(window, sinks)
     c.check(c.run(window, sinks, hint=new, tail=2), want, few=True)
 
