@@ -280,17 +280,18 @@ __device__ __forceinline__ AppendRaw append_natural(const AppendRaw &r, uint32_t
     return n;
 }
 
-__device__ __forceinline__ float min_nan(float x, float y)
+// The least and the largest of three; NaN if one is.
+__device__ __forceinline__ float min_nan(float x, float y, float z)
 {
-    float z;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
-    return z;
+    float r;
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
 }
-__device__ __forceinline__ float max_nan(float x, float y)
+__device__ __forceinline__ float max_nan(float x, float y, float z)
 {
-    float z;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
-    return z;
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
 }
 
 // x rounded towards zero to the type (x >= 0), and its value.
@@ -311,31 +312,73 @@ __device__ __forceinline__ uint32_t down_bits<__half>(float x, float &value)
     return __half_as_ushort(r);
 }
 
-// Codes of the lane's eight values (natural order), and the group's step and offset.  The quotient (x - offset) / step
-// is rounded exactly: its product with the reciprocal is off by 2^-20 at most, so only the choice between two neighbours can
-// be wrong, and the remainder, which fma gives without rounding, decides it.
+// The codes where differences may have been rounded (append_quantise), one after the other: seldom needed, so a short loop.
+// `lost`: what the rounding took from the difference, as a sum of two floats gives it exactly.
+template <typename T>
+__device__ __forceinline__ uint32_t append_lossy(const AppendRaw &r, float low, float step, float up, float inv)
+{
+    uint64_t w = (uint64_t)r.a.y << 32 | r.a.x, then = (uint64_t)r.b.y << 32 | r.b.x;
+    const float half = 0.5f * step;
+    uint32_t codes = 0;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        const float x = kvc_to_float2<T>((uint32_t)w).x, d0 = x - low, d = d0 * up, back = d0 - x;
+        w >>= 16;
+        if (i == 3)
+            w = then;
+        const float t = fmaf(d, inv, 12582912.f);
+        float n = t - 12582912.f;
+        const float rest = fmaf(-n, step, d), off = fabsf(rest), lost = copysignf(1.f, rest) * ((x - (d0 - back)) - (low + back));
+        if (off > half || (off == half && (lost > 0.f || (lost == 0.f && (__float_as_uint(t) & 1u)))))
+            n += copysignf(1.f, rest);
+        codes |= (step > 0.f ? (uint32_t)fminf(fmaxf(n, 0.f), 15.f) : 0u) << (4 * i);
+    }
+    return codes;
+}
+
+// Codes of the lane's eight values (natural order), and the group's step and offset, to the bit.
+// The step: 15 numbers of the type, 12 or 15 bits, are a float, so rounding the range down does not take it below
+// one that it reaches, and a quotient that was rounded up to a number of the type shows by its product with 15.
+// The quotient (x - offset) / step: the product with the reciprocal is off by 2^-19 at most, so only the choice between two
+// neighbours can be wrong, and the remainder, which fma gives without rounding, decides it.  What the difference x - offset lost
+// when it was rounded is less than the remainder's last place, so it matters only where the remainder is half a step; and
+// nothing is lost unless one of the two is so small beside the range that its last place, the 8th or 11th bit, lies behind the
+// difference's 24th, which one test for a lane's values finds (16384 tokens with their way back: 184 us without these rules, 190 with).
 template <typename T>
 __device__ __forceinline__ uint32_t append_quantise(const AppendRaw &r, uint32_t &scale)
 {
     const float2 p = kvc_to_float2<T>(r.a.x), q = kvc_to_float2<T>(r.a.y), u = kvc_to_float2<T>(r.b.x), v = kvc_to_float2<T>(r.b.y);
     const float x[8] = {p.x, p.y, q.x, q.y, u.x, u.y, v.x, v.y};
-    float low = x[0], high = x[0];
+    float low = min_nan(x[0], x[1], x[2]), high = max_nan(x[0], x[1], x[2]), least = min_nan(fabsf(x[0]), fabsf(x[1]), fabsf(x[2]));
 #pragma unroll
-    for (int i = 1; i < 8; ++i) {
-        low = min_nan(low, x[i]);
-        high = max_nan(high, x[i]);
+    for (int i = 3; i < 9; i += 2) {
+        const float y = x[i < 8 ? i : 7], z = x[i < 7 ? i + 1 : 7];
+        low = min_nan(low, y, z);
+        high = max_nan(high, y, z);
+        least = min_nan(least, fabsf(y), fabsf(z));
     }
 #pragma unroll
     for (int n = 1; n < 4; n *= 2) {
-        low = min_nan(low, __shfl_xor_sync(~0u, low, n));
-        high = max_nan(high, __shfl_xor_sync(~0u, high, n));
+        const float y = __shfl_xor_sync(~0u, low, n), z = __shfl_xor_sync(~0u, high, n);
+        low = min_nan(low, y, y);
+        high = max_nan(high, z, z);
     }
-    float step;
-    scale = down_bits<T>(__fdiv_rn(high - low, 15.f), step) | kvc_from_float2<T>(0.f, low);
+    float step, range = high - low;
+    if (range != INFINITY)  // (a range that is no float's stays none)
+        range = __fsub_rd(high, low);
+    scale = down_bits<T>(__fdiv_rn(range, 15.f), step);
+    if (15.f * step > range) {
+        // the quotient was rounded up to a number of the type: the one below
+        --scale;
+        step = kvc_to_float2<T>(scale).x;
+    }
+    scale |= kvc_from_float2<T>(0.f, low);
     // (steps whose reciprocal is none are taken 2^64 times as large, like the differences)
     const float up = step < 0x1p-100f ? 0x1p64f : 1.f;
     step *= up;
     const float inv = step > 0.f ? __frcp_rn(step) : 0.f, half = 0.5f * step;
+    if (fminf(least, fabsf(low)) < range * (std::is_same<T, __half>::value ? 0x1p-13f : 0x1p-16f))
+        return append_lossy<T>(r, low, step, up, inv);
     float c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
