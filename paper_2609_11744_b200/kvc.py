@@ -732,20 +732,25 @@ def kvc_map_tokens(layout, context_lens, new_lens, free_blocks, block_tables, cu
 
 
 def kvc_append(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, q_weight=None, k_weight=None,
-               eps: float = 1e-6, interleaved: bool = False, stream=None, _other=None) -> None:
+               eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
     """Norm and rotate queries and keys, write queries to q_out and keys and values to the pool's slots.
 
     q, q_out [T, Hq, D] (or both None), k, v [T, Hkv, D]: bf16 or fp16, any token and head strides;
     slots [T] int64; positions [T] int32 and cos_sin [max_positions, rot_dim] float32 (or both None:
-    no rotation); q_weight, k_weight [D] of the type of k, or None: no norm.
-    (_other: the calls below that take the same and more: their name, the pool's heads, axes and bytes of pair_axis.)"""
+    no rotation); q_weight, k_weight [D] of the type of k, or None: no norm."""
+    _append(layout, layer, q, k, v, q_out, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, stream, None)
+
+
+def _append(layout, layer, q, k, v, q_out, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, stream, other):
+    """kvc_append; other: None, or of the calls below, which take the same and more, their name, the pool's heads, axes and
+    bytes of pair_axis."""
     t, dev, L = _step_call()
     dt = k.dtype
     kind = t.kv.get(dt)
     if kind is None:
         raise TypeError("k must be torch.bfloat16 or torch.float16, not %s" % dt)
     n, hkv, dim = k.shape
-    have = layout.heads if _other is None else _other[1]
+    have = layout.heads if other is None else other[1]
     if (hkv, dim) != have:
         raise ValueError("k has %d heads of %d, the layout %d of %d" % ((hkv, dim) + have))
     if (q is None) != (q_out is None) or (positions is None) != (cos_sin is None):
@@ -760,18 +765,18 @@ def kvc_append(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, q_
     rot = rows = cs = pos = 0
     if cos_sin is not None:
         rows, rot = cos_sin.shape
-        pos = _arg(positions, "positions", t.i32, n if _other is None else n * _other[2], dev)
+        pos = _arg(positions, "positions", t.i32, n if other is None else n * other[2], dev)
         cs = _arg(cos_sin, "cos_sin", t.f32, rows * rot, dev)
     d = _APPEND_DESC.pack(layer, kind, qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, _arg(slots, "slots", t.i64, n, dev), pos, cs, rot,
                           0 if q_weight is None else _arg(q_weight, "q_weight", dt, dim, dev),
                           0 if k_weight is None else _arg(k_weight, "k_weight", dt, dim, dev), eps, n, hq, rot, rows,
                           1 if interleaved else 0, 0)
-    if _other is None:
+    if other is None:
         status = L.kvc_append(layout.handle, d, t.stream(dev) if stream is None else _stream(stream))
         if status:
             raise KvcError(status, "kvc_append")
         return
-    name, _, axes, pair_axis = _other
+    name, _, axes, pair_axis = other
     if len(pair_axis) != rot // 2:
         raise ValueError("pair_axis names the axes of %d pairs, a head has %d" % (len(pair_axis), rot // 2))
     status = getattr(L, name)(layout.handle, d + _AXES_DESC.pack(n, axes, 0, pair_axis),
@@ -790,7 +795,7 @@ def kvc_pair_axes(sections: Sequence[int], in_turns: bool = False) -> bytes:
 
 
 def _with_axes(name: str, heads, positions, pair_axis, cos_sin):
-    """kvc_append's _other for positions [T] or [A, T]."""
+    """_append's other for positions [T] or [A, T]."""
     many = positions is not None and positions.dim() == 2
     if pair_axis is None:
         if many and positions.shape[0] != 1:
@@ -803,8 +808,8 @@ def kvc_append_axes(layout, layer: int, q, k, v, q_out, slots, positions, cos_si
                     k_weight=None, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
     """kvc_append for positions with several axes: positions [A, T] int32, pair_axis: bytes of length
     rot_dim / 2, the axis that turns each pair (see kvc_pair_axes)."""
-    kvc_append(layout, layer, q, k, v, q_out, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, stream,
-               _with_axes("kvc_append_axes", layout.heads, positions, pair_axis, cos_sin))
+    _append(layout, layer, q, k, v, q_out, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, stream,
+            _with_axes("kvc_append_axes", layout.heads, positions, pair_axis, cos_sin))
 
 
 def _q4_heads(layout) -> Tuple[int, int]:
@@ -815,8 +820,8 @@ def _q4_heads(layout) -> Tuple[int, int]:
 def kvc_append_q4(layout, layer: int, q, k, v, q_out, slots, positions, cos_sin, pair_axis=None, q_weight=None,
                   k_weight=None, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
     """kvc_append into a pool held in 4 bits (kvc_layout_create_q4).  positions [T], or [A, T] with pair_axis."""
-    kvc_append(layout, layer, q, k, v, q_out, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, stream,
-               _with_axes("kvc_append_q4", _q4_heads(layout), positions, pair_axis, cos_sin))
+    _append(layout, layer, q, k, v, q_out, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, stream,
+            _with_axes("kvc_append_q4", _q4_heads(layout), positions, pair_axis, cos_sin))
 
 
 def kvc_read_q4(layout, layer: int, k_out, v_out, slots, stream=None) -> None:
