@@ -801,6 +801,8 @@ def _with_axes(name: str, heads, positions, pair_axis, cos_sin):
         if many and positions.shape[0] != 1:
             raise TypeError("positions with several axes need pair_axis")
         pair_axis = bytes(0 if cos_sin is None else cos_sin.shape[1] // 2)
+    elif isinstance(pair_axis, (int, float)):
+        raise TypeError("pair_axis is a byte for each pair, not %r" % (pair_axis,))
     return name, heads, positions.shape[0] if many else 1, bytes(pair_axis)
 
 
