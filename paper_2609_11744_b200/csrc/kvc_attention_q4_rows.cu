@@ -5,7 +5,7 @@
 //     q . k = sum over groups of (s * sum_d q_d c_d + f * sum_d q_d):
 // the codes are exact in the model's 16-bit type, so the first product runs on them, the steps multiply its 32-bit sums,
 // four a key, and offsets times sums of the query are a product of their own with the sums in three parts, which hold all
-// of their bits.  Values cannot be taken apart like that -- their sum is over keys, each with its own step -- so they
+// of their bits.  (Each query row comes times a power of two of its own, so that small ones are none of the type's smallest numbers.)  Values cannot be taken apart like that -- their sum is over keys, each with its own step -- so they
 // become f + s * c in that type (rounded once, as a 16-bit pool would hold them).  Against 64 bits the result is off by
 // 0.0026 in bf16 and 0.0003 in fp16: the values' rounding, the weights' (the matrix unit takes 16-bit operands of one type) and
 // the result's own, 0.0017.
@@ -164,22 +164,29 @@ __device__ __forceinline__ uint32_t load_unit(const KvcAttn &a, int32_t j, uint3
     return there;
 }
 
-// Powers of two that queries take with them into the first product, so that products with codes as numbers as they
-// stand (bf16: 2^-133 each) are none of the smallest: QUERY, and 1 / QUERY / (what a code in the low bits is worth).
+// Powers of two that queries take with them into the first product.  Each row has one of its own, which brings its largest
+// element near 2^TOP and is undone in the scores (exactly, like all of these): so queries of any size keep all of their bits.
+// Another one is for all: QUERY, for codes in the low bits, and QUERY / 16 for those in the high ones, so that products with
+// codes as numbers as they stand (bf16: 2^-133 each) are none of the smallest; BACK is 1 / QUERY / (what a code in the low bits
+// is worth).  fp16: the row's power is two factors, since one ends at 2^15.
 template <typename T>
 struct Scaling;
 template <>
 struct Scaling<__nv_bfloat16> {
-    static constexpr uint32_t QUERY = 0x5F805F80u, QUERY_HIGH = 0x5D805D80u;  // 2^64, 2^60
-    static constexpr float BACK = 0x1p69f;                                    // 2^(133 - 64)
+    static constexpr int TOP = 0, LEAST = -126, MOST = 126, FIRST = 126;
+    static constexpr int QUERY = 64;
+    static constexpr float BACK = 0x1p69f;  // 2^(133 - 64)
     static constexpr float SUM = 1.f;
+    static __device__ __forceinline__ uint32_t power(int e) { return (uint32_t)(e + 127) * 0x00800080u; }
     static __device__ __forceinline__ uint32_t times(uint32_t x, uint32_t f) { return kvc_mul_bf16x2(x, f); }
 };
 template <>
 struct Scaling<__half> {
-    static constexpr uint32_t QUERY = 0x3C003C00u, QUERY_HIGH = 0x2C002C00u;  // 1, 2^-4
+    static constexpr int TOP = 13, LEAST = -2, MOST = 30, FIRST = 15;
+    static constexpr int QUERY = 0;
     static constexpr float BACK = 0x1p24f;
     static constexpr float SUM = 0x1p-6f;  // of a query's sums, which may leave the type's range
+    static __device__ __forceinline__ uint32_t power(int e) { return (uint32_t)(e + 15) * 0x04000400u; }
     static __device__ __forceinline__ uint32_t times(uint32_t x, uint32_t f)
     {
         uint32_t r;
@@ -268,8 +275,10 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) kvc_attn_q4_row
     for (uint32_t n_units; c.s < n_seq && (n_units = run.count(c, units_at)) != 0;) {
         // ---- a new pair (or the rest of one): its queries as matrix operands, D x 8 NT
         const uint32_t row0 = c.rt * ROWS, rows = min((uint32_t)ROWS, (uint32_t)c.q.rows - row0);
+        using F = Scaling<T>;
         uint32_t qf[NT][2 * G][2], qs[NT][2];
         int32_t pos[NT][2];
+        float scale[NT][2];  // from products to scores, base 2: with the power of two of the column's row
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const uint32_t i = n * 8 + gr;
@@ -279,22 +288,42 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) kvc_attn_q4_row
                 const uint32_t row = row0 + i, tok = kvc_div_g(a, row);
                 src += (int64_t)(c.q.qa + (int32_t)tok) * a.q_tok + (int64_t)(c.h * a.g + (row - tok * a.g)) * a.q_head;
             }
-            float sums[G];
+            uint4 x[G];
+            uint32_t top = 0;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                uint4 x = make_uint4(0, 0, 0, 0);
+                x[g] = make_uint4(0, 0, 0, 0);
                 if (real)
-                    x = *reinterpret_cast<const uint4 *>(src + g * 64 + gc * 16);
-                using F = Scaling<T>;
-                qf[n][2 * g][0] = F::times(kvc_lows(x.x, x.z), F::QUERY);
-                qf[n][2 * g][1] = F::times(kvc_highs(x.x, x.z), F::QUERY_HIGH);
-                qf[n][2 * g + 1][0] = F::times(kvc_lows(x.y, x.w), F::QUERY);
-                qf[n][2 * g + 1][1] = F::times(kvc_highs(x.y, x.w), F::QUERY_HIGH);
-                const float2 p = kvc_to_float2<T>(x.x), q = kvc_to_float2<T>(x.y), u = kvc_to_float2<T>(x.z), v = kvc_to_float2<T>(x.w);
+                    x[g] = *reinterpret_cast<const uint4 *>(src + g * 64 + gc * 16);
+                top = __vmaxu2(__vmaxu2(__vmaxu2(top, x[g].x & 0x7FFF7FFFu), __vmaxu2(x[g].y & 0x7FFF7FFFu, x[g].z & 0x7FFF7FFFu)),
+                               x[g].w & 0x7FFF7FFFu);
+            }
+            // the row's power of two, from its largest element (none for infinity and NaN)
+            top = max(top & 0xFFFFu, top >> 16);
+            top = max(top, __shfl_xor_sync(~0u, top, 1));
+            top = max(top, __shfl_xor_sync(~0u, top, 2));
+            const int32_t size = (int32_t)(__float_as_uint(kvc_to_float2<T>(top).x) >> 23) - 127;
+            const int32_t power = size == 128 ? 0 : kvc_clamp(F::TOP - size, F::LEAST, F::MOST), first_power = min(power, F::FIRST);
+            const uint32_t first_by = F::power(first_power), low_by = F::power(power - first_power + F::QUERY),
+                           high_by = F::power(power - first_power + F::QUERY - 4);
+            float sums[G];
+            const float sum_by = __int_as_float((127 + power - first_power) << 23) * F::SUM;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                x[g] = make_uint4(F::times(x[g].x, first_by), F::times(x[g].y, first_by), F::times(x[g].z, first_by), F::times(x[g].w, first_by));
+                qf[n][2 * g][0] = F::times(kvc_lows(x[g].x, x[g].z), low_by);
+                qf[n][2 * g][1] = F::times(kvc_highs(x[g].x, x[g].z), high_by);
+                qf[n][2 * g + 1][0] = F::times(kvc_lows(x[g].y, x[g].w), low_by);
+                qf[n][2 * g + 1][1] = F::times(kvc_highs(x[g].y, x[g].w), high_by);
+                const float2 p = kvc_to_float2<T>(x[g].x), q = kvc_to_float2<T>(x[g].y), u = kvc_to_float2<T>(x[g].z), v = kvc_to_float2<T>(x[g].w);
                 float sum = ((p.x + p.y) + (q.x + q.y)) + ((u.x + u.y) + (v.x + v.y));
                 sum += __shfl_xor_sync(~0u, sum, 1);
-                sums[g] = (sum + __shfl_xor_sync(~0u, sum, 2)) * Scaling<T>::SUM;
+                sums[g] = (sum + __shfl_xor_sync(~0u, sum, 2)) * sum_by;
             }
+            // (a scale that no float is, of queries or scales at the end of the range, becomes the last that is one)
+            const float by = fminf(fmaxf(a.scale_log2 * __int_as_float((127 - power) << 23), 0x1p-126f), 0x1p125f);
+            scale[n][0] = __shfl_sync(~0u, by, gc * 8u);
+            scale[n][1] = __shfl_sync(~0u, by, gc * 8u + 4u);
             // The product of offsets and a query's sums: places 0-3 of the operand take the groups' sums rounded to the type, 4-7
             // and 8-11 what that leaves, twice over: all 24 bits.  This lane holds places 2 gc, 2 gc + 1 and the same + 8.
             const float s0 = G == 4 && (gc & 1u) ? sums[G / 2] : sums[0], s1 = G == 4 && (gc & 1u) ? sums[G - 1] : sums[1];
@@ -465,10 +494,10 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) kvc_attn_q4_row
                         float x = fmaxf(top[n][e], __shfl_xor_sync(~0u, top[n][e], 4));
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                        const float now = fmaxf(m[n][e], x * a.scale_log2);
+                        const float now = fmaxf(m[n][e], x * scale[n][e]);
                         const float f = m[n][e] == -INFINITY ? 0.f : exp2_fast(m[n][e] - now);
                         m[n][e] = now;
-                        limit[n][e] = now == -INFINITY ? -INFINITY : (now + 8.f) * (1.f / a.scale_log2);
+                        limit[n][e] = now == -INFINITY ? -INFINITY : __fdividef(now + 8.f, scale[n][e]);
                         l[n][e] *= f;
 #pragma unroll
                         for (int t = 0; t < S::MT; ++t) {
@@ -484,7 +513,7 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) kvc_attn_q4_row
                 for (int t = 0; t < KT; ++t) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[t][n][e] = exp2_fast(fmaf(s[t][n][e], a.scale_log2, e & 1 ? base1 : base0));
+                        s[t][n][e] = exp2_fast(fmaf(s[t][n][e], scale[n][e & 1], e & 1 ? base1 : base0));
                         l[n][e & 1] += s[t][n][e];
                     }
                     p[t][n][0] = transpose(kvc_from_float2<T>(s[t][n][0], s[t][n][1]));
