@@ -338,8 +338,8 @@ __global__ void __launch_bounds__(THREADS, Shape<D, NT>::BLOCKS) kvc_attn_q4_row
             qs[n][1] = !has || gc >= 2 ? 0u : third;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint32_t col = n * 8 + gc * 2 + e;  // (a column of no row sees all: it holds up no check)
-                pos[n][e] = col < rows ? kvc_row_pos(a, c.q, row0 + col) : 0x7FFFFFFF;
+                // (a column of no row sees what the last row does, so that it holds up no check whether all see a unit's keys)
+                pos[n][e] = kvc_row_pos(a, c.q, row0 + min(n * 8 + gc * 2 + e, rows - 1u));
             }
         }
         float o[NT][S::MT][4];
