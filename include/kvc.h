@@ -586,7 +586,7 @@ kvc_status kvc_read_q4(kvc_layout *layout, const kvc_read_q4_desc *desc, void *s
  * kernel for few rows the codes of a key are exact and the steps multiply the sums, elsewhere a
  * key is rounded to 11 bits.  A value is rounded to the dtype, as a 16-bit pool would hold it.  With many query rows blocks of
  * 4, 8, 16 or 32 tokens are the fast ones, and larger powers of two nearly so.  In bf16 values above 2^60 are not taken for
- * what they are, nor, with many query rows, queries and keys above 65504.  scale is at most KVC_Q4_MAX_SCALE (INVALID_ARG).  The workspace comes from
+ * what they are, nor, with many query rows, keys above 65504.  scale is at most KVC_Q4_MAX_SCALE (INVALID_ARG).  The workspace comes from
  * kvc_attention_q4_workspace_bytes. */
 #define KVC_Q4_MAX_SCALE 1e18f
 kvc_status kvc_attention_q4_workspace_bytes(kvc_layout *layout, uint32_t n_tokens, uint32_t n_requests,

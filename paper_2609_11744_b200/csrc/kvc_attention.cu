@@ -440,6 +440,8 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     a.g_shift = kvc_shift_of(a.g);
     a.block_shift = kvc_shift_of(a.block_size);
     a.scale_log2 = d->scale * 1.44269504088896341f;
+    if (q4)
+        a.scale_log2 = std::max(a.scale_log2, 0x1p-126f);  // (powers of two are added to its exponent)
     a.window = (int32_t)d->window;
     a.sinks = (int32_t)d->sinks;
     a.status = lay->d_status;

@@ -594,15 +594,16 @@ __device__ __forceinline__ void raw_role(const KvcAttn &a, const Segment *segmen
 
 // The first product over a pool in 4 bits is fp16's whatever the model's type: a key, offset + step * code, is rounded to 11 bits
 // and not to 8, which the log-sum-exp would show (of the 8192-token prompt off by 2e-7 of it, 1e-5 with 8; of fewer keys by
-// more).  Queries and keys of bf16 so end at 65504, and below 2^-14 they are off by 2^-25.
+// more).  Keys of bf16 so end at 65504, and below 2^-14 they are off by 2^-25, 15 times that for their step.
+// `by`: a power of two that brings them into fp16's range.
 template <typename T>
-__device__ __forceinline__ uint32_t first_operand(uint32_t x)
+__device__ __forceinline__ uint32_t first_operand(uint32_t x, float by = 1.f)
 {
     if constexpr (std::is_same<T, __half>::value) {
         return x;
     } else {
         const float2 v = kvc_to_float2<T>(x);
-        return kvc_from_float2<__half>(v.x, v.y);
+        return kvc_from_float2<__half>(v.x * by, v.y * by);
     }
 }
 
@@ -710,6 +711,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
 {
     using S = Shape<D, ROWS, Q4>;
     constexpr bool HELPED = Q4 && ROWS == 128;  // warps 8-15 make values
+    // queries of bf16 become fp16: each row times a power of two of its own, which the scores undo
+    constexpr bool SCALED = Q4 && !std::is_same<T, __half>::value;
     constexpr uint32_t READERS = Q4 && !HELPED ? SEGMENT_READERS + 1 : SEGMENT_READERS;
     constexpr uint32_t LOADERS = HELPED ? 4 : 1;
     const KvcAttn &a = args.a;
@@ -719,6 +722,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
     __shared__ uint32_t s_dead, s_tmem;
     __shared__ Segment segments[SEGMENTS];
     __shared__ RawBars raw;  // (Q4)
+    __shared__ int8_t row_power[2][ROWS / 128][SCALED ? 128 : 1];  // [queries loaded, odd or even][row tile][row]
     __shared__ float row_top[2][ROWS / 128][2][128], row_sum[ROWS / 128][2][128];  // ([tile of keys, odd or even])[row tile][half][row]
     // What touches no memory of the caller's comes before the wait for the stream's previous kernel.
     const uint32_t warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31u;
@@ -809,8 +813,11 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
         SegmentReader reader;
         Segment c, d;
         uint32_t s_parity = 0, o_parity = 0, slot = 0;  // parities: a bit for each barrier, of those that this warp waits for
+        uint32_t queries = 0;  // loads of this row tile's queries so far, odd or even
         // Queries of a segment: 16 bytes a thread and turn, rows of 128 bytes in the swizzle.  All scores
-        // of the segment before have been seen, so their operand may go.
+        // of the segment before have been seen, so their operand may go.  (The rows' powers of two have two places: a warp
+        // reads its rows' while others load the next segment's, but none loads those of the one after before all have loaded
+        // the next, whose scores it waits for.)
         const auto load_queries = [&](const Segment &c) {
             const uint32_t row0 = c.rt * ROWS + sub * 128u, rows_all = (uint32_t)c.q.rows;
             if (row0 >= rows_all || (ROWS == 128 && sub == 1))
@@ -821,6 +828,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             const uint32_t tok_step = kvc_div_g(a, STEP), head_step = STEP - tok_step * a.g;
             const unsigned char *src = a.q + (int64_t)c.q.qa * a.q_tok + (int64_t)(c.h * a.g) * a.q_head + chunk * 16u;
             unsigned char *dst = tiles_ptr + S::Q + sub * S::TILE + (chunk >> 3) * S::HALF;
+            queries ^= 1u;
             uint4 x[TURNS];
 #pragma unroll
             for (uint32_t e = 0; e < TURNS; ++e) {
@@ -834,11 +842,37 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     ++tok;
                 }
             }
+            uint32_t tops[TURNS / 2];  // a row's largest element, in D / 8 lanes, two rows a word
+            if constexpr (SCALED) {
+#pragma unroll
+                for (uint32_t e = 0; e < TURNS; e += 2) {
+                    const auto most = [](const uint4 &y) {
+                        return __vmaxu2(__vmaxu2(y.x & 0x7FFF7FFFu, y.y & 0x7FFF7FFFu), __vmaxu2(y.z & 0x7FFF7FFFu, y.w & 0x7FFF7FFFu));
+                    };
+                    const uint32_t top0 = most(x[e]), top1 = most(x[e + 1]);
+                    tops[e / 2] = __vmaxu2(kvc_lows(top0, top1), kvc_highs(top0, top1));
+                }
+#pragma unroll
+                for (uint32_t o = 1; o < D / 8; o *= 2)
+#pragma unroll
+                    for (uint32_t e = 0; e < TURNS / 2; ++e)
+                        tops[e] = __vmaxu2(tops[e], __shfl_xor_sync(~0u, tops[e], o));
+            }
 #pragma unroll
             for (uint32_t e = 0; e < TURNS; ++e) {
                 const uint32_t r = r0 + e * STEP;
+                float by = 1.f;
+                if constexpr (SCALED) {
+                    // the row's largest element near 2^13 (rows of infinity or NaN as they are), as far as the scale stays a float
+                    const int32_t size = (int32_t)((e & 1u ? tops[e / 2] >> 16 : tops[e / 2] & 0xFFFFu) >> 7) - 127;
+                    const int32_t scale_size = (__float_as_int(a.scale_log2) >> 23) - 127;
+                    const int32_t power = size == 128 ? 0 : kvc_clamp(13 - size, scale_size - 125, min(scale_size + 126, 126));
+                    by = __int_as_float((127 + power) << 23);
+                    if (chunk == 0)
+                        row_power[queries][sub][r] = (int8_t)power;
+                }
                 if constexpr (Q4) {  // the order that the keys' values come in
-                    x[e] = make_uint4(first_operand<T>(x[e].x), first_operand<T>(x[e].y), first_operand<T>(x[e].z), first_operand<T>(x[e].w));
+                    x[e] = make_uint4(first_operand<T>(x[e].x, by), first_operand<T>(x[e].y, by), first_operand<T>(x[e].z, by), first_operand<T>(x[e].w, by));
                     x[e] = make_uint4(kvc_lows(x[e].x, x[e].z), kvc_highs(x[e].x, x[e].z), kvc_lows(x[e].y, x[e].w), kvc_highs(x[e].y, x[e].w));
                 }
                 *reinterpret_cast<uint4 *>(dst + r * 128u + (((chunk & 7u) ^ (r & 7u)) << 4)) = x[e];
@@ -966,6 +1000,12 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                     tmem_ld32(s + 32, s_at + half * HK + 32);
                     uint32_t mask0, mask1;
                     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(mask0), "=r"(mask1) : "r"(smem_addr(&there[(slot + i) % THERE][half * 2])));
+                    float scale = a.scale_log2;  // from products to scores, base 2
+                    if constexpr (SCALED) {
+                        int32_t power;
+                        asm volatile("ld.shared.s8 %0, [%1];" : "=r"(power) : "r"(smem_addr(&row_power[queries][sub][tid])));
+                        scale = __int_as_float(__float_as_int(scale) - power * (1 << 23));
+                    }
                     tmem_wait_ld();
                     if (__any_sync(~0u, (mask0 & mask1) != ~0u || j0 + HK - 1 > pos || (j0 <= old && j0 + HK - 1 >= a.sinks))) {
                         // kvc_sees() for 32 keys at a time: at most pos, and after pos - window or before sinks
@@ -996,7 +1036,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                         ok = false;
                         break;
                     }
-                    top = fmaxf(top, row_top[i & 1u][sub][half ^ 1u][tid]) * a.scale_log2;
+                    top = fmaxf(top, row_top[i & 1u][sub][half ^ 1u][tid]) * scale;
                     if (i == 0) {
                         m = top;
                     } else {
@@ -1036,7 +1076,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                         }
                     }
                     const float base = m == -INFINITY ? 0.f : m;
-                    const uint64_t scale2 = kvc_pair(a.scale_log2, a.scale_log2), base2 = kvc_pair(-base, -base);
+                    const uint64_t scale2 = kvc_pair(scale, scale), base2 = kvc_pair(-base, -base);
                     uint64_t sum2 = 0;
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
