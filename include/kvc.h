@@ -582,9 +582,11 @@ typedef struct {
 kvc_status kvc_read_q4(kvc_layout *layout, const kvc_read_q4_desc *desc, void *stream);
 
 /* kvc_attention and kvc_attention_shared over a pool held in 4 bits, with the same descriptor and rules: masks,
- * lengths, clamps, groups, workspaces.  Products with keys and values are taken in the dtype with 32-bit sums: in the
- * kernel for few rows the codes of a key are exact and the steps multiply the sums, elsewhere a
- * key is rounded to 11 bits.  A value is rounded to the dtype, as a 16-bit pool would hold it.  With many query rows blocks of
+ * lengths, clamps, groups, workspaces.  Products with keys and values are taken in 16 bits with 32-bit sums.  Where 16 rows or fewer
+ * share a KV head's keys, the codes of a key are exact and the steps multiply the sums; with more rows a key is
+ * rounded to 11 bits, which moves a score by scale * sum |q k| * 2^-12 at most.  Rows that see 64 keys or fewer, whose
+ * log-sum-exp would show it, take what the rounding leaves as well (behind a shared prefix: if the prefix has 64 or fewer and the row's own
+ * position is below 64).  A value is rounded to the dtype, as a 16-bit pool would hold it.  With many query rows blocks of
  * 4, 8, 16 or 32 tokens are the fast ones, and larger powers of two nearly so.  In bf16 values above 2^60 are not taken for
  * what they are, nor, with many query rows, keys above 65504.  scale is at most KVC_Q4_MAX_SCALE (INVALID_ARG).  The workspace comes from
  * kvc_attention_q4_workspace_bytes. */

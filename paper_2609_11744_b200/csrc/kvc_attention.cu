@@ -452,13 +452,10 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
     // Sixteen rows or fewer fit the kernel for few rows, which reads the keys once for them; with more
     // it would read them once for every sixteen, and the matrix unit takes over.  Up to 128 rows it gets one
     // row tile and a deeper ring of keys.  (Whatever the lengths turn out to be, any of the three is right.)
-    // Over a pool held in 4 bits eight rows or fewer are one tile of columns, which leaves registers for a fourth block a SM.
-    // It takes keys for what they are besides, where the matrix unit's are rounded to 11 bits.  So up to 128 rows that can see
-    // 128 keys at most are its own too (32 requests of 20 rows: 18.8 us against 24.7 with 20 keys, 27.1 against 29.3 with
-    // 128), and any number that can see 64 at most in fp16, 16 in bf16, since a log-sum-exp over so few would show the
-    // rounding (one of 2 keys is off by 1.8e-4 of it, of 35 by 1.6e-5, of 180 by 4e-6; a bf16 step's 8 bits, times 4, seldom
-    // need more than 11: of 5 keys by 1e-5).  Over long prompts it takes 4.7 times as long (8192 tokens, window 128: 607 us
-    // against 130).
+    // Over a pool held in 4 bits eight rows or fewer are one tile of columns, of which an SM holds one block more (heads of 128:
+    // three and two).  Up to 128 rows whose table or window reaches 128 keys at most are for the kernel for few rows too: it starts
+    // sooner (32 requests of up to 5 drafted tokens, 20 rows a KV head, 20 to 128 keys: 19 us against 27).  Over long prompts it
+    // takes 4.7 times as long (8192 tokens, window 128: 607 us against 130).
     const uint64_t q_len = std::min<uint64_t>(d->max_q_len ? d->max_q_len : d->n_tokens, d->n_tokens);
     const uint64_t table = (uint64_t)a.max_blocks * a.block_size;
     const uint64_t reach = d->window ? std::min<uint64_t>(table, (uint64_t)d->window + d->sinks) : table;
@@ -466,7 +463,7 @@ kvc_status attention(kvc_layout *lay, const kvc_attention_desc *d, bool shared, 
         const uint64_t rows = tokens * a.g;
         if (q4 && rows <= KVC_ATTN_FEW_ROWS)
             return KVC_ATTN_FEW_ROWS;
-        if (q4 && reach <= (rows <= KVC_ATTN_TILE_ROWS ? 128u : bf16 ? 16u : 64u))
+        if (q4 && rows <= KVC_ATTN_TILE_ROWS && reach <= 128)
             return KVC_ATTN_SMALL_ROWS;
         return rows <= KVC_ATTN_SMALL_ROWS ? KVC_ATTN_SMALL_ROWS : rows <= KVC_ATTN_TILE_ROWS ? KVC_ATTN_TILE_ROWS : KVC_ATTN_MANY_ROWS;
     };

@@ -262,10 +262,24 @@ struct Segment {
     KvcRange r;
     uint32_t h, rt, t, n;  // KV head, row tile; first tile and number of tiles (0: the run is over)
     uint32_t pair;
+    uint32_t few;  // (Q4) some row sees few keys: their tiles come in two stages, what they are in 11 bits and what that leaves
     unsigned long long units_at;  // where the pair's units begin on the line
 };
 constexpr uint32_t SEGMENTS = 4;
 constexpr uint32_t SEGMENT_READERS = 19;  // 16 softmax warps, 2 loading warps, the issuing warp
+
+// Whether a row of the pair's row tile sees FEW_KEYS keys or fewer.  (The first row sees the fewest.  A prefix that is longer
+// counts as many, and so do own keys behind a prefix, whatever their number, by the row's position.)
+constexpr uint32_t FEW_KEYS = 64;
+template <int ROWS>
+__device__ __forceinline__ bool sees_few(const KvcAttn &a, const KvcCursor &c)
+{
+    if (a.phase == KVC_PHASE_PREFIX)
+        return (uint32_t)c.q.len <= FEW_KEYS;
+    const int32_t pos = c.q.pos + (int32_t)kvc_div_g(a, c.rt * ROWS);
+    const uint32_t reach = a.window ? (uint32_t)a.window + (uint32_t)a.sinks : ~0u;
+    return min(min((uint32_t)max(pos + 1, 0), (uint32_t)kvc_key_cap(a)), reach) <= FEW_KEYS;
+}
 
 // The next segment, copied to registers.  Every lane of the role's warp calls this.
 struct SegmentReader {
@@ -594,8 +608,9 @@ __device__ __forceinline__ void raw_role(const KvcAttn &a, const Segment *segmen
 
 // The first product over a pool in 4 bits is fp16's whatever the model's type: a key, offset + step * code, is rounded to 11 bits
 // and not to 8, which the log-sum-exp would show (of the 8192-token prompt off by 2e-7 of it, 1e-5 with 8; of fewer keys by
-// more).  Keys of bf16 so end at 65504, and below 2^-14 they are off by 2^-25, 15 times that for their step.
-// `by`: a power of two that brings them into fp16's range.
+// more).  fp16 ends at 65504 and has fewer bits below 2^-14, so each row of queries comes times a power of two of its own, `by`.
+// Keys do not: those of bf16 end at 65504, and steps, offsets and values below 2^-14 are off by 2^-25 each, a step up to 15 times
+// that.  (A power for 32 keys, found by their warp, which holds the others up: the 8192-token prompt 775 us instead of 733.)
 template <typename T>
 __device__ __forceinline__ uint32_t first_operand(uint32_t x, float by = 1.f)
 {
@@ -604,6 +619,35 @@ __device__ __forceinline__ uint32_t first_operand(uint32_t x, float by = 1.f)
     } else {
         const float2 v = kvc_to_float2<T>(x);
         return kvc_from_float2<__half>(v.x * by, v.y * by);
+    }
+}
+
+// The keys of a part, one a lane, by 32-bit arithmetic: rounded to 11 bits at `dst`, and what that leaves at `rest`.  (Short
+// loops, outside the one for ordinary tiles: it is seldom called.)
+template <typename T, int D, int HALF>
+__device__ __forceinline__ void keys_and_rest(uint32_t codes, uint32_t scales, uint32_t keep, uint32_t dst, uint32_t rest, uint32_t swap)
+{
+#pragma unroll 1
+    for (int g = 0; g < D / 32; ++g) {
+        uint32_t packed;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(packed) : "r"(scales + g * 4u));
+        const float2 sc = kvc_to_float2<T>(packed & keep);
+        const uint32_t to = (g >> 1) * HALF + (((g & 1) << 6) ^ swap);
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+            uint32_t w, x[4], y[4];
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(codes + g * 16u + k * 4u));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v0 = fmaf((float)(w >> (4 * i) & 15u), sc.x, sc.y), v1 = fmaf((float)(w >> (16 + 4 * i) & 15u), sc.x, sc.y);
+                x[i] = kvc_from_float2<__half>(v0, v1);
+                const float2 v = kvc_to_float2<__half>(x[i]);
+                y[i] = kvc_from_float2<__half>(v0 - v.x, v1 - v.y);
+            }
+            const uint32_t at = to ^ (k << 4);
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]));
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(rest + at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]));
+        }
     }
 }
 
@@ -637,6 +681,52 @@ __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segm
 #pragma unroll 1
     while (ok && reader.next(segments, bars, c, dead, a.status)) {
         const uint32_t tiles_n = c.n;
+        // a raw part is done with
+        const auto next_part = [&] {
+            if (lane == 0)
+                bar_arrive(smem_addr(&rb->empty[from]));
+            from += ROWS == 128 ? 4u : 1u;
+            if (from >= (uint32_t)S::PARTS) {
+                from -= S::PARTS;
+                parity ^= 1u;
+            }
+        };
+        const auto stage_full = [&] {
+            if (lane == 0)
+                bar_arrive(full + ring.stage * 8u);
+            ring.next();
+        };
+        if (KEYS && c.few) {  // a tile's keys in two stages
+#pragma unroll 1
+            for (uint32_t u = 0; u < tiles_n; ++u) {
+                Ring<STAGES> then = ring;
+                then.next();
+                if (!(ok = __all_sync(~0u, bar_wait(empty + ring.stage * 8u, ring.parity ^ 1u, dead, a.status) &&
+                                               bar_wait(empty + then.stage * 8u, then.parity ^ 1u, dead, a.status))))
+                    break;
+#pragma unroll 1
+                for (uint32_t p = 0; p < PER; ++p) {
+                    if (!(ok = __all_sync(~0u, bar_wait(smem_addr(&rb->full[from]), parity, dead, a.status))))
+                        break;
+                    const uint32_t is = rb->there[from], row = tiles + ((sub + p) * 32u + lane) * 128u, at = from * (2u * S::PART);
+                    if (lane == 0)
+                        there[slot][sub + p] = is;
+                    if (is != 0)  // (else whatever lies there: the scores are replaced)
+                        keys_and_rest<T, D, S::HALF>(code_at + at, scale_at + at, is >> lane & 1u ? ~0u : 0u, row + ring.stage * S::TILE,
+                                                     row + then.stage * S::TILE, swap);
+                    __syncwarp();
+                    next_part();
+                }
+                if (!ok)
+                    break;
+                fence_async();
+                __syncwarp();
+                stage_full();
+                stage_full();
+                slot = (slot + 1) % THERE;
+            }
+            continue;
+        }
 #pragma unroll 1
         for (uint32_t u = 0; u < tiles_n; ++u) {
             if (!(ok = __all_sync(~0u, bar_wait(empty + ring.stage * 8u, ring.parity ^ 1u, dead, a.status))))
@@ -686,21 +776,13 @@ __device__ __forceinline__ void value_role(const KvcAttn &a, const Segment *segm
                     }
                 }
                 __syncwarp();
-                if (lane == 0)
-                    bar_arrive(smem_addr(&rb->empty[from]));
-                from += ROWS == 128 ? 4u : 1u;
-                if (from >= (uint32_t)S::PARTS) {
-                    from -= S::PARTS;
-                    parity ^= 1u;
-                }
+                next_part();
             }
             if (!ok)
                 break;
             fence_async();
             __syncwarp();
-            if (lane == 0)
-                bar_arrive(full + ring.stage * 8u);
-            ring.next();
+            stage_full();
             slot = (slot + 1) % THERE;
         }
     }
@@ -1174,6 +1256,51 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
             while (reader.next(segments, &bars, c, dead, a.status)) {
                 const bool two = ROWS == 256 && uniform((uint32_t)c.q.rows - c.rt * ROWS > 128u);
                 const uint32_t n = uniform(c.n);
+                if (Q4 && uniform(c.few) != 0) {
+                    // Few keys: a tile's lie in two stages, what they are in 11 bits and what that leaves.  One tile after the other
+                    if (!wait(BAR(q_full), q_parity) || (two && !wait(BAR(q_full) + 8u, q_parity >> 1)))
+                        break;
+                    q_parity ^= two ? 3u : 1u;
+#pragma unroll 1
+                    for (uint32_t i = 0; ok && i < n; ++i) {
+                        Ring<S::KS> then = k;
+                        then.next();
+                        if (!wait(BAR(k_full) + k.stage * 8u, k.parity) || !wait(BAR(k_full) + then.stage * 8u, then.parity))
+                            break;
+#pragma unroll 1
+                        for (uint32_t sub = 0; sub < (two ? 2u : 1u); ++sub) {
+                            const uint32_t qa = q_at + sub * (S::TILE >> 4), d = tmem + COL_S + (two ? sub : i & 1u) * 128u;
+                            if (elect_one()) {
+#pragma unroll 1
+                                for (uint32_t e = 0; e < D / 8; ++e) {
+                                    const uint32_t at = ((e >> 2 & (D / 64 - 1)) * S::HALF + (e & 3u) * 32) >> 4;
+                                    mma_ss(d, qa + at, k_at + (e < D / 16 ? k.stage : then.stage) * (S::TILE >> 4) + at, KIND_S, e > 0);
+                                }
+                                mma_commit(bar + BAR(s_full) + (two ? sub : (i & 1u) * 2u) * 8u);
+                            }
+                            __syncwarp();
+                        }
+                        commit(BAR(k_empty) + k.stage * 8u);
+                        commit(BAR(k_empty) + then.stage * 8u);
+                        k = then;
+                        k.next();
+                        if (!wait(BAR(v_full) + v.stage * 8u, v.parity))
+                            break;
+#pragma unroll 1
+                        for (uint32_t sub = 0; ok && sub < (two ? 2u : 1u); ++sub) {
+                            products(sub, two ? sub : i & 1u, i == 0);
+                            if (ok && (!two || i + 1 == n))
+                                commit(BAR(o_done) + (two ? sub : (i & 1u) * 2u) * 8u);
+                        }
+                        if (!ok)
+                            break;
+                        commit(BAR(v_empty) + v.stage * 8u);
+                        v.next();
+                    }
+                    if (!ok)
+                        break;
+                    continue;
+                }
                 if (!wait(BAR(k_full) + k.stage * 8u, k.parity) || !wait(BAR(q_full), q_parity) ||
                     (two && !wait(BAR(q_full) + 8u, q_parity >> 1)))
                     break;
@@ -1259,6 +1386,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvc_attn_tiles_kernel(const __grid
                 s.rt = c.rt;
                 s.t = c.t;
                 s.pair = pair;
+                s.few = Q4 && sees_few<ROWS>(a, c);
                 s.units_at = units_at;
                 bar_arrive(smem_addr(&bars.seg_full[slot]));
                 if (++slot == SEGMENTS) {

@@ -12,8 +12,8 @@ What a row's error may come from, with w the softmax, half = eps / 2 of the type
                 and 4 of the groups, each cut to 2^-23 of the largest
     many rows   keys are rounded to 11 bits: scale * sum_d |q_d| (2^-12 |k_d| + a) and D + 8 cuts of 2^-23 of sum_d |q_d k_d|.
                 a: fp16's smallest numbers, 2^-25 of a key's rounding in fp16; in bf16 a step (times 15), an offset and the sum each,
-                17 * 2^-25, and of keys taken times a power of two much less, but at most 2^-14 of the largest of the 32 neighbours
-    and rows that see few keys  twice as many products, of the key and of what its rounding left: 2^-22 of |k_d|"""
+                17 * 2^-25
+    and rows that see few keys  twice as many products, of the key and of what its rounding left: 2^-22 |k_d| + 2^-25"""
 import math
 
 import torch
@@ -49,8 +49,6 @@ def attention(c, window=0, sinks=0, scale=None):
         if window:
             see &= (p - j < window) | (j < sinks)
         seen[a:b] = see.sum(-1)
-        near = torch.maximum(15 * ks.double(), ko.double().abs()).amax(-1)    # [key, Hkv]: of 32 neighbours
-        near = torch.nn.functional.pad(near, (0, 0, 0, -len(j) % 32)).unflatten(0, (-1, 32)).amax(1).repeat_interleave(32, 0)[: len(j)]
         for h in range(hkv):
             x = q[a:b, h * g: (h + 1) * g]
             s = (torch.einsum("tgd,kd->tgk", x, k[:, h]) * scale).masked_fill(~see[:, None], -math.inf)
@@ -62,10 +60,9 @@ def attention(c, window=0, sinks=0, scale=None):
             small[at] = see.sum(-1)[:, None] * v[:, h].abs().max()
             most = lambda e: (e * scale).masked_fill(~see[:, None], 0.0).amax(-1)
             both, one = torch.einsum("tgd,kd->tgk", x.abs(), k[:, h].abs()), x.abs().sum(-1, keepdim=True)
-            floor = torch.minimum(torch.tensor(17 * 2.0**-25, dtype=torch.float64), 2.0**-14 * near[:, h].cpu()).to(dev) if bf16 else torch.full_like(near[:, h], 2.0**-25)
             few[at] = most(torch.einsum("tgd,kd->tgk", x.abs(), size[:, h]) * (40 * 2.0**-23))
-            many[at] = most(both * (2.0**-12 + (d + 8) * 2.0**-23) + one * floor)
-            exact[at] = most(both * (2.0**-22 + (2 * d + 16) * 2.0**-23) + one * near[:, h] * 2.0**-33)
+            many[at] = most(both * (2.0**-12 + (d + 8) * 2.0**-23) + one * (17 if bf16 else 1) * 2.0**-25)
+            exact[at] = most(both * (2.0**-22 + (2 * d + 16) * 2.0**-23) + one * 2.0**-25)
     return out, lse, weight, few, many, exact, seen, small
 
 

@@ -1,23 +1,33 @@
 """Attention over a pool held in 4 bits on a B200, row by row against bounds of each row's own keys: queries of
-any size, and ordinary calls of few rows."""
+any size, rows that see few keys, and ordinary calls by either kernel."""
 import pytest
 import torch
 
+import q4_reference as q4
 import q4_row_bounds as bounds
+from paper_2609_11744_b200 import kvc
 from test_gpu_q4 import BF16, FP16, Case, heads
 
 pytestmark = pytest.mark.gpu
 
 
+def store(c):
+    for p in range(2):
+        c.pool[1, p] = q4.pack_slabs(*c.parts[p])
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP16])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("lens,new,h,block,window,sinks", [
-    ([1, 2, 127, 129, 700], [1] * 5, 2, 16, 0, 0), ([3000, 40], [2, 1], 3, 8, 100, 5), ([500, 9], [4, 3], 1, 16, 0, 0), ([900], [1], 7, 24, 64, 70)])
+    ([1, 2, 127, 129, 700], [1] * 5, 2, 16, 0, 0), ([3000, 40], [2, 1], 3, 8, 100, 5), ([500, 9], [4, 3], 1, 16, 0, 0), ([900], [1], 7, 24, 64, 70),
+    ([300, 77, 511], [300, 20, 1], 2, 16, 0, 0), ([900, 2000], [900, 100], 4, 64, 0, 0), ([700, 1500, 64], [650, 3, 64], 3, 8, 200, 7), ([2049], [257], 5, 2, 0, 0)])
 def test_ordinary_calls(dtype, d, lens, new, h, block, window, sinks):
     hq, hkv = heads(h)
     c = Case(dtype, lens, new, hq, hkv, d, block, seed=len(lens) + block, extra=300 // block + 1)
     want = bounds.attention(c, window, sinks)
-    bounds.check(c, c.run(window, sinks, hint=max(new)), want, "few")
+    few = max(new) * hq // hkv <= 16
+    bounds.check(c, c.run(window, sinks, hint=max(new)), want, "few" if few else "many")
+    bounds.check(c, c.run(window, sinks, hint=1 if not few else 0), want, "any")
 
 
 @pytest.mark.parametrize("dtype,q_power", [(FP16, -6), (FP16, -10), (FP16, -16), (FP16, 8), (BF16, -30), (BF16, -90), (BF16, 30), (BF16, 70)])
@@ -46,3 +56,51 @@ def test_rows_of_queries_of_different_sizes(dtype, new, h):
     for scale in (128**-0.5 * 2.0**-top, 128**-0.5 * 2.0**(16 - top)):   # (scores up to 2^20: 32 bits tell no more apart than that)
         want = bounds.attention(c, scale=scale)
         bounds.check(c, c.run(hint=new, scale=scale), want, "few" if new * hq // hkv <= 16 else "many")
+
+
+def test_a_key_that_is_not_finite_leaves_rows_that_do_not_see_it_alone():
+    """Keys of infinity and NaN in the middle of a prompt: rows before them, and behind a window, are what they were."""
+    for dtype in (BF16, FP16):
+        c = Case(dtype, [300], [300], 4, 1, 128, 16, seed=6, extra=9)
+        want, got = bounds.attention(c, 40, 0), c.run(40, 0, hint=300)
+        j = 150
+        at = (int(c.tables[0, j // 16]), j % 16)
+        for what in (float("inf"), float("nan")):
+            c.parts[0][1][at], c.parts[0][2][at] = what, what
+            store(c)
+            again = c.run(40, 0, hint=300)
+            keep = torch.ones(300, dtype=torch.bool)
+            keep[j: j + 40] = False
+            assert torch.isfinite(again[0][keep.cuda()]).all() and torch.isfinite(again[1][keep.cuda()]).all()
+            assert not torch.isfinite(again[1][~keep.cuda()]).any()
+            for a, b in zip(again, got):
+                a[~keep.cuda()] = b[~keep.cuda()]
+            bounds.check(c, again, want, "many")
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("extra", [0, 500])
+@pytest.mark.parametrize("d,lens,new,h,window,sinks", [
+    (128, [1, 2, 5, 700, 64, 65], [1, 2, 5, 700, 64, 65], 2, 0, 0), (64, [3, 900, 40], [3, 200, 40], 4, 0, 0), (128, [400], [400], 5, 64, 0), (64, [400, 300], [400, 290], 2, 20, 44),
+    (128, [700, 31], [300, 31], 4, 1, 3), (128, [50, 30, 3], [9, 9, 3], 4, 0, 0), (64, [300, 200], [300, 10], 1, 33, 0), (128, [129], [129], 6, 3, 61)])
+def test_rows_that_see_few_keys(dtype, extra, d, lens, new, h, window, sinks):
+    """Whatever the width of the table, the other requests of the call and the hint."""
+    hq, hkv = heads(h)
+    c = Case(dtype, lens, new, hq, hkv, d, 16, seed=5, extra=extra)
+    want = bounds.attention(c, window, sinks)
+    for hint in (max(new), 0, 1):
+        bounds.check(c, c.run(window, sinks, hint=hint), want, "any")
+    assert kvc.kvc_poll_device_status(c.lay) == (0, 0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("prefix", [16, 48, 64, 200])
+def test_rows_that_see_few_keys_behind_a_shared_prefix(dtype, prefix):
+    lens = [prefix + 3, prefix + 1, prefix + 12, 9]
+    new = [3, 1, 12, 9]
+    for h in (2, 4, 5):
+        hq, hkv = heads(h)
+        c = Case(dtype, lens, new, hq, hkv, 128, 16, seed=7, extra=100, shared=[(0, 3, -(-prefix // 16))])
+        want = bounds.attention(c)
+        for hint in (12, 0):
+            bounds.check(c, c.run(groups=([0, 3], [prefix]), hint=hint), want, "any")
