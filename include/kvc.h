@@ -476,7 +476,8 @@ kvc_status kvc_append(kvc_layout *layout, const kvc_append_desc *desc, void *str
  * Any block size; with many query rows, sizes that divide 128 from 8 up, and multiples of 128, are the
  * fast ones.
  * Strides in elements; pointers of q and out and strides in bytes are multiples of 16 bytes.  `out`
- * must not overlap q.  scale > 0.
+ * must not overlap q.  scale > 0.  Scores, scale * q . k, are meant to lie within +-2^26: larger ones are told apart by
+ * whole numbers only, and rows that have some may give zeros, infinities or NaN.
  * workspace: at least kvc_attention_workspace_bytes(...) bytes, 256-byte aligned, contents irrelevant
  * before and after.  Calls that may run at the same time (other streams, captured graphs that are
  * replayed concurrently) need workspaces of their own; calls on one stream can share one.
@@ -582,14 +583,18 @@ typedef struct {
 kvc_status kvc_read_q4(kvc_layout *layout, const kvc_read_q4_desc *desc, void *stream);
 
 /* kvc_attention and kvc_attention_shared over a pool held in 4 bits, with the same descriptor and rules: masks,
- * lengths, clamps, groups, workspaces.  Products with keys and values are taken in 16 bits with 32-bit sums.  Where 16 rows or fewer
- * share a KV head's keys, the codes of a key are exact and the steps multiply the sums; with more rows a key is
- * rounded to 11 bits, which moves a score by scale * sum |q k| * 2^-12 at most.  Rows that see 64 keys or fewer, whose
- * log-sum-exp would show it, take what the rounding leaves as well (behind a shared prefix: if the prefix has 64 or fewer and the row's own
- * position is below 64).  A value is rounded to the dtype, as a 16-bit pool would hold it.  With many query rows blocks of
- * 4, 8, 16 or 32 tokens are the fast ones, and larger powers of two nearly so.  In bf16 values above 2^60 are not taken for
- * what they are, nor, with many query rows, keys above 65504.  scale is at most KVC_Q4_MAX_SCALE (INVALID_ARG).  The workspace comes from
- * kvc_attention_q4_workspace_bytes. */
+ * lengths, clamps, groups, workspaces; the latter from kvc_attention_q4_workspace_bytes.  scale is at most
+ * KVC_Q4_MAX_SCALE (INVALID_ARG).  With many query rows blocks of 4, 8, 16 or 32 tokens are the fast ones, and larger
+ * powers of two nearly so.
+ * Products with keys and values are taken in 16 bits with 32-bit sums.  A value is rounded to the dtype, as a 16-bit
+ * pool would hold it.  Where 16 rows or fewer share a KV head's keys, the codes of a key are exact and the steps multiply
+ * the sums.  With more rows a key is rounded to 11 bits, which moves a score by scale * sum |q k| * 2^-12 at most; rows
+ * that see 64 keys or fewer, whose log-sum-exp would show it, take what the rounding leaves as well (behind a shared
+ * prefix: if that has 64 tokens or fewer and the row's own position is below 64).
+ * Sizes.  Queries may have any.  Values of bf16 are taken for what they are between 2^-60 and 2^60, keys of bf16 with 16
+ * rows or fewer between 2^-50 and 2^60.  With more rows keys of bf16 are taken as fp16's: infinite above 65504, and below
+ * 2^-14 a value and its offset are off by 2^-25, its step by as much for each unit of the code, so that small keys, with a
+ * scale to match, lose bits.  There alone the result depends on the number of rows, and on max_q_len. */
 #define KVC_Q4_MAX_SCALE 1e18f
 kvc_status kvc_attention_q4_workspace_bytes(kvc_layout *layout, uint32_t n_tokens, uint32_t n_requests,
                                             uint32_t n_q_heads, uint32_t n_groups, uint64_t *bytes);

@@ -1,4 +1,4 @@
-"""Attention over a pool held in 4 bits on a B200, row by row against bounds of each row's own keys: queries of
+"""Attention over a pool held in 4 bits on a B200, row by row against bounds of each row's own keys: queries and keys of
 any size, rows that see few keys, and ordinary calls by either kernel."""
 import pytest
 import torch
@@ -14,6 +14,15 @@ pytestmark = pytest.mark.gpu
 def store(c):
     for p in range(2):
         c.pool[1, p] = q4.pack_slabs(*c.parts[p])
+
+
+def keys_times(c, power):
+    """power: a whole number, or one a key [block, token]."""
+    f = torch.exp2(torch.as_tensor(power, dtype=torch.float32)).to("cuda")
+    for i in (1, 2):
+        x = c.parts[0][i]
+        c.parts[0][i] = (x.float() * (f[..., None, None] if f.dim() else f)).to(x.dtype)
+    store(c)
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP16])
@@ -56,6 +65,43 @@ def test_rows_of_queries_of_different_sizes(dtype, new, h):
     for scale in (128**-0.5 * 2.0**-top, 128**-0.5 * 2.0**(16 - top)):   # (scores up to 2^20: 32 bits tell no more apart than that)
         want = bounds.attention(c, scale=scale)
         bounds.check(c, c.run(hint=new, scale=scale), want, "few" if new * hq // hkv <= 16 else "many")
+
+
+@pytest.mark.parametrize("dtype,k_power", [(BF16, -40), (BF16, -24), (BF16, -10), (BF16, 18), (BF16, 40), (FP16, -10), (FP16, -16), (FP16, 9)])
+@pytest.mark.parametrize("d,lens,new,h,block", [(64, [333], [1], 0, 16), (128, [900, 70], [2, 1], 0, 24)])
+def test_keys_of_any_size(dtype, k_power, d, lens, new, h, block):
+    hq, hkv = heads(h)
+    c = Case(dtype, lens, new, hq, hkv, d, block, seed=3, extra=300 // block + 1)
+    keys_times(c, k_power)
+    scale = 2.0**-k_power * d**-0.5
+    bounds.check(c, c.run(hint=max(new), scale=scale), bounds.attention(c, scale=scale), "few")
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("k_power", [-20, -14, -8, -4, 4, 9, 12])
+@pytest.mark.parametrize("d,lens,new,h,block", [(128, [300, 129, 64], [100, 60, 3], 4, 16), (64, [600, 40], [600, 40], 2, 24), (128, [900], [9], 7, 128)])
+def test_keys_of_the_sizes_that_many_rows_take(dtype, k_power, d, lens, new, h, block):
+    """Up to 65504, and small ones off by 2^-25; whatever the hint."""
+    hq, hkv = heads(h)
+    c = Case(dtype, lens, new, hq, hkv, d, block, seed=3, extra=300 // block + 1)
+    keys_times(c, k_power if dtype is BF16 else min(k_power, 11))
+    scale = 2.0**-k_power * d**-0.5
+    want = bounds.attention(c, scale=scale)
+    bounds.check(c, c.run(hint=max(new), scale=scale), want, "many")
+    bounds.check(c, c.run(hint=1, scale=scale), want, "any")
+
+
+@pytest.mark.parametrize("new", [1, 20, 300])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 3)])
+def test_neighbouring_keys_of_different_sizes(new, window, sinks):
+    c = Case(BF16, [400], [new], 8, 2, 128, 16, seed=4, extra=9)
+    n = c.nb * c.block
+    # stretches of 32 keys of one size, and keys that differ from their neighbours
+    keys_times(c, ((torch.arange(n) // 32 * 13) % 30 - 20).view(c.nb, c.block))
+    keys_times(c, (torch.arange(n) * 5 % 7 - 3).view(c.nb, c.block))
+    for scale in (128**-0.5 * 2.0**-2, 128**-0.5 * 2.0**-9):
+        want = bounds.attention(c, window, sinks, scale)
+        bounds.check(c, c.run(window, sinks, hint=new, scale=scale), want, "few" if new == 1 else "many")
 
 
 def test_a_key_that_is_not_finite_leaves_rows_that_do_not_see_it_alone():
@@ -104,3 +150,29 @@ def test_rows_that_see_few_keys_behind_a_shared_prefix(dtype, prefix):
         want = bounds.attention(c)
         for hint in (12, 0):
             bounds.check(c, c.run(groups=([0, 3], [prefix]), hint=hint), want, "any")
+
+
+def test_one_graph_of_rows_of_all_kinds():
+    """A call captured once and replayed with other queries, keys and lengths: no power of two and no choice is kept."""
+    c = Case(BF16, [300, 500], [40, 30], 8, 2, 128, 16, seed=8, extra=9)
+    dev = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (c.lens, c.cu)]
+    q, out, lse = c.q.clone(), torch.zeros_like(c.q), torch.zeros(c.t, c.hq, device="cuda")
+    tables = c.tables.cuda()[:, : c.wide]
+    ws = torch.empty(kvc.kvc_attention_q4_workspace_bytes(c.lay, c.t, 2, c.hq), dtype=torch.uint8, device="cuda")
+    kvc.kvc_attention_q4(c.lay, 1, q, out, tables, *dev, ws, lse=lse, max_q_len=40)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kvc.kvc_attention_q4(c.lay, 1, q, out, tables, *dev, ws, lse=lse, max_q_len=40)
+    parts = [[x.clone() for x in p] for p in c.parts]
+    for q_power, k_power, lens in ((0, 0, [300, 500]), (20, -8, [40, 500]), (-30, 12, [300, 31]), (0, 0, [300, 500])):
+        c.parts = [[x.clone() for x in p] for p in parts]
+        keys_times(c, k_power)
+        q.copy_((c.q.float() * 2.0**q_power).to(BF16))
+        dev[0].copy_(torch.tensor(lens, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        keep, c.q, c.lens = c.q, q, lens
+        want = bounds.attention(c)
+        bounds.check(c, (out, lse), want, "many")
+        c.q = keep
