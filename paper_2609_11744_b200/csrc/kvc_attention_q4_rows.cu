@@ -5,9 +5,10 @@
 //     q . k = sum over groups of (s * sum_d q_d c_d + f * sum_d q_d):
 // the codes are exact in the model's 16-bit type, so the first product runs on them, the steps multiply its 32-bit sums,
 // four a key, and offsets times sums of the query are a product of their own with the sums in three parts, which hold all
-// of their bits.  (Each query row comes times a power of two of its own, so that small ones are none of the type's smallest numbers.)  Values cannot be taken apart like that -- their sum is over keys, each with its own step -- so they
-// become f + s * c in that type (rounded once, as a 16-bit pool would hold them).  Against 64 bits the result is off by
-// 0.0026 in bf16 and 0.0003 in fp16: the values' rounding, the weights' (the matrix unit takes 16-bit operands of one type) and
+// of their bits.  (Each query row comes times a power of two of its own, so that small ones are none of the type's smallest
+// numbers.)  The sum of values is over keys, each with its own step, so there a step would have to go into the weights, an
+// operand for each group; instead values become f + s * c in that type (rounded once, as a 16-bit pool would hold
+// them).  Against 64 bits the result is off by 0.0027 in bf16 and 0.0003 in fp16: the values' rounding, the weights' (the matrix unit takes 16-bit operands of one type) and
 // the result's own, 0.0017.
 //
 // Keys are the rows of the matrix instruction and queries its columns (16 x 8), since a KV head has 4 or 8 queries where
@@ -20,7 +21,7 @@
 // A block is four warps, each with its own 32 keys of every 128-key unit and its own ring of three stages filled by
 // asynchronous copies; the run of units that a block has, parts and joins are kvc_attention.h's.  A unit's weighted sum of
 // values is made beside the next unit's scores.  Measured: 64 requests of 128 to 32768 tokens (64 and 8 heads of 128), 282 MB
-// of codes and scales, in 87 us with the join (16-bit pool: 146); 16 requests of 80,000, 1.64 GB, in 382 us = 4.3 TB/s.
+// of codes and scales, in 86 us with the join (16-bit pool: 146); 16 requests of 80,000, 1.64 GB, in 376 us = 4.4 TB/s.
 // Bound by what a warp does for its keys, some 650 instructions a unit at 0.6 an issue slot: with three blocks a SM no unit
 // waits for its copies, and without the copies the call takes 7 % less.  Four blocks with two stages and 128 registers
 // (no such overlap): 92 us; keys in units of 64: 101; blocks of eight or sixteen warps: 97 and 123.

@@ -34,19 +34,21 @@
 // 0.0023 in bf16 (0.0017 with weights in 32 bits: the result's own rounding) and 0.0003 in fp16 (0.0002).
 //
 // Over a pool held in 4 bits (Q4) the matrix unit gets offset + step * code, rounded to fp16 for keys (first_operand) and to the
-// pool's type for values (as a 16-bit pool would hold them, but for a power of two: kvc_q4_device.h); the rest is the same.  Its keys come in raw parts, a quarter of a
+// pool's type for values (as a 16-bit pool would hold them, but for a power of two: kvc_q4_device.h); the rest is the same.  Where a
+// row sees few keys, a tile's keys take two stages, what they are in 11 bits and what that leaves.  Its keys come in raw parts, a quarter of a
 // tile of K and V each, which are copied as they lie (5/16 of the bytes) and made into values by other warps:
 //   256 rows  warp 19 walks the pairs and copies, warps 17 and 18 make values of K and of V
 //   128 rows  warps 17 and 18 copy, warps 8-15, which have no rows, make values: four of K, four of V
-// Measured: the 8192-token prompt in 720 us = 764 TFLOP/s in runs of thirty (16-bit pool: 588).  What bounds it is the pace
+// Measured: the 8192-token prompt in 719 us = 765 TFLOP/s in runs of thirty (16-bit pool: 588).  What bounds it is the pace
 // of the three warps beside the softmax, which hold it up: some 1450 cycles a part for its keys (three instructions a
 // pair), 1300 for its values or to copy it (half of them waits and copies' issue), against 1220 that the softmax of 256 rows takes.  Such a
 // warp runs at 3.4 cycles an instruction in straight lines, whose code the softmax keeps driving out of the instruction
 // cache, so its loops are short: 916 us with the value loop unrolled, 778 without, 724 with the steps of sixteen pairs side by
 // side, 692 with two instructions a pair, 675 with parts of whole blocks in a loop of their own and two groups a turn, 653
-// with results put in order instead of values; with keys of 11 bits 737, 720 with a key's scales masked before they are apart.  The softmax must keep its 104 registers (with 96 the 16-bit prompt takes
+// with results put in order instead of values; with keys of 11 bits 737, 720 with a key's scales masked before they are apart, 734 with a power of two for each row of queries, 719 with
+// what ends a part or a stage in functions of its own.  The softmax must keep its 104 registers (with 96 the 16-bit prompt takes
 // 1330 us), which leaves none for more warps.  With few rows in tiles of 128 (32 requests of up to 5 drafted tokens behind
-// 8000: 216 us) the softmax' chain is the bound, as over a 16-bit pool.  Against 64 bits the result is off by 0.0027 in bf16
+// 8000: 221 us) the softmax' chain is the bound, as over a 16-bit pool.  Against 64 bits the result is off by 0.0026 in bf16
 // (weights and values rounded) and 0.0004 in fp16.
 // Every wait is bounded; one that gives up makes all roles leave and is counted.
 #include <cuda.h>

@@ -260,9 +260,9 @@ struct AppendRaw {
 };
 
 // ---- the 4-bit form (kvc_append_q4): a lane's eight values make one word of codes, four lanes a group.
-// Measured: 16384 tokens of 64 + 16 heads of 128 in 163 us, against 141 for the write in 16 bits: 55 MB less to write, but a
+// Measured: 16384 tokens of 64 + 16 heads of 128 in 169 us, against 141 for the write in 16 bits: 55 MB less to write, but a
 // key's or value's head is some 150 instructions more (200 us with 12 blocks a SM and roundings by conversions, 175
-// with 16 blocks, 163 with roundings by sums).  Keys whose pairs are halves of a head change lanes first.
+// with 16 blocks, 163 with roundings by sums, 169 with the last bit of every code).  Keys whose pairs are halves of a head change lanes first.
 
 // A head's values from pieces of the two halves of its rotated part to eight neighbours a lane; the lanes behind
 // the `turned` ones hold theirs already.
