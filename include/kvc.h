@@ -594,7 +594,8 @@ kvc_status kvc_read_q4(kvc_layout *layout, const kvc_read_q4_desc *desc, void *s
  * Sizes.  Queries may have any.  Values of bf16 are taken for what they are between 2^-60 and 2^60, keys of bf16 with 16
  * rows or fewer between 2^-50 and 2^60.  With more rows keys of bf16 are taken as fp16's: infinite above 65504, and below
  * 2^-14 a value and its offset are off by 2^-25, its step by as much for each unit of the code, so that small keys, with a
- * scale to match, lose bits.  There alone the result depends on the number of rows, and on max_q_len. */
+ * scale to match, lose bits.  Beyond the roundings named above, there alone the result depends on the number of rows,
+ * and on max_q_len. */
 #define KVC_Q4_MAX_SCALE 1e18f
 kvc_status kvc_attention_q4_workspace_bytes(kvc_layout *layout, uint32_t n_tokens, uint32_t n_requests,
                                             uint32_t n_q_heads, uint32_t n_groups, uint64_t *bytes);
